@@ -321,6 +321,95 @@ int deft_tree_attn_decode_static(const deft_plan_t *plan, const void *dev_image,
                                  uint32_t flags, void *stream);
 
 /*
+ * The KV cache in 8 bits.  K and V are held in 8-bit floating point (e4m3: four significant bits, 2^-9 .. 448, one NaN), and
+ * every block of block_rows consecutive rows of the pool has, for each KV head, a scale: a power of two 2^(e - 127), kept as the
+ * byte e, 10 <= e <= 246.  A row's values are its bytes' values times the scale; every such product is a bf16 number.
+ *
+ * k, v             : device, bytes [n_rows, Hkv, d], 16-byte aligned
+ * k_scale, v_scale : device, bytes [ceil(n_rows / block_rows), Hkv]
+ * d                : 64 or 128
+ * block_rows       : a power of two, 1 .. 64.  A block should belong to one node of the tree: choose a page size that is a
+ *                    multiple of it, or with a contiguous cache begin nodes at multiples of it (block_rows = 1 suits any).
+ */
+typedef struct deft_cache_q8 {
+    void *k, *v;
+    void *k_scale, *v_scale;
+    int32_t n_rows, Hkv, d, block_rows;
+} deft_cache_q8_t;
+
+/*
+ * deft_tree_attn_decode over an 8-bit cache: softmax(scale * q K^T) V over the tokens of each query's path, K and V the values
+ * that the cache holds.  The plan, its image, the workspace, o, scale, flags and the errors are those of deft_tree_attn_decode
+ * (Hkv and d are the cache's); besides, a cache with fewer rows than the plan addresses is refused with DEFT_EINVAL.
+ * A float result (DEFT_OUT_F32) is computed with two-term softmax weights in every group, whatever the plan says.
+ * A NaN among the keys of a token makes the results NaN of exactly the queries that see it.  Values (V) must be finite, which
+ * those that deft_kv_store_q8 writes are: a token with weight 0 that is not on a query's path still takes part in its products.
+ */
+int deft_tree_attn_decode_q8(const deft_plan_t *plan, const void *dev_image, const void *q, const deft_cache_q8_t *cache, void *o,
+                             int32_t Hq, float scale, uint32_t flags, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Lists of cache rows or pages.  Which rows a decode iteration writes and which pages it copies is the same for every layer of a
+ * model, so it is worked out once on the host, as a plan is, uploaded, and used by the calls of all layers.  A list is immutable
+ * and owned by the library; release it with deft_kv_list_destroy.
+ *
+ * deft_kv_rows: rows[i], host int32[n] (NULL when n == 0), is the pool row of token i.  n_pool_rows and block_rows are those of
+ *     the cache.  Errors: DEFT_EINVAL (null, n < 0, a row outside the pool, a row twice, block_rows no power of two up to 64),
+ *     DEFT_ENOMEM.
+ * deft_kv_copies: page dst[i] of a pool of n_pool_pages pages becomes what page src[i] holds before the call, for all i at once:
+ *     a page may be copied to any number of pages, and be overwritten itself (chains, exchanges and cycles included).  Errors:
+ *     DEFT_EINVAL (null, n < 0, a page outside the pool, a destination twice), DEFT_ENOMEM.
+ * *out is NULL on error.
+ */
+typedef struct deft_kv_list_s deft_kv_list_t;
+int deft_kv_rows(const int32_t *rows, int32_t n, int32_t n_pool_rows, int32_t block_rows, deft_kv_list_t **out);
+int deft_kv_copies(const int32_t *src, const int32_t *dst, int32_t n, int32_t n_pool_pages, deft_kv_list_t **out);
+
+/* The device image of a list: as deft_plan_device_bytes and deft_plan_upload, captured streams included. */
+size_t deft_kv_list_device_bytes(const deft_kv_list_t *list);
+int deft_kv_list_upload(const deft_kv_list_t *list, void *dev_image, size_t bytes, void *stream);
+void deft_kv_list_destroy(deft_kv_list_t *list);
+
+/*
+ * Stores new tokens' K and V into an 8-bit cache: token i into row rows[i] of the list (deft_kv_rows).
+ *
+ * k, v     : device bf16, token i at k + i * k_stride (elements), [Hkv, d] contiguous there; 16-byte aligned, strides multiples
+ *            of 8 and at least Hkv * d (so slices of a fused projection's output can be stored as they are).
+ * A block is filled from its first row on.  Of a block that is written to, the rows in front of the lowest one written are kept,
+ * the others hold nothing yet: their bytes are left as they are and have no part in the scale.  The scale of (block, head) is
+ * the smallest that brings the largest magnitude written to 448 or below, or the block's old one if that is larger and rows are
+ * kept; where it grows, the kept rows are rounded to it (only values below 2^-6 of it lose bits).  Values are rounded to
+ * nearest, ties to even; what is above 448 * 2^119 becomes that.
+ * A token of which K or V holds an infinity or a NaN, in any of a head's elements, is stored for that head with a NaN in every
+ * element of its key and zeros for its value, and has no part in the scale.
+ * Errors: DEFT_EINVAL (null, misaligned, a list of copies, a cache smaller than the list's pool or with other blocks), DEFT_EHIP.
+ *
+ * deft_kv_load_q8 is the way back: token i of k and v (device bf16 [n, Hkv, d], contiguous, 16-byte aligned) is the value of row
+ * rows[i], exactly.  k or v may be NULL: then only the other is read.
+ */
+int deft_kv_store_q8(const deft_kv_list_t *list, const void *dev_image, const void *k, const void *v, int64_t k_stride,
+                     int64_t v_stride, const deft_cache_q8_t *cache, void *stream);
+int deft_kv_load_q8(const deft_kv_list_t *list, const void *dev_image, const deft_cache_q8_t *cache, void *k, void *v, void *stream);
+
+/*
+ * Copies pages, in place, in every one of n_pools pools (host arrays): pool i is n_pool_pages pages of page_bytes[i] bytes at
+ * device address pools[i], of any alignment.  K and V pools of all layers, bf16 or 8-bit, and the scales of 8-bit ones can go
+ * into one call (with page_size a multiple of block_rows a page has page_size / block_rows * Hkv bytes of scales).
+ * Errors: DEFT_EINVAL (null, a list of rows, n_pools < 0, page_bytes < 1, pools that overlap), DEFT_EHIP.
+ */
+int deft_kv_copy_pages(const deft_kv_list_t *list, const void *dev_image, void *const *pools, const int64_t *page_bytes, int32_t n_pools,
+                       void *stream);
+
+/*
+ * Which copies put a paged pool in order: every node's pages one after the other, nodes depth-first as deft_plan takes them,
+ * from page 0 on.  All pages behind them are free then, and a plan has as few pieces as it can.  node_page_ptr, page_ids: as for
+ * deft_plan_paged (n = node_page_ptr[n_nodes] pages); new_page_ids, src, dst: host int32[n], the new table and the copies to
+ * make, *n_copies of them (for deft_kv_copies).  Host only, nothing is moved.  Errors: DEFT_EINVAL (as for deft_plan_paged).
+ */
+int deft_compact_pages(const int32_t *node_page_ptr, const int32_t *page_ids, int32_t n_pool_pages, const int32_t *node_parent,
+                       int32_t n_nodes, int32_t *new_page_ids, int32_t *src, int32_t *dst, int32_t *n_copies);
+
+/*
  * Benchmark aid, not part of the method (no decode call uses it; it exists so that the benchmark can state
  * the machine's read rate next to stage 1's).  Reads `bytes` bytes at dev_buf once with 128-bit loads from
  * every compute unit (DEFT_PROBE_SINK_BYTES / 4 workgroups, grid-stride) and stores, for each workgroup, the xor of the

@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from typing import NamedTuple
 
 import numpy as np
 
@@ -37,6 +38,8 @@ def rows_per_query(g: int) -> int:
 EXPORTS = (
     "deft_plan", "deft_plan_paged", "deft_plan_update", "deft_plan_paged_update", "deft_suggest_chunk_size", "deft_plan_view", "deft_plan_rows", "deft_plan_device_bytes", "deft_plan_upload", "deft_workspace_bytes",
     "deft_tree_attn_decode", "deft_tree_attn_decode_static", "deft_stage1_partial_attention", "deft_stage2_global_reduction",
+    "deft_tree_attn_decode_q8", "deft_kv_rows", "deft_kv_copies", "deft_kv_list_device_bytes", "deft_kv_list_upload", "deft_kv_list_destroy",
+    "deft_kv_store_q8", "deft_kv_load_q8", "deft_kv_copy_pages", "deft_compact_pages",
     "deft_hbm_read_probe", "deft_plan_destroy", "deft_strerror", "deft_last_hip_error",
 )
 
@@ -68,6 +71,11 @@ _VIEW_ARRAYS = (
 
 class _PlanView(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in _VIEW_SCALARS] + [(n, t) for n, t, _ in _VIEW_ARRAYS]
+
+
+class _CacheQ8(ctypes.Structure):  # deft_cache_q8_t
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale")]
+                + [(n, ctypes.c_int32) for n in ("n_rows", "Hkv", "d", "block_rows")])
 
 
 class DeftError(RuntimeError):
@@ -132,6 +140,27 @@ def load_library():
     lib.deft_stage2_global_reduction.restype = ctypes.c_int
     lib.deft_stage2_global_reduction.argtypes = [vp, vp, vp, c32, c32, c32, ctypes.c_float, ctypes.c_uint32, vp, csz,
                                                  vp]
+    cache = ctypes.POINTER(_CacheQ8)
+    lib.deft_tree_attn_decode_q8.restype = ctypes.c_int
+    lib.deft_tree_attn_decode_q8.argtypes = [vp, vp, vp, cache, vp, c32, ctypes.c_float, ctypes.c_uint32, vp, csz, vp]
+    lib.deft_kv_rows.restype = ctypes.c_int
+    lib.deft_kv_rows.argtypes = [vp, c32, c32, c32, ctypes.POINTER(vp)]
+    lib.deft_kv_copies.restype = ctypes.c_int
+    lib.deft_kv_copies.argtypes = [vp, vp, c32, c32, ctypes.POINTER(vp)]
+    lib.deft_kv_list_device_bytes.restype = csz
+    lib.deft_kv_list_device_bytes.argtypes = [vp]
+    lib.deft_kv_list_upload.restype = ctypes.c_int
+    lib.deft_kv_list_upload.argtypes = [vp, vp, csz, vp]
+    lib.deft_kv_list_destroy.restype = None
+    lib.deft_kv_list_destroy.argtypes = [vp]
+    lib.deft_kv_store_q8.restype = ctypes.c_int
+    lib.deft_kv_store_q8.argtypes = [vp, vp, vp, vp, ctypes.c_int64, ctypes.c_int64, cache, vp]
+    lib.deft_kv_load_q8.restype = ctypes.c_int
+    lib.deft_kv_load_q8.argtypes = [vp, vp, cache, vp, vp, vp]
+    lib.deft_kv_copy_pages.restype = ctypes.c_int
+    lib.deft_kv_copy_pages.argtypes = [vp, vp, ctypes.POINTER(vp), ctypes.POINTER(ctypes.c_int64), c32, vp]
+    lib.deft_compact_pages.restype = ctypes.c_int
+    lib.deft_compact_pages.argtypes = [vp, vp, c32, vp, c32, vp, vp, vp, ctypes.POINTER(c32)]
     lib.deft_hbm_read_probe.restype = ctypes.c_int
     lib.deft_hbm_read_probe.argtypes = [vp, csz, vp, vp]
     lib.deft_plan_destroy.restype = None
@@ -404,4 +433,270 @@ def deft_tree_attn_decode(plan: Plan, q, k, v, out=None, scale: float = 0.0, out
         ws.data_ptr(), ws.numel() * ws.element_size(), raw)
     if rc != 0:
         _check(rc, "deft_tree_attn_decode")
+    return out
+
+
+# ---- the cache in 8 bits ----
+
+MAX_BLOCK_ROWS = 64
+MIN_SCALE_BYTE = 10  # the smallest scale, 2^(10 - 127): of blocks that hold nothing yet
+
+
+class CacheQ8(NamedTuple):
+    """A KV cache in 8-bit floating point (see deft_cache_q8_t): a row's K and V are its e4m3 values times the scale of its
+    block of `block_rows` rows and of the KV head, a power of two.  `alloc_kv_cache_q8` makes one."""
+
+    k: "torch.Tensor"        # float8_e4m3fn [n_rows, Hkv, d]
+    v: "torch.Tensor"
+    k_scale: "torch.Tensor"  # float8_e8m0fnu [ceil(n_rows / block_rows), Hkv]
+    v_scale: "torch.Tensor"
+    block_rows: int = 32
+
+
+def alloc_kv_cache_q8(n_rows: int, Hkv: int, d: int, block_rows: int = 32, device="cuda") -> CacheQ8:
+    """An empty 8-bit cache.  `block_rows` is a power of two up to 64; with a paged pool choose pages of a multiple of it, so
+    that a block belongs to one node.  K and V come from one allocation and are staggered as in alloc_kv_cache."""
+    import torch
+
+    if block_rows < 1 or block_rows > MAX_BLOCK_ROWS or block_rows & (block_rows - 1):
+        raise DeftError(-1, f"alloc_kv_cache_q8: block_rows must be a power of two up to {MAX_BLOCK_ROWS}")
+    pool, blocks = n_rows * Hkv * d, -(-n_rows // block_rows)
+    k_span = -(-pool // 1024) * 1024
+    buf = torch.empty(1024 + k_span + KV_STAGGER_BYTES + pool, dtype=torch.uint8, device=device)
+    k_off = (-buf.data_ptr()) % 1024
+    v_off = k_off + k_span + KV_STAGGER_BYTES
+    k, v = (buf[off:off + pool].view(torch.float8_e4m3fn).view(n_rows, Hkv, d) for off in (k_off, v_off))
+    scales = torch.full((2, blocks, Hkv), MIN_SCALE_BYTE, dtype=torch.uint8, device=device).view(torch.float8_e8m0fnu)
+    return CacheQ8(k, v, scales[0], scales[1], block_rows)
+
+
+def _cache_struct(cache: CacheQ8, what: str) -> _CacheQ8:
+    torch = _torch or _get_torch()
+    k, v, ks, vs, block = cache
+    if not (k.is_cuda and k.device == v.device == ks.device == vs.device):
+        raise DeftError(-1, f"{what}: the cache must be on one device (there is no CPU path)")
+    if not (k.dtype == v.dtype == torch.float8_e4m3fn and k.dim() == 3 and v.shape == k.shape and k.is_contiguous() and v.is_contiguous()):
+        raise DeftError(-1, f"{what}: k and v of the cache must both be contiguous [n_rows, Hkv, d] float8_e4m3fn tensors")
+    if type(block) is not int or not 0 < block <= MAX_BLOCK_ROWS or block & (block - 1):
+        raise DeftError(-1, f"{what}: block_rows must be a power of two up to {MAX_BLOCK_ROWS}")
+    n_rows, Hkv, d = k.shape
+    if not (ks.dtype == vs.dtype == torch.float8_e8m0fnu and ks.shape == vs.shape == (-(-n_rows // block), Hkv) and ks.is_contiguous()
+            and vs.is_contiguous()):
+        raise DeftError(-1, f"{what}: the scales must both be contiguous [ceil(n_rows / block_rows), Hkv] float8_e8m0fnu tensors")
+    return _CacheQ8(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), n_rows, Hkv, d, block)
+
+
+class _On:
+    """The device of a call's tensors as the current one, for as long as the call takes."""
+
+    def __init__(self, index: int):
+        torch = _torch or _get_torch()
+        self._other = None if torch._C._cuda_getDevice() == index else torch.cuda.device(index)
+
+    def __enter__(self):
+        if self._other is not None:
+            self._other.__enter__()
+
+    def __exit__(self, *exc):
+        if self._other is not None:
+            self._other.__exit__(*exc)
+
+
+class KVList:
+    """Owns a deft_kv_list_t handle (cache rows or copies of pages) and its device images.  Like a plan it is made once for
+    the calls of all layers."""
+
+    def __init__(self, handle, n: int, pool: int, block_rows: int = 0):
+        self._h = handle
+        self._images = {}  # device index -> (torch uint8 tensor, event, stream)
+        self.n, self.pool, self.block_rows = n, pool, block_rows
+
+    def __del__(self):
+        h, self._h = getattr(self, "_h", None), None
+        if h and _lib is not None:
+            _lib.deft_kv_list_destroy(h)
+
+    @property
+    def handle(self):
+        return self._h
+
+    def image(self, device, stream=None):
+        """Device image of the list, uploaded on first use.  A call on another stream than the upload's waits for it.  A graph
+        that captures the first use, or one while the upload may still be under way elsewhere, uploads an image of its own."""
+        torch = _torch or _get_torch()
+        index = torch.device(device).index
+        if index is None:
+            index = torch.cuda.current_device()
+        raw = _raw_stream(stream, index)
+        entry = self._images.get(index)
+        if entry is not None and entry[2] == raw:
+            return entry[0]
+        on = torch.cuda.ExternalStream(raw, device=torch.device("cuda", index)) if raw else torch.cuda.default_stream(index)
+        # what is allocated here is allocated for the stream that fills it: it goes to no other tensor while that has work left
+        with _On(index), torch.cuda.stream(on):
+            captured = torch.cuda.is_current_stream_capturing()
+            if entry is not None and (not captured or entry[1] is None):
+                img, event, first = entry
+                if not captured:
+                    img.record_stream(on)
+                    if event is not None and event.query():
+                        self._images[index] = (img, None, first)
+                    elif event is not None:
+                        on.wait_event(event)
+                return img
+            nbytes = int(load_library().deft_kv_list_device_bytes(self._h))
+            img = torch.empty(nbytes, dtype=torch.uint8, device=torch.device("cuda", index))
+            _check(_lib.deft_kv_list_upload(self._h, img.data_ptr(), nbytes, raw), "deft_kv_list_upload")
+            if not captured:
+                event = torch.cuda.Event()
+                event.record(on)
+                self._images[index] = (img, event, raw)
+        return img
+
+
+def deft_kv_rows(rows, n_pool_rows: int, block_rows: int = 32) -> KVList:
+    """The rows of an 8-bit cache that tokens 0, 1, ... go to or come from, for deft_kv_store_q8 and deft_kv_load_q8."""
+    r = _i32(rows)
+    out = ctypes.c_void_p()
+    _check(load_library().deft_kv_rows(_address(r), r.size, int(n_pool_rows), int(block_rows), ctypes.byref(out)), "deft_kv_rows")
+    return KVList(out, r.size, int(n_pool_rows), int(block_rows))
+
+
+def deft_kv_copies(src, dst, n_pool_pages: int) -> KVList:
+    """Copies of pages for deft_kv_copy_pages: page dst[i] becomes what page src[i] held, for all i at once."""
+    a, b = _i32(src), _i32(dst)
+    if a.size != b.size:
+        raise DeftError(-1, "deft_kv_copies: src and dst differ in length")
+    out = ctypes.c_void_p()
+    _check(load_library().deft_kv_copies(_address(a), _address(b), a.size, int(n_pool_pages), ctypes.byref(out)), "deft_kv_copies")
+    return KVList(out, a.size, int(n_pool_pages))
+
+
+def deft_compact_pages(node_page_ptr, page_ids, n_pool_pages: int, node_parent):
+    """(new page_ids, src, dst): the copies that put every node's pages in a row, nodes depth-first, from page 0 on."""
+    pp, pg, par = _i32(node_page_ptr), _i32(page_ids), _i32(node_parent)
+    if pp.size != par.size + 1 or (pp.size and int(pp[-1]) != pg.size):
+        raise DeftError(-1, "deft_compact_pages: tables differ in length")
+    new, src, dst = (np.zeros(max(1, pg.size), dtype=np.int32) for _ in range(3))
+    n = ctypes.c_int32()
+    _check(load_library().deft_compact_pages(_address(pp), _address(pg), int(n_pool_pages), _address(par), par.size, _address(new), _address(src),
+                                             _address(dst), ctypes.byref(n)), "deft_compact_pages")
+    return new[:pg.size], src[:n.value], dst[:n.value]
+
+
+def _rows_for(rows: KVList, cache: CacheQ8, what: str) -> _CacheQ8:
+    c = _cache_struct(cache, what)
+    if not rows.block_rows:
+        raise DeftError(-1, f"{what}: the list is one of copies, not of rows")
+    if rows.block_rows != c.block_rows or rows.pool > c.n_rows:
+        raise DeftError(-1, f"{what}: the list is for a larger cache, or for other blocks")
+    return c
+
+
+def deft_kv_store_q8(rows: KVList, k, v, cache: CacheQ8, stream=None) -> None:
+    """Stores the K and V of new tokens, bf16 [n, Hkv, d], into the rows of the list.  Tokens may lie apart (slices of a fused
+    projection's output), by a multiple of 16 bytes; the heads of one may not.  Asynchronous on `stream`."""
+    torch = _torch or _get_torch()
+    c = _rows_for(rows, cache, "deft_kv_store_q8")
+    shape = (rows.n, c.Hkv, c.d)
+    for name, t in (("k", k), ("v", v)):
+        if t.dtype != torch.bfloat16 or t.shape != shape or t.device != cache.k.device:
+            raise DeftError(-1, f"deft_kv_store_q8: {name} must be a bf16 [{shape[0]}, {shape[1]}, {shape[2]}] tensor on the cache's device")
+        if rows.n and (t.stride(2) != 1 or (c.Hkv > 1 and t.stride(1) != c.d)):
+            raise DeftError(-1, f"deft_kv_store_q8: the heads of a token of {name} must be contiguous")
+    if rows.n == 0:
+        return
+    index = cache.k.device.index
+    least = c.Hkv * c.d
+    ks, vs = (t.stride(0) if rows.n > 1 else max(least, t.stride(0) & ~7) for t in (k, v))  # (one token's stride says nothing)
+    with _On(index):
+        _check(_lib.deft_kv_store_q8(rows._h, rows.image(cache.k.device, stream).data_ptr(), k.data_ptr(), v.data_ptr(), ks, vs,
+                                     ctypes.byref(c), _raw_stream(stream, index)), "deft_kv_store_q8")
+
+
+def deft_kv_load_q8(rows: KVList, cache: CacheQ8, k=None, v=None, stream=None):
+    """(k, v), bf16 [n, Hkv, d]: the values of the list's rows.  Asynchronous on `stream`."""
+    torch = _torch or _get_torch()
+    c = _rows_for(rows, cache, "deft_kv_load_q8")
+    shape, dev = (rows.n, c.Hkv, c.d), cache.k.device
+    k, v = (torch.empty(shape, dtype=torch.bfloat16, device=dev) if t is None else t for t in (k, v))
+    for name, t in (("k", k), ("v", v)):
+        if t.dtype != torch.bfloat16 or t.shape != shape or not t.is_contiguous() or t.device != dev:
+            raise DeftError(-1, f"deft_kv_load_q8: {name} must be a contiguous bf16 [{shape[0]}, {shape[1]}, {shape[2]}] tensor on the cache's device")
+    if rows.n:
+        with _On(dev.index):
+            _check(_lib.deft_kv_load_q8(rows._h, rows.image(dev, stream).data_ptr(), ctypes.byref(c), k.data_ptr(), v.data_ptr(),
+                                        _raw_stream(stream, dev.index)), "deft_kv_load_q8")
+    return k, v
+
+
+def deft_kv_copy_pages(copies: KVList, pools, stream=None) -> None:
+    """Makes the copies of the list in every pool, in place.  pools: contiguous device tensors of any type, each the
+    n_pool_pages pages of one K or V cache, or of an 8-bit cache's scales.  Asynchronous on `stream`."""
+    if copies.block_rows:
+        raise DeftError(-1, "deft_kv_copy_pages: the list is one of rows, not of copies")
+    pools = list(pools)
+    if not pools:
+        return
+    dev = pools[0].device
+    sizes = []
+    for t in pools:
+        nbytes = t.numel() * t.element_size()
+        if not t.is_cuda or t.device != dev or not t.is_contiguous():
+            raise DeftError(-1, "deft_kv_copy_pages: pools must be contiguous tensors on one device (there is no CPU path)")
+        if copies.pool == 0 or nbytes == 0 or nbytes % copies.pool:
+            raise DeftError(-1, "deft_kv_copy_pages: a pool is not a whole number of bytes for each of the list's pages")
+        sizes.append(nbytes // copies.pool)
+    n = len(pools)
+    with _On(dev.index):
+        _check(load_library().deft_kv_copy_pages(copies._h, copies.image(dev, stream).data_ptr(), (ctypes.c_void_p * n)(*[t.data_ptr() for t in pools]),
+                                                 (ctypes.c_int64 * n)(*sizes), n, _raw_stream(stream, dev.index)), "deft_kv_copy_pages")
+
+
+def deft_tree_attn_decode_q8(plan: Plan, q, cache: CacheQ8, out=None, scale: float = 0.0, out_dtype=None, workspace=None, stream=None):
+    """deft_tree_attn_decode over an 8-bit cache.
+
+    q [nq,Hq,d]: contiguous bf16.  Returns o [nq,Hq,d] (bf16, or float32 when out_dtype / out says so: then with softmax weights
+    in two terms throughout).  Asynchronous on `stream` (default: torch's current stream).
+    """
+    torch = _torch or _get_torch()
+    bf16 = torch.bfloat16
+    c = _cache_struct(cache, "deft_tree_attn_decode_q8")
+    dev = cache.k.device
+    if q.dtype != bf16 or q.dim() != 3 or not q.is_contiguous() or q.device != dev:
+        raise DeftError(-1, "deft_tree_attn_decode_q8: q must be a contiguous 3-d bf16 tensor on the cache's device")
+    nq, Hq, d = q.shape
+    plan_nq, plan_rows = plan.limits()
+    if d != c.d:
+        raise DeftError(-1, "deft_tree_attn_decode_q8: q and the cache differ in d")
+    if nq != plan_nq:
+        raise DeftError(-1, "deft_tree_attn_decode_q8: q has a different number of queries than the plan")
+    if plan_rows > c.n_rows:
+        raise DeftError(-1, "deft_tree_attn_decode_q8: the plan addresses rows beyond the KV cache")
+    if out is None:
+        out = torch.empty((nq, Hq, d), dtype=out_dtype or bf16, device=dev)
+    elif out.shape != (nq, Hq, d) or not out.is_contiguous() or out.device != dev:
+        raise DeftError(-1, "deft_tree_attn_decode_q8: out must be a contiguous [nq, Hq, d] tensor on q's device")
+    if out.dtype == bf16:
+        flags = DEFT_OUT_BF16
+    elif out.dtype == torch.float32:
+        flags = DEFT_OUT_F32
+    else:
+        raise DeftError(-1, "deft_tree_attn_decode_q8: out must be bf16 or float32")
+    Hkv, index = c.Hkv, dev.index
+    if Hkv == 0 or Hq % Hkv:
+        raise DeftError(-1, "deft_tree_attn_decode_q8: Hq must be a multiple of Hkv")
+    raw = _raw_stream(stream, index)
+    with _On(index):
+        # an image that went out on this very stream, or that has landed, needs no ordering
+        entry = plan._images.get((Hq // Hkv, index))
+        img = entry[0] if entry is not None and (entry[2] == raw or entry[1] is None) else plan.image(Hq, Hkv, dev, stream)
+        ws = workspace if workspace is not None else plan._workspaces.get((Hq, Hkv, d, index))
+        if ws is None:
+            ws = plan.workspace(Hq, Hkv, d, dev)
+        rc = (_lib or load_library()).deft_tree_attn_decode_q8(
+            plan._h, img.data_ptr(), q.data_ptr(), ctypes.byref(c), out.data_ptr(), Hq, float(scale), flags, ws.data_ptr(),
+            ws.numel() * ws.element_size(), raw)
+    if rc != 0:
+        _check(rc, "deft_tree_attn_decode_q8")
     return out

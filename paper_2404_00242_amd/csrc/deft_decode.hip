@@ -37,6 +37,7 @@
 #include <type_traits>
 
 #include "deft_internal.h"
+#include "deft_device.h"
 
 // Partial-result workspace of deft_tree_attn_decode_static: device memory inside the code object, one copy
 // per GPU at its own address, held until the process ends.  Host code never uses this name as an address;
@@ -49,6 +50,7 @@ typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((ext_vector_type(4))) int32_t i32x4;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 
 struct Stage1Args {
     const uint16_t *q, *k, *v;
@@ -69,6 +71,39 @@ struct Stage1Args {
     int32_t n_slots;
 };
 
+// What K and V are held in.  Stage 1 is written for bf16 operands; a cache of another type differs in how a block's rows are
+// fetched and in what becomes of them before they are operands.
+struct Bf16Cache {
+    typedef uint16_t elem;
+    typedef Stage1Args Args;
+    struct Scales {};
+    static constexpr bool k8Bit = false;
+    // The values of d that a lane of group g holds for contraction step kk of S^T = K Q^T: eight from q_lane(g) + q_step(kk).
+    static __device__ __forceinline__ constexpr int q_lane(int g) { return 8 * g; }
+    static __device__ __forceinline__ constexpr int q_step(int kk) { return 32 * kk; }
+};
+
+// 8-bit floating point (e4m3), a scale for each (block of 2^block_shift rows, KV head), [blocks, Hkv] exponent bytes e for a
+// scale of 2^(e - 127).  A value times its scale has four significant bits, so it is a bf16 number, and v_cvt_scalef32_pk_bf16_fp8
+// makes two of them: from there on the two caches are one, and the results are those of a bf16 cache that holds the products.
+struct E4m3Cache {
+    typedef uint8_t elem;
+    struct Args : Stage1Args {
+        const uint8_t *k8, *v8, *k_scale, *v_scale;
+        int32_t block_shift;
+    };
+    struct Scales {
+        const uint8_t *k, *v;  // of this KV head
+        int shift, Hkv;
+        __device__ __forceinline__ uint32_t key(int row) const { return k[(size_t)(row >> shift) * Hkv]; }
+        __device__ __forceinline__ uint32_t value(int row) const { return v[(size_t)(row >> shift) * Hkv]; }
+    };
+    static constexpr bool k8Bit = true;
+    // a lane's 128-bit load of K holds 16 values of d: two steps
+    static __device__ __forceinline__ constexpr int q_lane(int g) { return 16 * g; }
+    static __device__ __forceinline__ constexpr int q_step(int kk) { return 64 * (kk >> 1) + 8 * (kk & 1); }
+};
+
 struct Stage2Args {
     const float *part_acc, *part_m, *part_l;
     const int32_t *q_head, *q_part_slot;
@@ -85,8 +120,9 @@ struct Stage2Args {
 // same tree 170.8 -> 166.0, 21 MB with d = 64 12.4 -> 12.1.
 
 // A whole call in one launch: stage 1's workgroups first, then those of stage 2
+template <typename C>
 struct CallArgs {
-    Stage1Args s1;
+    typename C::Args s1;
     Stage2Args s2;
     int32_t polls;  // most looks at a mark before stage 2 leaves a row to stage 1 (reduce_rows)
 };
@@ -112,6 +148,31 @@ __device__ __forceinline__ u32x4 load16_once(const uint16_t *p) {
 template <bool ONCE>
 __device__ __forceinline__ u32x4 load16_kv(const uint16_t *p) {
     return ONCE ? load16_once(p) : load16(p);
+}
+// of an 8-bit cache: 16 and 8 values
+template <bool ONCE>
+__device__ __forceinline__ u32x4 load16_kv(const uint8_t *p) {
+    return ONCE ? __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p)) : *reinterpret_cast<const u32x4 *>(p);
+}
+template <bool ONCE>
+__device__ __forceinline__ u32x2 load8_kv(const uint8_t *p) {
+    return ONCE ? __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(p)) : *reinterpret_cast<const u32x2 *>(p);
+}
+
+// Four e4m3 values times a scale, as four bf16 values.  The scale is a float's exponent.
+__device__ __forceinline__ u32x2 widen4(uint32_t x, float scale) {
+    return u32x2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, false)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, true))};
+}
+__device__ __forceinline__ u32x4 widen8(u32x2 x, float scale) {
+    const u32x2 a = widen4(x[0], scale), b = widen4(x[1], scale);
+    return u32x4{a[0], a[1], b[0], b[1]};
+}
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
+// The scale byte of token 4g + Q, from lanes that hold that of token 4g + n16 % 4 each.
+template <int Q>
+__device__ __forceinline__ float scale_of_token(uint32_t byte) {
+    return scale_of((uint32_t)__builtin_amdgcn_update_dpp((int)byte, (int)byte, 0x55 * Q, 0xf, 0xf, false));
 }
 
 // Partial results.  SHARED: in a call of one launch they are stored past the L2 of their XCD, and read past the reader's,
@@ -176,9 +237,10 @@ constexpr int kXbufBytes = 64 * 1024;  // LDS register-exchange area: 2 token pa
 static_assert(4 * DEFT_MAX_CHUNK * sizeof(int32_t) <= kXbufBytes, "piece records are parked in the exchange area");
 
 // What a wave needs to know about its chunk to address tokens.
+template <typename C>
 struct ChunkCtx {
-    const uint16_t *kbase, *vbase;  // K/V pointers already offset to this head and this lane's d slice
-    const uint16_t *khead, *vhead;  // the same without the lane's slice (wave-uniform), and the slices in bytes
+    const typename C::elem *kbase, *vbase;  // K/V pointers already offset to this head and this lane's d slice
+    const typename C::elem *khead, *vhead;  // the same without the lane's slice (wave-uniform), and the slices in bytes
     uint32_t klane, vlane;
     size_t row_stride;              // elements between consecutive token rows
     const int32_t *s_row, *s_qlo, *s_qhi;  // LDS per-token table (only when !uniform), padded to whole blocks
@@ -187,6 +249,7 @@ struct ChunkCtx {
     int begin0, qlo0, qhi0;
     int fresh;                      // blocks after which a new reference is taken (RowState), less one; -1: never
     int n16, g;
+    typename C::Scales scales;
 };
 
 // One 32-token block as MFMA operands: K as the A operand of S^T = K Q^T (token 16a + n16, d = 32kk + 8g..+7),
@@ -198,8 +261,34 @@ struct KVRegs {
     u32x4 v[8];
 };
 
+// The same block of an 8-bit cache, as loaded: of K a lane holds d = 64i + 16g..+15 of token 16a + n16, which serve steps 2i
+// and 2i + 1 (E4m3Cache::q_step), of V the same tokens and d as above.  Scales of tokens 16a + n16 and 16a + 4g + n16 % 4.
+template <int D>
+struct KVBytes {
+    u32x4 k[2][D / 64];
+    u32x2 v[8];
+    uint32_t ks[2], vs[2];
+};
+template <int D>
+__device__ __forceinline__ void widen_k(const u32x4 (&x)[D / 64], uint32_t byte, bf16x8 (&k)[D / 32]) {
+    const float scale = scale_of(byte);
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) {
+        k[2 * i] = __builtin_bit_cast(bf16x8, widen8(u32x2{x[i][0], x[i][1]}, scale));
+        k[2 * i + 1] = __builtin_bit_cast(bf16x8, widen8(u32x2{x[i][2], x[i][3]}, scale));
+    }
+}
+// four tokens of a lane, 4g..4g+3 of a tile
+__device__ __forceinline__ void widen_v(const u32x2 *x, uint32_t byte, u32x4 *v) {
+    v[0] = widen8(x[0], scale_of_token<0>(byte));
+    v[1] = widen8(x[1], scale_of_token<1>(byte));
+    v[2] = widen8(x[2], scale_of_token<2>(byte));
+    v[3] = widen8(x[3], scale_of_token<3>(byte));
+}
+
 // physical row of chunk position x; positions past the chunk's end give a row that exists (their scores are masked)
-__device__ __forceinline__ int tok_row(const ChunkCtx &c, int x) {
+template <typename C>
+__device__ __forceinline__ int tok_row(const ChunkCtx<C> &c, int x) {
     return c.uniform ? c.begin0 + min(x, c.clen - 1) : c.s_row[x];
 }
 
@@ -208,7 +297,7 @@ __device__ __forceinline__ int tok_row(const ChunkCtx &c, int x) {
 // instructions on every path the compiler can count exactly how many younger loads may stay in flight when
 // an older block is consumed, which is what keeps the software pipeline full.
 template <int D>
-__device__ __forceinline__ void load_k(KVRegs<D> &r, const ChunkCtx &c, int x0, bool valid) {
+__device__ __forceinline__ void load_k(KVRegs<D> &r, const ChunkCtx<Bf16Cache> &c, int x0, bool valid) {
     if (!valid) x0 = 0;
 #pragma unroll
     for (int aa = 0; aa < 2; ++aa) {
@@ -219,7 +308,7 @@ __device__ __forceinline__ void load_k(KVRegs<D> &r, const ChunkCtx &c, int x0, 
     }
 }
 template <int D>
-__device__ __forceinline__ void load_v(KVRegs<D> &r, const ChunkCtx &c, int x0, bool valid) {
+__device__ __forceinline__ void load_v(KVRegs<D> &r, const ChunkCtx<Bf16Cache> &c, int x0, bool valid) {
     if (!valid) x0 = 0;
 #pragma unroll
     for (int aa = 0; aa < 2; ++aa)
@@ -228,6 +317,63 @@ __device__ __forceinline__ void load_v(KVRegs<D> &r, const ChunkCtx &c, int x0, 
             const int rowv = valid ? tok_row(c, x0 + 16 * aa + 4 * c.g + i) : c.begin0;
             r.v[4 * aa + i] = load16_once(c.vbase + (size_t)rowv * c.row_stride);
         }
+}
+
+template <int D>
+__device__ __forceinline__ void load_k(KVBytes<D> &r, const ChunkCtx<E4m3Cache> &c, int x0, bool valid) {
+    if (!valid) x0 = 0;
+#pragma unroll
+    for (int aa = 0; aa < 2; ++aa) {
+        const int row = valid ? tok_row(c, x0 + 16 * aa + c.n16) : c.begin0;
+        const uint8_t *kp = c.kbase + (size_t)row * c.row_stride;
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) r.k[aa][i] = load16_kv<true>(kp + 64 * i);
+        r.ks[aa] = c.scales.key(row);
+    }
+}
+template <int D>
+__device__ __forceinline__ void load_v(KVBytes<D> &r, const ChunkCtx<E4m3Cache> &c, int x0, bool valid) {
+    if (!valid) x0 = 0;
+#pragma unroll
+    for (int aa = 0; aa < 2; ++aa) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int row = valid ? tok_row(c, x0 + 16 * aa + 4 * c.g + i) : c.begin0;
+            r.v[4 * aa + i] = load8_kv<true>(c.vbase + (size_t)row * c.row_stride);
+        }
+        r.vs[aa] = c.scales.value(valid ? tok_row(c, x0 + 16 * aa + 4 * c.g + (c.n16 & 3)) : c.begin0);
+    }
+}
+
+// A loaded block's operands: K for the scores, V row-major for pv_block.
+template <int D>
+__device__ __forceinline__ const bf16x8 (&keys(const KVRegs<D> &r))[2][D / 32] { return r.k; }
+template <int D>
+__device__ __forceinline__ const u32x4 (&values(const KVRegs<D> &r))[8] { return r.v; }
+template <int D>
+struct WideKeys {
+    typedef const bf16x8 (&ref)[2][D / 32];
+    bf16x8 k[2][D / 32];
+    __device__ __forceinline__ operator ref() const { return k; }
+};
+struct WideValues {
+    typedef const u32x4 (&ref)[8];
+    u32x4 v[8];
+    __device__ __forceinline__ operator ref() const { return v; }
+};
+template <int D>
+__device__ __forceinline__ WideKeys<D> keys(const KVBytes<D> &r) {
+    WideKeys<D> x;
+    widen_k<D>(r.k[0], r.ks[0], x.k[0]);
+    widen_k<D>(r.k[1], r.ks[1], x.k[1]);
+    return x;
+}
+template <int D>
+__device__ __forceinline__ WideValues values(const KVBytes<D> &r) {
+    WideValues x;
+    widen_v(r.v, r.vs[0], x.v);
+    widen_v(r.v + 4, r.vs[1], x.v + 4);
+    return x;
 }
 
 // Running softmax state of one row (held redundantly by the row's four lanes).
@@ -301,8 +447,8 @@ __device__ __forceinline__ void qk_block(const bf16x8 (&k)[2][D / 32], const Til
 // mask: a token is visible to plan position qpos iff qlo <= qpos < qhi of the node piece it belongs to.
 // A full block of a single-piece chunk is visible to every row of the chunk's group: nothing to mask
 // (rows past the group's end have Q = 0, finite scores, and are never written).
-template <int D, int NT>
-__device__ __forceinline__ void mask_block(const ChunkCtx &c, int x0, const TileState<D> (&ts)[NT], f32x4 (&sacc)[NT][2]) {
+template <int D, int NT, typename C>
+__device__ __forceinline__ void mask_block(const ChunkCtx<C> &c, int x0, const TileState<D> (&ts)[NT], f32x4 (&sacc)[NT][2]) {
     if (!(c.uniform && x0 + 32 <= c.clen)) {
 #pragma unroll
         for (int aa = 0; aa < 2; ++aa) {
@@ -453,8 +599,8 @@ __device__ __forceinline__ void pv_block(const u32x4 (&v)[8], const bf16x8 (&pre
     }
 }
 
-template <int D, int NT, bool PRECISE>
-__device__ __forceinline__ void compute_block(const KVRegs<D> &r, const ChunkCtx &c, int x0, TileState<D> (&ts)[NT],
+template <int D, int NT, bool PRECISE, typename C>
+__device__ __forceinline__ void compute_block(const KVRegs<D> &r, const ChunkCtx<C> &c, int x0, TileState<D> (&ts)[NT],
                                               const float cs, const float inv_cs) {
     f32x4 sacc[NT][2];
     qk_block<D, NT>(r.k, ts, sacc);
@@ -474,27 +620,27 @@ __device__ __forceinline__ void compute_block(const KVRegs<D> &r, const ChunkCtx
 // front of the other workgroup's loads longer.  Stage 1, two blocks -> one reloaded whole -> in halves: sixteen
 // sequences (148 MB) 29.9 -> 28.8 -> 27.8 us, few-shot prefix (149 MB) 28.7 -> 28.7 -> 27.7, reasoning tree of 256
 // queries (456 MB) 96.2 -> 94.5 -> 93.6.
-template <int D>
+template <int D, typename C>
 struct SplitPipe {
-    KVRegs<D> r;
-    __device__ __forceinline__ void prime(const ChunkCtx &ctx, int wave, int nblk) {
+    std::conditional_t<C::k8Bit, KVBytes<D>, KVRegs<D>> r;
+    __device__ __forceinline__ void prime(const ChunkCtx<C> &ctx, int wave, int nblk) {
         load_k<D>(r, ctx, wave * 32, wave < nblk);
         load_v<D>(r, ctx, wave * 32, wave < nblk);
     }
     template <bool PRECISE>
-    __device__ __forceinline__ void run(const ChunkCtx &ctx, int wave, int nblk, TileState<D> (&ts)[1], float cs) {
+    __device__ __forceinline__ void run(const ChunkCtx<C> &ctx, int wave, int nblk, TileState<D> (&ts)[1], float cs) {
         for (int blk = wave; blk < nblk; blk += kWaves) {
             const int next = blk + kWaves;
             f32x4 sacc[1][2];
             bf16x8 preg[1], plo[1];
-            qk_block<D, 1>(r.k, ts, sacc);
+            qk_block<D, 1>(keys(r), ts, sacc);
             load_k<D>(r, ctx, next * 32, next < nblk);
             __builtin_amdgcn_sched_barrier(0);  // the loads go out here, not behind the softmax
             mask_block<D, 1>(ctx, blk * 32, ts, sacc);
             shift_block<D, 1>(ts, sacc, cs);
             raise_block<D, 1>(ts, sacc);
             weights_block<D, 1, PRECISE>(ts, sacc, cs, preg, plo);
-            pv_block<D, 1, PRECISE>(r.v, preg, plo, ts);
+            pv_block<D, 1, PRECISE>(values(r), preg, plo, ts);
             load_v<D>(r, ctx, next * 32, next < nblk);
         }
     }
@@ -506,16 +652,71 @@ struct SplitPipe {
 // 2*KK + j).  With TR = 2 wave t fetches K tile t and V tokens 4t..4t+3; with TR = 4 waves 0 and 1 fetch the
 // two K tiles and waves 2 and 3 four V tokens each.  Either way every 2*d-byte token row is read whole, by
 // one wave, in back-to-back loads.
-template <int D, int TR>
+template <int D, int TR, typename C>
 struct Share {
     static constexpr int KK = D / 32;
     static constexpr int NSLOT = 2 * KK + 8;
     static constexpr int NX = TR == 2 ? KK + 4 : (KK > 4 ? KK : 4);
     u32x4 x[NX];
 };
+// Of an 8-bit cache, as loaded; the wave that fetched a share widens it before it passes it on, so each byte is widened once
+// in a workgroup and what lies in LDS is what a bf16 cache would have put there.
+template <int D, int TR>
+struct Share<D, TR, E4m3Cache> {
+    static constexpr int KK = D / 32;
+    static constexpr int NSLOT = 2 * KK + 8;
+    static constexpr int NX = TR == 2 ? KK + 4 : (KK > 4 ? KK : 4);
+    u32x4 k[D / 64];
+    u32x2 v[4];
+    uint32_t ks, vs;
+};
 
 template <int D, int TR>
-__device__ __forceinline__ void share_issue(Share<D, TR> &s, const ChunkCtx &c, int t, int x0, bool valid) {
+__device__ __forceinline__ const u32x4 (&share_rows(const Share<D, TR, Bf16Cache> &s, int))[Share<D, TR, Bf16Cache>::NX] { return s.x; }
+template <int NX>
+struct WideRows {
+    typedef const u32x4 (&ref)[NX];
+    u32x4 x[NX];
+    __device__ __forceinline__ operator ref() const { return x; }
+};
+template <int D, int TR>
+__device__ __forceinline__ WideRows<Share<D, TR, E4m3Cache>::NX> share_rows(const Share<D, TR, E4m3Cache> &s, int t) {
+    constexpr int KK = D / 32;
+    WideRows<Share<D, TR, E4m3Cache>::NX> r;
+    if (TR == 2 || t < 2) {
+        bf16x8 k[KK];
+        widen_k<D>(s.k, s.ks, k);
+#pragma unroll
+        for (int q = 0; q < KK; ++q) r.x[q] = __builtin_bit_cast(u32x4, k[q]);
+    }
+    if (TR == 2)
+        widen_v(s.v, s.vs, r.x + KK);
+    else if (t >= 2)
+        widen_v(s.v, s.vs, r.x);
+    return r;
+}
+
+template <int D, int TR>
+__device__ __forceinline__ void share_issue(Share<D, TR, E4m3Cache> &s, const ChunkCtx<E4m3Cache> &c, int t, int x0, bool valid) {
+    if (!valid) x0 = 0;
+    if (TR == 2 || t < 2) {
+        const int row = valid ? tok_row(c, x0 + 16 * t + c.n16) : c.begin0;
+        const uint8_t *kp = c.kbase + (size_t)row * c.row_stride;
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) s.k[i] = load16_kv<TR == 2>(kp + 64 * i);
+        s.ks = c.scales.key(row);
+    }
+    if (TR == 2 || t >= 2) {
+        const int x = x0 + 16 * (TR == 2 ? t : t - 2) + 4 * c.g;
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            s.v[q] = load8_kv<TR == 2>(c.vbase + (size_t)(valid ? tok_row(c, x + q) : c.begin0) * c.row_stride);
+        s.vs = c.scales.value(valid ? tok_row(c, x + (c.n16 & 3)) : c.begin0);
+    }
+}
+
+template <int D, int TR>
+__device__ __forceinline__ void share_issue(Share<D, TR, Bf16Cache> &s, const ChunkCtx<Bf16Cache> &c, int t, int x0, bool valid) {
     constexpr int KK = D / 32;
     if (!valid) x0 = 0;
     if (TR == 2 || t < 2) {
@@ -539,22 +740,24 @@ __device__ __forceinline__ void share_issue(Share<D, TR> &s, const ChunkCtx &c, 
     }
 }
 
-template <int D, int TR, int NT, bool PRECISE>
-__device__ __forceinline__ void share_step(Share<D, TR> &s, const ChunkCtx &c, u32x4 *xs, int t, int lane, int blk,
+template <int D, int TR, int NT, bool PRECISE, typename C>
+__device__ __forceinline__ void share_step(Share<D, TR, C> &s, const ChunkCtx<C> &c, u32x4 *xs, int t, int lane, int blk,
                                            int next_blk, int nblk, TileState<D> (&ts)[NT], float cs, float inv_cs) {
     constexpr int KK = D / 32;
     const bool live = blk < nblk;
     if (live) {
+        const auto &rows = share_rows(s, t);
+        const u32x4(&x)[Share<D, TR, C>::NX] = rows;
         if (TR == 2 || t < 2) {
 #pragma unroll
-            for (int q = 0; q < KK; ++q) xs[(t * KK + q) * 64 + lane] = s.x[q];
+            for (int q = 0; q < KK; ++q) xs[(t * KK + q) * 64 + lane] = x[q];
         }
         if (TR == 2) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) xs[(2 * KK + 4 * t + q) * 64 + lane] = s.x[KK + q];
+            for (int q = 0; q < 4; ++q) xs[(2 * KK + 4 * t + q) * 64 + lane] = x[KK + q];
         } else if (t >= 2) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) xs[(2 * KK + 4 * (t - 2) + q) * 64 + lane] = s.x[q];
+            for (int q = 0; q < 4; ++q) xs[(2 * KK + 4 * (t - 2) + q) * 64 + lane] = x[q];
         }
     }
     __syncthreads();
@@ -573,19 +776,19 @@ __device__ __forceinline__ void share_step(Share<D, TR> &s, const ChunkCtx &c, u
 
 // Used for tasks of two row tiles (TR = 2, NT = 1: two waves per tile, the two pairs take alternate blocks);
 // wider tasks go through WidePipe below.
-template <int D, int TR, int NT>
+template <int D, int TR, int NT, typename C>
 struct SharedPipe {
-    using S = Share<D, TR>;
+    using S = Share<D, TR, C>;
     static constexpr int NP = kWaves / TR;  // token parts: part p takes blocks p, p+NP, ...
     static constexpr int DEPTH = 2;  // blocks whose shares a wave keeps in flight
-    Share<D, TR> st[DEPTH];
-    __device__ __forceinline__ void prime(const ChunkCtx &ctx, int wave, int nblk) {
+    S st[DEPTH];
+    __device__ __forceinline__ void prime(const ChunkCtx<C> &ctx, int wave, int nblk) {
         const int t = wave % TR, part = wave / TR;
 #pragma unroll
         for (int u = 0; u < DEPTH; ++u) share_issue<D, TR>(st[u], ctx, t, (part + u * NP) * 32, part + u * NP < nblk);
     }
     template <bool PRECISE>
-    __device__ __forceinline__ void run(const ChunkCtx &ctx, u32x4 *xbuf, int wave, int lane, int nblk,
+    __device__ __forceinline__ void run(const ChunkCtx<C> &ctx, u32x4 *xbuf, int wave, int lane, int nblk,
                                         TileState<D> (&ts)[NT], float cs, float inv_cs) {
         const int t = wave % TR, part = wave / TR;
         const int iters = (nblk + NP - 1) / NP;  // the same for every wave: barriers stay aligned
@@ -621,10 +824,10 @@ struct SharedPipe {
 //      queries x 4 heads over 32768 tokens in chunks of 1024 (equal-token split) 175 -> 163, 20000 tokens under 40
 //      branches 89.8 -> 77.3, 32768 under 40 branches, 7 heads a KV head, 104.7 -> 91.0; where such tasks are few among
 //      many narrow ones a second block costs 2 % (256-query reasoning tree, balanced split, 97.7 -> 99.9).
-template <int D, int NT, bool UNIFORM, int DEPTH>
+template <int D, int NT, bool UNIFORM, int DEPTH, typename C>
 struct WidePipe {
     static constexpr int KK = D / 32;
-    using S = Share<D, 4>;
+    using S = Share<D, 4, C>;
     S st[DEPTH];
     uint32_t lane_row, lane_col;  // UNIFORM: first row of this lane's loads inside a block, byte offset inside a row
 
@@ -632,8 +835,25 @@ struct WidePipe {
     // chunk's last row) * row bytes + the lane's column; a K loader reads four 64-byte columns of one row, a V
     // loader one column of four rows.  No branch on any path: blocks past the end repeat the last block, so the same four load instructions are
     // issued whatever happens and the compiler's s_waitcnt vmcnt counts stay exact.
-    __device__ __forceinline__ void issue(S &sh, const ChunkCtx &c, int t, int blk, int nblk) {
-        if (UNIFORM) {
+    __device__ __forceinline__ void issue(S &sh, const ChunkCtx<C> &c, int t, int blk, int nblk) {
+        if constexpr (UNIFORM && C::k8Bit) {
+            const int blk_e = min(blk, nblk - 1);
+            const uint32_t row_bytes = (uint32_t)c.row_stride;
+            const size_t first = ((size_t)c.begin0 + 32 * (size_t)blk_e) * row_bytes;
+            const int lim = min(31, c.clen - 1 - 32 * blk_e), row0 = c.begin0 + 32 * blk_e;
+            if (t < 2) {
+                const int row = min((int)lane_row, lim);
+                const uint8_t *base = c.khead + first;
+#pragma unroll
+                for (int i = 0; i < D / 64; ++i) sh.k[i] = load16_kv<false>(base + ((uint32_t)row * row_bytes + lane_col + 64u * i));
+                sh.ks = c.scales.key(row0 + row);
+            } else {
+                const uint8_t *base = c.vhead + first;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) sh.v[q] = load8_kv<false>(base + ((uint32_t)min((int)lane_row + q, lim) * row_bytes + lane_col));
+                sh.vs = c.scales.value(row0 + min((int)lane_row + (c.n16 & 3), lim));
+            }
+        } else if constexpr (UNIFORM) {
             static_assert(KK == 4 || !UNIFORM, "a K loader issues four loads");
             const int blk_e = min(blk, nblk - 1);
             const uint32_t row_bytes = (uint32_t)c.row_stride * 2;
@@ -653,7 +873,7 @@ struct WidePipe {
         }
     }
 
-    __device__ __forceinline__ void prime(const ChunkCtx &ctx, int wave, int nblk) {
+    __device__ __forceinline__ void prime(const ChunkCtx<C> &ctx, int wave, int nblk) {
         lane_row = wave < 2 ? 16 * wave + ctx.n16 : 16 * (wave - 2) + 4 * ctx.g;
         lane_col = wave < 2 ? ctx.klane : ctx.vlane;
 #pragma unroll
@@ -661,10 +881,12 @@ struct WidePipe {
     }
 
     // pass this wave's share of a block to the others and fetch the share of a later block
-    __device__ __forceinline__ void exchange(S &sh, const ChunkCtx &c, u32x4 *xs, int t, int lane, int next_blk, int nblk) {
+    __device__ __forceinline__ void exchange(S &sh, const ChunkCtx<C> &c, u32x4 *xs, int t, int lane, int next_blk, int nblk) {
+        const auto &rows = share_rows(sh, t);
+        const u32x4(&x)[S::NX] = rows;
         if (t < 2) {
 #pragma unroll
-            for (int q = 0; q < KK; ++q) xs[(t * KK + q) * 64 + lane] = sh.x[q];
+            for (int q = 0; q < KK; ++q) xs[(t * KK + q) * 64 + lane] = x[q];
         } else {
             // V: this wave holds tokens 16(t-2) + 4g + {0..3}, i.e. the token pairs p = 2(t-2) and 2(t-2) + 1 of
             // every lane's eight; it interleaves them once for all four waves (pv_block, READY) and writes its
@@ -672,7 +894,7 @@ struct WidePipe {
             uint2 *xh = reinterpret_cast<uint2 *>(xs + 2 * KK * 64) + (t - 2);
 #pragma unroll
             for (int c2 = 0; c2 < 4; ++c2) {
-                const uint32_t lo0 = sh.x[0][c2], hi0 = sh.x[1][c2], lo1 = sh.x[2][c2], hi1 = sh.x[3][c2];
+                const uint32_t lo0 = x[0][c2], hi0 = x[1][c2], lo1 = x[2][c2], hi1 = x[3][c2];
                 xh[((2 * c2) * 64 + lane) * 2] = make_uint2(__builtin_amdgcn_perm(hi0, lo0, 0x05040100u),
                                                             __builtin_amdgcn_perm(hi1, lo1, 0x05040100u));
                 xh[((2 * c2 + 1) * 64 + lane) * 2] = make_uint2(__builtin_amdgcn_perm(hi0, lo0, 0x07060302u),
@@ -699,7 +921,7 @@ struct WidePipe {
     // fills the matrix pipe as it is, and what is kept alive across them costs more (64 queries x 4 heads, reasoning tree
     // of two-term weights, 22.6 us with the branch, 24.7 without; 256 queries, 286-token root, 29.5 and 33.3).
     template <bool PRECISE, bool WHOLE>
-    __device__ __forceinline__ void step(S &sh, const ChunkCtx &c, u32x4 *xs, int t, int lane, int blk, int nblk,
+    __device__ __forceinline__ void step(S &sh, const ChunkCtx<C> &c, u32x4 *xs, int t, int lane, int blk, int nblk,
                                          TileState<D> (&ts)[NT], f32x4 (&sacc)[NT][2], u32x4 (&vreg)[8], float cs,
                                          float inv_cs, bool fresh = false) {
         exchange(sh, c, xs, t, lane, blk + DEPTH, nblk);
@@ -722,7 +944,7 @@ struct WidePipe {
     }
 
     template <bool PRECISE>
-    __device__ __forceinline__ void run(const ChunkCtx &ctx, u32x4 *xbuf, int wave, int lane, int nblk,
+    __device__ __forceinline__ void run(const ChunkCtx<C> &ctx, u32x4 *xbuf, int wave, int lane, int nblk,
                                         TileState<D> (&ts)[NT], float cs, float inv_cs) {
         const int t = wave;
         constexpr int STAGE = S::NSLOT * 64;  // u32x4 per LDS exchange stage; stage (blk & 1) holds block blk
@@ -797,17 +1019,17 @@ struct ResidentLds {
     static_assert(4 * kResidentTokens<D> <= kRows, "piece records are parked in the merge buffers");
 };
 
-template <int D>
+template <int D, typename C>
 struct ResidentTask {
     static constexpr int KK = D / 32, VW = D / 16, NB = kResidentBlocks<D>;
     bf16x8 k[NB][2][KK];  // A operand of S^T = K Q^T, as in KVRegs
     u32x4 vt[NB][VW];     // A operand of product c' of O^T += V^T P^T: row n16 of it is d = VW * n16 + c'
     bf16x8 q[KK];
-    typedef __attribute__((ext_vector_type(VW / 2))) uint32_t vrow;  // VW values of one token, as loaded
+    typedef __attribute__((ext_vector_type(VW / 2))) uint32_t vrow;  // VW values of one token
 
     // Blocks 0..NA-1 of this wave.  Positions past the chunk's end repeat its last row (their scores are masked).
     template <int NA>
-    __device__ __forceinline__ void load(vrow (&v)[NA][8], const ChunkCtx &c, const uint16_t *k_lane, const uint16_t *v_lane,
+    __device__ __forceinline__ void load(vrow (&v)[NA][8], const ChunkCtx<Bf16Cache> &c, const uint16_t *k_lane, const uint16_t *v_lane,
                                          int wave) {
 #pragma unroll
         for (int b = 0; b < NA; ++b) {
@@ -825,6 +1047,49 @@ struct ResidentTask {
             }
         }
     }
+    // Of an 8-bit cache: first all loads, then what is made of them.
+    template <int NA>
+    __device__ __forceinline__ void load(vrow (&v)[NA][8], const ChunkCtx<E4m3Cache> &c, const uint8_t *k_lane, const uint8_t *v_lane,
+                                         int wave) {
+        typedef std::conditional_t<D == 128, u32x2, uint32_t> vbytes;  // VW values
+        u32x4 kb[NA][2][D / 64];
+        vbytes vb[NA][8];
+        uint32_t ks[NA][2], vs[NA][2];
+#pragma unroll
+        for (int b = 0; b < NA; ++b) {
+            const int x0 = 32 * (wave + kWaves * b);
+#pragma unroll
+            for (int aa = 0; aa < 2; ++aa) {
+                const int row = tok_row(c, min(x0 + 16 * aa + c.n16, c.clen - 1));
+                const uint8_t *kp = k_lane + (size_t)row * c.row_stride;
+#pragma unroll
+                for (int i = 0; i < D / 64; ++i) kb[b][aa][i] = load16_kv<false>(kp + 64 * i);
+                ks[b][aa] = c.scales.key(row);
+                vs[b][aa] = c.scales.value(tok_row(c, min(x0 + 16 * aa + 4 * c.g + (c.n16 & 3), c.clen - 1)));
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int x = min(x0 + 16 * (j >> 2) + 4 * c.g + (j & 3), c.clen - 1);
+                vb[b][j] = *reinterpret_cast<const vbytes *>(v_lane + (size_t)tok_row(c, x) * c.row_stride);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int b = 0; b < NA; ++b)
+#pragma unroll
+            for (int aa = 0; aa < 2; ++aa) {
+                widen_k<D>(kb[b][aa], ks[b][aa], k[b][aa]);
+                const float scale[4] = {scale_of_token<0>(vs[b][aa]), scale_of_token<1>(vs[b][aa]), scale_of_token<2>(vs[b][aa]),
+                                        scale_of_token<3>(vs[b][aa])};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if constexpr (D == 128)
+                        v[b][4 * aa + i] = widen8(vb[b][4 * aa + i], scale[i]);
+                    else
+                        v[b][4 * aa + i] = widen4(vb[b][4 * aa + i], scale[i]);
+                }
+            }
+    }
     // 2x2 interleave of token pairs, see pv_block; done once for all tiles
     template <int NA>
     __device__ __forceinline__ void interleave(const vrow (&v)[NA][8]) {
@@ -841,13 +1106,13 @@ struct ResidentTask {
     }
     __device__ __forceinline__ void load_q(const uint16_t *q_lane, int row) {
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk) q[kk] = __builtin_bit_cast(bf16x8, load16(q_lane + (size_t)row * D + 32 * kk));
+        for (int kk = 0; kk < KK; ++kk) q[kk] = __builtin_bit_cast(bf16x8, load16(q_lane + (size_t)row * D + C::q_step(kk)));
     }
 
     // One wave's share of one tile: scores of its NA blocks, softmax over them, products, into the merge buffer.
     // `between` runs once the scores are under way: the sum over the waves of the tile before.
     template <int NA, bool MASK, bool PRECISE, typename F>
-    __device__ __forceinline__ void tile(const ChunkCtx &c, int wave, int qpos, int vis_lo, int vis_hi, const uint16_t *q_lane,
+    __device__ __forceinline__ void tile(const ChunkCtx<C> &c, int wave, int qpos, int vis_lo, int vis_hi, const uint16_t *q_lane,
                                          int next_row, float cs, float *buf, F &&between) {
         const u32x4 one4 = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};  // eight bf16 1.0
         const bf16x8 ones = __builtin_bit_cast(bf16x8, one4);
@@ -922,7 +1187,7 @@ struct ResidentTask {
     }
 
     // this wave's part of a tile's result: the lane owns d in [D/4 * g, D/4 * (g+1)) of row n16, d = VW * (4g + i) + c'
-    __device__ __forceinline__ void publish(const ChunkCtx &c, int wave, const f32x4 (&o)[VW], float m, float l, float *buf) {
+    __device__ __forceinline__ void publish(const ChunkCtx<C> &c, int wave, const f32x4 (&o)[VW], float m, float l, float *buf) {
         float *dst = buf + (wave * 16 + c.n16) * ResidentLds<D>::kPitch + (D / 4) * c.g;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -938,7 +1203,7 @@ struct ResidentTask {
     // The tiles of the task, one barrier each: a wave writes its part of tile t, and adds up four rows of that tile
     // while it works on tile t + 1 in the other buffer.
     template <int NA, bool MASK, bool PRECISE, bool SHARED>
-    __device__ __forceinline__ LeftRows run(const Stage1Args &a, const ChunkCtx &c, float *lds, int wave, int lane, int ntiles,
+    __device__ __forceinline__ LeftRows run(const Stage1Args &a, const ChunkCtx<C> &c, float *lds, int wave, int lane, int ntiles,
                                             int rows, const uint16_t *q_lane, int vis_lo, int vis_hi) {
         using L = ResidentLds<D>;
         const int32_t *row_q = reinterpret_cast<const int32_t *>(lds + L::kRows), *row_pos = row_q + kTaskRows;
@@ -1009,8 +1274,17 @@ struct ResidentTask {
     }
 };
 
-template <int D, bool PRECISE, bool SHARED>
-__device__ __forceinline__ LeftRows resident_task(const Stage1Args &a, const int32_t *it, int h, unsigned char *s_raw) {
+__device__ __forceinline__ const uint16_t *cache_k(const Stage1Args &a) { return a.k; }
+__device__ __forceinline__ const uint16_t *cache_v(const Stage1Args &a) { return a.v; }
+__device__ __forceinline__ const uint8_t *cache_k(const E4m3Cache::Args &a) { return a.k8; }
+__device__ __forceinline__ const uint8_t *cache_v(const E4m3Cache::Args &a) { return a.v8; }
+__device__ __forceinline__ void set_scales(Bf16Cache::Scales &, const Stage1Args &, int) {}
+__device__ __forceinline__ void set_scales(E4m3Cache::Scales &s, const E4m3Cache::Args &a, int h) {
+    s = {a.k_scale + h, a.v_scale + h, a.block_shift, a.Hkv};
+}
+
+template <int D, bool PRECISE, bool SHARED, typename C>
+__device__ __forceinline__ LeftRows resident_task(const typename C::Args &a, const int32_t *it, int h, unsigned char *s_raw) {
     using L = ResidentLds<D>;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -1023,7 +1297,8 @@ __device__ __forceinline__ LeftRows resident_task(const Stage1Args &a, const int
     uint32_t *row_out = reinterpret_cast<uint32_t *>(row_pos + kTaskRows), *row_rec = row_out + kTaskRows;
     int32_t *s_row = reinterpret_cast<int32_t *>(lds + L::kTokens), *s_qlo = s_row + kResidentTokens<D>,
             *s_qhi = s_qlo + kResidentTokens<D>;
-    ChunkCtx c{};
+    ChunkCtx<C> c{};
+    set_scales(c.scales, a, h);
     c.row_stride = (size_t)a.Hkv * D;
     c.s_row = s_row;
     c.s_qlo = s_qlo;
@@ -1035,8 +1310,9 @@ __device__ __forceinline__ LeftRows resident_task(const Stage1Args &a, const int
     c.g = lane >> 4;
     const int nblk = (c.clen + 31) >> 5;
     const int rows = min(16 * ntiles, width * a.G - 16 * tile0);  // of this task
-    const uint16_t *k_lane = a.k + (size_t)h * D + 8 * c.g, *v_lane = a.v + (size_t)h * D + (D / 16) * c.n16;
-    const uint16_t *q_lane = a.q + 8 * c.g;
+    const typename C::elem *k_lane = cache_k(a) + (size_t)h * D + C::q_lane(c.g),
+                            *v_lane = cache_v(a) + (size_t)h * D + (D / 16) * c.n16;
+    const uint16_t *q_lane = a.q + C::q_lane(c.g);
 
     // The rows of the task: where Q comes from and where the partial result goes (rows past the end repeat the last).
     // One thread per row; the query index is asked for here and waited for in finish_rows, behind the K/V loads.
@@ -1090,11 +1366,11 @@ __device__ __forceinline__ LeftRows resident_task(const Stage1Args &a, const int
         }
     }
 
-    ResidentTask<D> T;
+    ResidentTask<D, C> T;
     LeftRows left;
     auto go = [&](auto na) {
         constexpr int NA = decltype(na)::value;
-        typename ResidentTask<D>::vrow v[NA > 0 ? NA : 1][8];
+        typename ResidentTask<D, C>::vrow v[NA > 0 ? NA : 1][8];
         if constexpr (NA > 0) T.template load<NA>(v, c, k_lane, v_lane, wave);
         if (nseg == 1) {  // (the K/V loads needed no table: they are under way)
             finish_rows();
@@ -1147,8 +1423,8 @@ __device__ __forceinline__ LeftRows resident_task(const Stage1Args &a, const int
 // reaches the workspace.
 //
 // PRECISE selects two-term softmax weights (see compute_block).
-template <int D, bool PRECISE, bool SHARED>
-__device__ __forceinline__ LeftRows streaming_task(const Stage1Args &a, const int32_t *it, int h, unsigned char *s_raw) {
+template <int D, bool PRECISE, bool SHARED, typename C>
+__device__ __forceinline__ LeftRows streaming_task(const typename C::Args &a, const int32_t *it, int h, unsigned char *s_raw) {
     constexpr int KK = D / 32;  // k-steps of the Q.K^T contraction
     // The P.V product runs as 8 MFMAs per block (a lane loads 8 d of V per token).  With D = 64 lanes
     // n16 >= 8 repeat the loads of n16 - 8 and half of each product is discarded; that shape only occurs
@@ -1177,14 +1453,15 @@ __device__ __forceinline__ LeftRows streaming_task(const Stage1Args &a, const in
     const int clen = it[deft::kItLen];
     const int TR = ntiles <= 1 ? 1 : (ntiles == 2 ? 2 : 4);  // waves that split the rows; 4 / TR token parts
 
-    ChunkCtx ctx;
+    ChunkCtx<C> ctx;
+    set_scales(ctx.scales, a, h);
     ctx.row_stride = (size_t)a.Hkv * D;
-    ctx.kbase = a.k + (size_t)h * D + 8 * g;
-    ctx.vbase = a.v + (size_t)h * D + 8 * (D == 128 ? n16 : (n16 & 7));
-    ctx.khead = a.k + (size_t)h * D;
-    ctx.vhead = a.v + (size_t)h * D;
+    ctx.kbase = cache_k(a) + (size_t)h * D + C::q_lane(g);
+    ctx.vbase = cache_v(a) + (size_t)h * D + 8 * (D == 128 ? n16 : (n16 & 7));
+    ctx.khead = cache_k(a) + (size_t)h * D;
+    ctx.vhead = cache_v(a) + (size_t)h * D;
     ctx.klane = 16u * g;
-    ctx.vlane = 16u * (D == 128 ? n16 : (n16 & 7));
+    ctx.vlane = 8u * sizeof(typename C::elem) * (D == 128 ? n16 : (n16 & 7));
     ctx.s_row = s_row;
     ctx.s_qlo = s_qlo;
     ctx.s_qhi = s_qhi;
@@ -1261,10 +1538,10 @@ __device__ __forceinline__ LeftRows streaming_task(const Stage1Args &a, const in
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             if (u >= ntw) break;
-            const uint16_t *qp = a.q + ((size_t)q_user[u] * a.Hq + (size_t)h * a.G + q_head[u]) * D + 8 * g;
+            const uint16_t *qp = a.q + ((size_t)q_user[u] * a.Hq + (size_t)h * a.G + q_head[u]) * D + C::q_lane(g);
 #pragma unroll
             for (int kk = 0; kk < KK; ++kk)
-                ts[u].q[kk] = __builtin_bit_cast(bf16x8, ts[u].qpos >= 0 ? load16(qp + 32 * kk) : z);
+                ts[u].q[kk] = __builtin_bit_cast(bf16x8, ts[u].qpos >= 0 ? load16(qp + C::q_step(kk)) : z);
         }
         __builtin_amdgcn_s_waitcnt(0);  // vmcnt(0) expcnt(0) lgkmcnt(0)
     };
@@ -1272,32 +1549,32 @@ __device__ __forceinline__ LeftRows streaming_task(const Stage1Args &a, const in
     TileState<D>(&ts1)[1] = reinterpret_cast<TileState<D>(&)[1]>(ts);  // the one-tile paths use ts[0] only
 
     if (TR == 1) {
-        SplitPipe<D> pipe;
+        SplitPipe<D, C> pipe;
         pipe.prime(ctx, wave, nblk);
         load_q(1);
         pipe.template run<PRECISE>(ctx, wave, nblk, ts1, a.c);
     } else if (TR == 2) {
-        SharedPipe<D, 2, 1> pipe;
+        SharedPipe<D, 2, 1, C> pipe;
         pipe.prime(ctx, wave, nblk);
         load_q(1);
         pipe.template run<PRECISE>(ctx, xbuf, wave, lane, nblk, ts1, a.c, inv_cs);
     } else if (NTW == 1 && ctx.uniform) {
-        WidePipe<D, 1, D == 128, 1> pipe;
+        WidePipe<D, 1, D == 128, 1, C> pipe;
         pipe.prime(ctx, wave, nblk);
         load_q(1);
         pipe.template run<PRECISE>(ctx, xbuf, wave, lane, nblk, ts1, a.c, inv_cs);
     } else if (NTW == 1) {
-        WidePipe<D, 1, false, 1> pipe;
+        WidePipe<D, 1, false, 1, C> pipe;
         pipe.prime(ctx, wave, nblk);
         load_q(1);
         pipe.template run<PRECISE>(ctx, xbuf, wave, lane, nblk, ts1, a.c, inv_cs);
     } else if (ctx.uniform) {
-        WidePipe<D, 2, D == 128, 2> pipe;  // the fast addressing is written for four loads per K loader
+        WidePipe<D, 2, D == 128, 2, C> pipe;  // the fast addressing is written for four loads per K loader
         pipe.prime(ctx, wave, nblk);
         load_q(2);
         pipe.template run<PRECISE>(ctx, xbuf, wave, lane, nblk, ts, a.c, inv_cs);
     } else {
-        WidePipe<D, 2, false, 2> pipe;
+        WidePipe<D, 2, false, 2, C> pipe;
         pipe.prime(ctx, wave, nblk);
         load_q(2);
         pipe.template run<PRECISE>(ctx, xbuf, wave, lane, nblk, ts, a.c, inv_cs);
@@ -1403,9 +1680,10 @@ __device__ __forceinline__ bool is_resident(const Stage1Args &a, const int32_t *
            it[deft::kItNTiles] <= (D == 128 && it[deft::kItPieces] == 1 ? a.resident_one : a.resident_many);
 }
 
-template <int D, bool PRECISE, bool SHARED>
-__device__ __forceinline__ LeftRows run_task(const Stage1Args &a, const int32_t *it, int h, unsigned char *s_raw) {
-    return is_resident<D>(a, it) ? resident_task<D, PRECISE, SHARED>(a, it, h, s_raw) : streaming_task<D, PRECISE, SHARED>(a, it, h, s_raw);
+template <int D, bool PRECISE, bool SHARED, typename C>
+__device__ __forceinline__ LeftRows run_task(const typename C::Args &a, const int32_t *it, int h, unsigned char *s_raw) {
+    return is_resident<D>(a, it) ? resident_task<D, PRECISE, SHARED, C>(a, it, h, s_raw)
+                                 : streaming_task<D, PRECISE, SHARED, C>(a, it, h, s_raw);
 }
 
 // A run of several chunks with the same queries leaves its result in the slots of the first and marks those of the others
@@ -1478,7 +1756,6 @@ __device__ __forceinline__ void store_out(const Stage2Args &a, size_t at, f32x4 
     if (a.out_f32) {
         *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(a.out) + at) = x;
     } else {
-        typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
         u32x2 pk = {pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
         *reinterpret_cast<u32x2 *>(reinterpret_cast<uint16_t *>(a.out) + at) = pk;
     }
@@ -1612,11 +1889,12 @@ constexpr uint32_t kReduceGroups = 8;
 constexpr int kReduceLoads = 16;  // loads of a wave in flight, each of 16 bytes a lane: 32 partial results at d = 128, 64 at d = 64
 
 // Plan query p, query head qh: the list of its partial results.
+template <typename C>
 struct RowParts {
-    const CallArgs &call;
+    const CallArgs<C> &call;
     const int32_t *rec;
     int n, q_user, s0, qh, kvh, lane, first;  // first: slot of partial result `lane`, where the record holds one
-    __device__ __forceinline__ RowParts(const CallArgs &c, int p, int head, int l) : call(c), qh(head), lane(l) {
+    __device__ __forceinline__ RowParts(const CallArgs<C> &c, int p, int head, int l) : call(c), qh(head), lane(l) {
         rec = c.s2.q_head + (size_t)p * c.s2.head_ints;
         first = rec[min(deft::kQueryHeadFixed + lane, c.s2.head_ints - 1)];
         n = rec[0], q_user = rec[1], s0 = rec[2];
@@ -1668,11 +1946,11 @@ struct RowParts {
 };
 
 // Merges a row whose partial results are all there.
-template <int D>
-__device__ __forceinline__ void merge_row(const RowParts &row) {
+template <int D, typename C>
+__device__ __forceinline__ void merge_row(const RowParts<C> &row) {
     using R = Stage2Row<D>;
     constexpr int kLoads = kReduceLoads;
-    const CallArgs &call = row.call;
+    const CallArgs<C> &call = row.call;
     const Stage2Args &a = call.s2;
     const int lane = row.lane, n = row.n, qh = row.qh;
     const int sub = lane / R::kLanes, col = lane - sub * R::kLanes;
@@ -1729,24 +2007,24 @@ __device__ __forceinline__ void merge_row(const RowParts &row) {
 }
 
 // Stage 2's waves.
-template <int D>
-__device__ __forceinline__ void reduce_rows(const CallArgs &call, uint32_t group, uint32_t groups) {
+template <int D, typename C>
+__device__ __forceinline__ void reduce_rows(const CallArgs<C> &call, uint32_t group, uint32_t groups) {
     const Stage2Args &a = call.s2;
     const uint32_t rows = (uint32_t)a.nq * (uint32_t)a.Hq, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     for (uint32_t r = kWaves * group + wave; r < rows; r += kWaves * groups) {
         const int p = divide(r, a.Hq, a.inv_Hq);
-        const RowParts row(call, p, r - p * a.Hq, threadIdx.x & 63);
+        const RowParts<C> row(call, p, r - p * a.Hq, threadIdx.x & 63);
         if (row.complete(call.polls) || row.leave()) merge_row<D>(row);
     }
 }
 
 // A wave of stage 1 to which rows of its task were left.
-template <int D>
-__device__ __forceinline__ void merge_left_rows(const CallArgs &call, const int32_t *it, int h, const LeftRows &x) {
+template <int D, typename C>
+__device__ __forceinline__ void merge_left_rows(const CallArgs<C> &call, const int32_t *it, int h, const LeftRows &x) {
     const int G = call.s1.G, first = 16 * it[deft::kItTile0];
     for (uint64_t left = __ballot(x.left); left; left &= left - 1) {
         const int r = first + __builtin_amdgcn_readlane(x.row, __builtin_ctzll(left)), pl = divide(r, G, call.s1.inv_G);
-        const RowParts row(call, it[deft::kItQlo] + pl, h * G + r - pl * G, threadIdx.x & 63);
+        const RowParts<C> row(call, it[deft::kItQlo] + pl, h * G + r - pl * G, threadIdx.x & 63);
         if (row.leave()) merge_row<D>(row);
     }
 }
@@ -1754,14 +2032,14 @@ __device__ __forceinline__ void merge_left_rows(const CallArgs &call, const int3
 // SHARED: a whole call in one launch, stage 2 included.
 //   items   deft::kItemInts int32 per work item, see deft_internal.h
 //   tasks   workgroups of stage 1
-template <int D, int WEIGHTS, bool SHARED>
-__global__ __launch_bounds__(64 * kWaves, 2) void deft_stage1(const int32_t *items, uint32_t Hkv, uint32_t inv_Hkv, uint32_t tasks, CallArgs call) {
+template <int D, int WEIGHTS, bool SHARED, typename C>
+__global__ __launch_bounds__(64 * kWaves, 2) void deft_stage1(const int32_t *items, uint32_t Hkv, uint32_t inv_Hkv, uint32_t tasks, CallArgs<C> call) {
     extern __shared__ __attribute__((aligned(16))) unsigned char s_raw[];
     if (SHARED && blockIdx.x >= tasks) {
         reduce_rows<D>(call, blockIdx.x - tasks, gridDim.x - tasks);
         return;
     }
-    const Stage1Args &a = call.s1;
+    const typename C::Args &a = call.s1;
     const int item = divide(blockIdx.x, Hkv, inv_Hkv);
     // KV head of this workgroup.  Workgroups b and b + 256 land on the same compute unit (the dispatcher goes
     // round the 256 units), and with Hkv dividing 256 they would stream the same head: K and V rows whose
@@ -1772,8 +2050,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void deft_stage1(const int32_t *ite
     const int h = turned - divide(turned, Hkv, inv_Hkv) * Hkv;
     const int32_t *it = items + (size_t)item * deft::kItemInts;
     if (it[deft::kItChunks] > 1) mark_empty(a, it, h);  // (first: behind the task its descriptor would have to be read again)
-    const LeftRows left = WEIGHTS == kTwoTerm || (WEIGHTS == kMixed && it[deft::kItPrecise]) ? run_task<D, true, SHARED>(a, it, h, s_raw)
-                                                                                              : run_task<D, false, SHARED>(a, it, h, s_raw);
+    const LeftRows left = WEIGHTS == kTwoTerm || (WEIGHTS == kMixed && it[deft::kItPrecise]) ? run_task<D, true, SHARED, C>(a, it, h, s_raw)
+                                                                                              : run_task<D, false, SHARED, C>(a, it, h, s_raw);
     if (SHARED && __any(left.left)) merge_left_rows<D>(call, it, h, left);
 }
 
@@ -1832,29 +2110,30 @@ bool hip_ok(hipError_t e, const char *what) {
 
 // The kernels may use more than the default 64 KB of dynamic LDS: the limit of all variants is raised once
 // per device, at the first call that launches one of them.
-template <int D>
+template <int D, typename C>
 bool configure_stage1() {
-    static std::atomic<uint64_t> configured;  // bit i set: done on device i (one flag per head dimension)
+    static std::atomic<uint64_t> configured;  // bit i set: done on device i (one flag per head dimension and cache type)
     int dev = 0;
     if (!hip_ok(hipGetDevice(&dev), "hipGetDevice")) return false;
     if (dev >= 0 && dev < 64 && ((configured.load(std::memory_order_acquire) >> dev) & 1)) return true;
     const int bytes = kXbufBytes + 3 * DEFT_MAX_CHUNK * (int)sizeof(int32_t);
     static_assert(ResidentLds<D>::kWords * 4 <= kXbufBytes + 3 * DEFT_MAX_CHUNK * (int)sizeof(int32_t), "LDS limit");
-    for (const void *f : {reinterpret_cast<const void *>(&deft_stage1<D, kBf16, false>),
-                          reinterpret_cast<const void *>(&deft_stage1<D, kTwoTerm, false>),
-                          reinterpret_cast<const void *>(&deft_stage1<D, kMixed, false>),
-                          reinterpret_cast<const void *>(&deft_stage1<D, kBf16, true>),
-                          reinterpret_cast<const void *>(&deft_stage1<D, kTwoTerm, true>),
-                          reinterpret_cast<const void *>(&deft_stage1<D, kMixed, true>)})
+    for (const void *f : {reinterpret_cast<const void *>(&deft_stage1<D, kBf16, false, C>),
+                          reinterpret_cast<const void *>(&deft_stage1<D, kTwoTerm, false, C>),
+                          reinterpret_cast<const void *>(&deft_stage1<D, kMixed, false, C>),
+                          reinterpret_cast<const void *>(&deft_stage1<D, kBf16, true, C>),
+                          reinterpret_cast<const void *>(&deft_stage1<D, kTwoTerm, true, C>),
+                          reinterpret_cast<const void *>(&deft_stage1<D, kMixed, true, C>)})
         if (!hip_ok(hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, bytes), "deft_stage1 LDS size")) return false;
     if (dev >= 0 && dev < 64) configured.fetch_or(1ull << dev, std::memory_order_release);
     return true;
 }
 
-template <int D, bool SHARED>
-bool launch_stage1(const deft::TaskSet &T, CallArgs a, unsigned reduce_groups, const uint8_t *image, hipStream_t stream) {
+// two_term: for every task
+template <int D, bool SHARED, typename C>
+bool launch_stage1(const deft::TaskSet &T, CallArgs<C> a, unsigned reduce_groups, bool two_term, const uint8_t *image, hipStream_t stream) {
     if (T.n_items == 0) return true;
-    if (!configure_stage1<D>()) return false;
+    if (!configure_stage1<D, C>()) return false;
     Stage1Args &a1 = a.s1;
     const int32_t *items = reinterpret_cast<const int32_t *>(image + T.off_items);
     a1.n_items = T.n_items;
@@ -1862,9 +2141,9 @@ bool launch_stage1(const deft::TaskSet &T, CallArgs a, unsigned reduce_groups, c
     a1.resident_many = deft::kMaxTilesPerTask;
     const size_t lds = std::max(kXbufBytes + 3 * (size_t)a1.table_len * sizeof(int32_t), (size_t)ResidentLds<D>::kWords * 4);
     const uint32_t Hkv = (uint32_t)a1.Hkv, tasks = (uint32_t)T.n_items * Hkv;
-    auto *kernel = T.n_items_precise == 0           ? &deft_stage1<D, kBf16, SHARED>
-                   : T.n_items_precise == T.n_items ? &deft_stage1<D, kTwoTerm, SHARED>
-                                                    : &deft_stage1<D, kMixed, SHARED>;
+    auto *kernel = two_term || T.n_items_precise == T.n_items ? &deft_stage1<D, kTwoTerm, SHARED, C>
+                   : T.n_items_precise == 0                   ? &deft_stage1<D, kBf16, SHARED, C>
+                                                              : &deft_stage1<D, kMixed, SHARED, C>;
     hipLaunchKernelGGL(kernel, dim3(tasks + reduce_groups), dim3(64 * kWaves), lds, stream, items, Hkv, inverse(Hkv), tasks, a);
     return hip_ok(hipGetLastError(), "deft_stage1 launch");
 }
@@ -1901,6 +2180,8 @@ struct Call {
     float *marks = nullptr;  // null: the workspace has no room for them
     float c = 0.f;
     hipStream_t stream = nullptr;
+    const deft_cache_q8_t *cache = nullptr;  // of a call on an 8-bit cache
+    bool two_term = false;  // weights of every task in two terms
 };
 
 // The tasks of a whole call.  Chunks are cut anew into as many runs as the KV heads of the first upload ask for; with fewer heads
@@ -1978,15 +2259,30 @@ bool stage1_inputs_ok(const void *q, const void *k, const void *v) {
     return q && k && v && aligned16(q) && aligned16(k) && aligned16(v);
 }
 
+void cache_args(const Call &, Stage1Args &) {}
+void cache_args(const Call &call, E4m3Cache::Args &a) {
+    a.k8 = static_cast<const uint8_t *>(call.cache->k);
+    a.v8 = static_cast<const uint8_t *>(call.cache->v);
+    a.k_scale = static_cast<const uint8_t *>(call.cache->k_scale);
+    a.v_scale = static_cast<const uint8_t *>(call.cache->v_scale);
+    a.block_shift = __builtin_ctz((unsigned)call.cache->block_rows);
+}
+
+template <bool SHARED, typename C>
+bool launch_stage1(const deft::TaskSet &T, const CallArgs<C> &a, unsigned groups, const Call &call, int32_t d) {
+    return d == 128 ? launch_stage1<128, SHARED, C>(T, a, groups, call.two_term, call.img, call.stream)
+                    : launch_stage1<64, SHARED, C>(T, a, groups, call.two_term, call.img, call.stream);
+}
+
+template <typename C>
 int run_stage1(const deft_plan_t *plan, const Call &call, const deft::TaskSet &T, const void *q, const void *k, const void *v, int32_t Hq,
                int32_t Hkv, int32_t d) {
     if (plan->n_chunks() == 0) return DEFT_OK;
     if (!stage1_inputs_ok(q, k, v)) return DEFT_EINVAL;
-    CallArgs a{};
+    CallArgs<C> a{};
     stage1_args(call, q, k, v, Hq, Hkv, a.s1);
-    const bool ok = d == 128 ? launch_stage1<128, false>(T, a, 0, call.img, call.stream)
-                             : launch_stage1<64, false>(T, a, 0, call.img, call.stream);
-    return ok ? DEFT_OK : DEFT_EHIP;
+    cache_args(call, a.s1);
+    return launch_stage1<false, C>(T, a, 0, call, d) ? DEFT_OK : DEFT_EHIP;
 }
 
 int run_stage2(const deft_plan_t *plan, const Call &call, const deft::TaskSet &T, void *o, int32_t Hq, int32_t d, uint32_t flags) {
@@ -2014,12 +2310,14 @@ uint64_t new_ticket() {
 }
 
 // Both stages in one launch.
+template <typename C>
 int run_call(const deft_plan_t *plan, const Call &call, const void *q, const void *k, const void *v, void *o, int32_t Hq,
              int32_t Hkv, int32_t d, uint32_t flags, int32_t polls) {
     if (!stage1_inputs_ok(q, k, v)) return DEFT_EINVAL;
     const deft::TaskSet &T = whole_call(call, Hkv, d);
-    CallArgs a{};
+    CallArgs<C> a{};
     stage1_args(call, q, k, v, Hq, Hkv, a.s1);
+    cache_args(call, a.s1);
     stage2_args(plan, call, T, o, Hq, flags, a.s2);
     a.s1.marks = call.marks;
     a.s1.ticket = new_ticket();
@@ -2027,9 +2325,7 @@ int run_call(const deft_plan_t *plan, const Call &call, const void *q, const voi
     a.polls = polls;
     const unsigned rows = (unsigned)plan->nq * (unsigned)Hq;
     const unsigned groups = std::min((rows + kWaves - 1) / kWaves, kReduceGroups);
-    const bool ok = d == 128 ? launch_stage1<128, true>(T, a, groups, call.img, call.stream)
-                             : launch_stage1<64, true>(T, a, groups, call.img, call.stream);
-    return ok ? DEFT_OK : DEFT_EHIP;
+    return launch_stage1<true, C>(T, a, groups, call, d) ? DEFT_OK : DEFT_EHIP;
 }
 
 // Whether what is enqueued on a stream now is recorded and run later, any number of times.  (The null stream's never is.)
@@ -2057,7 +2353,7 @@ bool one_launch(const deft_plan_t *plan, const Call &call, int32_t Hq, int32_t H
     const deft::TaskSet &T = whole_call(call, Hkv, d);
     if (!call.marks || plan->nq == 0 || T.n_items == 0) return false;
     const int64_t batch = d == 128 ? kReduceLoads * Stage2Row<128>::kRows : kReduceLoads * Stage2Row<64>::kRows;
-    const int64_t rows = (int64_t)plan->nq * Hq, parts = T.max_parts, bytes = (int64_t)plan->n_flat * Hkv * d * 4;
+    const int64_t rows = (int64_t)plan->nq * Hq, parts = T.max_parts, bytes = (int64_t)plan->n_flat * Hkv * d * (call.cache ? 2 : 4);
     const bool pays = rows <= kWavesOfRows ? (parts <= batch && bytes <= (40 << 20)) || (parts <= 2 * batch && bytes <= (16 << 20))
                                            : rows <= 2 * kWavesOfRows && 2 * parts <= batch && bytes <= (16 << 20);
     return pays && !is_captured(call.stream);
@@ -2163,6 +2459,19 @@ int upload_staged(void *dev_image, const uint8_t *src, size_t bytes, hipStream_t
 
 }  // namespace
 
+namespace deft {
+bool hip_ok(hipError_t e, const char *what) { return ::hip_ok(e, what); }
+
+int upload_image(void *dev_image, const uint8_t *src, size_t bytes, hipStream_t st) {
+    const int staged = upload_staged(dev_image, src, bytes, st);
+    if (staged != 0) return staged > 0 ? DEFT_OK : DEFT_EHIP;
+    // an image larger than a staging slot goes from the plan's own (pageable) copy, and the call waits for it
+    if (!::hip_ok(hipMemcpyAsync(dev_image, src, bytes, hipMemcpyHostToDevice, st), "plan upload")) return DEFT_EHIP;
+    if (!::hip_ok(hipStreamSynchronize(st), "plan upload sync")) return DEFT_EHIP;
+    return DEFT_OK;
+}
+}  // namespace deft
+
 extern "C" const char *deft_last_hip_error(void) { return g_hip_error.c_str(); }
 
 extern "C" int deft_hbm_read_probe(const void *dev_buf, size_t bytes, void *dev_sink, void *stream) {
@@ -2183,15 +2492,7 @@ extern "C" int deft_plan_upload(deft_plan_t *plan, int32_t Hq, int32_t Hkv, void
         return DEFT_ENOMEM;
     }
     if (bytes < S->bytes) return DEFT_EWORKSPACE;
-    hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    const int staged = upload_staged(dev_image, S->host_image.data(), S->bytes, st);
-    if (staged < 0) return DEFT_EHIP;
-    if (staged > 0) return DEFT_OK;
-    // an image larger than a staging slot goes from the plan's own (pageable) copy, and the call waits for it
-    if (!hip_ok(hipMemcpyAsync(dev_image, S->host_image.data(), S->bytes, hipMemcpyHostToDevice, st), "plan upload"))
-        return DEFT_EHIP;
-    if (!hip_ok(hipStreamSynchronize(st), "plan upload sync")) return DEFT_EHIP;
-    return DEFT_OK;
+    return deft::upload_image(dev_image, S->host_image.data(), S->bytes, reinterpret_cast<hipStream_t>(stream));
 }
 
 extern "C" int deft_stage1_partial_attention(const deft_plan_t *plan, const void *dev_image, const void *q,
@@ -2200,7 +2501,7 @@ extern "C" int deft_stage1_partial_attention(const deft_plan_t *plan, const void
     Call call;
     int rc = prepare(plan, dev_image, Hq, Hkv, d, scale, workspace, workspace_bytes, stream, call);
     if (rc != DEFT_OK) return rc;
-    return run_stage1(plan, call, call.S->by_chunk, q, k, v, Hq, Hkv, d);
+    return run_stage1<Bf16Cache>(plan, call, call.S->by_chunk, q, k, v, Hq, Hkv, d);
 }
 
 extern "C" int deft_stage2_global_reduction(const deft_plan_t *plan, const void *dev_image, void *o, int32_t Hq,
@@ -2213,16 +2514,21 @@ extern "C" int deft_stage2_global_reduction(const deft_plan_t *plan, const void 
 }
 
 namespace {
-int decode(const deft_plan_t *plan, const void *dev_image, const void *q, const void *k, const void *v, void *o, int32_t Hq, int32_t Hkv,
-           int32_t d, float scale, uint32_t flags, void *workspace, size_t workspace_bytes, void *stream, int32_t polls) {
+// cache: null for bf16 k and v
+template <typename C>
+int decode(const deft_plan_t *plan, const void *dev_image, const void *q, const void *k, const void *v, const deft_cache_q8_t *cache, void *o,
+           int32_t Hq, int32_t Hkv, int32_t d, float scale, uint32_t flags, void *workspace, size_t workspace_bytes, void *stream,
+           int32_t polls) {
     Call call;
+    call.cache = cache;
+    call.two_term = cache && flags == DEFT_OUT_F32;
     int rc = prepare(plan, dev_image, Hq, Hkv, d, scale, workspace, workspace_bytes, stream, call);
     if (rc != DEFT_OK) return rc;
     // check both stages' arguments before launching anything
     if (flags != DEFT_OUT_BF16 && flags != DEFT_OUT_F32) return DEFT_EINVAL;
     if (plan->nq > 0 && (!o || !aligned16(o))) return DEFT_EINVAL;
-    if (one_launch(plan, call, Hq, Hkv, d)) return run_call(plan, call, q, k, v, o, Hq, Hkv, d, flags, polls);
-    rc = run_stage1(plan, call, whole_call(call, Hkv, d), q, k, v, Hq, Hkv, d);
+    if (one_launch(plan, call, Hq, Hkv, d)) return run_call<C>(plan, call, q, k, v, o, Hq, Hkv, d, flags, polls);
+    rc = run_stage1<C>(plan, call, whole_call(call, Hkv, d), q, k, v, Hq, Hkv, d);
     if (rc != DEFT_OK) return rc;
     return run_stage2(plan, call, whole_call(call, Hkv, d), o, Hq, d, flags);
 }
@@ -2231,14 +2537,22 @@ int decode(const deft_plan_t *plan, const void *dev_image, const void *q, const 
 extern "C" int deft_tree_attn_decode(const deft_plan_t *plan, const void *dev_image, const void *q, const void *k,
                                      const void *v, void *o, int32_t Hq, int32_t Hkv, int32_t d, float scale,
                                      uint32_t flags, void *workspace, size_t workspace_bytes, void *stream) {
-    return decode(plan, dev_image, q, k, v, o, Hq, Hkv, d, scale, flags, workspace, workspace_bytes, stream, kMarkPolls);
+    return decode<Bf16Cache>(plan, dev_image, q, k, v, nullptr, o, Hq, Hkv, d, scale, flags, workspace, workspace_bytes, stream, kMarkPolls);
+}
+
+extern "C" int deft_tree_attn_decode_q8(const deft_plan_t *plan, const void *dev_image, const void *q, const deft_cache_q8_t *cache, void *o,
+                                        int32_t Hq, float scale, uint32_t flags, void *workspace, size_t workspace_bytes, void *stream) {
+    if (!plan || !deft::cache_ok(cache)) return DEFT_EINVAL;
+    if (deft_plan_rows(plan) > cache->n_rows) return DEFT_EINVAL;
+    return decode<E4m3Cache>(plan, dev_image, q, cache->k, cache->v, cache, o, Hq, cache->Hkv, cache->d, scale, flags, workspace,
+                             workspace_bytes, stream, kMarkPolls);
 }
 
 extern "C" int deft_decode_polls(const deft_plan_t *plan, const void *dev_image, const void *q, const void *k, const void *v, void *o,
                                  int32_t Hq, int32_t Hkv, int32_t d, float scale, uint32_t flags, void *workspace,
                                  size_t workspace_bytes, void *stream, int32_t polls) {
     if (polls < 1 || polls > kMarkPolls) return DEFT_EINVAL;
-    return decode(plan, dev_image, q, k, v, o, Hq, Hkv, d, scale, flags, workspace, workspace_bytes, stream, polls);
+    return decode<Bf16Cache>(plan, dev_image, q, k, v, nullptr, o, Hq, Hkv, d, scale, flags, workspace, workspace_bytes, stream, polls);
 }
 
 namespace {

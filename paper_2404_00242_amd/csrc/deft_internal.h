@@ -1,6 +1,7 @@
 // Internal definitions shared by the planner (host C++) and the decode launcher (HIP).
 #pragma once
 
+#include <atomic>
 #include <cstdint>
 #include <map>
 #include <mutex>
@@ -124,6 +125,8 @@ struct deft_plan_s {
     int32_t n_chunks() const { return (int32_t)chunk_qlo.size(); }
     int32_t n_segs() const { return (int32_t)seg_len.size(); }
     int32_t n_slots() const { return chunk_slot_base.empty() ? 0 : chunk_slot_base.back(); }
+
+    mutable std::atomic<int64_t> rows{-1};  // see deft_plan_rows; -1: not asked for yet
 
     // schedules by G, built on demand (the canonical arrays above never change)
     mutable std::mutex mu;

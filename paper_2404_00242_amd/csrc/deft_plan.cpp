@@ -676,9 +676,13 @@ extern "C" int deft_plan_view(const deft_plan_t *P, deft_plan_view_t *out) {
 }
 
 extern "C" int64_t deft_plan_rows(const deft_plan_t *P) {
-    int64_t rows = 0;
-    if (P)
+    if (!P) return 0;
+    int64_t rows = P->rows.load(std::memory_order_relaxed);
+    if (rows < 0) {  // (a plan never changes)
+        rows = 0;
         for (int32_t s = 0; s < P->n_segs(); ++s) rows = std::max(rows, (int64_t)P->seg_tok_begin[s] + P->seg_len[s]);
+        P->rows.store(rows, std::memory_order_relaxed);
+    }
     return rows;
 }
 

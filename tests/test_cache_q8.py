@@ -1,0 +1,547 @@
+"""The 8-bit KV cache on the GPU: what is stored and read back against the definition in 64 bits (oracle/cache_q8.py), bit for
+bit; attention over it against the fp64 oracle on the values that it holds; copies of pages; all of them together."""
+
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from oracle import cache_q8 as model
+from paper_2404_00242_amd import binding, workloads as wl
+
+pytestmark = pytest.mark.gpu
+
+
+def dev():
+    return torch.device("cuda:0")
+
+
+def new_cache(rows, Hkv, d, block, seed=0):
+    """A cache with earlier contents in every byte, NaN among them, and its model."""
+    rng = np.random.default_rng(seed)
+    c = binding.alloc_kv_cache_q8(rows, Hkv, d, block, dev())
+    m = {"block": block}
+    for which in ("k", "v"):
+        m[which] = rng.integers(0, 256, (rows, Hkv, d)).astype(np.uint8)
+        m[which + "_scale"] = rng.integers(model.SCALE_MIN, model.SCALE_MAX + 1, (-(-rows // block), Hkv)).astype(np.uint8)
+    put(c, m)
+    return c, m
+
+
+def put(c, m):
+    for which in ("k", "v", "k_scale", "v_scale"):
+        getattr(c, which).view(torch.uint8).copy_(torch.from_numpy(m[which]))
+
+
+def same_bytes(c, m):
+    """Equal to the model's bytes; of a NaN the sign is not defined."""
+    for which in ("k_scale", "v_scale", "k", "v"):
+        x = getattr(c, which).view(torch.uint8).cpu().numpy()
+        differ = x != m[which]
+        if which in "kv":
+            differ &= ((x & 127) != 127) | ((m[which] & 127) != 127)
+        assert not differ.any(), (which, np.argwhere(differ)[:5])
+
+
+def tokens(n, Hkv, d, seed, spread=3.0, special=True):
+    """bf16 K and V of very different magnitudes, as slices of one tensor; some rows of zeros, infinities, NaN, extremes."""
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn((n, 3, Hkv, d), generator=g) * torch.exp(spread * torch.randn((n, 3, Hkv, 1), generator=g))
+    if special and n > 12:
+        x[1, 1:] = 0
+        x[2, 1, 0, 3], x[3, 2, Hkv - 1, d - 1], x[4, 1, 0, 0] = float("inf"), float("nan"), -float("inf")
+        x[5, 1] *= 1e38 / x[5, 1].abs().max()
+        x[6, 2, 0, 7] = -3.38e38
+        x[7, 1:] *= 1e-38
+        x[8, 1:] *= 1e-30
+        x[9, 1] = torch.where(x[9, 1] > 0, 448.0, 1.0)  # on e4m3's values
+        x[10, 2] = 1.9375  # between two of them
+    x = x.to(torch.bfloat16)
+    return x[:, 1], x[:, 2]
+
+
+def to_gpu(k, v):
+    """Both on the GPU with the token stride that they have as slices."""
+    base = torch.empty((k.shape[0], 3) + tuple(k.shape[1:]), dtype=torch.bfloat16, device=dev())
+    base[:, 1], base[:, 2] = k.to(dev()), v.to(dev())
+    return base[:, 1], base[:, 2]
+
+
+def store_both(c, m, rows, k, v, stream=None):
+    lst = binding.deft_kv_rows(rows, c.k.shape[0], c.block_rows)
+    binding.deft_kv_store_q8(lst, *to_gpu(k, v), c, stream=stream)
+    model.store(m, rows, k.double().numpy(), v.double().numpy())
+    return lst
+
+
+# ---- rows in and out ----
+
+@pytest.mark.parametrize("block", [1, 2, 4, 8, 16, 32, 64])
+@pytest.mark.parametrize("Hkv,d", [(1, 64), (3, 64), (2, 128), (5, 128), (8, 128)])
+def test_store_is_the_definition_bit_for_bit(Hkv, d, block):
+    rows = 5 * 64 + 7  # the last block is short
+    c, m = new_cache(rows, Hkv, d, block, 3)
+    rng = np.random.default_rng([Hkv, d, block])
+    # a prompt in pages of any order, then tokens one by one and in groups behind what is there, loud ones among them
+    order = rng.permutation(rows // 64) * 64
+    filled = [[int(b), 0] for b in order] + [[320, 0]]
+    where = np.concatenate([np.arange(b, b + 37) for b, _ in filled[:3]])
+    store_both(c, m, where, *tokens(len(where), Hkv, d, 1))
+    same_bytes(c, m)
+    for f in filled[:3]:
+        f[1] = 37
+    for step in range(6):
+        at = []
+        for f, room in zip(filled, [64] * 5 + [7]):
+            n = int(min(room - f[1], rng.integers(0, 1 + 3 * (step % 2) + 1)))
+            at += [f[0] + f[1] + i for i in range(n)]
+            f[1] += n
+        at = np.array(at, dtype=np.int64)[rng.permutation(len(at))] if at else np.zeros(0, np.int64)
+        if len(at):
+            store_both(c, m, at, *tokens(len(at), Hkv, d, 10 + step, spread=4.0, special=step == 3))
+            same_bytes(c, m)
+
+
+@pytest.mark.parametrize("block,d", [(1, 64), (16, 128), (64, 64), (64, 128)])
+def test_one_token_and_none(block, d):
+    c, m = new_cache(70, 2, d, block, 5)
+    store_both(c, m, [69], *tokens(1, 2, d, 2))
+    same_bytes(c, m)
+    k = torch.zeros((0, 2, d), dtype=torch.bfloat16, device=dev())
+    binding.deft_kv_store_q8(binding.deft_kv_rows([], 70, block), k, k, c)
+    assert [x.shape[0] for x in binding.deft_kv_load_q8(binding.deft_kv_rows([], 70, block), c)] == [0, 0]
+    same_bytes(c, m)
+    # rows written a second time, the lowest of the block among them: what was there is forgotten
+    store_both(c, m, [64], *tokens(1, 2, d, 3))
+    store_both(c, m, [64, 65], *tokens(2, 2, d, 4))
+    same_bytes(c, m)
+
+
+def test_a_scale_that_grows_past_everything_kept():
+    # from the smallest scale to the largest: what was kept becomes zeros, signs stay, NaN stay
+    c, m = new_cache(32, 2, 128, 32, 6)
+    k, v = tokens(14, 2, 128, 7)
+    store_both(c, m, np.arange(14), torch.sign(k) * 1e-36, torch.sign(v) * 1e-36)
+    big = torch.full((1, 2, 128), 3e38, dtype=torch.bfloat16)
+    store_both(c, m, [14], big, -big)
+    same_bytes(c, m)
+    assert int(m["k_scale"].max()) == model.SCALE_MAX and (E := m["k"][0, 0] & 127).max() == 0 and E.size
+
+
+@pytest.mark.parametrize("Hkv,d,block", [(1, 64, 1), (5, 64, 8), (3, 128, 16), (8, 128, 64)])
+@pytest.mark.parametrize("n", [1, 17, 300])
+def test_load_gives_the_values_exactly(Hkv, d, block, n):
+    c, m = new_cache(333, Hkv, d, block, n)
+    m["v"] = np.where((m["v"] & 127) == 127, 0, m["v"]).astype(np.uint8)
+    put(c, m)
+    rows = np.random.default_rng(n).permutation(333)[:n]
+    lst = binding.deft_kv_rows(rows, 333, block)
+    k, v = binding.deft_kv_load_q8(lst, c)
+    assert k.dtype == torch.bfloat16
+    for got, which in ((k, "k"), (v, "v")):
+        want = model.values(m, which, rows)  # bf16 numbers: 0 is what they may be off
+        assert np.array_equal(got.double().cpu().numpy(), want, equal_nan=True)
+    into = torch.full((n, Hkv, d), 7.0, dtype=torch.bfloat16, device=dev())
+    lib = binding.load_library()
+    cs = binding._cache_struct(c, "")
+    img = lst.image(dev())
+    for kp, vp, which in ((into.data_ptr(), None, "k"), (None, into.data_ptr(), "v")):
+        assert lib.deft_kv_load_q8(lst.handle, img.data_ptr(), ctypes.byref(cs), kp, vp, torch.cuda.current_stream().cuda_stream) == 0
+        assert np.array_equal(into.double().cpu().numpy(), model.values(m, which, rows), equal_nan=True)
+
+
+# ---- attention ----
+
+def filled(t, block, seed, rows=None, paged=None, spread=0.4):
+    """(q, cache, its model, K and V of the tree's contiguous rows as the cache holds them) with seeded tokens in every row."""
+    Q, K, V = wl.make_qkv(t, seed)
+    g = torch.Generator().manual_seed(seed)
+    K = (K.float() * torch.exp(spread * torch.randn((t.ntok, t.Hkv, 1), generator=g))).to(torch.bfloat16)
+    row_of = np.arange(t.ntok) if paged is None else paged
+    owned = np.nonzero(row_of >= 0)[0]
+    c = binding.alloc_kv_cache_q8(rows or t.ntok, t.Hkv, t.d, block, dev())
+    for x in c[:2]:  # a NaN wherever no token is: such rows must not be read as tokens
+        x.view(torch.uint8).fill_(127)
+    lst = binding.deft_kv_rows(row_of[owned], rows or t.ntok, block)
+    binding.deft_kv_store_q8(lst, K[owned].to(dev()), V[owned].to(dev()), c)
+    kv = []
+    for x in binding.deft_kv_load_q8(lst, c):
+        full = torch.zeros((t.ntok, t.Hkv, t.d), dtype=torch.bfloat16)
+        full[owned] = x.cpu()
+        kv.append(full)
+    return Q, c, kv[0], kv[1]
+
+
+def bound(ref, ref_abs, f32):
+    """How far a result may be from the fp64 attention of the same values, as a share of the attention of |V|.  Weights in two
+    bf16 terms carry 2^-16 (the second term's rounding, 2^-8 of 2^-8) in numerator and denominator, 2^-15 together; in one term
+    2^-7 together.  Scores are fp32 sums of up to 128 products: their roundings, 2^-24 each, add up like sqrt(128) of them,
+    relative to |q||k| / sqrt(d) < 40 (|q| and |k| / 3.3 are about sqrt(d) here), 3e-5 in a weight, 6e-5 together.  Hence 2^-13
+    with two terms, 2^-7 + 2^-13 with one; a bf16 result is rounded by 2^-8 of itself."""
+    return (2.0 ** -13 + (0 if f32 else 2.0 ** -7)) * ref_abs + (0 if f32 else 2.0 ** -8) * np.abs(ref) + 1e-7
+
+
+def check(t, plan, Q, c, K, V, f32, scale=None, got=None):
+    if got is None:
+        got = binding.deft_tree_attn_decode_q8(plan, Q.to(dev()), c, out_dtype=torch.float32 if f32 else None, scale=scale or 0.0)
+    args = (t.node_tok_begin, t.node_tok_len, t.node_parent, t.query_node)
+    ref = oracle.tree_attention(Q, K, V, *args, scale=scale)
+    ref_abs = oracle.tree_attention(Q, K, V.abs(), *args, scale=scale)
+    x = got.double().cpu().numpy()
+    assert np.isfinite(x).all()
+    over = np.abs(x - ref) / bound(ref, ref_abs, f32)
+    assert over.max() <= 1.0, (t.name, over.max())
+    return got
+
+
+def plan_of(t, chunk=0, flags=0):
+    return binding.deft_plan(t.node_tok_begin, t.node_tok_len, t.node_parent, t.query_node, t.ntok, chunk, flags)
+
+
+@pytest.mark.parametrize("f32", [True, False])
+@pytest.mark.parametrize("Hq,Hkv,d,block", [(4, 4, 64, 32), (4, 2, 64, 1), (6, 1, 128, 16), (8, 2, 128, 64), (5, 5, 128, 8), (28, 4, 128, 2), (32, 8, 64, 4)])
+@pytest.mark.parametrize("seed", range(3))
+def test_random_forests(seed, Hq, Hkv, d, block, f32):
+    t = wl.random_tree(40 + seed, n_nodes=23, max_len=(40, 150, 400)[seed], nq=19, Hq=Hq, Hkv=Hkv, d=d, n_roots=1 + seed)
+    Q, c, K, V = filled(t, block, seed)
+    for chunk in (32, 128, 512):
+        check(t, plan_of(t, chunk), Q, c, K, V, f32)
+    check(t, plan_of(t, 128, binding.DEFT_SPLIT_BALANCED | binding.rows_per_query(Hq // Hkv)), Q, c, K, V, f32)
+
+
+def star(prefix, branches, length, Hq, Hkv, d, seed=5):
+    return wl._finish(f"star{prefix}_{branches}", [prefix] + [length] * branches, [-1] + [0] * branches,
+                      list(range(1, branches + 1)) if branches else [0], Hq, Hkv, d, seed)
+
+
+# one, two, three to four and five to eight row tiles to a task, resident and streamed, one piece and several; several rounds
+@pytest.mark.parametrize("prefix,branches,length,Hq,Hkv,d", [
+    (1, 0, 0, 4, 4, 64), (33, 0, 0, 8, 2, 128), (700, 3, 5, 8, 8, 128), (2000, 9, 31, 4, 4, 128), (3000, 7, 64, 16, 4, 64),
+    (1500, 12, 90, 16, 4, 128), (2500, 20, 33, 32, 8, 128), (1300, 30, 257, 32, 8, 64), (6000, 60, 3, 32, 8, 128), (900, 130, 40, 8, 1, 128),
+    (8191, 0, 0, 32, 8, 128)])
+@pytest.mark.parametrize("f32", [True, False])
+def test_groups_of_every_width(prefix, branches, length, Hq, Hkv, d, f32):
+    t = star(prefix, branches, length, Hq, Hkv, d)
+    Q, c, K, V = filled(t, 32, 11)
+    g = binding.rows_per_query(Hq // Hkv)
+    for chunk, flags in ((0, 0), (256, 0), (1024, binding.DEFT_SPLIT_BALANCED | g), (512, binding.DEFT_PRECISE_WEIGHTS), (128, binding.DEFT_GROUP_QUERY),
+                         (1024, binding.DEFT_SPLIT_NODE)):
+        check(t, plan_of(t, chunk, flags), Q, c, K, V, f32)
+
+
+@pytest.mark.parametrize("page,block,d", [(1, 1, 64), (16, 16, 128), (16, 4, 64), (64, 32, 128), (64, 64, 128)])
+def test_paged_pools(page, block, d):
+    for seed, make in enumerate((lambda: wl.random_tree(3, n_nodes=30, max_len=200, nq=40, Hq=8, Hkv=2, d=d), lambda: star(900, 24, 70, 16, 4, d))):
+        t = make()
+        ptr, ids, n_pool, row_of = wl.to_paged(t, page, seed)
+        Q, c, K, V = filled(t, block, seed, n_pool * page, row_of)
+        for chunk in (128, 512):
+            plan = binding.deft_plan_paged(ptr, ids, page, n_pool, t.node_tok_len, t.node_parent, t.query_node, chunk)
+            for f32 in (True, False):
+                check(t, plan, Q, c, K, V, f32)
+
+
+def test_benchmark_trees_scale_and_a_given_output():
+    for i in (1, 2, 3):
+        t = wl.make_config(i)
+        Q, c, K, V = filled(t, 32, i)
+        chunk = binding.deft_suggest_chunk_size(t.node_tok_len, t.node_parent, t.query_node, t.Hq, t.Hkv)
+        plan = plan_of(t, chunk)
+        check(t, plan, Q, c, K, V, False, scale=0.05)
+        out = torch.full((t.nq, t.Hq, t.d), float("nan"), device=dev())
+        assert binding.deft_tree_attn_decode_q8(plan, Q.to(dev()), c, out=out, scale=0.05) is out
+        check(t, plan, Q, c, K, V, True, scale=0.05, got=out)
+
+
+def test_the_results_are_those_of_a_bf16_cache_with_the_same_values():
+    # the same plan, weights and order of sums but for the order of d inside a score
+    for t in (wl.make_config(2), star(6000, 60, 3, 32, 8, 128), wl.random_tree(9, n_nodes=20, max_len=300, nq=30, Hq=8, Hkv=2, d=64)):
+        Q, c, K, V = filled(t, 64, 4)
+        plan = plan_of(t, 512)
+        a = binding.deft_tree_attn_decode_q8(plan, Q.to(dev()), c).double()
+        b = binding.deft_tree_attn_decode(plan, Q.to(dev()), K.to(dev()), V.to(dev())).double()
+        # a score's other rounding moves a weight to a neighbouring bf16 number now and then: far less than one rounding of all
+        assert float((a - b).norm() / b.norm()) < 2.0 ** -9
+
+
+def test_empty_paths_and_no_queries():
+    t = wl._finish("hollow", [0, 5, 0, 40], [-1, 0, 0, -1], [0, 1, 2, 3, 3], 8, 2, 64, 3)
+    Q, c, K, V = filled(t, 16, 2)
+    got = check(t, plan_of(t), Q, c, K, V, True)
+    assert bool((got[0] == 0).all()) and bool((got[2] == 0).all())
+    none = binding.deft_plan(t.node_tok_begin, t.node_tok_len, t.node_parent, [], t.ntok)
+    assert binding.deft_tree_attn_decode_q8(none, Q[:0].to(dev()), c).shape == (0, 8, 64)
+
+
+@pytest.mark.parametrize("d,prefix", [(64, 100), (128, 100), (128, 3000)])
+def test_a_token_that_is_not_a_number_reaches_those_who_see_it_and_no_others(d, prefix):
+    t = star(prefix, 40, 9, 8, 2, d)
+    Q, K, V = wl.make_qkv(t, 8)
+    spoiled = {3: "k", 17: "v", 31: "v"}  # branch -> where its token has an infinity or a NaN, head 1
+    for b, which in spoiled.items():
+        x = K if which == "k" else V
+        x[int(t.node_tok_begin[b]) + 4, 1, d - 1] = float("inf") if b == 17 else float("nan")
+    c = binding.alloc_kv_cache_q8(t.ntok, 2, d, 1, dev())
+    lst = binding.deft_kv_rows(np.arange(t.ntok), t.ntok, 1)
+    binding.deft_kv_store_q8(lst, K.to(dev()), V.to(dev()), c)
+    for chunk in (32, 128, 512):
+        for f32 in (True, False):
+            o = binding.deft_tree_attn_decode_q8(plan_of(t, chunk), Q.to(dev()), c, out_dtype=torch.float32 if f32 else None)
+            nan = torch.isnan(o).cpu()
+            want = torch.zeros((t.nq, 8), dtype=torch.bool)
+            for j in range(t.nq):
+                want[j, 4:] = (j + 1) in spoiled
+            assert torch.equal(nan.all(-1), want) and torch.equal(nan.any(-1), want)
+
+
+def test_pools_beyond_four_gib():
+    # two nodes at the two ends of a pool of 4.4e9 bytes: rows, blocks and pages past 32 bits of bytes
+    Hkv, d, rows = 8, 128, (1 << 22) + (1 << 17)
+    n = 300
+    t = wl._finish("far", [n, n], [-1, 0], [1, 0, 1], 16, Hkv, d, 3, begins=[64, rows - n - 5], ntok=rows)
+    small = wl._finish("near", [n, n], [-1, 0], [1, 0, 1], 16, Hkv, d, 3)
+    Q, K, V = wl.make_qkv(small)
+    c = binding.alloc_kv_cache_q8(rows, Hkv, d, 64, dev())
+    at = np.concatenate([64 + np.arange(n), rows - n - 5 + np.arange(n)])
+    lst = binding.deft_kv_rows(at, rows, 64)
+    binding.deft_kv_store_q8(lst, K.to(dev()), V.to(dev()), c)
+    K8, V8 = (x.cpu() for x in binding.deft_kv_load_q8(lst, c))
+    m = {"block": 64, "k": np.zeros((2 * 640, Hkv, d), np.uint8), "v": np.zeros((2 * 640, Hkv, d), np.uint8),
+         "k_scale": np.full((20, Hkv), 10, np.uint8), "v_scale": np.full((20, Hkv), 10, np.uint8)}  # as a new cache has them
+    near = np.where(at < 640, at, at - (rows - 640) + 640)  # (rows is a multiple of 64: the same places in their blocks)
+    model.store(m, near, K.double().numpy(), V.double().numpy())
+    assert np.array_equal(K8.double().numpy(), model.values(m, "k", near)) and np.array_equal(V8.double().numpy(), model.values(m, "v", near))
+    for f32 in (True, False):
+        got = binding.deft_tree_attn_decode_q8(plan_of(t, 128), Q.to(dev()), c, out_dtype=torch.float32 if f32 else None)
+        check(small, None, Q, c, K8, V8, f32, got=got)
+    # the last page of 64 rows to the first, and back to another
+    pages = rows // 64
+    copies = binding.deft_kv_copies([pages - 2, pages - 2], [0, pages - 1], pages)
+    binding.deft_kv_copy_pages(copies, [c.k, c.v, c.k_scale, c.v_scale])
+    for x in c[:2]:
+        x = x.view(torch.uint8)
+        assert torch.equal(x[:64], x[rows - 128:rows - 64]) and torch.equal(x[rows - 64:], x[:64])
+    del c
+    torch.cuda.empty_cache()
+
+
+# ---- copies of pages ----
+
+def copied(x, pages, src, dst):
+    y = x.reshape(pages, -1).clone()
+    y[dst] = x.reshape(pages, -1)[src]
+    return y.reshape(x.shape)
+
+
+def random_copies(rng, pages, kind):
+    order = rng.permutation(pages)
+    n = int(rng.integers(1, pages + 1))
+    dst = order[:n]
+    if kind == "any":
+        src = rng.integers(0, pages, n)
+    elif kind == "cycle":
+        src = np.roll(dst, 1)
+    elif kind == "chain":
+        src = np.minimum(dst + 1, pages - 1)
+    else:
+        n = max(1, n // 2)
+        dst, src = order[:n], rng.choice(order[n:], n) if n < pages else order[:n]
+    return src, dst
+
+
+@pytest.mark.parametrize("kind", ["any", "cycle", "chain", "fork"])
+@pytest.mark.parametrize("page_bytes,skew", [(16384, 0), (4096, 0), (48, 0), (24, 8), (20, 4), (10, 2), (7, 1), (1, 0), (8, 0)])
+def test_copies_of_pages(kind, page_bytes, skew):
+    rng = np.random.default_rng([page_bytes, len(kind)])
+    for pages in (1, 2, 37, 300):
+        src, dst = random_copies(rng, pages, kind)
+        copies = binding.deft_kv_copies(src, dst, pages)
+        base = torch.randint(0, 256, (skew + pages * page_bytes + 64,), dtype=torch.uint8, device=dev())
+        pool = base[skew:skew + pages * page_bytes]
+        want = copied(pool, pages, torch.from_numpy(src).to(dev()), torch.from_numpy(dst).to(dev()))
+        edges = base[:skew].clone(), base[skew + pages * page_bytes:].clone()
+        binding.deft_kv_copy_pages(copies, [pool])
+        assert torch.equal(pool, want)
+        assert torch.equal(base[:skew], edges[0]) and torch.equal(base[skew + pages * page_bytes:], edges[1])
+
+
+def test_copies_in_many_pools_of_several_kinds():
+    rng = np.random.default_rng(1)
+    pages = 50
+    src, dst = random_copies(rng, pages, "any")
+    copies = binding.deft_kv_copies(src, dst, pages)
+    pools = []
+    for layer in range(70):  # more pools than one launch takes, more sizes of pages too
+        pools += [torch.randn((pages * 4, 3, 64), device=dev()).to(torch.bfloat16) for _ in range(2)]
+        pools.append(torch.randint(0, 256, (pages, 1 + layer % 6), dtype=torch.uint8, device=dev()))
+        pools.append(torch.randint(0, 9, (pages, 2, 3), dtype=torch.int64, device=dev()))
+    want = [copied(x.view(torch.uint8), pages, torch.from_numpy(src).to(dev()), torch.from_numpy(dst).to(dev())) for x in pools]
+    binding.deft_kv_copy_pages(copies, pools)
+    for x, y in zip(pools, want):
+        assert torch.equal(x.view(torch.uint8), y)
+    binding.deft_kv_copy_pages(binding.deft_kv_copies([], [], pages), pools)
+    binding.deft_kv_copy_pages(copies, [])
+    for bad in ([pools[0], pools[0]], [pools[0][:-1]], [pools[0][:0]], [pools[0].transpose(0, 1)], [pools[0].cpu()]):
+        with pytest.raises(binding.DeftError):
+            binding.deft_kv_copy_pages(copies, bad)
+
+
+# ---- refusals of the binding ----
+
+def test_refusals():
+    t = star(60, 3, 4, 8, 2, 64)
+    Q, c, K, V = filled(t, 16, 1)
+    plan, q = plan_of(t), Q.to(dev())
+    k = K.to(dev())
+    rows = binding.deft_kv_rows([0, 1], t.ntok, 16)
+    copies = binding.deft_kv_copies([0], [1], t.ntok)
+    two = k[:2]
+    attend = binding.deft_tree_attn_decode_q8
+    store, load, copy = binding.deft_kv_store_q8, binding.deft_kv_load_q8, binding.deft_kv_copy_pages
+    for call in (
+        lambda: attend(plan, q.float(), c), lambda: attend(plan, q[:2], c), lambda: attend(plan, Q, c), lambda: attend(plan, q[..., :32].contiguous(), c),
+        lambda: attend(plan, q.transpose(0, 1), c), lambda: attend(plan, q[:, :7].contiguous(), c), lambda: attend(plan, q, c, out_dtype=torch.float16),
+        lambda: attend(plan, q, c, out=torch.empty((1, 8, 64), device=dev())), lambda: attend(plan, q, c._replace(k=c.k.view(torch.uint8))),
+        lambda: attend(plan, q, c._replace(k=c.k[:-1])), lambda: attend(plan, q, c._replace(k_scale=c.k_scale[:-1])),
+        lambda: attend(plan, q, c._replace(v_scale=c.v_scale.view(torch.uint8))), lambda: attend(plan, q, c._replace(block_rows=32)),
+        lambda: attend(plan, q, c._replace(block_rows=24)), lambda: attend(plan, q, binding.alloc_kv_cache_q8(t.ntok - 1, 2, 64, 16)),
+        lambda: attend(plan, q, c, workspace=torch.empty(64, dtype=torch.uint8, device=dev())),
+        lambda: store(rows, two.float(), two, c), lambda: store(rows, two, k[:3], c), lambda: store(rows, two.cpu(), two.cpu(), c),
+        lambda: store(rows, two.transpose(1, 2), two, c), lambda: store(copies, two, two, c), lambda: store(rows, two[:, :1], two[:, :1], c),
+        lambda: store(rows, two[:1].expand(2, 2, 64), two, c), lambda: store(binding.deft_kv_rows([0, 1], t.ntok, 8), two, two, c),
+        lambda: store(binding.deft_kv_rows([0, 1], t.ntok + 1, 16), two, two, c),
+        lambda: load(rows, c, k=two.float()), lambda: load(rows, c, v=k[:3]), lambda: load(rows, c, k=torch.empty((2, 64, 2), dtype=torch.bfloat16, device=dev()).transpose(1, 2)),
+        lambda: load(copies, c), lambda: copy(rows, [k])):
+        with pytest.raises(binding.DeftError):
+            call()
+    # a token's K and V at an address or a stride that 128-bit loads cannot take
+    flat = torch.zeros(2 * 132 + 8, dtype=torch.bfloat16, device=dev())
+    for x in (flat[1:1 + 256].view(2, 2, 64), flat[:264].view(2, 132)[:, :128].view(2, 2, 64)):
+        with pytest.raises(binding.DeftError):
+            store(rows, x, two, c)
+    check(t, plan, Q, c, K, V, True)
+
+
+# ---- streams and graphs ----
+
+def test_other_streams_wait_for_the_image():
+    t = star(300, 9, 20, 8, 2, 128)
+    for _ in range(3):
+        c, m = new_cache(t.ntok, 2, 128, 16, 2)
+        k, v = tokens(t.ntok, 2, 128, 3, special=False)
+        kg, vg = to_gpu(k, v)
+        a, b = torch.cuda.Stream(), torch.cuda.Stream()
+        torch.cuda.synchronize()
+        lst = binding.deft_kv_rows(np.arange(t.ntok), t.ntok, 16)
+        with torch.cuda.stream(a):
+            binding.deft_kv_store_q8(lst, kg, vg, c)
+        b.wait_stream(a)
+        k8, _ = binding.deft_kv_load_q8(lst, c, stream=b.cuda_stream)
+        torch.cuda.synchronize()
+        model.store(m, np.arange(t.ntok), k.double().numpy(), v.double().numpy())
+        same_bytes(c, m)
+        assert np.array_equal(k8.double().cpu().numpy(), model.values(m, "k"))
+
+
+@pytest.mark.parametrize("elsewhere", [False, True])
+def test_a_captured_iteration_is_replayed_with_eager_work_between(elsewhere):
+    # store, copy, read back and attend in one graph; lists uploaded before, by the capture's stream or another, and inside it
+    t = star(500, 12, 16, 8, 2, 128)
+    Q, c, K, V = filled(t, 16, 5)
+    plan, q = plan_of(t, 128), Q.to(dev())
+    pages = t.ntok // 16
+    at = (t.node_tok_begin + t.node_tok_len - 1)[1:]
+    rows, copies = binding.deft_kv_rows(at, t.ntok, 16), None
+    k, v = (x[:12].to(dev()).clone() for x in (K, V))
+    side = torch.cuda.Stream()
+
+    def iteration(rows, copies):
+        binding.deft_kv_store_q8(rows, k, v, c)
+        binding.deft_kv_copy_pages(copies, [x.view(torch.uint8).view(-1)[:pages * 16 * x[0].numel() // (1 if x.dim() == 3 else 16)] for x in c[:4]])
+        return binding.deft_tree_attn_decode_q8(plan, q, c), *binding.deft_kv_load_q8(rows, c)
+
+    make = lambda: binding.deft_kv_copies([1, 2, 3], [2, 3, 4], pages)  # noqa: E731
+    with torch.cuda.stream(side):
+        iteration(rows, make())
+    torch.cuda.synchronize()
+    if elsewhere:
+        rows = binding.deft_kv_rows(at, t.ntok, 16)
+        binding.deft_kv_load_q8(rows, c)  # uploaded by the default stream
+    start = [x.view(torch.uint8).clone() for x in c[:4]]
+    inside = make()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        got = iteration(rows, inside)
+    for step in range(4):
+        for x, y in zip(c[:4], start):
+            x.view(torch.uint8).copy_(y)
+        k.normal_()
+        v.normal_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        after = [x.view(torch.uint8).clone() for x in c[:4]]
+        replayed = [x.clone() for x in got]
+        for x, y in zip(c[:4], start):
+            x.view(torch.uint8).copy_(y)
+        want = iteration(rows, make())
+        torch.cuda.synchronize()
+        assert all(torch.equal(x.view(torch.uint8), y) for x, y in zip(c[:4], after))
+        assert all(torch.equal(x, y) for x, y in zip(want, replayed))
+
+
+# ---- all of them, as a serving loop uses them ----
+
+@pytest.mark.parametrize("page,block,d", [(16, 16, 128), (32, 8, 64)])
+def test_a_decode_loop_over_an_8_bit_pool(page, block, d):
+    Hq, Hkv, n_pool = 8, 2, 160
+    sim = wl.DecodeLoopSim(3, prompt_len=333, width=6, page_size=page, n_pool_pages=n_pool)
+    c = binding.alloc_kv_cache_q8(n_pool * page, Hkv, d, block, dev())
+    bf = binding.alloc_kv_cache(n_pool * page, Hkv, d, dev())  # a second model's cache, bf16, moves along
+    m = {"block": block, **{w: getattr(c, w).view(torch.uint8).cpu().numpy().copy() for w in ("k", "v", "k_scale", "v_scale")}}
+    g = torch.Generator().manual_seed(1)
+    held, plan = [0] * len(sim.lens), None
+
+    def row(u, i):
+        return sim.pages[u][i // page] * page + i % page
+
+    for it in range(14):
+        if it % 3 == 2:
+            sim.branch(2 + it % 2)
+        if it == 8:
+            sim.prune(2)
+        if it:
+            sim.step()
+        held += [0] * (len(sim.lens) - len(held))
+        at = np.array([row(u, i) for u in range(len(sim.lens)) for i in range(held[u], sim.lens[u])])
+        held = list(sim.lens)
+        k, v = (torch.randn((len(at), Hkv, d), generator=g).mul_(1 + it % 4).to(torch.bfloat16) for _ in range(2))
+        store_both(c, m, at, k, v)
+        for pool, x in zip(bf, (k, v)):
+            pool[torch.from_numpy(at).to(dev())] = x.to(dev())
+        if it in (5, 11):  # the pool is put in order
+            ptr, ids, lens, parent, _ = sim.tables()
+            new, src, dst = binding.deft_compact_pages(ptr, ids, n_pool, parent)
+            binding.deft_kv_copy_pages(binding.deft_kv_copies(src, dst, n_pool), [c.k, c.v, c.k_scale, c.v_scale, *bf])
+            for w in ("k", "v", "k_scale", "v_scale"):
+                y = m[w].reshape(n_pool, -1)
+                y[dst] = y[src]
+            sim.pages = [[int(p) for p in new[ptr[u]:ptr[u + 1]]] for u in range(len(lens))]
+            sim.free = [p for p in range(n_pool) if p not in set(new.tolist())]
+            plan = None
+        same_bytes(c, m)
+        ptr, ids, lens, parent, leaves = sim.tables()
+        plan = binding.deft_plan_paged(ptr, ids, page, n_pool, lens, parent, leaves, 128, prev=plan)
+        Q = torch.randn((len(leaves), Hq, d), generator=g).to(torch.bfloat16)
+        tables = (ptr, ids, page, lens, parent, leaves)
+        K8, V8 = (torch.from_numpy(model.values(m, w)).nan_to_num(0.0, 0.0, 0.0).to(torch.bfloat16) for w in "kv")
+        ref = oracle.tree_attention_paged(Q, K8, V8, *tables)
+        ref_abs = oracle.tree_attention_paged(Q, K8, V8.abs(), *tables)
+        for f32 in (True, False):
+            got = binding.deft_tree_attn_decode_q8(plan, Q.to(dev()), c, out_dtype=torch.float32 if f32 else None)
+            assert (np.abs(got.double().cpu().numpy() - ref) <= bound(ref, ref_abs, f32)).all(), it
+        got = binding.deft_tree_attn_decode(plan, Q.to(dev()), *bf).double().cpu()
+        plain = oracle.tree_attention_paged(Q, *(x.cpu() for x in bf), *tables)
+        assert float(np.abs(got.numpy() - plain).max()) <= 2e-3 + 1e-2 * np.abs(plain).max()
