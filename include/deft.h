@@ -326,7 +326,7 @@ int deft_tree_attn_decode_static(const deft_plan_t *plan, const void *dev_image,
  * byte e, 10 <= e <= 246.  A row's values are its bytes' values times the scale; every such product is a bf16 number.
  *
  * k, v             : device, bytes [n_rows, Hkv, d], 16-byte aligned
- * k_scale, v_scale : device, bytes [ceil(n_rows / block_rows), Hkv]
+ * k_scale, v_scale : device, bytes [ceil(n_rows / block_rows), Hkv], 4-byte aligned and read in whole 4-byte words
  * d                : 64 or 128
  * block_rows       : a power of two, 1 .. 64.  A block should belong to one node of the tree: choose a page size that is a
  *                    multiple of it, or with a contiguous cache begin nodes at multiples of it (block_rows = 1 suits any).

@@ -8,8 +8,10 @@ a call fails, an exception is raised.
 
 from __future__ import annotations
 
+import array
 import ctypes
 import os
+import struct
 from typing import NamedTuple
 
 import numpy as np
@@ -71,11 +73,6 @@ _VIEW_ARRAYS = (
 
 class _PlanView(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in _VIEW_SCALARS] + [(n, t) for n, t, _ in _VIEW_ARRAYS]
-
-
-class _CacheQ8(ctypes.Structure):  # deft_cache_q8_t
-    _fields_ = ([(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale")]
-                + [(n, ctypes.c_int32) for n in ("n_rows", "Hkv", "d", "block_rows")])
 
 
 class DeftError(RuntimeError):
@@ -140,7 +137,7 @@ def load_library():
     lib.deft_stage2_global_reduction.restype = ctypes.c_int
     lib.deft_stage2_global_reduction.argtypes = [vp, vp, vp, c32, c32, c32, ctypes.c_float, ctypes.c_uint32, vp, csz,
                                                  vp]
-    cache = ctypes.POINTER(_CacheQ8)
+    cache = vp  # (the bytes of a deft_cache_q8_t: _pack_cache)
     lib.deft_tree_attn_decode_q8.restype = ctypes.c_int
     lib.deft_tree_attn_decode_q8.argtypes = [vp, vp, vp, cache, vp, c32, ctypes.c_float, ctypes.c_uint32, vp, csz, vp]
     lib.deft_kv_rows.restype = ctypes.c_int
@@ -158,7 +155,7 @@ def load_library():
     lib.deft_kv_load_q8.restype = ctypes.c_int
     lib.deft_kv_load_q8.argtypes = [vp, vp, cache, vp, vp, vp]
     lib.deft_kv_copy_pages.restype = ctypes.c_int
-    lib.deft_kv_copy_pages.argtypes = [vp, vp, ctypes.POINTER(vp), ctypes.POINTER(ctypes.c_int64), c32, vp]
+    lib.deft_kv_copy_pages.argtypes = [vp, vp, vp, vp, c32, vp]
     lib.deft_compact_pages.restype = ctypes.c_int
     lib.deft_compact_pages.argtypes = [vp, vp, c32, vp, c32, vp, vp, vp, ctypes.POINTER(c32)]
     lib.deft_hbm_read_probe.restype = ctypes.c_int
@@ -448,7 +445,7 @@ class CacheQ8(NamedTuple):
 
     k: "torch.Tensor"        # float8_e4m3fn [n_rows, Hkv, d]
     v: "torch.Tensor"
-    k_scale: "torch.Tensor"  # float8_e8m0fnu [ceil(n_rows / block_rows), Hkv]
+    k_scale: "torch.Tensor"  # float8_e8m0fnu [ceil(n_rows / block_rows), Hkv], beginning at a multiple of 4 bytes
     v_scale: "torch.Tensor"
     block_rows: int = 32
 
@@ -466,40 +463,39 @@ def alloc_kv_cache_q8(n_rows: int, Hkv: int, d: int, block_rows: int = 32, devic
     k_off = (-buf.data_ptr()) % 1024
     v_off = k_off + k_span + KV_STAGGER_BYTES
     k, v = (buf[off:off + pool].view(torch.float8_e4m3fn).view(n_rows, Hkv, d) for off in (k_off, v_off))
-    scales = torch.full((2, blocks, Hkv), MIN_SCALE_BYTE, dtype=torch.uint8, device=device).view(torch.float8_e8m0fnu)
-    return CacheQ8(k, v, scales[0], scales[1], block_rows)
+    scales = [torch.full((blocks, Hkv), MIN_SCALE_BYTE, dtype=torch.uint8, device=device).view(torch.float8_e8m0fnu) for _ in range(2)]
+    return CacheQ8(k, v, *scales, block_rows)
 
 
-def _cache_struct(cache: CacheQ8, what: str) -> _CacheQ8:
+_pack_cache = struct.Struct("4P4i").pack  # deft_cache_q8_t
+
+
+def _cache_args(cache: CacheQ8, what: str):
+    """(a deft_cache_q8_t, its device's index, n_rows, Hkv, d) of a cache that is one."""
     torch = _torch or _get_torch()
     k, v, ks, vs, block = cache
-    if not (k.is_cuda and k.device == v.device == ks.device == vs.device):
+    index = k.get_device()
+    if index < 0 or not index == v.get_device() == ks.get_device() == vs.get_device():
         raise DeftError(-1, f"{what}: the cache must be on one device (there is no CPU path)")
-    if not (k.dtype == v.dtype == torch.float8_e4m3fn and k.dim() == 3 and v.shape == k.shape and k.is_contiguous() and v.is_contiguous()):
+    shape = k.shape
+    if not (k.dtype == v.dtype == torch.float8_e4m3fn and len(shape) == 3 and v.shape == shape and k.is_contiguous() and v.is_contiguous()):
         raise DeftError(-1, f"{what}: k and v of the cache must both be contiguous [n_rows, Hkv, d] float8_e4m3fn tensors")
     if type(block) is not int or not 0 < block <= MAX_BLOCK_ROWS or block & (block - 1):
         raise DeftError(-1, f"{what}: block_rows must be a power of two up to {MAX_BLOCK_ROWS}")
-    n_rows, Hkv, d = k.shape
-    if not (ks.dtype == vs.dtype == torch.float8_e8m0fnu and ks.shape == vs.shape == (-(-n_rows // block), Hkv) and ks.is_contiguous()
+    n_rows, Hkv, d = shape
+    blocks = ks.shape
+    if not (ks.dtype == vs.dtype == torch.float8_e8m0fnu and blocks == vs.shape and blocks == (-(-n_rows // block), Hkv) and ks.is_contiguous()
             and vs.is_contiguous()):
         raise DeftError(-1, f"{what}: the scales must both be contiguous [ceil(n_rows / block_rows), Hkv] float8_e8m0fnu tensors")
-    return _CacheQ8(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), n_rows, Hkv, d, block)
+    ksp, vsp = ks.data_ptr(), vs.data_ptr()
+    if (ksp | vsp) & 3:
+        raise DeftError(-1, f"{what}: the scales must begin at a multiple of 4 bytes")
+    return _pack_cache(k.data_ptr(), v.data_ptr(), ksp, vsp, n_rows, Hkv, d, block), index, n_rows, Hkv, d
 
 
-class _On:
-    """The device of a call's tensors as the current one, for as long as the call takes."""
-
-    def __init__(self, index: int):
-        torch = _torch or _get_torch()
-        self._other = None if torch._C._cuda_getDevice() == index else torch.cuda.device(index)
-
-    def __enter__(self):
-        if self._other is not None:
-            self._other.__enter__()
-
-    def __exit__(self, *exc):
-        if self._other is not None:
-            self._other.__exit__(*exc)
+def _elsewhere(index: int) -> bool:
+    """Whether the current device is another one: a call then makes its tensors' device the current one, and starts again."""
+    return (_torch or _get_torch())._C._cuda_getDevice() != index
 
 
 class KVList:
@@ -527,13 +523,16 @@ class KVList:
         index = torch.device(device).index
         if index is None:
             index = torch.cuda.current_device()
-        raw = _raw_stream(stream, index)
+        return self._image(index, _raw_stream(stream, index))
+
+    def _image(self, index: int, raw: int):
         entry = self._images.get(index)
         if entry is not None and entry[2] == raw:
             return entry[0]
+        torch = _torch or _get_torch()
         on = torch.cuda.ExternalStream(raw, device=torch.device("cuda", index)) if raw else torch.cuda.default_stream(index)
         # what is allocated here is allocated for the stream that fills it: it goes to no other tensor while that has work left
-        with _On(index), torch.cuda.stream(on):
+        with torch.cuda.device(index), torch.cuda.stream(on):
             captured = torch.cuda.is_current_stream_capturing()
             if entry is not None and (not captured or entry[1] is None):
                 img, event, first = entry
@@ -584,49 +583,60 @@ def deft_compact_pages(node_page_ptr, page_ids, n_pool_pages: int, node_parent):
     return new[:pg.size], src[:n.value], dst[:n.value]
 
 
-def _rows_for(rows: KVList, cache: CacheQ8, what: str) -> _CacheQ8:
-    c = _cache_struct(cache, what)
-    if not rows.block_rows:
-        raise DeftError(-1, f"{what}: the list is one of copies, not of rows")
-    if rows.block_rows != c.block_rows or rows.pool > c.n_rows:
-        raise DeftError(-1, f"{what}: the list is for a larger cache, or for other blocks")
-    return c
+def _rows_for(rows: KVList, cache: CacheQ8, what: str):
+    args = _cache_args(cache, what)
+    if rows.block_rows != cache.block_rows or rows.pool > args[2]:
+        raise DeftError(-1, f"{what}: the list is one of copies, or for a larger cache or other blocks")
+    return args
 
 
 def deft_kv_store_q8(rows: KVList, k, v, cache: CacheQ8, stream=None) -> None:
     """Stores the K and V of new tokens, bf16 [n, Hkv, d], into the rows of the list.  Tokens may lie apart (slices of a fused
     projection's output), by a multiple of 16 bytes; the heads of one may not.  Asynchronous on `stream`."""
     torch = _torch or _get_torch()
-    c = _rows_for(rows, cache, "deft_kv_store_q8")
-    shape = (rows.n, c.Hkv, c.d)
-    for name, t in (("k", k), ("v", v)):
-        if t.dtype != torch.bfloat16 or t.shape != shape or t.device != cache.k.device:
-            raise DeftError(-1, f"deft_kv_store_q8: {name} must be a bf16 [{shape[0]}, {shape[1]}, {shape[2]}] tensor on the cache's device")
-        if rows.n and (t.stride(2) != 1 or (c.Hkv > 1 and t.stride(1) != c.d)):
-            raise DeftError(-1, f"deft_kv_store_q8: the heads of a token of {name} must be contiguous")
-    if rows.n == 0:
+    c, index, _, Hkv, d = _rows_for(rows, cache, "deft_kv_store_q8")
+    n, bf16, strides = rows.n, torch.bfloat16, []
+    shape = (n, Hkv, d)
+    for t in (k, v):
+        if t.dtype != bf16 or t.shape != shape or t.get_device() != index:
+            raise DeftError(-1, f"deft_kv_store_q8: k and v must be bf16 [{n}, {Hkv}, {d}] tensors on the cache's device")
+        token, head, one = t.stride()
+        if n and (one != 1 or (Hkv > 1 and head != d)):
+            raise DeftError(-1, "deft_kv_store_q8: the heads of a token must be contiguous")
+        strides.append(token if n > 1 else Hkv * d)  # (one token's stride says nothing)
+    if n == 0:
         return
-    index = cache.k.device.index
-    least = c.Hkv * c.d
-    ks, vs = (t.stride(0) if rows.n > 1 else max(least, t.stride(0) & ~7) for t in (k, v))  # (one token's stride says nothing)
-    with _On(index):
-        _check(_lib.deft_kv_store_q8(rows._h, rows.image(cache.k.device, stream).data_ptr(), k.data_ptr(), v.data_ptr(), ks, vs,
-                                     ctypes.byref(c), _raw_stream(stream, index)), "deft_kv_store_q8")
+    if _elsewhere(index):
+        with torch.cuda.device(index):
+            return deft_kv_store_q8(rows, k, v, cache, stream)
+    raw = _raw_stream(stream, index)
+    rc = _lib.deft_kv_store_q8(rows._h, rows._image(index, raw).data_ptr(), k.data_ptr(), v.data_ptr(), strides[0], strides[1], c, raw)
+    if rc != 0:
+        _check(rc, "deft_kv_store_q8")
 
 
 def deft_kv_load_q8(rows: KVList, cache: CacheQ8, k=None, v=None, stream=None):
     """(k, v), bf16 [n, Hkv, d]: the values of the list's rows.  Asynchronous on `stream`."""
     torch = _torch or _get_torch()
-    c = _rows_for(rows, cache, "deft_kv_load_q8")
-    shape, dev = (rows.n, c.Hkv, c.d), cache.k.device
-    k, v = (torch.empty(shape, dtype=torch.bfloat16, device=dev) if t is None else t for t in (k, v))
-    for name, t in (("k", k), ("v", v)):
-        if t.dtype != torch.bfloat16 or t.shape != shape or not t.is_contiguous() or t.device != dev:
-            raise DeftError(-1, f"deft_kv_load_q8: {name} must be a contiguous bf16 [{shape[0]}, {shape[1]}, {shape[2]}] tensor on the cache's device")
-    if rows.n:
-        with _On(dev.index):
-            _check(_lib.deft_kv_load_q8(rows._h, rows.image(dev, stream).data_ptr(), ctypes.byref(c), k.data_ptr(), v.data_ptr(),
-                                        _raw_stream(stream, dev.index)), "deft_kv_load_q8")
+    c, index, _, Hkv, d = _rows_for(rows, cache, "deft_kv_load_q8")
+    shape, bf16 = (rows.n, Hkv, d), torch.bfloat16
+    if k is None:
+        k = torch.empty(shape, dtype=bf16, device=cache.k.device)
+    elif k.dtype != bf16 or k.shape != shape or not k.is_contiguous() or k.get_device() != index:
+        raise DeftError(-1, f"deft_kv_load_q8: k must be a contiguous bf16 [{rows.n}, {Hkv}, {d}] tensor on the cache's device")
+    if v is None:
+        v = torch.empty(shape, dtype=bf16, device=cache.k.device)
+    elif v.dtype != bf16 or v.shape != shape or not v.is_contiguous() or v.get_device() != index:
+        raise DeftError(-1, f"deft_kv_load_q8: v must be a contiguous bf16 [{rows.n}, {Hkv}, {d}] tensor on the cache's device")
+    if rows.n == 0:
+        return k, v
+    if _elsewhere(index):
+        with torch.cuda.device(index):
+            return deft_kv_load_q8(rows, cache, k, v, stream)
+    raw = _raw_stream(stream, index)
+    rc = _lib.deft_kv_load_q8(rows._h, rows._image(index, raw).data_ptr(), c, k.data_ptr(), v.data_ptr(), raw)
+    if rc != 0:
+        _check(rc, "deft_kv_load_q8")
     return k, v
 
 
@@ -638,19 +648,25 @@ def deft_kv_copy_pages(copies: KVList, pools, stream=None) -> None:
     pools = list(pools)
     if not pools:
         return
-    dev = pools[0].device
-    sizes = []
+    index, pages = pools[0].get_device(), copies.pool
+    at, sizes = array.array("Q"), array.array("q")
     for t in pools:
-        nbytes = t.numel() * t.element_size()
-        if not t.is_cuda or t.device != dev or not t.is_contiguous():
-            raise DeftError(-1, "deft_kv_copy_pages: pools must be contiguous tensors on one device (there is no CPU path)")
-        if copies.pool == 0 or nbytes == 0 or nbytes % copies.pool:
+        if t.get_device() != index or not t.is_contiguous():
+            index = -1
+        nbytes = t.nbytes
+        if pages == 0 or nbytes == 0 or nbytes % pages:
             raise DeftError(-1, "deft_kv_copy_pages: a pool is not a whole number of bytes for each of the list's pages")
-        sizes.append(nbytes // copies.pool)
-    n = len(pools)
-    with _On(dev.index):
-        _check(load_library().deft_kv_copy_pages(copies._h, copies.image(dev, stream).data_ptr(), (ctypes.c_void_p * n)(*[t.data_ptr() for t in pools]),
-                                                 (ctypes.c_int64 * n)(*sizes), n, _raw_stream(stream, dev.index)), "deft_kv_copy_pages")
+        at.append(t.data_ptr())
+        sizes.append(nbytes // pages)
+    if index < 0:
+        raise DeftError(-1, "deft_kv_copy_pages: pools must be contiguous tensors on one device (there is no CPU path)")
+    if _elsewhere(index):
+        with (_torch or _get_torch()).cuda.device(index):
+            return deft_kv_copy_pages(copies, pools, stream)
+    raw = _raw_stream(stream, index)
+    rc = load_library().deft_kv_copy_pages(copies._h, copies._image(index, raw).data_ptr(), at.buffer_info()[0], sizes.buffer_info()[0], len(pools), raw)
+    if rc != 0:
+        _check(rc, "deft_kv_copy_pages")
 
 
 def deft_tree_attn_decode_q8(plan: Plan, q, cache: CacheQ8, out=None, scale: float = 0.0, out_dtype=None, workspace=None, stream=None):
@@ -661,21 +677,25 @@ def deft_tree_attn_decode_q8(plan: Plan, q, cache: CacheQ8, out=None, scale: flo
     """
     torch = _torch or _get_torch()
     bf16 = torch.bfloat16
-    c = _cache_struct(cache, "deft_tree_attn_decode_q8")
-    dev = cache.k.device
-    if q.dtype != bf16 or q.dim() != 3 or not q.is_contiguous() or q.device != dev:
+    c, index, n_rows, Hkv, d = _cache_args(cache, "deft_tree_attn_decode_q8")
+    if q.dtype != bf16 or q.dim() != 3 or not q.is_contiguous() or q.get_device() != index:
         raise DeftError(-1, "deft_tree_attn_decode_q8: q must be a contiguous 3-d bf16 tensor on the cache's device")
-    nq, Hq, d = q.shape
-    plan_nq, plan_rows = plan.limits()
-    if d != c.d:
+    shape = nq, Hq, dq = q.shape
+    if dq != d:
         raise DeftError(-1, "deft_tree_attn_decode_q8: q and the cache differ in d")
+    if Hkv == 0 or Hq == 0 or Hq % Hkv:
+        raise DeftError(-1, "deft_tree_attn_decode_q8: Hq must be a multiple of Hkv")
+    plan_nq, plan_rows = plan.limits()
     if nq != plan_nq:
         raise DeftError(-1, "deft_tree_attn_decode_q8: q has a different number of queries than the plan")
-    if plan_rows > c.n_rows:
+    if plan_rows > n_rows:
         raise DeftError(-1, "deft_tree_attn_decode_q8: the plan addresses rows beyond the KV cache")
-    if out is None:
-        out = torch.empty((nq, Hq, d), dtype=out_dtype or bf16, device=dev)
-    elif out.shape != (nq, Hq, d) or not out.is_contiguous() or out.device != dev:
+    if out is None:  # (see deft_tree_attn_decode)
+        if type(q) is torch.Tensor and (out_dtype is None or out_dtype == bf16):
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        else:
+            out = torch.empty(shape, dtype=out_dtype or bf16, device=q.device)
+    elif out.shape != shape or not out.is_contiguous() or out.get_device() != index:
         raise DeftError(-1, "deft_tree_attn_decode_q8: out must be a contiguous [nq, Hq, d] tensor on q's device")
     if out.dtype == bf16:
         flags = DEFT_OUT_BF16
@@ -683,20 +703,18 @@ def deft_tree_attn_decode_q8(plan: Plan, q, cache: CacheQ8, out=None, scale: flo
         flags = DEFT_OUT_F32
     else:
         raise DeftError(-1, "deft_tree_attn_decode_q8: out must be bf16 or float32")
-    Hkv, index = c.Hkv, dev.index
-    if Hkv == 0 or Hq % Hkv:
-        raise DeftError(-1, "deft_tree_attn_decode_q8: Hq must be a multiple of Hkv")
+    if _elsewhere(index):
+        with torch.cuda.device(index):
+            return deft_tree_attn_decode_q8(plan, q, cache, out, scale, None, workspace, stream)
     raw = _raw_stream(stream, index)
-    with _On(index):
-        # an image that went out on this very stream, or that has landed, needs no ordering
-        entry = plan._images.get((Hq // Hkv, index))
-        img = entry[0] if entry is not None and (entry[2] == raw or entry[1] is None) else plan.image(Hq, Hkv, dev, stream)
-        ws = workspace if workspace is not None else plan._workspaces.get((Hq, Hkv, d, index))
-        if ws is None:
-            ws = plan.workspace(Hq, Hkv, d, dev)
-        rc = (_lib or load_library()).deft_tree_attn_decode_q8(
-            plan._h, img.data_ptr(), q.data_ptr(), ctypes.byref(c), out.data_ptr(), Hq, float(scale), flags, ws.data_ptr(),
-            ws.numel() * ws.element_size(), raw)
+    # an image that went out on this very stream, or that has landed, needs no ordering
+    entry = plan._images.get((Hq // Hkv, index))
+    img = entry[0] if entry is not None and (entry[2] == raw or entry[1] is None) else plan.image(Hq, Hkv, q.device, stream)
+    ws = workspace if workspace is not None else plan._workspaces.get((Hq, Hkv, d, index))
+    if ws is None:
+        ws = plan.workspace(Hq, Hkv, d, q.device)
+    rc = (_lib or load_library()).deft_tree_attn_decode_q8(
+        plan._h, img.data_ptr(), q.data_ptr(), c, out.data_ptr(), Hq, float(scale), flags, ws.data_ptr(), ws.numel() * ws.element_size(), raw)
     if rc != 0:
         _check(rc, "deft_tree_attn_decode_q8")
     return out

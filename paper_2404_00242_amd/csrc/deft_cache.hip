@@ -196,80 +196,120 @@ __global__ __launch_bounds__(256) void deft_load_q8(LoadArgs a) {
 // ---- copies of pages ----
 // A thread owns the same few bytes of every page of one pool, and makes a chain's copies of them one after the other in the
 // list's order: pages may be read and overwritten in one call without a second copy of anything, because no other thread ever
-// touches those bytes.  Up to kAhead loads of a chain are in flight; that no page is overwritten before it was read makes it right
-// to ask for all of them before the first is stored.
-constexpr int kAhead = 8;
+// touches those bytes.  That no page is overwritten before it was read makes it right to ask for later pages ahead of the stores.
+// Most chains are one copy long (forks), so a thread takes four words where that leaves enough threads; all lanes of a wave have
+// one chain where pages are that large, and its steps come by scalar loads.
 constexpr int kMaxPools = 256;  // to a launch, 2 KB of its arguments
 constexpr int kMaxClasses = 4;  // sizes of pages among them
 constexpr uint32_t kMaxGroups = 1u << 16;  // workgroups to a pool; more work goes round
+constexpr uint32_t kManyWaves = 4096;      // of four words to a thread: half of what the chip holds
 
 struct PoolClass {
     uint32_t begin_group, begin_pool;  // first workgroup, first pool
-    uint32_t groups;                   // workgroups of a pool
+    uint32_t groups, inv_groups;       // workgroups of a pool
     uint32_t width;                    // bytes that a thread moves at a time: 16, 8, 4, 2 or 1
-    uint32_t words, inv_words;         // threads that a page takes, at `width` bytes each
-    uint32_t tiles;                    // chains * words / 256, rounded up
+    uint32_t per_thread;               // such words to a thread, of 64 * per_thread consecutive ones to a wave; 0: see below
+    uint32_t words;                    // of a page
+    uint32_t per_page, inv_per_page;   // waves to a page; with per_thread = 0 threads, of any number of pages to a wave
     uint32_t unused;
+    uint64_t items;                    // waves or threads of a pool
     int64_t page_bytes;
 };
 struct CopyArgs {
     const u32x4 *chains;   // {first, count, held, -}, see deft::CopyChain
     const u32x2 *steps;    // {src, dst}
-    uint32_t n_chains, n_classes;
+    uint32_t n_classes;
     PoolClass classes[kMaxClasses];
     uint8_t *pools[kMaxPools];
 };
 static_assert(sizeof(CopyArgs) <= 4096, "arguments of a kernel");
 
-template <typename T>
-__device__ __forceinline__ void copy_chain(const CopyArgs &a, uint8_t *pool, int64_t page_bytes, uint32_t chain, uint32_t word) {
+// The copies of one chain, W words to a thread: this lane's first is `word`, the others come 64 behind each other.  `kAhead` steps'
+// words are in flight.  UNIFORM: the chain is all lanes'; they fetch 64 of its steps at a time, one each (step by step, a
+// scalar load in front of every copy, a cycle of 150 pages took half as long again).
+template <typename T, int W, bool UNIFORM>
+__device__ __forceinline__ void copy_chain(const CopyArgs &a, uint8_t *pool, int64_t page_bytes, uint32_t chain, uint32_t word, uint32_t words) {
+    constexpr int kAhead = W == 1 ? 16 : 4;
     const u32x4 head = a.chains[chain];
-    const uint32_t count = head[1];
+    T *base = reinterpret_cast<T *>(pool) + word;
     const u32x2 *steps = a.steps + head[0];
-    uint8_t *base = pool + (size_t)word * sizeof(T);
-    auto at = [&](uint32_t page) { return reinterpret_cast<T *>(base + (int64_t)page * page_bytes); };
-    T held{};
-    uint32_t n = count;
+    auto load = [&](T(&x)[W], uint32_t page) {
+        const T *p = reinterpret_cast<const T *>(reinterpret_cast<const uint8_t *>(base) + (int64_t)page * page_bytes);
+#pragma unroll
+        for (int w = 0; w < W; ++w)
+            if (word + 64 * w < words) x[w] = p[64 * w];
+    };
+    auto store = [&](const T(&x)[W], uint32_t page) {
+        T *p = reinterpret_cast<T *>(reinterpret_cast<uint8_t *>(base) + (int64_t)page * page_bytes);
+#pragma unroll
+        for (int w = 0; w < W; ++w)
+            if (word + 64 * w < words) p[64 * w] = x[w];
+    };
+    T held[W];
+    uint32_t n = head[1];
     if (head[2]) {  // the last step's page is overwritten before its turn: read now, and here before anything is stored
-        --n;
-        held = *at(steps[n][0]);
+        load(held, steps[--n][0]);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
-    for (uint32_t i = 0; i < n; i += kAhead) {
-        T x[kAhead];
-        uint32_t to[kAhead];
+    for (uint32_t first = 0; first < n; first += 64) {
+        const uint32_t m = min(64u, n - first);
+        u32x2 mine{};
+        if (UNIFORM) mine = steps[first + min(threadIdx.x & 63, m - 1)];
+        auto step = [&](uint32_t i) {
+            if (UNIFORM) return u32x2{(uint32_t)__builtin_amdgcn_readlane((int)mine[0], (int)i), (uint32_t)__builtin_amdgcn_readlane((int)mine[1], (int)i)};
+            return steps[first + i];
+        };
+        for (uint32_t i = 0; i < m; i += kAhead) {
+            T x[kAhead][W];
+            uint32_t to[kAhead];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const u32x2 s = steps[min(i + u, n - 1)];
-            to[u] = s[1];
-            if (i + u < n) x[u] = *at(s[0]);
+            for (int u = 0; u < kAhead; ++u)
+                if (i + u < m) {
+                    const u32x2 s = step(i + u);
+                    to[u] = s[1];
+                    load(x[u], s[0]);
+                }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+                if (i + u < m) store(x[u], to[u]);
         }
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-            if (i + u < n) *at(to[u]) = x[u];
     }
-    if (head[2]) *at(steps[n][1]) = held;
+    if (head[2]) store(held, steps[n][1]);
+}
+
+template <typename T>
+__device__ __forceinline__ void copy_part(const CopyArgs &a, const PoolClass &c, uint8_t *pool, uint32_t group) {
+    if (c.per_thread == 0) {  // pages of less than a wave
+        for (uint64_t i = (uint64_t)group * 256 + threadIdx.x; i < c.items; i += (uint64_t)c.groups * 256) {
+            const uint32_t chain = i >> 32 ? (uint32_t)(i / c.per_page) : divide((uint32_t)i, c.per_page, c.inv_per_page);
+            copy_chain<T, 1, false>(a, pool, c.page_bytes, chain, (uint32_t)(i - (uint64_t)chain * c.per_page), c.words);
+        }
+        return;
+    }
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    for (uint64_t i = (uint64_t)group * 4 + wave; i < c.items; i += (uint64_t)c.groups * 4) {
+        const uint32_t chain = i >> 32 ? (uint32_t)(i / c.per_page) : divide((uint32_t)i, c.per_page, c.inv_per_page);
+        const uint32_t first = (uint32_t)(i - (uint64_t)chain * c.per_page) * 64;
+        if (c.per_thread == 4)
+            copy_chain<T, 4, true>(a, pool, c.page_bytes, chain, 4 * first + lane, c.words);
+        else
+            copy_chain<T, 1, true>(a, pool, c.page_bytes, chain, first + lane, c.words);
+    }
 }
 
 __global__ __launch_bounds__(256) void deft_copy_pages(CopyArgs a) {
     uint32_t k = 0;
     while (k + 1 < a.n_classes && blockIdx.x >= a.classes[k + 1].begin_group) ++k;
     const PoolClass &c = a.classes[k];
-    const uint32_t group = blockIdx.x - c.begin_group, pool = group / c.groups;
+    const uint32_t group = blockIdx.x - c.begin_group, pool = divide(group, c.groups, c.inv_groups);
     uint8_t *base = a.pools[c.begin_pool + pool];
-    for (uint32_t tile = group - pool * c.groups; tile < c.tiles; tile += c.groups) {
-        const uint64_t i = (uint64_t)tile * 256 + threadIdx.x;
-        // (chain, word of the page); beyond 32 bits only with pages of one word
-        const uint32_t chain = i >> 32 ? (uint32_t)(i / c.words) : divide((uint32_t)i, c.words, c.inv_words);
-        if (chain >= a.n_chains) return;
-        const uint32_t word = (uint32_t)(i - (uint64_t)chain * c.words);
-        switch (c.width) {
-            case 16: copy_chain<u32x4>(a, base, c.page_bytes, chain, word); break;
-            case 8: copy_chain<u32x2>(a, base, c.page_bytes, chain, word); break;
-            case 4: copy_chain<uint32_t>(a, base, c.page_bytes, chain, word); break;
-            case 2: copy_chain<uint16_t>(a, base, c.page_bytes, chain, word); break;
-            default: copy_chain<uint8_t>(a, base, c.page_bytes, chain, word); break;
-        }
+    const uint32_t part = group - pool * c.groups;
+    switch (c.width) {
+        case 16: copy_part<u32x4>(a, c, base, part); break;
+        case 8: copy_part<u32x2>(a, c, base, part); break;
+        case 4: copy_part<uint32_t>(a, c, base, part); break;
+        case 2: copy_part<uint16_t>(a, c, base, part); break;
+        default: copy_part<uint8_t>(a, c, base, part); break;
     }
 }
 
@@ -394,7 +434,6 @@ extern "C" int deft_kv_copy_pages(const deft_kv_list_t *list, const void *dev_im
         CopyArgs a{};
         a.chains = reinterpret_cast<const u32x4 *>(img);
         a.steps = reinterpret_cast<const u32x2 *>(img + list->off_entries);
-        a.n_chains = (uint32_t)list->heads;
         uint32_t n = 0, groups = 0;
         for (; i < todo.size() && n < kMaxPools; ++i) {
             const Pool &p = todo[i];
@@ -405,12 +444,17 @@ extern "C" int deft_kv_copy_pages(const deft_kv_list_t *list, const void *dev_im
                 c.begin_pool = n;
                 c.width = p.width;
                 c.words = (uint32_t)(p.page / p.width);
-                c.inv_words = inverse(c.words);
                 c.page_bytes = p.page;
-                const uint64_t tiles = ((uint64_t)c.words * a.n_chains + 255) / 256;
-                c.tiles = (uint32_t)std::min<uint64_t>(tiles, UINT32_MAX - kMaxGroups);
-                if (c.tiles != tiles) return DEFT_EINVAL;
-                c.groups = std::min(c.tiles, kMaxGroups / 2);
+                size_t alike = 1;  // pools of this class
+                while (i + alike < todo.size() && todo[i + alike].page == p.page && todo[i + alike].width == p.width) ++alike;
+                const uint64_t chains = (uint64_t)list->heads, wide = (c.words + 255) / 256;
+                c.per_thread = c.words < 64 ? 0 : wide * chains * alike >= kManyWaves ? 4 : 1;
+                c.per_page = c.per_thread == 0 ? c.words : c.per_thread == 4 ? (uint32_t)wide : (c.words + 63) / 64;
+                c.inv_per_page = inverse(c.per_page);
+                c.items = chains * c.per_page;
+                const uint64_t per_group = c.per_thread == 0 ? 256 : 4;
+                c.groups = (uint32_t)std::min<uint64_t>((c.items + per_group - 1) / per_group, kMaxGroups / 2);
+                c.inv_groups = inverse(c.groups);
             }
             a.pools[n++] = p.at;
             groups += a.classes[a.n_classes - 1].groups;

@@ -78,9 +78,6 @@ struct Bf16Cache {
     typedef Stage1Args Args;
     struct Scales {};
     static constexpr bool k8Bit = false;
-    // The values of d that a lane of group g holds for contraction step kk of S^T = K Q^T: eight from q_lane(g) + q_step(kk).
-    static __device__ __forceinline__ constexpr int q_lane(int g) { return 8 * g; }
-    static __device__ __forceinline__ constexpr int q_step(int kk) { return 32 * kk; }
 };
 
 // 8-bit floating point (e4m3), a scale for each (block of 2^block_shift rows, KV head), [blocks, Hkv] exponent bytes e for a
@@ -94,14 +91,13 @@ struct E4m3Cache {
     };
     struct Scales {
         const uint8_t *k, *v;  // of this KV head
-        int shift, Hkv;
-        __device__ __forceinline__ uint32_t key(int row) const { return k[(size_t)(row >> shift) * Hkv]; }
-        __device__ __forceinline__ uint32_t value(int row) const { return v[(size_t)(row >> shift) * Hkv]; }
+        uint32_t shift, Hkv;
+        uint32_t k_row, v_row;  // bytes of n16 and of 4g rows
+        // (one 64-bit multiply-add; a size_t product is three multiplications, 16 cycles each)
+        __device__ __forceinline__ const uint8_t *key(uint32_t row) const { return k + (uint64_t)(row >> shift) * Hkv; }
+        __device__ __forceinline__ const uint8_t *value(uint32_t row) const { return v + (uint64_t)(row >> shift) * Hkv; }
     };
     static constexpr bool k8Bit = true;
-    // a lane's 128-bit load of K holds 16 values of d: two steps
-    static __device__ __forceinline__ constexpr int q_lane(int g) { return 16 * g; }
-    static __device__ __forceinline__ constexpr int q_step(int kk) { return 64 * (kk >> 1) + 8 * (kk & 1); }
 };
 
 struct Stage2Args {
@@ -168,11 +164,26 @@ __device__ __forceinline__ u32x4 widen8(u32x2 x, float scale) {
     const u32x2 a = widen4(x[0], scale), b = widen4(x[1], scale);
     return u32x4{a[0], a[1], b[0], b[1]};
 }
-__device__ __forceinline__ float scale_of(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
-// The scale byte of token 4g + Q, from lanes that hold that of token 4g + n16 % 4 each.
+// A scale on its way: the word that its byte lies in, and the byte's address.  Whole words, because of a byte that is in flight
+// from one round of a loop to the next the compiler clears the upper bits at the end of the loop, and waits there for every load
+// (long context, stage 1, 141 us with bytes, 115 without scales).
+struct ScaleWord {
+    uint32_t word, at;
+    __device__ __forceinline__ float value() const { return __builtin_bit_cast(float, __builtin_amdgcn_ubfe(word, 8 * at, 8) << 23); }
+};
+__device__ __forceinline__ ScaleWord load_scale(const uint8_t *p) {
+    const uint32_t at = (uint32_t)reinterpret_cast<uintptr_t>(p);
+    return {*reinterpret_cast<const uint32_t *>(p - (at & 3)), at};
+}
+// base: at a word's beginning
+__device__ __forceinline__ ScaleWord load_scale(const uint8_t *base, uint32_t at) {
+    return {*reinterpret_cast<const uint32_t *>(base + (at & ~3u)), at};
+}
+// The scale of token 4g + Q, from lanes that hold that of token 4g + n16 % 4 each.
 template <int Q>
-__device__ __forceinline__ float scale_of_token(uint32_t byte) {
-    return scale_of((uint32_t)__builtin_amdgcn_update_dpp((int)byte, (int)byte, 0x55 * Q, 0xf, 0xf, false));
+__device__ __forceinline__ float scale_of_token(float scale) {
+    const int x = __builtin_bit_cast(int, scale);
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(x, x, 0x55 * Q, 0xf, 0xf, false));
 }
 
 // Partial results.  SHARED: in a call of one launch they are stored past the L2 of their XCD, and read past the reader's,
@@ -261,17 +272,22 @@ struct KVRegs {
     u32x4 v[8];
 };
 
-// The same block of an 8-bit cache, as loaded: of K a lane holds d = 64i + 16g..+15 of token 16a + n16, which serve steps 2i
-// and 2i + 1 (E4m3Cache::q_step), of V the same tokens and d as above.  Scales of tokens 16a + n16 and 16a + 4g + n16 % 4.
+// The same block of an 8-bit cache, as loaded.  K comes 16 values to a load: a lane holds d = 64i + 16g..+15 of its token, which
+// are two steps of the contraction; any order of d will do as long as Q has the same (q_column).  Scales are those of tokens
+// 16a + n16 and 16a + 4g + n16 % 4.
 template <int D>
 struct KVBytes {
     u32x4 k[2][D / 64];
     u32x2 v[8];
-    uint32_t ks[2], vs[2];
+    ScaleWord ks[2], vs[2];
 };
+// The first of the eight values of d that a lane of group g holds for step kk.  PAIRS: of K loaded as in KVBytes.
+template <bool PAIRS>
+__device__ __forceinline__ constexpr int q_column(int g, int kk) {
+    return PAIRS ? 64 * (kk >> 1) + 16 * g + 8 * (kk & 1) : 32 * kk + 8 * g;
+}
 template <int D>
-__device__ __forceinline__ void widen_k(const u32x4 (&x)[D / 64], uint32_t byte, bf16x8 (&k)[D / 32]) {
-    const float scale = scale_of(byte);
+__device__ __forceinline__ void widen_k(const u32x4 (&x)[D / 64], float scale, bf16x8 (&k)[D / 32]) {
 #pragma unroll
     for (int i = 0; i < D / 64; ++i) {
         k[2 * i] = __builtin_bit_cast(bf16x8, widen8(u32x2{x[i][0], x[i][1]}, scale));
@@ -279,11 +295,11 @@ __device__ __forceinline__ void widen_k(const u32x4 (&x)[D / 64], uint32_t byte,
     }
 }
 // four tokens of a lane, 4g..4g+3 of a tile
-__device__ __forceinline__ void widen_v(const u32x2 *x, uint32_t byte, u32x4 *v) {
-    v[0] = widen8(x[0], scale_of_token<0>(byte));
-    v[1] = widen8(x[1], scale_of_token<1>(byte));
-    v[2] = widen8(x[2], scale_of_token<2>(byte));
-    v[3] = widen8(x[3], scale_of_token<3>(byte));
+__device__ __forceinline__ void widen_v(const u32x2 *x, float scale, u32x4 *v) {
+    v[0] = widen8(x[0], scale_of_token<0>(scale));
+    v[1] = widen8(x[1], scale_of_token<1>(scale));
+    v[2] = widen8(x[2], scale_of_token<2>(scale));
+    v[3] = widen8(x[3], scale_of_token<3>(scale));
 }
 
 // physical row of chunk position x; positions past the chunk's end give a row that exists (their scores are masked)
@@ -319,29 +335,84 @@ __device__ __forceinline__ void load_v(KVRegs<D> &r, const ChunkCtx<Bf16Cache> &
         }
 }
 
-template <int D>
-__device__ __forceinline__ void load_k(KVBytes<D> &r, const ChunkCtx<E4m3Cache> &c, int x0, bool valid) {
-    if (!valid) x0 = 0;
+// Where the tokens of block `blk` of an 8-bit cache lie.  A token of it is given as r, the same in all lanes, and what the lane
+// adds to that: n16 (K) or 4g (V).  UNIFORM: the chunk's rows are consecutive (see is_near), so a token is (wave-uniform
+// pointer of the block) + a 32-bit offset, the smaller one of the token's and of the chunk's last row: two additions and a
+// minimum, where a product takes 16 cycles.  A block past the end is the last one again.
+template <bool UNIFORM>
+struct BlockAt {
+    const ChunkCtx<E4m3Cache> &c;
+    const uint8_t *k, *v, *ks, *vs;
+    int x0, lim, low;
+    bool valid;
+    uint32_t pitch, last, ks_rest, vs_rest;
+    __device__ __forceinline__ BlockAt(const ChunkCtx<E4m3Cache> &ctx, int blk, int nblk) : c(ctx), pitch((uint32_t)ctx.row_stride) {
+        if (UNIFORM) {
+            x0 = 32 * min(blk, nblk - 1);
+            lim = min(31, c.clen - 1 - x0);
+            last = lim * pitch;
+            const uint32_t row = (uint32_t)(c.begin0 + x0), block = row >> c.scales.shift;
+            low = (int)(row - (block << c.scales.shift));
+            k = c.khead + (uint64_t)row * pitch;
+            v = c.vhead + (uint64_t)row * pitch;
+            // the first row's scales: the word, and what is left
+            ks = c.scales.k + (uint64_t)block * c.scales.Hkv;
+            vs = c.scales.v + (uint64_t)block * c.scales.Hkv;
+            ks_rest = (uint32_t)reinterpret_cast<uintptr_t>(ks) & 3;
+            vs_rest = (uint32_t)reinterpret_cast<uintptr_t>(vs) & 3;
+            ks -= ks_rest;
+            vs -= vs_rest;
+        } else {
+            valid = blk < nblk;
+            x0 = valid ? 32 * blk : 0;
+        }
+    }
+    __device__ __forceinline__ uint32_t row(int r, int lane) const { return (uint32_t)(valid ? tok_row(c, x0 + r + lane) : c.begin0); }
+    __device__ __forceinline__ uint32_t near(int r, uint32_t lane_bytes) const { return min(lane_bytes + (uint32_t)r * pitch, last); }
+    __device__ __forceinline__ const uint8_t *key(int r, uint32_t col) const {
+        return UNIFORM ? k + (near(r, c.scales.k_row) + col) : c.khead + ((uint64_t)row(r, c.n16) * pitch + col);
+    }
+    __device__ __forceinline__ const uint8_t *value(int r) const {
+        return UNIFORM ? v + (near(r, c.scales.v_row) + c.vlane) : c.vhead + ((uint64_t)row(r, 4 * c.g) * pitch + c.vlane);
+    }
+    // the scale of token r + lane
+    __device__ __forceinline__ ScaleWord scale(const uint8_t *head, uint32_t rest, int r, int lane) const {
+        const uint32_t block = (uint32_t)(low + min(r + lane, lim)) >> c.scales.shift;  // counted from the first row's
+        uint32_t offset;  // (both factors are below 2^24; written as a product it becomes a 32-bit one, 16 cycles)
+        asm("v_mul_u32_u24 %0, %1, %2" : "=v"(offset) : "s"(c.scales.Hkv), "v"(block));
+        return load_scale(head, offset + rest);
+    }
+    __device__ __forceinline__ ScaleWord key_scale(int r) const {
+        return UNIFORM ? scale(ks, ks_rest, r, c.n16) : load_scale(c.scales.key(row(r, c.n16)));
+    }
+    __device__ __forceinline__ ScaleWord value_scale(int r) const {  // of token r + 4g + n16 % 4
+        const int lane = 4 * c.g + (c.n16 & 3);
+        return UNIFORM ? scale(vs, vs_rest, r, lane) : load_scale(c.scales.value(row(r, lane)));
+    }
+};
+// Whether BlockAt<true> can be used.
+__device__ __forceinline__ bool is_near(const ChunkCtx<Bf16Cache> &c) { return c.uniform; }
+__device__ __forceinline__ bool is_near(const ChunkCtx<E4m3Cache> &c) { return c.uniform && c.scales.Hkv <= (1u << 16); }
+
+template <int D, bool UNIFORM>
+__device__ __forceinline__ void load_k(KVBytes<D> &r, const ChunkCtx<E4m3Cache> &c, int blk, int nblk) {
+    const BlockAt<UNIFORM> b(c, blk, nblk);
 #pragma unroll
     for (int aa = 0; aa < 2; ++aa) {
-        const int row = valid ? tok_row(c, x0 + 16 * aa + c.n16) : c.begin0;
-        const uint8_t *kp = c.kbase + (size_t)row * c.row_stride;
+        const uint8_t *kp = b.key(16 * aa, 16 * c.g);
 #pragma unroll
         for (int i = 0; i < D / 64; ++i) r.k[aa][i] = load16_kv<true>(kp + 64 * i);
-        r.ks[aa] = c.scales.key(row);
+        r.ks[aa] = b.key_scale(16 * aa);
     }
 }
-template <int D>
-__device__ __forceinline__ void load_v(KVBytes<D> &r, const ChunkCtx<E4m3Cache> &c, int x0, bool valid) {
-    if (!valid) x0 = 0;
+template <int D, bool UNIFORM>
+__device__ __forceinline__ void load_v(KVBytes<D> &r, const ChunkCtx<E4m3Cache> &c, int blk, int nblk) {
+    const BlockAt<UNIFORM> b(c, blk, nblk);
 #pragma unroll
     for (int aa = 0; aa < 2; ++aa) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int row = valid ? tok_row(c, x0 + 16 * aa + 4 * c.g + i) : c.begin0;
-            r.v[4 * aa + i] = load8_kv<true>(c.vbase + (size_t)row * c.row_stride);
-        }
-        r.vs[aa] = c.scales.value(valid ? tok_row(c, x0 + 16 * aa + 4 * c.g + (c.n16 & 3)) : c.begin0);
+        for (int i = 0; i < 4; ++i) r.v[4 * aa + i] = load8_kv<true>(b.value(16 * aa + i));
+        r.vs[aa] = b.value_scale(16 * aa);
     }
 }
 
@@ -364,15 +435,15 @@ struct WideValues {
 template <int D>
 __device__ __forceinline__ WideKeys<D> keys(const KVBytes<D> &r) {
     WideKeys<D> x;
-    widen_k<D>(r.k[0], r.ks[0], x.k[0]);
-    widen_k<D>(r.k[1], r.ks[1], x.k[1]);
+    widen_k<D>(r.k[0], r.ks[0].value(), x.k[0]);
+    widen_k<D>(r.k[1], r.ks[1].value(), x.k[1]);
     return x;
 }
 template <int D>
 __device__ __forceinline__ WideValues values(const KVBytes<D> &r) {
     WideValues x;
-    widen_v(r.v, r.vs[0], x.v);
-    widen_v(r.v + 4, r.vs[1], x.v + 4);
+    widen_v(r.v, r.vs[0].value(), x.v);
+    widen_v(r.v + 4, r.vs[1].value(), x.v + 4);
     return x;
 }
 
@@ -620,29 +691,52 @@ __device__ __forceinline__ void compute_block(const KVRegs<D> &r, const ChunkCtx
 // front of the other workgroup's loads longer.  Stage 1, two blocks -> one reloaded whole -> in halves: sixteen
 // sequences (148 MB) 29.9 -> 28.8 -> 27.8 us, few-shot prefix (149 MB) 28.7 -> 28.7 -> 27.7, reasoning tree of 256
 // queries (456 MB) 96.2 -> 94.5 -> 93.6.
-template <int D, typename C>
+// An 8-bit block is half as many bytes in flight and half the registers, and takes more instructions between its loads: two
+// blocks per wave there.
+template <int D, bool UNIFORM, typename C>
 struct SplitPipe {
-    std::conditional_t<C::k8Bit, KVBytes<D>, KVRegs<D>> r;
+    static constexpr int DEPTH = C::k8Bit ? 2 : 1;
+    std::conditional_t<C::k8Bit, KVBytes<D>, KVRegs<D>> r[DEPTH];
     __device__ __forceinline__ void prime(const ChunkCtx<C> &ctx, int wave, int nblk) {
-        load_k<D>(r, ctx, wave * 32, wave < nblk);
-        load_v<D>(r, ctx, wave * 32, wave < nblk);
+        if constexpr (!C::k8Bit) {
+            load_k<D>(r[0], ctx, wave * 32, wave < nblk);
+            load_v<D>(r[0], ctx, wave * 32, wave < nblk);
+        } else {
+#pragma unroll
+            for (int u = 0; u < DEPTH; ++u) {
+                load_k<D, UNIFORM>(r[u], ctx, wave + u * kWaves, nblk);
+                load_v<D, UNIFORM>(r[u], ctx, wave + u * kWaves, nblk);
+            }
+        }
+    }
+    template <bool PRECISE>
+    __device__ __forceinline__ void step(int u, const ChunkCtx<C> &ctx, int blk, int next, int nblk, TileState<D> (&ts)[1], float cs) {
+        f32x4 sacc[1][2];
+        bf16x8 preg[1], plo[1];
+        qk_block<D, 1>(keys(r[u]), ts, sacc);
+        if constexpr (C::k8Bit)
+            load_k<D, UNIFORM>(r[u], ctx, next, nblk);
+        else
+            load_k<D>(r[u], ctx, next * 32, next < nblk);
+        __builtin_amdgcn_sched_barrier(0);  // the loads go out here, not behind the softmax
+        mask_block<D, 1>(ctx, blk * 32, ts, sacc);
+        shift_block<D, 1>(ts, sacc, cs);
+        raise_block<D, 1>(ts, sacc);
+        weights_block<D, 1, PRECISE>(ts, sacc, cs, preg, plo);
+        pv_block<D, 1, PRECISE>(values(r[u]), preg, plo, ts);
+        if constexpr (C::k8Bit)
+            load_v<D, UNIFORM>(r[u], ctx, next, nblk);
+        else
+            load_v<D>(r[u], ctx, next * 32, next < nblk);
     }
     template <bool PRECISE>
     __device__ __forceinline__ void run(const ChunkCtx<C> &ctx, int wave, int nblk, TileState<D> (&ts)[1], float cs) {
-        for (int blk = wave; blk < nblk; blk += kWaves) {
-            const int next = blk + kWaves;
-            f32x4 sacc[1][2];
-            bf16x8 preg[1], plo[1];
-            qk_block<D, 1>(keys(r), ts, sacc);
-            load_k<D>(r, ctx, next * 32, next < nblk);
-            __builtin_amdgcn_sched_barrier(0);  // the loads go out here, not behind the softmax
-            mask_block<D, 1>(ctx, blk * 32, ts, sacc);
-            shift_block<D, 1>(ts, sacc, cs);
-            raise_block<D, 1>(ts, sacc);
-            weights_block<D, 1, PRECISE>(ts, sacc, cs, preg, plo);
-            pv_block<D, 1, PRECISE>(values(r), preg, plo, ts);
-            load_v<D>(r, ctx, next * 32, next < nblk);
-        }
+        int blk = wave;
+        for (; blk + (DEPTH - 1) * kWaves < nblk; blk += DEPTH * kWaves)
+#pragma unroll
+            for (int u = 0; u < DEPTH; ++u)
+                step<PRECISE>(u, ctx, blk + u * kWaves, blk + (u + DEPTH) * kWaves, nblk, ts, cs);
+        if (DEPTH > 1 && blk < nblk) step<PRECISE>(0, ctx, blk, nblk, nblk, ts, cs);
     }
 };
 
@@ -660,15 +754,16 @@ struct Share {
     u32x4 x[NX];
 };
 // Of an 8-bit cache, as loaded; the wave that fetched a share widens it before it passes it on, so each byte is widened once
-// in a workgroup and what lies in LDS is what a bf16 cache would have put there.
+// in a workgroup and what lies in LDS is what a bf16 cache would have put there.  TR = 4: a wave has K or V alone, and both are
+// loaded eight values at a time: the same loads on either path, with no branch around them, for the exact waits of WidePipe
+// (K 16 at a time and a branch: 209 us for the long context, against 145).
 template <int D, int TR>
 struct Share<D, TR, E4m3Cache> {
     static constexpr int KK = D / 32;
     static constexpr int NSLOT = 2 * KK + 8;
     static constexpr int NX = TR == 2 ? KK + 4 : (KK > 4 ? KK : 4);
-    u32x4 k[D / 64];
-    u32x2 v[4];
-    uint32_t ks, vs;
+    u32x2 x[NX];  // (TR = 2: K first, two entries to a load)
+    ScaleWord ks, vs;  // (TR = 4: one of the two)
 };
 
 template <int D, int TR>
@@ -684,34 +779,54 @@ __device__ __forceinline__ WideRows<Share<D, TR, E4m3Cache>::NX> share_rows(cons
     constexpr int KK = D / 32;
     WideRows<Share<D, TR, E4m3Cache>::NX> r;
     if (TR == 2 || t < 2) {
-        bf16x8 k[KK];
-        widen_k<D>(s.k, s.ks, k);
+        const float scale = s.ks.value();
 #pragma unroll
-        for (int q = 0; q < KK; ++q) r.x[q] = __builtin_bit_cast(u32x4, k[q]);
+        for (int q = 0; q < KK; ++q) r.x[q] = widen8(s.x[q], scale);
     }
     if (TR == 2)
-        widen_v(s.v, s.vs, r.x + KK);
+        widen_v(s.x + KK, s.vs.value(), r.x + KK);
     else if (t >= 2)
-        widen_v(s.v, s.vs, r.x);
+        widen_v(s.x, s.ks.value(), r.x);
     return r;
 }
 
-template <int D, int TR>
-__device__ __forceinline__ void share_issue(Share<D, TR, E4m3Cache> &s, const ChunkCtx<E4m3Cache> &c, int t, int x0, bool valid) {
-    if (!valid) x0 = 0;
-    if (TR == 2 || t < 2) {
-        const int row = valid ? tok_row(c, x0 + 16 * t + c.n16) : c.begin0;
-        const uint8_t *kp = c.kbase + (size_t)row * c.row_stride;
+template <int D, int TR, bool UNIFORM>
+__device__ __forceinline__ void issue_share(Share<D, TR, E4m3Cache> &s, const ChunkCtx<E4m3Cache> &c, int t, int blk, int nblk) {
+    constexpr int KK = D / 32;
+    const BlockAt<UNIFORM> b(c, blk, nblk);
+    if constexpr (TR == 4 && UNIFORM) {
+        static_assert(KK == 4, "a K loader issues four loads");
+        // K loader: four 32-byte columns of row 16t + n16; V loader: rows 16(t - 2) + 4g .. + 3
+        const bool kl = t < 2;
+        const int first = 16 * (kl ? t : t - 2);
+        const uint32_t lane_bytes = kl ? c.scales.k_row : c.scales.v_row, col = kl ? c.klane : c.vlane;
+        const uint8_t *base = kl ? b.k : b.v;
 #pragma unroll
-        for (int i = 0; i < D / 64; ++i) s.k[i] = load16_kv<TR == 2>(kp + 64 * i);
-        s.ks = c.scales.key(row);
+        for (int q = 0; q < 4; ++q) s.x[q] = load8_kv<false>(base + (b.near(first + (kl ? 0 : q), lane_bytes) + (col + (kl ? 32u * q : 0u))));
+        s.ks = b.scale(kl ? b.ks : b.vs, kl ? b.ks_rest : b.vs_rest, first, kl ? c.n16 : 4 * c.g + (c.n16 & 3));
+        return;
+    }
+    if (TR == 2 || t < 2) {
+        if (TR == 2) {
+            const uint8_t *kp = b.key(16 * t, 16 * c.g);
+#pragma unroll
+            for (int i = 0; i < KK / 2; ++i) {
+                const u32x4 y = load16_kv<true>(kp + 64 * i);
+                s.x[2 * i] = u32x2{y[0], y[1]};
+                s.x[2 * i + 1] = u32x2{y[2], y[3]};
+            }
+        } else {
+            const uint8_t *kp = b.key(16 * t, 8 * c.g);
+#pragma unroll
+            for (int q = 0; q < KK; ++q) s.x[q] = load8_kv<false>(kp + 32 * q);
+        }
+        s.ks = b.key_scale(16 * t);
     }
     if (TR == 2 || t >= 2) {
-        const int x = x0 + 16 * (TR == 2 ? t : t - 2) + 4 * c.g;
+        const int first = 16 * (TR == 2 ? t : t - 2);
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-            s.v[q] = load8_kv<TR == 2>(c.vbase + (size_t)(valid ? tok_row(c, x + q) : c.begin0) * c.row_stride);
-        s.vs = c.scales.value(valid ? tok_row(c, x + (c.n16 & 3)) : c.begin0);
+        for (int q = 0; q < 4; ++q) s.x[(TR == 2 ? KK : 0) + q] = load8_kv<TR == 2>(b.value(first + q));
+        (TR == 2 ? s.vs : s.ks) = b.value_scale(first);
     }
 }
 
@@ -740,7 +855,7 @@ __device__ __forceinline__ void share_issue(Share<D, TR, Bf16Cache> &s, const Ch
     }
 }
 
-template <int D, int TR, int NT, bool PRECISE, typename C>
+template <int D, int TR, int NT, bool PRECISE, bool UNIFORM, typename C>
 __device__ __forceinline__ void share_step(Share<D, TR, C> &s, const ChunkCtx<C> &c, u32x4 *xs, int t, int lane, int blk,
                                            int next_blk, int nblk, TileState<D> (&ts)[NT], float cs, float inv_cs) {
     constexpr int KK = D / 32;
@@ -761,7 +876,10 @@ __device__ __forceinline__ void share_step(Share<D, TR, C> &s, const ChunkCtx<C>
         }
     }
     __syncthreads();
-    share_issue<D, TR>(s, c, t, next_blk * 32, next_blk < nblk);
+    if constexpr (C::k8Bit)
+        issue_share<D, TR, UNIFORM>(s, c, t, next_blk, nblk);
+    else
+        share_issue<D, TR>(s, c, t, next_blk * 32, next_blk < nblk);
     if (live) {
         KVRegs<D> r;
 #pragma unroll
@@ -776,7 +894,7 @@ __device__ __forceinline__ void share_step(Share<D, TR, C> &s, const ChunkCtx<C>
 
 // Used for tasks of two row tiles (TR = 2, NT = 1: two waves per tile, the two pairs take alternate blocks);
 // wider tasks go through WidePipe below.
-template <int D, int TR, int NT, typename C>
+template <int D, int TR, int NT, bool UNIFORM, typename C>
 struct SharedPipe {
     using S = Share<D, TR, C>;
     static constexpr int NP = kWaves / TR;  // token parts: part p takes blocks p, p+NP, ...
@@ -785,7 +903,12 @@ struct SharedPipe {
     __device__ __forceinline__ void prime(const ChunkCtx<C> &ctx, int wave, int nblk) {
         const int t = wave % TR, part = wave / TR;
 #pragma unroll
-        for (int u = 0; u < DEPTH; ++u) share_issue<D, TR>(st[u], ctx, t, (part + u * NP) * 32, part + u * NP < nblk);
+        for (int u = 0; u < DEPTH; ++u) {
+            if constexpr (C::k8Bit)
+                issue_share<D, TR, UNIFORM>(st[u], ctx, t, part + u * NP, nblk);
+            else
+                share_issue<D, TR>(st[u], ctx, t, (part + u * NP) * 32, part + u * NP < nblk);
+        }
     }
     template <bool PRECISE>
     __device__ __forceinline__ void run(const ChunkCtx<C> &ctx, u32x4 *xbuf, int wave, int lane, int nblk,
@@ -801,7 +924,7 @@ struct SharedPipe {
                 const int blk = part + it * NP;
                 // LDS exchange stages alternate; stage (it & 1) was last read two steps ago, before the
                 // barrier of the previous step
-                share_step<D, TR, NT, PRECISE>(st[u], ctx, xb + (it & 1) * S::NSLOT * 64, t, lane, blk, blk + DEPTH * NP, nblk,
+                share_step<D, TR, NT, PRECISE, UNIFORM>(st[u], ctx, xb + (it & 1) * S::NSLOT * 64, t, lane, blk, blk + DEPTH * NP, nblk,
                                       ts, cs, inv_cs);
             }
         }
@@ -836,23 +959,8 @@ struct WidePipe {
     // loader one column of four rows.  No branch on any path: blocks past the end repeat the last block, so the same four load instructions are
     // issued whatever happens and the compiler's s_waitcnt vmcnt counts stay exact.
     __device__ __forceinline__ void issue(S &sh, const ChunkCtx<C> &c, int t, int blk, int nblk) {
-        if constexpr (UNIFORM && C::k8Bit) {
-            const int blk_e = min(blk, nblk - 1);
-            const uint32_t row_bytes = (uint32_t)c.row_stride;
-            const size_t first = ((size_t)c.begin0 + 32 * (size_t)blk_e) * row_bytes;
-            const int lim = min(31, c.clen - 1 - 32 * blk_e), row0 = c.begin0 + 32 * blk_e;
-            if (t < 2) {
-                const int row = min((int)lane_row, lim);
-                const uint8_t *base = c.khead + first;
-#pragma unroll
-                for (int i = 0; i < D / 64; ++i) sh.k[i] = load16_kv<false>(base + ((uint32_t)row * row_bytes + lane_col + 64u * i));
-                sh.ks = c.scales.key(row0 + row);
-            } else {
-                const uint8_t *base = c.vhead + first;
-#pragma unroll
-                for (int q = 0; q < 4; ++q) sh.v[q] = load8_kv<false>(base + ((uint32_t)min((int)lane_row + q, lim) * row_bytes + lane_col));
-                sh.vs = c.scales.value(row0 + min((int)lane_row + (c.n16 & 3), lim));
-            }
+        if constexpr (C::k8Bit) {
+            issue_share<D, 4, UNIFORM>(sh, c, t, blk, nblk);
         } else if constexpr (UNIFORM) {
             static_assert(KK == 4 || !UNIFORM, "a K loader issues four loads");
             const int blk_e = min(blk, nblk - 1);
@@ -1054,7 +1162,7 @@ struct ResidentTask {
         typedef std::conditional_t<D == 128, u32x2, uint32_t> vbytes;  // VW values
         u32x4 kb[NA][2][D / 64];
         vbytes vb[NA][8];
-        uint32_t ks[NA][2], vs[NA][2];
+        ScaleWord ks[NA][2], vs[NA][2];
 #pragma unroll
         for (int b = 0; b < NA; ++b) {
             const int x0 = 32 * (wave + kWaves * b);
@@ -1064,8 +1172,8 @@ struct ResidentTask {
                 const uint8_t *kp = k_lane + (size_t)row * c.row_stride;
 #pragma unroll
                 for (int i = 0; i < D / 64; ++i) kb[b][aa][i] = load16_kv<false>(kp + 64 * i);
-                ks[b][aa] = c.scales.key(row);
-                vs[b][aa] = c.scales.value(tok_row(c, min(x0 + 16 * aa + 4 * c.g + (c.n16 & 3), c.clen - 1)));
+                ks[b][aa] = load_scale(c.scales.key(row));
+                vs[b][aa] = load_scale(c.scales.value(tok_row(c, min(x0 + 16 * aa + 4 * c.g + (c.n16 & 3), c.clen - 1))));
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -1078,9 +1186,9 @@ struct ResidentTask {
         for (int b = 0; b < NA; ++b)
 #pragma unroll
             for (int aa = 0; aa < 2; ++aa) {
-                widen_k<D>(kb[b][aa], ks[b][aa], k[b][aa]);
-                const float scale[4] = {scale_of_token<0>(vs[b][aa]), scale_of_token<1>(vs[b][aa]), scale_of_token<2>(vs[b][aa]),
-                                        scale_of_token<3>(vs[b][aa])};
+                widen_k<D>(kb[b][aa], ks[b][aa].value(), k[b][aa]);
+                const float mine = vs[b][aa].value();
+                const float scale[4] = {scale_of_token<0>(mine), scale_of_token<1>(mine), scale_of_token<2>(mine), scale_of_token<3>(mine)};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     if constexpr (D == 128)
@@ -1106,7 +1214,7 @@ struct ResidentTask {
     }
     __device__ __forceinline__ void load_q(const uint16_t *q_lane, int row) {
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk) q[kk] = __builtin_bit_cast(bf16x8, load16(q_lane + (size_t)row * D + C::q_step(kk)));
+        for (int kk = 0; kk < KK; ++kk) q[kk] = __builtin_bit_cast(bf16x8, load16(q_lane + (size_t)row * D + q_column<C::k8Bit>(0, kk)));
     }
 
     // One wave's share of one tile: scores of its NA blocks, softmax over them, products, into the merge buffer.
@@ -1278,9 +1386,12 @@ __device__ __forceinline__ const uint16_t *cache_k(const Stage1Args &a) { return
 __device__ __forceinline__ const uint16_t *cache_v(const Stage1Args &a) { return a.v; }
 __device__ __forceinline__ const uint8_t *cache_k(const E4m3Cache::Args &a) { return a.k8; }
 __device__ __forceinline__ const uint8_t *cache_v(const E4m3Cache::Args &a) { return a.v8; }
-__device__ __forceinline__ void set_scales(Bf16Cache::Scales &, const Stage1Args &, int) {}
-__device__ __forceinline__ void set_scales(E4m3Cache::Scales &s, const E4m3Cache::Args &a, int h) {
-    s = {a.k_scale + h, a.v_scale + h, a.block_shift, a.Hkv};
+template <int D>
+__device__ __forceinline__ void set_scales(Bf16Cache::Scales &, const Stage1Args &, int, int) {}
+template <int D>
+__device__ __forceinline__ void set_scales(E4m3Cache::Scales &s, const E4m3Cache::Args &a, int h, int lane) {
+    const uint32_t pitch = (uint32_t)a.Hkv * D;
+    s = {a.k_scale + h, a.v_scale + h, (uint32_t)a.block_shift, (uint32_t)a.Hkv, (lane & 15) * pitch, (lane >> 4) * 4 * pitch};
 }
 
 template <int D, bool PRECISE, bool SHARED, typename C>
@@ -1298,7 +1409,7 @@ __device__ __forceinline__ LeftRows resident_task(const typename C::Args &a, con
     int32_t *s_row = reinterpret_cast<int32_t *>(lds + L::kTokens), *s_qlo = s_row + kResidentTokens<D>,
             *s_qhi = s_qlo + kResidentTokens<D>;
     ChunkCtx<C> c{};
-    set_scales(c.scales, a, h);
+    set_scales<D>(c.scales, a, h, lane);
     c.row_stride = (size_t)a.Hkv * D;
     c.s_row = s_row;
     c.s_qlo = s_qlo;
@@ -1310,9 +1421,9 @@ __device__ __forceinline__ LeftRows resident_task(const typename C::Args &a, con
     c.g = lane >> 4;
     const int nblk = (c.clen + 31) >> 5;
     const int rows = min(16 * ntiles, width * a.G - 16 * tile0);  // of this task
-    const typename C::elem *k_lane = cache_k(a) + (size_t)h * D + C::q_lane(c.g),
+    const typename C::elem *k_lane = cache_k(a) + (size_t)h * D + q_column<C::k8Bit>(c.g, 0),
                             *v_lane = cache_v(a) + (size_t)h * D + (D / 16) * c.n16;
-    const uint16_t *q_lane = a.q + C::q_lane(c.g);
+    const uint16_t *q_lane = a.q + q_column<C::k8Bit>(c.g, 0);
 
     // The rows of the task: where Q comes from and where the partial result goes (rows past the end repeat the last).
     // One thread per row; the query index is asked for here and waited for in finish_rows, behind the K/V loads.
@@ -1454,13 +1565,13 @@ __device__ __forceinline__ LeftRows streaming_task(const typename C::Args &a, co
     const int TR = ntiles <= 1 ? 1 : (ntiles == 2 ? 2 : 4);  // waves that split the rows; 4 / TR token parts
 
     ChunkCtx<C> ctx;
-    set_scales(ctx.scales, a, h);
+    set_scales<D>(ctx.scales, a, h, lane);
     ctx.row_stride = (size_t)a.Hkv * D;
-    ctx.kbase = cache_k(a) + (size_t)h * D + C::q_lane(g);
+    ctx.kbase = cache_k(a) + (size_t)h * D + 8 * g;
     ctx.vbase = cache_v(a) + (size_t)h * D + 8 * (D == 128 ? n16 : (n16 & 7));
     ctx.khead = cache_k(a) + (size_t)h * D;
     ctx.vhead = cache_v(a) + (size_t)h * D;
-    ctx.klane = 16u * g;
+    ctx.klane = 8u * sizeof(typename C::elem) * g;
     ctx.vlane = 8u * sizeof(typename C::elem) * (D == 128 ? n16 : (n16 & 7));
     ctx.s_row = s_row;
     ctx.s_qlo = s_qlo;
@@ -1533,50 +1644,73 @@ __device__ __forceinline__ LeftRows streaming_task(const typename C::Args &a, co
 #pragma unroll
         for (int cc = 0; cc < 8; ++cc) ts[u].o[cc] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    auto load_q = [&](int ntw) {
+    auto load_q = [&](int ntw, auto pairs) {
+        constexpr bool kPairs = decltype(pairs)::value;
         const u32x4 z = {0, 0, 0, 0};
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             if (u >= ntw) break;
-            const uint16_t *qp = a.q + ((size_t)q_user[u] * a.Hq + (size_t)h * a.G + q_head[u]) * D + C::q_lane(g);
+            const uint16_t *qp = a.q + ((size_t)q_user[u] * a.Hq + (size_t)h * a.G + q_head[u]) * D + q_column<kPairs>(g, 0);
 #pragma unroll
             for (int kk = 0; kk < KK; ++kk)
-                ts[u].q[kk] = __builtin_bit_cast(bf16x8, ts[u].qpos >= 0 ? load16(qp + C::q_step(kk)) : z);
+                ts[u].q[kk] = __builtin_bit_cast(bf16x8, ts[u].qpos >= 0 ? load16(qp + q_column<kPairs>(0, kk)) : z);
         }
         __builtin_amdgcn_s_waitcnt(0);  // vmcnt(0) expcnt(0) lgkmcnt(0)
     };
     const float inv_cs = 1.0f / a.c;  // turns a reference in exponent units back into score units
     TileState<D>(&ts1)[1] = reinterpret_cast<TileState<D>(&)[1]>(ts);  // the one-tile paths use ts[0] only
 
+    const std::bool_constant<C::k8Bit> pairs;
+    const std::false_type plain;
     if (TR == 1) {
-        SplitPipe<D, C> pipe;
-        pipe.prime(ctx, wave, nblk);
-        load_q(1);
-        pipe.template run<PRECISE>(ctx, wave, nblk, ts1, a.c);
+        if constexpr (C::k8Bit) {
+            auto split = [&](auto uniform) {
+                SplitPipe<D, decltype(uniform)::value, C> pipe;
+                pipe.prime(ctx, wave, nblk);
+                load_q(1, pairs);
+                pipe.template run<PRECISE>(ctx, wave, nblk, ts1, a.c);
+            };
+            if (is_near(ctx)) split(std::true_type()); else split(std::false_type());
+        } else {
+            SplitPipe<D, false, C> pipe;
+            pipe.prime(ctx, wave, nblk);
+            load_q(1, pairs);
+            pipe.template run<PRECISE>(ctx, wave, nblk, ts1, a.c);
+        }
     } else if (TR == 2) {
-        SharedPipe<D, 2, 1, C> pipe;
-        pipe.prime(ctx, wave, nblk);
-        load_q(1);
-        pipe.template run<PRECISE>(ctx, xbuf, wave, lane, nblk, ts1, a.c, inv_cs);
-    } else if (NTW == 1 && ctx.uniform) {
+        if constexpr (C::k8Bit) {
+            auto shared = [&](auto uniform) {
+                SharedPipe<D, 2, 1, decltype(uniform)::value, C> pipe;
+                pipe.prime(ctx, wave, nblk);
+                load_q(1, pairs);
+                pipe.template run<PRECISE>(ctx, xbuf, wave, lane, nblk, ts1, a.c, inv_cs);
+            };
+            if (is_near(ctx)) shared(std::true_type()); else shared(std::false_type());
+        } else {
+            SharedPipe<D, 2, 1, false, C> pipe;
+            pipe.prime(ctx, wave, nblk);
+            load_q(1, pairs);
+            pipe.template run<PRECISE>(ctx, xbuf, wave, lane, nblk, ts1, a.c, inv_cs);
+        }
+    } else if (NTW == 1 && (C::k8Bit ? is_near(ctx) : ctx.uniform)) {
         WidePipe<D, 1, D == 128, 1, C> pipe;
         pipe.prime(ctx, wave, nblk);
-        load_q(1);
+        load_q(1, plain);
         pipe.template run<PRECISE>(ctx, xbuf, wave, lane, nblk, ts1, a.c, inv_cs);
     } else if (NTW == 1) {
         WidePipe<D, 1, false, 1, C> pipe;
         pipe.prime(ctx, wave, nblk);
-        load_q(1);
+        load_q(1, plain);
         pipe.template run<PRECISE>(ctx, xbuf, wave, lane, nblk, ts1, a.c, inv_cs);
-    } else if (ctx.uniform) {
+    } else if (C::k8Bit ? is_near(ctx) : ctx.uniform) {
         WidePipe<D, 2, D == 128, 2, C> pipe;  // the fast addressing is written for four loads per K loader
         pipe.prime(ctx, wave, nblk);
-        load_q(2);
+        load_q(2, plain);
         pipe.template run<PRECISE>(ctx, xbuf, wave, lane, nblk, ts, a.c, inv_cs);
     } else {
         WidePipe<D, 2, false, 2, C> pipe;
         pipe.prime(ctx, wave, nblk);
-        load_q(2);
+        load_q(2, plain);
         pipe.template run<PRECISE>(ctx, xbuf, wave, lane, nblk, ts, a.c, inv_cs);
     }
 

@@ -57,10 +57,10 @@ def test_null_arguments_are_refused():
 
 
 def _cache(k=1 << 12, v=1 << 13, ks=16, vs=16, n_rows=64, Hkv=2, d=64, block=16):
-    return binding._CacheQ8(k, v, ks, vs, n_rows, Hkv, d, block)
+    return binding._pack_cache(k, v, ks, vs, n_rows, Hkv, d, block)
 
 
-@pytest.mark.parametrize("bad", [dict(k=0), dict(v=0), dict(ks=0), dict(vs=0), dict(k=8), dict(v=24), dict(n_rows=63), dict(Hkv=0), dict(d=96),
+@pytest.mark.parametrize("bad", [dict(k=0), dict(v=0), dict(ks=0), dict(vs=0), dict(k=8), dict(v=24), dict(ks=17), dict(vs=18), dict(n_rows=63), dict(Hkv=0), dict(d=96),
                                  dict(block=8), dict(block=48), dict(block=0), dict(n_rows=-1)])
 def test_calls_refuse_a_cache_that_is_none_or_not_the_lists(bad):
     # all of these are refused before anything is launched: no address here is one
@@ -68,15 +68,15 @@ def test_calls_refuse_a_cache_that_is_none_or_not_the_lists(bad):
     rows = binding.deft_kv_rows([3, 63], 64, 16)
     x = ctypes.c_void_p(1 << 14)
     c = _cache(**bad)
-    assert lib.deft_kv_store_q8(rows.handle, x, x, x, 128, 128, ctypes.byref(c), None) == EINVAL
-    assert lib.deft_kv_load_q8(rows.handle, x, ctypes.byref(c), x, x, None) == EINVAL
+    assert lib.deft_kv_store_q8(rows.handle, x, x, x, 128, 128, c, None) == EINVAL
+    assert lib.deft_kv_load_q8(rows.handle, x, c, x, x, None) == EINVAL
 
 
 def test_calls_refuse_other_arguments():
     lib = binding.load_library()
     rows, copies = binding.deft_kv_rows([3, 63], 64, 16), binding.deft_kv_copies([0], [1], 4)
     x, odd = ctypes.c_void_p(1 << 14), ctypes.c_void_p((1 << 14) + 8)
-    c = ctypes.byref(_cache())
+    c = _cache()
     store = lambda *a: lib.deft_kv_store_q8(*a, c, None)  # noqa: E731
     for k_stride, v_stride in ((120, 128), (128, 120), (132, 128), (128, 130), (-128, 128)):
         assert store(rows.handle, x, x, x, k_stride, v_stride) == EINVAL
@@ -113,9 +113,9 @@ def test_attention_refuses_a_cache_that_is_none_or_too_small():
     call = lambda c: lib.deft_tree_attn_decode_q8(plan.handle, x, x, c, x, 2, 0.0, 0, x, 1 << 20, None)  # noqa: E731
     assert call(None) == EINVAL
     for bad in (dict(k=0), dict(vs=0), dict(v=8), dict(block=24), dict(d=32), dict(n_rows=59), dict(Hkv=3)):
-        assert call(ctypes.byref(_cache(**bad))) == EINVAL
-    assert call(ctypes.byref(_cache())) == -5  # a cache that is one; the plan has no image yet
-    assert lib.deft_tree_attn_decode_q8(None, x, x, ctypes.byref(_cache()), x, 2, 0.0, 0, x, 1 << 20, None) == EINVAL
+        assert call(_cache(**bad)) == EINVAL
+    assert call(_cache()) == -5  # a cache that is one; the plan has no image yet
+    assert lib.deft_tree_attn_decode_q8(None, x, x, _cache(), x, 2, 0.0, 0, x, 1 << 20, None) == EINVAL
 
 
 def test_binding_refuses_host_tensors():
