@@ -327,10 +327,11 @@ int deft_tree_attn_decode_static(const deft_plan_t *plan, const void *dev_image,
  *
  * k, v             : device, bytes [n_rows, Hkv, d], 16-byte aligned
  * k_scale, v_scale : device, bytes [ceil(n_rows / block_rows), Hkv], 4-byte aligned and read in whole 4-byte words
- * d                : 64 or 128
+ * Hkv, d           : at most DEFT_MAX_Q8_HEADS; 64 or 128
  * block_rows       : a power of two, 1 .. 64.  A block should belong to one node of the tree: choose a page size that is a
  *                    multiple of it, or with a contiguous cache begin nodes at multiples of it (block_rows = 1 suits any).
  */
+#define DEFT_MAX_Q8_HEADS 65536
 typedef struct deft_cache_q8 {
     void *k, *v;
     void *k_scale, *v_scale;

@@ -336,19 +336,19 @@ __device__ __forceinline__ void load_v(KVRegs<D> &r, const ChunkCtx<Bf16Cache> &
 }
 
 // Where the tokens of block `blk` of an 8-bit cache lie.  A token of it is given as r, the same in all lanes, and what the lane
-// adds to that: n16 (K) or 4g (V).  UNIFORM: the chunk's rows are consecutive (see is_near), so a token is (wave-uniform
+// adds to that: n16 (K) or 4g (V).  UNIFORM: the chunk is one piece, its rows are consecutive, so a token is (wave-uniform
 // pointer of the block) + a 32-bit offset, the smaller one of the token's and of the chunk's last row: two additions and a
-// minimum, where a product takes 16 cycles.  A block past the end is the last one again.
+// minimum.  Otherwise rows come from the per-token table, four to a read for V.  A block past the end is the last one again: no
+// branch around any load.
 template <bool UNIFORM>
 struct BlockAt {
     const ChunkCtx<E4m3Cache> &c;
     const uint8_t *k, *v, *ks, *vs;
     int x0, lim, low;
-    bool valid;
     uint32_t pitch, last, ks_rest, vs_rest;
     __device__ __forceinline__ BlockAt(const ChunkCtx<E4m3Cache> &ctx, int blk, int nblk) : c(ctx), pitch((uint32_t)ctx.row_stride) {
+        x0 = 32 * min(blk, nblk - 1);
         if (UNIFORM) {
-            x0 = 32 * min(blk, nblk - 1);
             lim = min(31, c.clen - 1 - x0);
             last = lim * pitch;
             const uint32_t row = (uint32_t)(c.begin0 + x0), block = row >> c.scales.shift;
@@ -362,18 +362,23 @@ struct BlockAt {
             vs_rest = (uint32_t)reinterpret_cast<uintptr_t>(vs) & 3;
             ks -= ks_rest;
             vs -= vs_rest;
-        } else {
-            valid = blk < nblk;
-            x0 = valid ? 32 * blk : 0;
         }
     }
-    __device__ __forceinline__ uint32_t row(int r, int lane) const { return (uint32_t)(valid ? tok_row(c, x0 + r + lane) : c.begin0); }
-    __device__ __forceinline__ uint32_t near(int r, uint32_t lane_bytes) const { return min(lane_bytes + (uint32_t)r * pitch, last); }
-    __device__ __forceinline__ const uint8_t *key(int r, uint32_t col) const {
-        return UNIFORM ? k + (near(r, c.scales.k_row) + col) : c.khead + ((uint64_t)row(r, c.n16) * pitch + col);
+    __device__ __forceinline__ uint32_t row(int r, int lane) const { return (uint32_t)c.s_row[x0 + r + lane]; }
+    // lane_bytes: those of the rows that the lane adds, and of its column
+    __device__ __forceinline__ uint32_t near(int r, uint32_t lane_bytes, uint32_t col) const {
+        return min(lane_bytes + (uint32_t)r * pitch, last + col);
     }
-    __device__ __forceinline__ const uint8_t *value(int r) const {
-        return UNIFORM ? v + (near(r, c.scales.v_row) + c.vlane) : c.vhead + ((uint64_t)row(r, 4 * c.g) * pitch + c.vlane);
+    __device__ __forceinline__ const uint8_t *key(int r, uint32_t col) const {
+        return UNIFORM ? k + near(r, c.scales.k_row + col, col) : c.khead + ((uint64_t)row(r, c.n16) * pitch + col);
+    }
+    // tokens r + 4g .. + 3, r a multiple of 16
+    __device__ __forceinline__ void values(int r, const uint8_t *(&at)[4]) const {
+        i32x4 rows{};
+        if (!UNIFORM) rows = *reinterpret_cast<const i32x4 *>(&c.s_row[x0 + r + 4 * c.g]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            at[i] = UNIFORM ? v + near(r + i, c.scales.v_row + c.vlane, c.vlane) : c.vhead + ((uint64_t)(uint32_t)rows[i] * pitch + c.vlane);
     }
     // the scale of token r + lane
     __device__ __forceinline__ ScaleWord scale(const uint8_t *head, uint32_t rest, int r, int lane) const {
@@ -390,9 +395,6 @@ struct BlockAt {
         return UNIFORM ? scale(vs, vs_rest, r, lane) : load_scale(c.scales.value(row(r, lane)));
     }
 };
-// Whether BlockAt<true> can be used.
-__device__ __forceinline__ bool is_near(const ChunkCtx<Bf16Cache> &c) { return c.uniform; }
-__device__ __forceinline__ bool is_near(const ChunkCtx<E4m3Cache> &c) { return c.uniform && c.scales.Hkv <= (1u << 16); }
 
 template <int D, bool UNIFORM>
 __device__ __forceinline__ void load_k(KVBytes<D> &r, const ChunkCtx<E4m3Cache> &c, int blk, int nblk) {
@@ -410,8 +412,10 @@ __device__ __forceinline__ void load_v(KVBytes<D> &r, const ChunkCtx<E4m3Cache> 
     const BlockAt<UNIFORM> b(c, blk, nblk);
 #pragma unroll
     for (int aa = 0; aa < 2; ++aa) {
+        const uint8_t *at[4];
+        b.values(16 * aa, at);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) r.v[4 * aa + i] = load8_kv<true>(b.value(16 * aa + i));
+        for (int i = 0; i < 4; ++i) r.v[4 * aa + i] = load8_kv<true>(at[i]);
         r.vs[aa] = b.value_scale(16 * aa);
     }
 }
@@ -802,7 +806,7 @@ __device__ __forceinline__ void issue_share(Share<D, TR, E4m3Cache> &s, const Ch
         const uint32_t lane_bytes = kl ? c.scales.k_row : c.scales.v_row, col = kl ? c.klane : c.vlane;
         const uint8_t *base = kl ? b.k : b.v;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) s.x[q] = load8_kv<false>(base + (b.near(first + (kl ? 0 : q), lane_bytes) + (col + (kl ? 32u * q : 0u))));
+        for (int q = 0; q < 4; ++q) s.x[q] = load8_kv<false>(base + (b.near(first + (kl ? 0 : q), lane_bytes + col, col) + (kl ? 32u * q : 0u)));
         s.ks = b.scale(kl ? b.ks : b.vs, kl ? b.ks_rest : b.vs_rest, first, kl ? c.n16 : 4 * c.g + (c.n16 & 3));
         return;
     }
@@ -824,8 +828,10 @@ __device__ __forceinline__ void issue_share(Share<D, TR, E4m3Cache> &s, const Ch
     }
     if (TR == 2 || t >= 2) {
         const int first = 16 * (TR == 2 ? t : t - 2);
+        const uint8_t *at[4];
+        b.values(first, at);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) s.x[(TR == 2 ? KK : 0) + q] = load8_kv<TR == 2>(b.value(first + q));
+        for (int q = 0; q < 4; ++q) s.x[(TR == 2 ? KK : 0) + q] = load8_kv<TR == 2>(at[q]);
         (TR == 2 ? s.vs : s.ks) = b.value_scale(first);
     }
 }
@@ -1670,7 +1676,7 @@ __device__ __forceinline__ LeftRows streaming_task(const typename C::Args &a, co
                 load_q(1, pairs);
                 pipe.template run<PRECISE>(ctx, wave, nblk, ts1, a.c);
             };
-            if (is_near(ctx)) split(std::true_type()); else split(std::false_type());
+            if (ctx.uniform) split(std::true_type()); else split(std::false_type());
         } else {
             SplitPipe<D, false, C> pipe;
             pipe.prime(ctx, wave, nblk);
@@ -1685,14 +1691,14 @@ __device__ __forceinline__ LeftRows streaming_task(const typename C::Args &a, co
                 load_q(1, pairs);
                 pipe.template run<PRECISE>(ctx, xbuf, wave, lane, nblk, ts1, a.c, inv_cs);
             };
-            if (is_near(ctx)) shared(std::true_type()); else shared(std::false_type());
+            if (ctx.uniform) shared(std::true_type()); else shared(std::false_type());
         } else {
             SharedPipe<D, 2, 1, false, C> pipe;
             pipe.prime(ctx, wave, nblk);
             load_q(1, pairs);
             pipe.template run<PRECISE>(ctx, xbuf, wave, lane, nblk, ts1, a.c, inv_cs);
         }
-    } else if (NTW == 1 && (C::k8Bit ? is_near(ctx) : ctx.uniform)) {
+    } else if (NTW == 1 && ctx.uniform) {
         WidePipe<D, 1, D == 128, 1, C> pipe;
         pipe.prime(ctx, wave, nblk);
         load_q(1, plain);
@@ -1702,7 +1708,7 @@ __device__ __forceinline__ LeftRows streaming_task(const typename C::Args &a, co
         pipe.prime(ctx, wave, nblk);
         load_q(1, plain);
         pipe.template run<PRECISE>(ctx, xbuf, wave, lane, nblk, ts1, a.c, inv_cs);
-    } else if (C::k8Bit ? is_near(ctx) : ctx.uniform) {
+    } else if (ctx.uniform) {
         WidePipe<D, 2, D == 128, 2, C> pipe;  // the fast addressing is written for four loads per K loader
         pipe.prime(ctx, wave, nblk);
         load_q(2, plain);

@@ -60,7 +60,7 @@ def _cache(k=1 << 12, v=1 << 13, ks=16, vs=16, n_rows=64, Hkv=2, d=64, block=16)
     return binding._pack_cache(k, v, ks, vs, n_rows, Hkv, d, block)
 
 
-@pytest.mark.parametrize("bad", [dict(k=0), dict(v=0), dict(ks=0), dict(vs=0), dict(k=8), dict(v=24), dict(ks=17), dict(vs=18), dict(n_rows=63), dict(Hkv=0), dict(d=96),
+@pytest.mark.parametrize("bad", [dict(k=0), dict(v=0), dict(ks=0), dict(vs=0), dict(k=8), dict(v=24), dict(ks=17), dict(vs=18), dict(n_rows=63), dict(Hkv=0), dict(Hkv=65537), dict(d=96),
                                  dict(block=8), dict(block=48), dict(block=0), dict(n_rows=-1)])
 def test_calls_refuse_a_cache_that_is_none_or_not_the_lists(bad):
     # all of these are refused before anything is launched: no address here is one
