@@ -325,7 +325,7 @@ int deft_tree_attn_decode_static(const deft_plan_t *plan, const void *dev_image,
  * every block of block_rows consecutive rows of the pool has, for each KV head, a scale: a power of two 2^(e - 127), kept as the
  * byte e, 10 <= e <= 246.  A row's values are its bytes' values times the scale; every such product is a bf16 number.
  *
- * k, v             : device, bytes [n_rows, Hkv, d], 16-byte aligned
+ * k, v             : device, bytes [n_rows, Hkv, d], 16-byte aligned (these four may be NULL when n_rows == 0)
  * k_scale, v_scale : device, bytes [ceil(n_rows / block_rows), Hkv], 4-byte aligned and read in whole 4-byte words
  * Hkv, d           : at most DEFT_MAX_Q8_HEADS; 64 or 128
  * block_rows       : a power of two, 1 .. 64.  A block should belong to one node of the tree: choose a page size that is a

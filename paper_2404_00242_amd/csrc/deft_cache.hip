@@ -430,13 +430,13 @@ extern "C" int deft_kv_copy_pages(const deft_kv_list_t *list, const void *dev_im
             todo.push_back({static_cast<uint8_t *>(pools[i]), page_bytes[i], (uint32_t)width});
         }
         std::sort(todo.begin(), todo.end(), [](const Pool &a, const Pool &b) { return a.at < b.at; });
+        for (size_t i = 1; i < todo.size(); ++i)
+            if (todo[i].at - todo[i - 1].at < todo[i - 1].page * list->pool) return DEFT_EINVAL;
+        if (list->heads == 0) return DEFT_OK;
+        std::stable_sort(todo.begin(), todo.end(), [](const Pool &a, const Pool &b) { return a.page != b.page ? a.page > b.page : a.width > b.width; });
     } catch (...) {
         return DEFT_ENOMEM;
     }
-    for (size_t i = 1; i < todo.size(); ++i)
-        if (todo[i].at - todo[i - 1].at < todo[i - 1].page * list->pool) return DEFT_EINVAL;
-    if (list->heads == 0) return DEFT_OK;
-    std::stable_sort(todo.begin(), todo.end(), [](const Pool &a, const Pool &b) { return a.page != b.page ? a.page > b.page : a.width > b.width; });
     const uint8_t *img = static_cast<const uint8_t *>(dev_image);
     for (size_t i = 0; i < todo.size();) {
         CopyArgs a{};

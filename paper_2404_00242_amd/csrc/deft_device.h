@@ -17,7 +17,8 @@ inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 
 
 // Whether a cache's description is one: what any call on it asks for before it reads from it.
 inline bool cache_ok(const deft_cache_q8_t *c) {
-    if (!c || !c->k || !c->v || !c->k_scale || !c->v_scale || !aligned16(c->k) || !aligned16(c->v)) return false;
+    if (!c || !aligned16(c->k) || !aligned16(c->v)) return false;
+    if (c->n_rows > 0 && (!c->k || !c->v || !c->k_scale || !c->v_scale)) return false;
     if ((reinterpret_cast<uintptr_t>(c->k_scale) | reinterpret_cast<uintptr_t>(c->v_scale)) & 3) return false;
     if (c->n_rows < 0 || c->Hkv <= 0 || c->Hkv > DEFT_MAX_Q8_HEADS || (c->d != 64 && c->d != 128)) return false;
     return c->block_rows >= 1 && c->block_rows <= 64 && (c->block_rows & (c->block_rows - 1)) == 0;

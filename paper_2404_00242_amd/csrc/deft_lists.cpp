@@ -53,20 +53,32 @@ int build_rows(const int32_t *rows, int32_t n, int32_t n_pool_rows, int32_t bloc
 // read at the chain's beginning.  What hangs from one page that is not overwritten can be done in any order: a chain to each.
 int build_copies(const int32_t *src, const int32_t *dst, int32_t n, int32_t n_pool_pages, deft_kv_list_s &list) {
     using deft::CopyStep;
-    std::vector<int32_t> from((size_t)n_pool_pages, -1), first_out((size_t)n_pool_pages, -1), next_out((size_t)n_pool_pages, -1);
+    // the pages that have a part in it, numbered by themselves: a few copies in a large pool cost what a few copies cost
+    std::vector<int32_t> pages;
+    pages.reserve(2 * (size_t)n);
     for (int32_t i = 0; i < n; ++i) {
         if (src[i] < 0 || src[i] >= n_pool_pages || dst[i] < 0 || dst[i] >= n_pool_pages) return DEFT_EINVAL;
-        if (from[dst[i]] >= 0) return DEFT_EINVAL;
-        from[dst[i]] = src[i];
+        pages.push_back(src[i]);
+        pages.push_back(dst[i]);
     }
-    for (int32_t i = n - 1; i >= 0; --i) {  // copies out of a page as a list of destinations
-        if (src[i] == dst[i]) continue;
-        next_out[dst[i]] = first_out[src[i]];
-        first_out[src[i]] = dst[i];
+    std::sort(pages.begin(), pages.end());
+    pages.erase(std::unique(pages.begin(), pages.end()), pages.end());
+    auto number = [&](int32_t page) { return (int32_t)(std::lower_bound(pages.begin(), pages.end(), page) - pages.begin()); };
+    const int32_t n_pages = (int32_t)pages.size();
+    std::vector<int32_t> from((size_t)n_pages, -1), first_out((size_t)n_pages, -1), next_out((size_t)n_pages, -1);
+    for (int32_t i = 0; i < n; ++i) {
+        const int32_t d = number(dst[i]);
+        if (from[d] >= 0) return DEFT_EINVAL;
+        from[d] = number(src[i]);
+    }
+    for (int32_t d = n_pages - 1; d >= 0; --d) {  // copies out of a page as a list of destinations
+        if (from[d] < 0 || from[d] == d) continue;
+        next_out[d] = first_out[from[d]];
+        first_out[from[d]] = d;
     }
     std::vector<deft::CopyChain> chains;
     std::vector<CopyStep> steps;
-    std::vector<char> done((size_t)n_pool_pages, 0);  // pages the copy into which has its place
+    std::vector<char> done((size_t)n_pages, 0);  // pages the copy into which has its place
     std::vector<int32_t> path;
     // the copies below `top` and, last, the one into it; next: the copies out of a page that are still to come
     std::vector<int32_t> next(first_out);
@@ -81,14 +93,14 @@ int build_copies(const int32_t *src, const int32_t *dst, int32_t n, int32_t n_po
             }
             path.pop_back();
             if (p == top && !into_top) continue;
-            steps.push_back({from[p], p});
+            steps.push_back({pages[from[p]], pages[p]});
             done[p] = 1;
         }
     };
     auto open = [&] { chains.push_back({(int32_t)steps.size(), 0, 0, 0}); };
     auto close = [&] { chains.back().count = (int32_t)steps.size() - chains.back().first; };
     auto moved = [&](int32_t p) { return from[p] >= 0 && from[p] != p; };
-    for (int32_t p = 0; p < n_pool_pages; ++p) {
+    for (int32_t p = 0; p < n_pages; ++p) {
         if (moved(p)) continue;  // not overwritten: every copy out of it begins a chain
         for (int32_t c = first_out[p]; c >= 0; c = next_out[c]) {
             open();
@@ -97,7 +109,7 @@ int build_copies(const int32_t *src, const int32_t *dst, int32_t n, int32_t n_po
         }
     }
     std::vector<int32_t> ring;
-    for (int32_t p = 0; p < n_pool_pages; ++p) {
+    for (int32_t p = 0; p < n_pages; ++p) {
         if (!moved(p) || done[p]) continue;
         // what is left are cycles and what hangs from them: go back until a page comes again, it is on the cycle
         ring.clear();
@@ -111,7 +123,7 @@ int build_copies(const int32_t *src, const int32_t *dst, int32_t n, int32_t n_po
         for (int32_t y : ring) done[y] = 1;
         open();
         for (int32_t y : ring) subtree(y, false);
-        for (int32_t y : ring) steps.push_back({from[y], y});
+        for (int32_t y : ring) steps.push_back({pages[from[y]], pages[y]});
         close();
         chains.back().held = 1;
     }
@@ -170,11 +182,10 @@ extern "C" int deft_compact_pages(const int32_t *node_page_ptr, const int32_t *p
     const int32_t n = node_page_ptr[n_nodes];
     if (n > n_pool_pages || (n > 0 && (!page_ids || !new_page_ids || !src || !dst))) return DEFT_EINVAL;
     try {
-        std::vector<char> owned((size_t)n_pool_pages, 0);
-        for (int32_t i = 0; i < n; ++i) {
-            if (page_ids[i] < 0 || page_ids[i] >= n_pool_pages || owned[page_ids[i]]) return DEFT_EINVAL;
-            owned[page_ids[i]] = 1;
-        }
+        std::vector<int32_t> owned(page_ids, page_ids + n);
+        std::sort(owned.begin(), owned.end());
+        if (n > 0 && (owned.front() < 0 || owned.back() >= n_pool_pages)) return DEFT_EINVAL;
+        if (std::adjacent_find(owned.begin(), owned.end()) != owned.end()) return DEFT_EINVAL;
         // sibling lists in ascending order; roots are the children of node n_nodes
         std::vector<int32_t> child((size_t)n_nodes + 1, -1), sibling((size_t)n_nodes, -1), path;
         for (int32_t u = n_nodes - 1; u >= 0; --u) {

@@ -271,6 +271,9 @@ def test_empty_paths_and_no_queries():
     Q, c, K, V = filled(t, 16, 2)
     got = check(t, plan_of(t), Q, c, K, V, True)
     assert bool((got[0] == 0).all()) and bool((got[2] == 0).all())
+    nothing = binding.alloc_kv_cache_q8(0, 2, 64, 16, dev())
+    hollow = binding.deft_plan([0, 0], [0, 0], [-1, 0], [1, 0, 1], 0)
+    assert bool((binding.deft_tree_attn_decode_q8(hollow, Q[:3].to(dev()), nothing) == 0).all())
     none = binding.deft_plan(t.node_tok_begin, t.node_tok_len, t.node_parent, [], t.ntok)
     assert binding.deft_tree_attn_decode_q8(none, Q[:0].to(dev()), c).shape == (0, 8, 64)
 
