@@ -145,15 +145,10 @@ template <bool ONCE>
 __device__ __forceinline__ u32x4 load16_kv(const uint16_t *p) {
     return ONCE ? load16_once(p) : load16(p);
 }
-// of an 8-bit cache: 16 and 8 values
-template <bool ONCE>
-__device__ __forceinline__ u32x4 load16_kv(const uint8_t *p) {
-    return ONCE ? __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p)) : *reinterpret_cast<const u32x4 *>(p);
-}
-template <bool ONCE>
-__device__ __forceinline__ u32x2 load8_kv(const uint8_t *p) {
-    return ONCE ? __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(p)) : *reinterpret_cast<const u32x2 *>(p);
-}
+// of an 8-bit cache: 16 and 8 values, always through the caches (non-temporal loads cost 1 to 5 % there: K is asked for in halves
+// of a line)
+__device__ __forceinline__ u32x4 load16_q8(const uint8_t *p) { return *reinterpret_cast<const u32x4 *>(p); }
+__device__ __forceinline__ u32x2 load8_q8(const uint8_t *p) { return *reinterpret_cast<const u32x2 *>(p); }
 
 // Four e4m3 values times a scale, as four bf16 values.  The scale is a float's exponent.
 __device__ __forceinline__ u32x2 widen4(uint32_t x, float scale) {
@@ -183,7 +178,7 @@ __device__ __forceinline__ ScaleWord load_scale(const uint8_t *base, uint32_t at
 template <int Q>
 __device__ __forceinline__ float scale_of_token(float scale) {
     const int x = __builtin_bit_cast(int, scale);
-    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(x, x, 0x55 * Q, 0xf, 0xf, false));
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(x, 0x55 * Q, 0xf, 0xf, false));
 }
 
 // Partial results.  SHARED: in a call of one launch they are stored past the L2 of their XCD, and read past the reader's,
@@ -403,7 +398,7 @@ __device__ __forceinline__ void load_k(KVBytes<D> &r, const ChunkCtx<E4m3Cache> 
     for (int aa = 0; aa < 2; ++aa) {
         const uint8_t *kp = b.key(16 * aa, 16 * c.g);
 #pragma unroll
-        for (int i = 0; i < D / 64; ++i) r.k[aa][i] = load16_kv<true>(kp + 64 * i);
+        for (int i = 0; i < D / 64; ++i) r.k[aa][i] = load16_q8(kp + 64 * i);
         r.ks[aa] = b.key_scale(16 * aa);
     }
 }
@@ -415,7 +410,7 @@ __device__ __forceinline__ void load_v(KVBytes<D> &r, const ChunkCtx<E4m3Cache> 
         const uint8_t *at[4];
         b.values(16 * aa, at);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) r.v[4 * aa + i] = load8_kv<true>(at[i]);
+        for (int i = 0; i < 4; ++i) r.v[4 * aa + i] = load8_q8(at[i]);
         r.vs[aa] = b.value_scale(16 * aa);
     }
 }
@@ -695,52 +690,42 @@ __device__ __forceinline__ void compute_block(const KVRegs<D> &r, const ChunkCtx
 // front of the other workgroup's loads longer.  Stage 1, two blocks -> one reloaded whole -> in halves: sixteen
 // sequences (148 MB) 29.9 -> 28.8 -> 27.8 us, few-shot prefix (149 MB) 28.7 -> 28.7 -> 27.7, reasoning tree of 256
 // queries (456 MB) 96.2 -> 94.5 -> 93.6.
-// An 8-bit block is half as many bytes in flight and half the registers, and takes more instructions between its loads: two
-// blocks per wave there.
+// The same for an 8-bit cache: a second and a third block in flight per wave, and two blocks worked on at once, change nothing or
+// cost 2 % (stage 1, few-shot and reasoning tree).
 template <int D, bool UNIFORM, typename C>
 struct SplitPipe {
-    static constexpr int DEPTH = C::k8Bit ? 2 : 1;
-    std::conditional_t<C::k8Bit, KVBytes<D>, KVRegs<D>> r[DEPTH];
+    std::conditional_t<C::k8Bit, KVBytes<D>, KVRegs<D>> r;
     __device__ __forceinline__ void prime(const ChunkCtx<C> &ctx, int wave, int nblk) {
-        if constexpr (!C::k8Bit) {
-            load_k<D>(r[0], ctx, wave * 32, wave < nblk);
-            load_v<D>(r[0], ctx, wave * 32, wave < nblk);
+        if constexpr (C::k8Bit) {
+            load_k<D, UNIFORM>(r, ctx, wave, nblk);
+            load_v<D, UNIFORM>(r, ctx, wave, nblk);
         } else {
-#pragma unroll
-            for (int u = 0; u < DEPTH; ++u) {
-                load_k<D, UNIFORM>(r[u], ctx, wave + u * kWaves, nblk);
-                load_v<D, UNIFORM>(r[u], ctx, wave + u * kWaves, nblk);
-            }
+            load_k<D>(r, ctx, wave * 32, wave < nblk);
+            load_v<D>(r, ctx, wave * 32, wave < nblk);
         }
     }
     template <bool PRECISE>
-    __device__ __forceinline__ void step(int u, const ChunkCtx<C> &ctx, int blk, int next, int nblk, TileState<D> (&ts)[1], float cs) {
-        f32x4 sacc[1][2];
-        bf16x8 preg[1], plo[1];
-        qk_block<D, 1>(keys(r[u]), ts, sacc);
-        if constexpr (C::k8Bit)
-            load_k<D, UNIFORM>(r[u], ctx, next, nblk);
-        else
-            load_k<D>(r[u], ctx, next * 32, next < nblk);
-        __builtin_amdgcn_sched_barrier(0);  // the loads go out here, not behind the softmax
-        mask_block<D, 1>(ctx, blk * 32, ts, sacc);
-        shift_block<D, 1>(ts, sacc, cs);
-        raise_block<D, 1>(ts, sacc);
-        weights_block<D, 1, PRECISE>(ts, sacc, cs, preg, plo);
-        pv_block<D, 1, PRECISE>(values(r[u]), preg, plo, ts);
-        if constexpr (C::k8Bit)
-            load_v<D, UNIFORM>(r[u], ctx, next, nblk);
-        else
-            load_v<D>(r[u], ctx, next * 32, next < nblk);
-    }
-    template <bool PRECISE>
     __device__ __forceinline__ void run(const ChunkCtx<C> &ctx, int wave, int nblk, TileState<D> (&ts)[1], float cs) {
-        int blk = wave;
-        for (; blk + (DEPTH - 1) * kWaves < nblk; blk += DEPTH * kWaves)
-#pragma unroll
-            for (int u = 0; u < DEPTH; ++u)
-                step<PRECISE>(u, ctx, blk + u * kWaves, blk + (u + DEPTH) * kWaves, nblk, ts, cs);
-        if (DEPTH > 1 && blk < nblk) step<PRECISE>(0, ctx, blk, nblk, nblk, ts, cs);
+        for (int blk = wave; blk < nblk; blk += kWaves) {
+            const int next = blk + kWaves;
+            f32x4 sacc[1][2];
+            bf16x8 preg[1], plo[1];
+            qk_block<D, 1>(keys(r), ts, sacc);
+            if constexpr (C::k8Bit)
+                load_k<D, UNIFORM>(r, ctx, next, nblk);
+            else
+                load_k<D>(r, ctx, next * 32, next < nblk);
+            __builtin_amdgcn_sched_barrier(0);  // the loads go out here, not behind the softmax
+            mask_block<D, 1>(ctx, blk * 32, ts, sacc);
+            shift_block<D, 1>(ts, sacc, cs);
+            raise_block<D, 1>(ts, sacc);
+            weights_block<D, 1, PRECISE>(ts, sacc, cs, preg, plo);
+            pv_block<D, 1, PRECISE>(values(r), preg, plo, ts);
+            if constexpr (C::k8Bit)
+                load_v<D, UNIFORM>(r, ctx, next, nblk);
+            else
+                load_v<D>(r, ctx, next * 32, next < nblk);
+        }
     }
 };
 
@@ -806,7 +791,7 @@ __device__ __forceinline__ void issue_share(Share<D, TR, E4m3Cache> &s, const Ch
         const uint32_t lane_bytes = kl ? c.scales.k_row : c.scales.v_row, col = kl ? c.klane : c.vlane;
         const uint8_t *base = kl ? b.k : b.v;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) s.x[q] = load8_kv<false>(base + (b.near(first + (kl ? 0 : q), lane_bytes + col, col) + (kl ? 32u * q : 0u)));
+        for (int q = 0; q < 4; ++q) s.x[q] = load8_q8(base + (b.near(first + (kl ? 0 : q), lane_bytes + col, col) + (kl ? 32u * q : 0u)));
         s.ks = b.scale(kl ? b.ks : b.vs, kl ? b.ks_rest : b.vs_rest, first, kl ? c.n16 : 4 * c.g + (c.n16 & 3));
         return;
     }
@@ -815,14 +800,14 @@ __device__ __forceinline__ void issue_share(Share<D, TR, E4m3Cache> &s, const Ch
             const uint8_t *kp = b.key(16 * t, 16 * c.g);
 #pragma unroll
             for (int i = 0; i < KK / 2; ++i) {
-                const u32x4 y = load16_kv<true>(kp + 64 * i);
+                const u32x4 y = load16_q8(kp + 64 * i);
                 s.x[2 * i] = u32x2{y[0], y[1]};
                 s.x[2 * i + 1] = u32x2{y[2], y[3]};
             }
         } else {
             const uint8_t *kp = b.key(16 * t, 8 * c.g);
 #pragma unroll
-            for (int q = 0; q < KK; ++q) s.x[q] = load8_kv<false>(kp + 32 * q);
+            for (int q = 0; q < KK; ++q) s.x[q] = load8_q8(kp + 32 * q);
         }
         s.ks = b.key_scale(16 * t);
     }
@@ -831,7 +816,7 @@ __device__ __forceinline__ void issue_share(Share<D, TR, E4m3Cache> &s, const Ch
         const uint8_t *at[4];
         b.values(first, at);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) s.x[(TR == 2 ? KK : 0) + q] = load8_kv<TR == 2>(at[q]);
+        for (int q = 0; q < 4; ++q) s.x[(TR == 2 ? KK : 0) + q] = load8_q8(at[q]);
         (TR == 2 ? s.vs : s.ks) = b.value_scale(first);
     }
 }
@@ -1177,7 +1162,7 @@ struct ResidentTask {
                 const int row = tok_row(c, min(x0 + 16 * aa + c.n16, c.clen - 1));
                 const uint8_t *kp = k_lane + (size_t)row * c.row_stride;
 #pragma unroll
-                for (int i = 0; i < D / 64; ++i) kb[b][aa][i] = load16_kv<false>(kp + 64 * i);
+                for (int i = 0; i < D / 64; ++i) kb[b][aa][i] = load16_q8(kp + 64 * i);
                 ks[b][aa] = load_scale(c.scales.key(row));
                 vs[b][aa] = load_scale(c.scales.value(tok_row(c, min(x0 + 16 * aa + 4 * c.g + (c.n16 & 3), c.clen - 1))));
             }
