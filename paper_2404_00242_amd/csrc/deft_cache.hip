@@ -204,12 +204,14 @@ __global__ __launch_bounds__(256) void deft_load_q8(LoadArgs a) {
 // list's order: pages may be read and overwritten in one call without a second copy of anything, because no other thread ever
 // touches those bytes.  That no page is overwritten before it was read makes it right to ask for later pages ahead of the stores.
 // Most chains are one copy long (forks), so a thread takes four words where that leaves enough threads; all lanes of a wave have
-// one chain where pages are that large.  The stores are not kept in the caches.  40 pages of 16 rows in 64 bf16 pools, 168 MB
-// moved: a word to a thread 51 us, four 38, and with such stores 30.6 (5.5 TB/s; a copy of 1 GiB 5.15).
+// one chain where pages are that large.  The stores are not kept in the caches.  Bound by HBM: 40 pages of 16 rows in 64 bf16
+// pools, 168 MB moved, a word to a thread 51 us, four 38, and with such stores 30.6 (5.5 TB/s; a copy of 1 GiB 5.15).
 constexpr int kMaxPools = 256;  // to a launch, 2 KB of its arguments
 constexpr int kMaxClasses = 4;  // sizes of pages among them
 constexpr uint32_t kMaxGroups = 1u << 16;  // workgroups to a pool; more work goes round
-constexpr uint32_t kManyWaves = 4096;      // of four words to a thread: half of what the chip holds
+// Waves of four words to a thread from which on a thread takes four: a quarter of what the chip holds.  us, one word -> four: 1024
+// waves 5.6 -> 6.1, 5.3 -> 6.1 and 5.2 -> 4.8; 2048 8.0 -> 7.6 and 7.6 -> 6.1; 4096 13.8 -> 10.4; 20480 51 -> 30; 65536 152 -> 87.
+constexpr uint32_t kManyWaves = 2048;
 
 struct PoolClass {
     uint32_t begin_group, begin_pool;  // first workgroup, first pool
