@@ -15,8 +15,9 @@
  *     memory on the current device.  The library allocates no device memory (only, at
  *     the first deft_plan_upload on a device, 5 MiB of pinned host memory for staging):
  *     Q/K/V/O, the plan's device image and the workspace all belong to the caller.
- *   - deft_tree_attn_decode only enqueues kernels on the given stream; it does not
- *     synchronise.  Calls that share a workspace must be ordered by the caller.
+ *   - deft_tree_attn_decode and the calls on caches and pools only enqueue kernels on the given stream;
+ *     they do not synchronise.  Calls that share a workspace, and calls of which one writes what the other
+ *     reads or writes, must be ordered by the caller.
  */
 #ifndef DEFT_H_
 #define DEFT_H_
@@ -341,7 +342,8 @@ typedef struct deft_cache_q8 {
 /*
  * deft_tree_attn_decode over an 8-bit cache: softmax(scale * q K^T) V over the tokens of each query's path, K and V the values
  * that the cache holds.  The plan, its image, the workspace, o, scale, flags and the errors are those of deft_tree_attn_decode
- * (Hkv and d are the cache's); besides, a cache with fewer rows than the plan addresses is refused with DEFT_EINVAL.
+ * (Hkv and d are the cache's); besides, a cache with fewer rows than the plan addresses is refused with DEFT_EINVAL.  (The ordinary
+ * call that has to come before a captured one is one of this kind.)
  * A float result (DEFT_OUT_F32) is computed with two-term softmax weights in every group, whatever the plan says.
  * A NaN among the keys of a token makes the results NaN of exactly the queries that see it.  Values (V) must be finite, which
  * those that deft_kv_store_q8 writes are: a token with weight 0 that is not on a query's path still takes part in its products.

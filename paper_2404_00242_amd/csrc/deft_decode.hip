@@ -13,6 +13,8 @@
 //                                                   16-bit interleave in registers (v_perm_b32),
 //                                                   B = P^T, which is S^T's accumulator layout as is
 //
+// A cache in 8 bits (E4m3Cache) is widened to the same operands in registers.
+//
 // Each token row of one head (2*d bytes, contiguous) is fetched from HBM exactly once per task and every
 // byte of every 64-byte sector requested is used.  A narrow group (one row tile) splits the chunk's
 // tokens over the four waves, each keeping a block of loads in flight in registers.  A wider group
