@@ -385,7 +385,8 @@ void deft_kv_list_destroy(deft_kv_list_t *list);
  * nearest, ties to even; what is above 448 * 2^119 becomes that.
  * A token of which K or V holds an infinity or a NaN, in any of a head's elements, is stored for that head with a NaN in every
  * element of its key and zeros for its value, and has no part in the scale.
- * Errors: DEFT_EINVAL (null, misaligned, a list of copies, a cache smaller than the list's pool or with other blocks), DEFT_EHIP.
+ * Errors: DEFT_EINVAL (null, misaligned, a list of copies, a cache smaller than the list's pool or with other blocks or with K and V
+ * in one place), DEFT_EHIP.
  *
  * deft_kv_load_q8 is the way back: token i of k and v (device bf16 [n, Hkv, d], contiguous, 16-byte aligned) is the value of row
  * rows[i], exactly.  k or v may be NULL: then only the other is read.

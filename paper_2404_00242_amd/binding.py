@@ -183,6 +183,15 @@ def _i32(x):
     return np.ascontiguousarray(np.asarray(x), dtype=np.int32).reshape(-1)
 
 
+def _indices(x, what: str):
+    """_i32 of whole numbers that int32 holds: others are refused and not cut short."""
+    a = np.asarray(x)
+    if a.dtype != np.int32 and a.size:
+        if a.dtype.kind not in "iu" or int(a.min()) < -(1 << 31) or int(a.max()) >= 1 << 31:
+            raise DeftError(-1, f"{what}: rows, pages and tables are whole numbers of 32 bits")
+    return _i32(a)
+
+
 def _address(x):
     """Address of an _i32 array's data, None for an empty one."""
     return x.__array_interface__["data"][0] if x.size else None
@@ -474,13 +483,14 @@ def _cache_args(cache: CacheQ8, what: str):
     """(a deft_cache_q8_t, its device's index, n_rows, Hkv, d) of a cache that is one."""
     torch = _torch or _get_torch()
     k, v, ks, vs, block = cache
+    block = int(block)
     index = k.get_device()
     if index < 0 or not index == v.get_device() == ks.get_device() == vs.get_device():
         raise DeftError(-1, f"{what}: the cache must be on one device (there is no CPU path)")
     shape = k.shape
     if not (k.dtype == v.dtype == torch.float8_e4m3fn and len(shape) == 3 and v.shape == shape and k.is_contiguous() and v.is_contiguous()):
         raise DeftError(-1, f"{what}: k and v of the cache must both be contiguous [n_rows, Hkv, d] float8_e4m3fn tensors")
-    if type(block) is not int or not 0 < block <= MAX_BLOCK_ROWS or block & (block - 1):
+    if not 0 < block <= MAX_BLOCK_ROWS or block & (block - 1):
         raise DeftError(-1, f"{what}: block_rows must be a power of two up to {MAX_BLOCK_ROWS}")
     n_rows, Hkv, d = shape
     blocks = ks.shape
@@ -518,7 +528,8 @@ class KVList:
 
     def image(self, device, stream=None):
         """Device image of the list, uploaded on first use.  A call on another stream than the upload's waits for it.  A graph
-        that captures the first use, or one while the upload may still be under way elsewhere, uploads an image of its own."""
+        that captures the first use, or one while the upload may still be under way elsewhere, uploads an image of its own, for
+        each call: ask for the image before the capture.  The list has to live as long as a graph that uses it."""
         torch = _torch or _get_torch()
         index = torch.device(device).index
         if index is None:
@@ -555,7 +566,7 @@ class KVList:
 
 def deft_kv_rows(rows, n_pool_rows: int, block_rows: int = 32) -> KVList:
     """The rows of an 8-bit cache that tokens 0, 1, ... go to or come from, for deft_kv_store_q8 and deft_kv_load_q8."""
-    r = _i32(rows)
+    r = _indices(rows, "deft_kv_rows")
     out = ctypes.c_void_p()
     _check(load_library().deft_kv_rows(_address(r), r.size, int(n_pool_rows), int(block_rows), ctypes.byref(out)), "deft_kv_rows")
     return KVList(out, r.size, int(n_pool_rows), int(block_rows))
@@ -563,7 +574,7 @@ def deft_kv_rows(rows, n_pool_rows: int, block_rows: int = 32) -> KVList:
 
 def deft_kv_copies(src, dst, n_pool_pages: int) -> KVList:
     """Copies of pages for deft_kv_copy_pages: page dst[i] becomes what page src[i] held, for all i at once."""
-    a, b = _i32(src), _i32(dst)
+    a, b = _indices(src, "deft_kv_copies"), _indices(dst, "deft_kv_copies")
     if a.size != b.size:
         raise DeftError(-1, "deft_kv_copies: src and dst differ in length")
     out = ctypes.c_void_p()
@@ -573,7 +584,7 @@ def deft_kv_copies(src, dst, n_pool_pages: int) -> KVList:
 
 def deft_compact_pages(node_page_ptr, page_ids, n_pool_pages: int, node_parent):
     """(new page_ids, src, dst): the copies that put every node's pages in a row, nodes depth-first, from page 0 on."""
-    pp, pg, par = _i32(node_page_ptr), _i32(page_ids), _i32(node_parent)
+    pp, pg, par = (_indices(x, "deft_compact_pages") for x in (node_page_ptr, page_ids, node_parent))
     if pp.size != par.size + 1 or (pp.size and int(pp[-1]) != pg.size):
         raise DeftError(-1, "deft_compact_pages: tables differ in length")
     new, src, dst = (np.zeros(max(1, pg.size), dtype=np.int32) for _ in range(3))

@@ -364,6 +364,7 @@ extern "C" int deft_kv_store_q8(const deft_kv_list_t *list, const void *dev_imag
                                 int64_t v_stride, const deft_cache_q8_t *cache, void *stream) {
     if (!rows_fit(list, dev_image, cache)) return DEFT_EINVAL;
     if (list->entries == 0) return DEFT_OK;
+    if (cache->k == cache->v || cache->k_scale == cache->v_scale) return DEFT_EINVAL;
     const int64_t least = (int64_t)cache->Hkv * cache->d;
     if (!k || !v || !deft::aligned16(k) || !deft::aligned16(v)) return DEFT_EINVAL;
     if (k_stride < least || v_stride < least || (k_stride & 7) || (v_stride & 7)) return DEFT_EINVAL;
@@ -389,7 +390,7 @@ extern "C" int deft_kv_store_q8(const deft_kv_list_t *list, const void *dev_imag
 extern "C" int deft_kv_load_q8(const deft_kv_list_t *list, const void *dev_image, const deft_cache_q8_t *cache, void *k, void *v, void *stream) {
     if (!rows_fit(list, dev_image, cache)) return DEFT_EINVAL;
     if (list->entries == 0 || (!k && !v)) return DEFT_OK;
-    if (!deft::aligned16(k) || !deft::aligned16(v)) return DEFT_EINVAL;
+    if (!deft::aligned16(k) || !deft::aligned16(v) || k == v) return DEFT_EINVAL;
     const int64_t per_row = (int64_t)cache->Hkv * cache->d / 16, threads = per_row * list->entries;
     if (threads > INT32_MAX - 512) return DEFT_EINVAL;  // threads of a launch are counted in 32 bits, K's and V's together
     const uint8_t *img = static_cast<const uint8_t *>(dev_image);

@@ -24,7 +24,8 @@ def test_lists_under_the_sanitizers(tmp_path):
 
 
 @pytest.mark.parametrize("rows,pool,block", [([0, 4], 4, 1), ([-1], 4, 1), ([3, 1, 3], 4, 2), ([1, 1], 4, 64), ([0], 0, 1), ([0], 4, 0),
-                                             ([0], 4, 3), ([0], 4, 128), ([0], -1, 1)])
+                                             ([0], 4, 3), ([0], 4, 128), ([0], -1, 1), ([1 << 32], 4, 1), ([-(1 << 32) + 1], 4, 1), ([0.5], 4, 1),
+                                             (["0"], 4, 1)])
 def test_row_lists_that_are_refused(rows, pool, block):
     with pytest.raises(binding.DeftError) as e:
         binding.deft_kv_rows(rows, pool, block)
@@ -32,7 +33,7 @@ def test_row_lists_that_are_refused(rows, pool, block):
 
 
 @pytest.mark.parametrize("src,dst,pool", [([0, 1], [2, 2], 4), ([4], [0], 4), ([0], [4], 4), ([-1], [0], 4), ([0], [-1], 4), ([0], [0], 0),
-                                          ([1, 1], [1, 1], 4), ([0, 1], [2], 4)])
+                                          ([1, 1], [1, 1], 4), ([0, 1], [2], 4), ([1 << 33], [0], 4), ([0], [(1 << 32) + 1], 4)])
 def test_copies_that_are_refused(src, dst, pool):
     with pytest.raises(binding.DeftError) as e:
         binding.deft_kv_copies(src, dst, pool)
@@ -75,8 +76,11 @@ def test_calls_refuse_a_cache_that_is_none_or_not_the_lists(bad):
 def test_calls_refuse_other_arguments():
     lib = binding.load_library()
     rows, copies = binding.deft_kv_rows([3, 63], 64, 16), binding.deft_kv_copies([0], [1], 4)
-    x, odd = ctypes.c_void_p(1 << 14), ctypes.c_void_p((1 << 14) + 8)
-    c = _cache()
+    x, y, odd = ctypes.c_void_p(1 << 14), ctypes.c_void_p(1 << 15), ctypes.c_void_p((1 << 14) + 8)
+    c = _cache(vs=32)
+    for same in (dict(v=1 << 12, vs=32), dict()):  # K and V, or their scales, in one place
+        assert lib.deft_kv_store_q8(rows.handle, x, x, x, 128, 128, _cache(**same), None) == EINVAL
+    assert lib.deft_kv_load_q8(rows.handle, x, c, y, y, None) == EINVAL
     store = lambda *a: lib.deft_kv_store_q8(*a, c, None)  # noqa: E731
     for k_stride, v_stride in ((120, 128), (128, 120), (132, 128), (128, 130), (-128, 128)):
         assert store(rows.handle, x, x, x, k_stride, v_stride) == EINVAL
@@ -158,7 +162,7 @@ def test_a_pool_in_order_has_every_nodes_pages_in_a_row_depth_first(seed):
 
 @pytest.mark.parametrize("ptr,ids,pool,parent", [
     ([0, 1], [4], 4, [-1]), ([0, 1], [-1], 4, [-1]), ([0, 2], [1, 1], 4, [-1]), ([0, 1, 2], [0, 0], 4, [-1, 0]), ([0, 2, 1], [0], 4, [-1, 0]),
-    ([1, 1], [0], 4, [-1]), ([0, 1], [0], 4, [0]), ([0, 1, 2], [0, 1], 4, [1, 0]), ([0, 1], [0], 4, [1]), ([0, 1], [0], 4, [-2]), ([0, 2], [0, 1], 1, [-1])])
+    ([1, 1], [0], 4, [-1]), ([0, 1], [0], 4, [0]), ([0, 1, 2], [0, 1], 4, [1, 0]), ([0, 1], [0], 4, [1]), ([0, 1], [0], 4, [-2]), ([0, 2], [0, 1], 1, [-1]), ([0, 1], [1 << 32], 4, [-1])])
 def test_tables_that_are_refused(ptr, ids, pool, parent):
     with pytest.raises(binding.DeftError) as e:
         binding.deft_compact_pages(ptr, ids, pool, parent)
