@@ -785,8 +785,7 @@ template <int D, int TR, bool UNIFORM>
 __device__ __forceinline__ void issue_share(Share<D, TR, E4m3Cache> &s, const ChunkCtx<E4m3Cache> &c, int t, int blk, int nblk) {
     constexpr int KK = D / 32;
     const BlockAt<UNIFORM> b(c, blk, nblk);
-    if constexpr (TR == 4 && UNIFORM) {
-        static_assert(KK == 4, "a K loader issues four loads");
+    if constexpr (TR == 4 && UNIFORM && KK == 4) {  // a K loader issues four loads, as a V loader does
         // K loader: four 32-byte columns of row 16t + n16; V loader: rows 16(t - 2) + 4g .. + 3
         const bool kl = t < 2;
         const int first = 16 * (kl ? t : t - 2);
@@ -940,7 +939,8 @@ struct SharedPipe {
 //      queries x 4 heads over 32768 tokens in chunks of 1024 (equal-token split) 175 -> 163, 20000 tokens under 40
 //      branches 89.8 -> 77.3, 32768 under 40 branches, 7 heads a KV head, 104.7 -> 91.0; where such tasks are few among
 //      many narrow ones a second block costs 2 % (256-query reasoning tree, balanced split, 97.7 -> 99.9).
-template <int D, int NT, bool UNIFORM, int DEPTH, typename C>
+//      NEAR: the same, for an 8-bit cache's addresses alone (BlockAt), which serve any head dimension.
+template <int D, int NT, bool UNIFORM, bool NEAR, int DEPTH, typename C>
 struct WidePipe {
     static constexpr int KK = D / 32;
     using S = Share<D, 4, C>;
@@ -953,7 +953,7 @@ struct WidePipe {
     // issued whatever happens and the compiler's s_waitcnt vmcnt counts stay exact.
     __device__ __forceinline__ void issue(S &sh, const ChunkCtx<C> &c, int t, int blk, int nblk) {
         if constexpr (C::k8Bit) {
-            issue_share<D, 4, UNIFORM>(sh, c, t, blk, nblk);
+            issue_share<D, 4, NEAR>(sh, c, t, blk, nblk);
         } else if constexpr (UNIFORM) {
             static_assert(KK == 4 || !UNIFORM, "a K loader issues four loads");
             const int blk_e = min(blk, nblk - 1);
@@ -1686,22 +1686,22 @@ __device__ __forceinline__ LeftRows streaming_task(const typename C::Args &a, co
             pipe.template run<PRECISE>(ctx, xbuf, wave, lane, nblk, ts1, a.c, inv_cs);
         }
     } else if (NTW == 1 && ctx.uniform) {
-        WidePipe<D, 1, D == 128, 1, C> pipe;
+        WidePipe<D, 1, D == 128, true, 1, C> pipe;
         pipe.prime(ctx, wave, nblk);
         load_q(1, plain);
         pipe.template run<PRECISE>(ctx, xbuf, wave, lane, nblk, ts1, a.c, inv_cs);
     } else if (NTW == 1) {
-        WidePipe<D, 1, false, 1, C> pipe;
+        WidePipe<D, 1, false, false, 1, C> pipe;
         pipe.prime(ctx, wave, nblk);
         load_q(1, plain);
         pipe.template run<PRECISE>(ctx, xbuf, wave, lane, nblk, ts1, a.c, inv_cs);
     } else if (ctx.uniform) {
-        WidePipe<D, 2, D == 128, 2, C> pipe;  // the fast addressing is written for four loads per K loader
+        WidePipe<D, 2, D == 128, true, 2, C> pipe;  // the fast addressing is written for four loads per K loader
         pipe.prime(ctx, wave, nblk);
         load_q(2, plain);
         pipe.template run<PRECISE>(ctx, xbuf, wave, lane, nblk, ts, a.c, inv_cs);
     } else {
-        WidePipe<D, 2, false, 2, C> pipe;
+        WidePipe<D, 2, false, false, 2, C> pipe;
         pipe.prime(ctx, wave, nblk);
         load_q(2, plain);
         pipe.template run<PRECISE>(ctx, xbuf, wave, lane, nblk, ts, a.c, inv_cs);

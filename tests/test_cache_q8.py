@@ -229,6 +229,17 @@ def test_groups_of_every_width(prefix, branches, length, Hq, Hkv, d, f32):
         check(t, plan_of(t, chunk, flags), Q, c, K, V, f32)
 
 
+# three and more row tiles to a task, one piece, too long to be held in registers, first row inside a block; two to a wave last
+@pytest.mark.parametrize("prefix,branches,Hq,Hkv", [(6000, 60, 32, 8), (9000, 30, 64, 32), (20011, 40, 64, 8)])
+@pytest.mark.parametrize("d,block", [(64, 64), (64, 4), (128, 32)])
+@pytest.mark.parametrize("f32", [True, False])
+def test_long_pieces_under_many_queries(prefix, branches, Hq, Hkv, d, block, f32):
+    t = wl._finish("long", [13, prefix] + [3] * branches, [-1, -1] + [1] * branches, list(range(2, branches + 2)), Hq, Hkv, d, 3)
+    Q, c, K, V = filled(t, block, 9)
+    for chunk, flags in ((1024, 0), (2048, 0), (1024, binding.DEFT_SPLIT_BALANCED | binding.rows_per_query(Hq // Hkv))):
+        check(t, plan_of(t, chunk, flags), Q, c, K, V, f32)
+
+
 @pytest.mark.parametrize("page,block,d", [(1, 1, 64), (16, 16, 128), (16, 4, 64), (64, 32, 128), (64, 64, 128)])
 def test_paged_pools(page, block, d):
     for seed, make in enumerate((lambda: wl.random_tree(3, n_nodes=30, max_len=200, nq=40, Hq=8, Hkv=2, d=d), lambda: star(900, 24, 70, 16, 4, d))):
