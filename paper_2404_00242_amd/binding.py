@@ -192,6 +192,14 @@ def _indices(x, what: str):
     return _i32(a)
 
 
+def _size(x, what: str) -> int:
+    """A number of rows or pages, the same."""
+    n = int(x)
+    if not -(1 << 31) <= n < 1 << 31:
+        raise DeftError(-1, f"{what}: sizes are whole numbers of 32 bits")
+    return n
+
+
 def _address(x):
     """Address of an _i32 array's data, None for an empty one."""
     return x.__array_interface__["data"][0] if x.size else None
@@ -493,6 +501,8 @@ def _cache_args(cache: CacheQ8, what: str):
     if not 0 < block <= MAX_BLOCK_ROWS or block & (block - 1):
         raise DeftError(-1, f"{what}: block_rows must be a power of two up to {MAX_BLOCK_ROWS}")
     n_rows, Hkv, d = shape
+    if n_rows >= 1 << 31 or Hkv >= 1 << 31 or d >= 1 << 31:
+        raise DeftError(-1, f"{what}: a cache's sizes are whole numbers of 32 bits")
     blocks = ks.shape
     if not (ks.dtype == vs.dtype == torch.float8_e8m0fnu and blocks == vs.shape and blocks == (-(-n_rows // block), Hkv) and ks.is_contiguous()
             and vs.is_contiguous()):
@@ -566,20 +576,20 @@ class KVList:
 
 def deft_kv_rows(rows, n_pool_rows: int, block_rows: int = 32) -> KVList:
     """The rows of an 8-bit cache that tokens 0, 1, ... go to or come from, for deft_kv_store_q8 and deft_kv_load_q8."""
-    r = _indices(rows, "deft_kv_rows")
+    r, pool, block = _indices(rows, "deft_kv_rows"), _size(n_pool_rows, "deft_kv_rows"), _size(block_rows, "deft_kv_rows")
     out = ctypes.c_void_p()
-    _check(load_library().deft_kv_rows(_address(r), r.size, int(n_pool_rows), int(block_rows), ctypes.byref(out)), "deft_kv_rows")
-    return KVList(out, r.size, int(n_pool_rows), int(block_rows))
+    _check(load_library().deft_kv_rows(_address(r), r.size, pool, block, ctypes.byref(out)), "deft_kv_rows")
+    return KVList(out, r.size, pool, block)
 
 
 def deft_kv_copies(src, dst, n_pool_pages: int) -> KVList:
     """Copies of pages for deft_kv_copy_pages: page dst[i] becomes what page src[i] held, for all i at once."""
-    a, b = _indices(src, "deft_kv_copies"), _indices(dst, "deft_kv_copies")
+    a, b, pool = _indices(src, "deft_kv_copies"), _indices(dst, "deft_kv_copies"), _size(n_pool_pages, "deft_kv_copies")
     if a.size != b.size:
         raise DeftError(-1, "deft_kv_copies: src and dst differ in length")
     out = ctypes.c_void_p()
-    _check(load_library().deft_kv_copies(_address(a), _address(b), a.size, int(n_pool_pages), ctypes.byref(out)), "deft_kv_copies")
-    return KVList(out, a.size, int(n_pool_pages))
+    _check(load_library().deft_kv_copies(_address(a), _address(b), a.size, pool, ctypes.byref(out)), "deft_kv_copies")
+    return KVList(out, a.size, pool)
 
 
 def deft_compact_pages(node_page_ptr, page_ids, n_pool_pages: int, node_parent):
@@ -589,7 +599,7 @@ def deft_compact_pages(node_page_ptr, page_ids, n_pool_pages: int, node_parent):
         raise DeftError(-1, "deft_compact_pages: tables differ in length")
     new, src, dst = (np.zeros(max(1, pg.size), dtype=np.int32) for _ in range(3))
     n = ctypes.c_int32()
-    _check(load_library().deft_compact_pages(_address(pp), _address(pg), int(n_pool_pages), _address(par), par.size, _address(new), _address(src),
+    _check(load_library().deft_compact_pages(_address(pp), _address(pg), _size(n_pool_pages, "deft_compact_pages"), _address(par), par.size, _address(new), _address(src),
                                              _address(dst), ctypes.byref(n)), "deft_compact_pages")
     return new[:pg.size], src[:n.value], dst[:n.value]
 

@@ -167,3 +167,11 @@ def test_tables_that_are_refused(ptr, ids, pool, parent):
     with pytest.raises(binding.DeftError) as e:
         binding.deft_compact_pages(ptr, ids, pool, parent)
     assert e.value.status == EINVAL
+
+
+def test_sizes_that_32_bits_do_not_hold():
+    for call in (lambda: binding.deft_kv_rows([0], (1 << 32) + 4), lambda: binding.deft_kv_rows([0], 4, (1 << 32) + 32), lambda: binding.deft_kv_copies([0], [1], (1 << 32) + 4),
+                 lambda: binding.deft_compact_pages([0, 1], [0], (1 << 32) + 4, [-1])):
+        with pytest.raises(binding.DeftError) as e:
+            call()
+        assert e.value.status == EINVAL
