@@ -309,6 +309,39 @@ def _raw_stream(stream, index: int) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _torch_stream(raw: int, index: int):
+    """The stream of a handle, for torch."""
+    cuda = _get_torch().cuda
+    return cuda.ExternalStream(raw, device=index) if raw else cuda.default_stream(index)
+
+
+class _OnStream:
+    """What a call does on another stream than torch's current one: inside, that stream is the current one, so that memory which
+    the call makes goes to no tensor of the current stream, and from none whose work there is still to come.  The caller has the
+    results on the stream that it came from: `made` says so to the allocator."""
+
+    def __init__(self, raw: int, index: int):
+        cuda = _get_torch().cuda
+        self._here, self._on = cuda.current_stream(index), cuda.stream(_torch_stream(raw, index))
+
+    def __enter__(self):
+        self._on.__enter__()
+        return self
+
+    def __exit__(self, *error):
+        return self._on.__exit__(*error)
+
+    def made(self, tensor):
+        tensor.record_stream(self._here)
+        return tensor
+
+
+def _other_stream(stream, index: int):
+    """_OnStream where `stream` is not torch's current one, else None."""
+    raw = _raw_stream(stream, index)
+    return None if raw == _get_torch()._C._cuda_getCurrentRawStream(index) else _OnStream(raw, index)
+
+
 def _stream_ptr(stream, device):
     import torch
 
@@ -394,7 +427,7 @@ def deft_tree_attn_decode(plan: Plan, q, k, v, out=None, scale: float = 0.0, out
 
     q [nq,Hq,d], k/v [ntok,Hkv,d]: contiguous bf16 CUDA(HIP) tensors.  Returns o [nq,Hq,d] (bf16, or
     float32 when out_dtype / out says so), in the caller's query order.  Asynchronous on `stream`
-    (default: torch's current stream).
+    (default: torch's current stream); the current stream has to wait for another one before it reads o.
     """
     torch = _torch or _get_torch()
     bf16 = torch.bfloat16
@@ -415,6 +448,12 @@ def deft_tree_attn_decode(plan: Plan, q, k, v, out=None, scale: float = 0.0, out
     if plan_rows > ntok:
         raise DeftError(-1, "deft_tree_attn_decode: the plan addresses rows beyond the KV cache")
     dev = q.device
+    index = dev.index
+    other = None if stream is None else _other_stream(stream, index)
+    if other is not None:
+        with other:
+            got = deft_tree_attn_decode(plan, q, k, v, out, scale, out_dtype, workspace)
+        return other.made(got) if out is None else got
     if out is None:
         # (empty_like costs half a microsecond less than naming shape, type and device; its format is named because a q of one
         # query, sliced from a wider tensor, is contiguous under strides that the output should not have; of a q that is a
@@ -434,7 +473,6 @@ def deft_tree_attn_decode(plan: Plan, q, k, v, out=None, scale: float = 0.0, out
         flags = DEFT_OUT_F32
     else:
         raise DeftError(-1, "deft_tree_attn_decode: out must be bf16 or float32")
-    index = dev.index
     raw = _raw_stream(stream, index)
     # an image that went out on this very stream, or that has landed, needs no ordering
     entry = plan._images.get((Hq // Hkv, index))
@@ -637,10 +675,16 @@ def deft_kv_store_q8(rows: KVList, k, v, cache: CacheQ8, stream=None) -> None:
 
 
 def deft_kv_load_q8(rows: KVList, cache: CacheQ8, k=None, v=None, stream=None):
-    """(k, v), bf16 [n, Hkv, d]: the values of the list's rows.  Asynchronous on `stream`."""
+    """(k, v), bf16 [n, Hkv, d]: the values of the list's rows.  Asynchronous on `stream`; the current stream has to wait for
+    another one before it reads them."""
     torch = _torch or _get_torch()
     c, index, _, Hkv, d = _rows_for(rows, cache, "deft_kv_load_q8")
     shape, bf16 = (rows.n, Hkv, d), torch.bfloat16
+    other = None if stream is None else _other_stream(stream, index)
+    if other is not None:
+        with other:
+            got = deft_kv_load_q8(rows, cache, k, v)
+        return tuple(other.made(x) if given is None else x for x, given in zip(got, (k, v)))
     if k is None:
         k = torch.empty(shape, dtype=bf16, device=cache.k.device)
     elif k.dtype != bf16 or k.shape != shape or not k.is_contiguous() or k.get_device() != index:
@@ -694,7 +738,8 @@ def deft_tree_attn_decode_q8(plan: Plan, q, cache: CacheQ8, out=None, scale: flo
     """deft_tree_attn_decode over an 8-bit cache.
 
     q [nq,Hq,d]: contiguous bf16.  Returns o [nq,Hq,d] (bf16, or float32 when out_dtype / out says so: then with softmax weights
-    in two terms throughout).  Asynchronous on `stream` (default: torch's current stream).
+    in two terms throughout).  Asynchronous on `stream` (default: torch's current stream); the current stream has to wait for
+    another one before it reads o.
     """
     torch = _torch or _get_torch()
     bf16 = torch.bfloat16
@@ -711,6 +756,11 @@ def deft_tree_attn_decode_q8(plan: Plan, q, cache: CacheQ8, out=None, scale: flo
         raise DeftError(-1, "deft_tree_attn_decode_q8: q has a different number of queries than the plan")
     if plan_rows > n_rows:
         raise DeftError(-1, "deft_tree_attn_decode_q8: the plan addresses rows beyond the KV cache")
+    other = None if stream is None else _other_stream(stream, index)
+    if other is not None:
+        with other:
+            got = deft_tree_attn_decode_q8(plan, q, cache, out, scale, out_dtype, workspace)
+        return other.made(got) if out is None else got
     if out is None:  # (see deft_tree_attn_decode)
         if type(q) is torch.Tensor and (out_dtype is None or out_dtype == bf16):
             out = torch.empty_like(q, memory_format=torch.contiguous_format)

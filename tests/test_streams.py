@@ -1,0 +1,126 @@
+"""Calls on another stream than torch's current one: what they allocate, and what two streams or two graphs may do at once."""
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2404_00242_amd import binding, workloads as wl
+
+pytestmark = pytest.mark.gpu
+
+
+def dev():
+    return torch.device("cuda:0")
+
+
+def star(prefix, branches, length, Hq, Hkv, d):
+    return wl._finish("star", [prefix] + [length] * branches, [-1] + [0] * branches, list(range(1, branches + 1)), Hq, Hkv, d, 5)
+
+
+def some_milliseconds():
+    """Work for the current stream, about 20 ms of it."""
+    x = torch.ones((8192, 8192), dtype=torch.bfloat16, device=dev())
+    for _ in range(20):
+        torch.mm(x, x)
+
+
+class Calls:
+    """Attention over both caches and rows read back, on one tree: what they give as a dict of tensors."""
+
+    def __init__(self, chunk=128, nq=9):
+        self.t = t = star(700, nq, 40, 8, 2, 128)
+        self.q, self.k, self.v = (x.to(dev()) for x in wl.make_qkv(t))
+        self.cache = binding.alloc_kv_cache_q8(t.ntok, 2, 128, 16, dev())
+        self.rows = binding.deft_kv_rows(np.arange(t.ntok), t.ntok, 16)
+        binding.deft_kv_store_q8(self.rows, self.k, self.v, self.cache)
+        self.plan = self.new_plan(chunk)
+
+    def new_plan(self, chunk=128):
+        t = self.t
+        return binding.deft_plan(t.node_tok_begin, t.node_tok_len, t.node_parent, t.query_node, t.ntok, chunk)
+
+    def call(self, name, stream=None):
+        if name == "bf16":
+            return [binding.deft_tree_attn_decode(self.plan, self.q, self.k, self.v, stream=stream)]
+        if name == "q8":
+            return [binding.deft_tree_attn_decode_q8(self.plan, self.q, self.cache, stream=stream)]
+        if name == "q8_f32":
+            return [binding.deft_tree_attn_decode_q8(self.plan, self.q, self.cache, out_dtype=torch.float32, stream=stream)]
+        return list(binding.deft_kv_load_q8(self.rows, self.cache, stream=stream))
+
+
+NAMES = ["bf16", "q8", "q8_f32", "load"]
+
+
+@pytest.mark.parametrize("as_handle", [False, True])
+@pytest.mark.parametrize("name", NAMES)
+def test_a_result_takes_no_memory_that_the_current_stream_still_reads(name, as_handle):
+    c = Calls()
+    want = c.call(name)
+    other = torch.cuda.Stream()
+    c.call(name, other)  # images, workspaces
+    torch.cuda.synchronize()
+    for _ in range(3):
+        held = [torch.full_like(x, 3.0) for x in want]
+        read = [torch.zeros_like(x) for x in want]
+        torch.cuda.synchronize()
+        some_milliseconds()
+        for x, y in zip(held, read):
+            y.copy_(x)
+        x = None
+        del held  # the allocator has these blocks back, the copies have not run
+        got = c.call(name, other.cuda_stream if as_handle else other)
+        torch.cuda.synchronize()
+        assert all(bool((y == 3).all()) for y in read)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_a_result_that_is_dropped_early_is_not_the_current_streams_to_reuse(name):
+    c = Calls()
+    want = c.call(name)
+    other = torch.cuda.Stream()
+    c.call(name, other)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        with torch.cuda.stream(other):
+            some_milliseconds()
+        c.call(name, other)  # dropped before it was written
+        new = [torch.full_like(x, 5.0) for x in want]
+        torch.cuda.synchronize()
+        assert all(bool((x == 5).all()) for x in new)
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_a_result_is_kept_while_the_current_stream_reads_it(name):
+    c = Calls()
+    want = c.call(name)
+    other = torch.cuda.Stream()
+    c.call(name, other)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        got = c.call(name, other)
+        torch.cuda.current_stream().wait_stream(other)
+        some_milliseconds()
+        read = [x.clone() for x in got]
+        x = None
+        del got
+        with torch.cuda.stream(other):  # what it would give these blocks to
+            new = [torch.full_like(x, 7.0) for x in want]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(read, want))
+        assert all(bool((x == 7).all()) for x in new)
+
+
+@pytest.mark.parametrize("name", ["bf16", "q8"])
+def test_an_output_that_is_given_stays_the_callers(name):
+    c = Calls()
+    want = c.call(name)[0]
+    out, other = torch.zeros_like(want), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    if name == "bf16":
+        got = binding.deft_tree_attn_decode(c.plan, c.q, c.k, c.v, out=out, stream=other)
+    else:
+        got = binding.deft_tree_attn_decode_q8(c.plan, c.q, c.cache, out=out, stream=other)
+    torch.cuda.synchronize()
+    assert got is out and torch.equal(out, want)
