@@ -162,6 +162,8 @@ def load_library():
     lib.deft_hbm_read_probe.argtypes = [vp, csz, vp, vp]
     lib.deft_plan_destroy.restype = None
     lib.deft_plan_destroy.argtypes = [vp]
+    lib.deft_capture_id.restype = ctypes.c_uint64
+    lib.deft_capture_id.argtypes = [vp]
     lib.deft_strerror.restype = ctypes.c_char_p
     lib.deft_strerror.argtypes = [ctypes.c_int]
     lib.deft_last_hip_error.restype = ctypes.c_char_p
@@ -211,7 +213,7 @@ class Plan:
     def __init__(self, handle, nq=None):
         self._h = handle
         self._images = {}      # (G, device index) -> (torch uint8 tensor holding the device image, event, stream)
-        self._workspaces = {}  # (Hq, Hkv, d, device index) -> torch uint8 tensor
+        self._workspaces = {}  # (Hq, Hkv, d, device index, stream, capture) -> torch uint8 tensor
         self._view = None
         self._nq = nq          # queries, and rows a KV cache must have; a plan never changes
         self._rows = None
@@ -287,17 +289,27 @@ class Plan:
                 stream.wait_event(uploaded)
         return img
 
-    def workspace(self, Hq: int, Hkv: int, d: int, device):
-        import torch
+    def workspace(self, Hq: int, Hkv: int, d: int, device, stream=None):
+        """The workspace of calls on a stream (default: torch's current stream).  Calls of two streams may overlap, and so may
+        replays of two graphs and eager calls: each stream has a workspace of its own, and each capture on it another, which a
+        graph's replays need the plan for."""
+        torch = _get_torch()
+        index = torch.device(device).index
+        if index is None:
+            index = torch.cuda.current_device()
+        raw = _raw_stream(stream, index)
+        return self._workspace(Hq, Hkv, d, index, raw, _capture(raw) if raw else 0)
 
-        device = torch.device(device)
-        key = (Hq, Hkv, d, device.index)
+    def _workspace(self, Hq, Hkv, d, index, raw, capture):
+        key = (Hq, Hkv, d, index, raw, capture)
         ws = self._workspaces.get(key)
         if ws is None:
             nbytes = self.workspace_bytes(Hq, Hkv, d)
             if nbytes == 0:
                 raise DeftError(-1, "deft_workspace_bytes: invalid head shape")
-            ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+            torch = _get_torch()
+            with torch.cuda.stream(_torch_stream(raw, index)):  # (nothing else is given its memory while that stream uses it)
+                ws = torch.empty(nbytes, dtype=torch.uint8, device=torch.device("cuda", index))
             self._workspaces[key] = ws
         return ws
 
@@ -307,6 +319,11 @@ def _raw_stream(stream, index: int) -> int:
     if stream is None:
         return _get_torch()._C._cuda_getCurrentRawStream(index)
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+def _capture(raw: int) -> int:
+    """Number of the capture that a stream other than the null stream is in, 0 if it is in none."""
+    return load_library().deft_capture_id(raw)
 
 
 def _torch_stream(raw: int, index: int):
@@ -477,9 +494,12 @@ def deft_tree_attn_decode(plan: Plan, q, k, v, out=None, scale: float = 0.0, out
     # an image that went out on this very stream, or that has landed, needs no ordering
     entry = plan._images.get((Hq // Hkv, index))
     img = entry[0] if entry is not None and (entry[2] == raw or entry[1] is None) else plan.image(Hq, Hkv, dev, stream)
-    ws = workspace if workspace is not None else plan._workspaces.get((Hq, Hkv, d, index))
+    ws = workspace
     if ws is None:
-        ws = plan.workspace(Hq, Hkv, d, dev)
+        capture = _capture(raw) if raw else 0
+        ws = plan._workspaces.get((Hq, Hkv, d, index, raw, capture))
+        if ws is None:
+            ws = plan._workspace(Hq, Hkv, d, index, raw, capture)
     rc = (_lib or load_library()).deft_tree_attn_decode(
         plan._h, img.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), Hq, Hkv, d, float(scale), flags,
         ws.data_ptr(), ws.numel() * ws.element_size(), raw)
@@ -781,9 +801,12 @@ def deft_tree_attn_decode_q8(plan: Plan, q, cache: CacheQ8, out=None, scale: flo
     # an image that went out on this very stream, or that has landed, needs no ordering
     entry = plan._images.get((Hq // Hkv, index))
     img = entry[0] if entry is not None and (entry[2] == raw or entry[1] is None) else plan.image(Hq, Hkv, q.device, stream)
-    ws = workspace if workspace is not None else plan._workspaces.get((Hq, Hkv, d, index))
+    ws = workspace
     if ws is None:
-        ws = plan.workspace(Hq, Hkv, d, q.device)
+        capture = _capture(raw) if raw else 0
+        ws = plan._workspaces.get((Hq, Hkv, d, index, raw, capture))
+        if ws is None:
+            ws = plan._workspace(Hq, Hkv, d, index, raw, capture)
     rc = (_lib or load_library()).deft_tree_attn_decode_q8(
         plan._h, img.data_ptr(), q.data_ptr(), c, out.data_ptr(), Hq, float(scale), flags, ws.data_ptr(), ws.numel() * ws.element_size(), raw)
     if rc != 0:

@@ -2675,6 +2675,16 @@ extern "C" int deft_tree_attn_decode_q8(const deft_plan_t *plan, const void *dev
                              workspace_bytes, stream, kMarkPolls);
 }
 
+extern "C" uint64_t deft_capture_id(void *stream) {
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    unsigned long long id = 0;
+    if (hipStreamGetCaptureInfo(static_cast<hipStream_t>(stream), &capture, &id) != hipSuccess) {
+        (void)hipGetLastError();
+        return 0;
+    }
+    return capture == hipStreamCaptureStatusActive ? id : 0;
+}
+
 extern "C" int deft_decode_polls(const deft_plan_t *plan, const void *dev_image, const void *q, const void *k, const void *v, void *o,
                                  int32_t Hq, int32_t Hkv, int32_t d, float scale, uint32_t flags, void *workspace,
                                  size_t workspace_bytes, void *stream, int32_t polls) {

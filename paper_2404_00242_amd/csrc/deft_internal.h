@@ -144,6 +144,10 @@ const Schedule *get_schedule(const deft_plan_t *plan, int32_t group, int32_t Hkv
 const Schedule *find_schedule(const deft_plan_t *plan, int32_t group);
 }  // namespace deft
 
+// Number of the capture that a stream is in, 0 if it is in none.  Not part of the interface; the binding keeps by it what the calls
+// of one graph share.
+extern "C" uint64_t deft_capture_id(void *stream);
+
 // deft_tree_attn_decode with another limit to the wait inside a call of one launch, 1 .. the library's: the result does not
 // depend on it.  Not part of the interface; the tests see with it that a wait which is given up costs no result.
 extern "C" int deft_decode_polls(const deft_plan_t *plan, const void *dev_image, const void *q, const void *k, const void *v, void *o,
