@@ -207,12 +207,63 @@ def _address(x):
     return x.__array_interface__["data"][0] if x.size else None
 
 
+class _Images:
+    """Device images of a plan or a list, torch uint8 tensors, by a key.
+
+    An upload only enqueues the copy, on the stream of the call that needs the image first.  An event recorded behind it is kept
+    until it has passed, and a call on another stream makes that stream wait for it; the allocator is told of every stream that
+    uses the image.  A graph that is captured before the copy has landed uploads an image of its own, once: no eager call may
+    use that one, which holds nothing before a replay.  (Of a stream that is itself being captured the runtime does not say
+    whether an earlier event has passed.  Its upload came before the capture, and torch.cuda.graph begins one by waiting for the
+    device.)"""
+
+    class _Image:
+        __slots__ = ("tensor", "event", "first", "streams")  # first: the upload's stream; streams: those that need do nothing more
+
+    def __init__(self):
+        self.of = {}  # key, or (key, capture) -> _Image
+
+    def get(self, key, index, raw, capture, nbytes, upload):
+        torch = _get_torch()
+        x = self.of.get(key)
+        own = capture and (x is None or not self._landed(x))
+        if own:
+            key = key, capture
+            x = self.of.get(key)
+        on = _torch_stream(raw, index)
+        if x is None:
+            x = self._Image()
+            with torch.cuda.device(index), torch.cuda.stream(on):  # (its memory goes to no other tensor while that stream uses it)
+                n = nbytes()
+                x.tensor, x.event = torch.empty(n, dtype=torch.uint8, device=torch.device("cuda", index)), torch.cuda.Event()
+                upload(x.tensor.data_ptr(), n)
+                x.event.record(on)
+            x.first, x.streams = raw, {raw}
+            self.of[key] = x
+        elif raw not in x.streams:
+            if own or not self._landed(x):
+                on.wait_event(x.event)
+            if own or not capture:
+                x.streams.add(raw)
+            if not capture:
+                x.tensor.record_stream(on)
+        return x.tensor
+
+    @staticmethod
+    def _landed(x):
+        if x.event is None or (x.first and _capture(x.first)):
+            return True
+        if x.event.query():
+            x.event = None
+        return x.event is None
+
+
 class Plan:
     """Owns a deft_plan_t handle and, per Hq/Hkv ratio, the device image uploaded for it."""
 
     def __init__(self, handle, nq=None):
         self._h = handle
-        self._images = {}      # (G, device index) -> (torch uint8 tensor holding the device image, event, stream)
+        self._images = _Images()  # by (G, device index)
         self._workspaces = {}  # (Hq, Hkv, d, device index, stream, capture) -> torch uint8 tensor
         self._view = None
         self._nq = nq          # queries, and rows a KV cache must have; a plan never changes
@@ -256,38 +307,26 @@ class Plan:
         return int(load_library().deft_workspace_bytes(self._h, Hq, Hkv, d))
 
     def image(self, Hq: int, Hkv: int, device, stream=None):
-        """Device image for this Hq/Hkv ratio, uploaded on first use (memory comes from torch).
+        """Device image for this Hq/Hkv ratio, uploaded on first use (memory comes from torch); see _Images.  The plan has to live
+        as long as a graph that uses it."""
+        torch = _get_torch()
+        index = torch.device(device).index
+        if index is None:
+            index = torch.cuda.current_device()
+        raw = _raw_stream(stream, index)
+        return self._image(Hq, Hkv, index, raw, _capture(raw) if raw else 0)
 
-        deft_plan_upload only enqueues the copy on the stream of that first call.  An event recorded behind it
-        is kept with the image, and a later call on another stream makes that stream wait for the event, so
-        that no kernel can read the image before the copy has landed."""
-        import torch
-
-        device = torch.device(device)
-        if stream is None:
-            stream = torch.cuda.current_stream(device)
-        key = (Hq // Hkv, device.index)
-        entry = self._images.get(key)
-        if entry is None:
-            nbytes = self.device_bytes(Hq, Hkv)
-            if nbytes == 0:
+    def _image(self, Hq, Hkv, index, raw, capture):
+        def nbytes():
+            n = self.device_bytes(Hq, Hkv)
+            if n == 0:
                 raise DeftError(-1, "deft_plan_device_bytes: invalid Hq/Hkv")
-            img = torch.empty(nbytes, dtype=torch.uint8, device=device)
-            st = _stream_ptr(stream, device)
-            _check(load_library().deft_plan_upload(self._h, Hq, Hkv, img.data_ptr(), nbytes, st), "deft_plan_upload")
-            uploaded = None
-            if hasattr(stream, "record_event"):
-                uploaded = torch.cuda.Event()
-                stream.record_event(uploaded)
-            entry = (img, uploaded, getattr(stream, "cuda_stream", stream))
-            self._images[key] = entry
-        img, uploaded, on = entry
-        if uploaded is not None:
-            if uploaded.query():  # the copy has landed: nothing to order any more
-                self._images[key] = (img, None, on)
-            elif getattr(stream, "cuda_stream", stream) != on and hasattr(stream, "wait_event"):
-                stream.wait_event(uploaded)
-        return img
+            return n
+
+        def upload(at, n):
+            _check(_lib.deft_plan_upload(self._h, Hq, Hkv, at, n, raw), "deft_plan_upload")
+
+        return self._images.get((Hq // Hkv, index), index, raw, capture, nbytes, upload)
 
     def workspace(self, Hq: int, Hkv: int, d: int, device, stream=None):
         """The workspace of calls on a stream (default: torch's current stream).  Calls of two streams may overlap, and so may
@@ -357,14 +396,6 @@ def _other_stream(stream, index: int):
     """_OnStream where `stream` is not torch's current one, else None."""
     raw = _raw_stream(stream, index)
     return None if raw == _get_torch()._C._cuda_getCurrentRawStream(index) else _OnStream(raw, index)
-
-
-def _stream_ptr(stream, device):
-    import torch
-
-    if stream is None:
-        stream = torch.cuda.current_stream(device)
-    return ctypes.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
 
 def deft_suggest_chunk_size(node_tok_len, node_parent, query_node, Hq: int, Hkv: int, flags: int = 0) -> int:
@@ -491,12 +522,11 @@ def deft_tree_attn_decode(plan: Plan, q, k, v, out=None, scale: float = 0.0, out
     else:
         raise DeftError(-1, "deft_tree_attn_decode: out must be bf16 or float32")
     raw = _raw_stream(stream, index)
-    # an image that went out on this very stream, or that has landed, needs no ordering
-    entry = plan._images.get((Hq // Hkv, index))
-    img = entry[0] if entry is not None and (entry[2] == raw or entry[1] is None) else plan.image(Hq, Hkv, dev, stream)
+    capture = _capture(raw) if raw else 0
+    image = plan._images.of.get((Hq // Hkv, index))
+    img = image.tensor if image is not None and not capture and raw in image.streams else plan._image(Hq, Hkv, index, raw, capture)
     ws = workspace
     if ws is None:
-        capture = _capture(raw) if raw else 0
         ws = plan._workspaces.get((Hq, Hkv, d, index, raw, capture))
         if ws is None:
             ws = plan._workspace(Hq, Hkv, d, index, raw, capture)
@@ -582,7 +612,7 @@ class KVList:
 
     def __init__(self, handle, n: int, pool: int, block_rows: int = 0):
         self._h = handle
-        self._images = {}  # device index -> (torch uint8 tensor, event, stream)
+        self._images = _Images()  # by device index
         self.n, self.pool, self.block_rows = n, pool, block_rows
 
     def __del__(self):
@@ -595,9 +625,7 @@ class KVList:
         return self._h
 
     def image(self, device, stream=None):
-        """Device image of the list, uploaded on first use.  A call on another stream than the upload's waits for it.  A graph
-        that captures the first use, or one while the upload may still be under way elsewhere, uploads an image of its own, for
-        each call: ask for the image before the capture.  The list has to live as long as a graph that uses it."""
+        """Device image of the list, uploaded on first use; see _Images.  The list has to live as long as a graph that uses it."""
         torch = _torch or _get_torch()
         index = torch.device(device).index
         if index is None:
@@ -605,31 +633,15 @@ class KVList:
         return self._image(index, _raw_stream(stream, index))
 
     def _image(self, index: int, raw: int):
-        entry = self._images.get(index)
-        if entry is not None and entry[2] == raw:
-            return entry[0]
-        torch = _torch or _get_torch()
-        on = torch.cuda.ExternalStream(raw, device=torch.device("cuda", index)) if raw else torch.cuda.default_stream(index)
-        # what is allocated here is allocated for the stream that fills it: it goes to no other tensor while that has work left
-        with torch.cuda.device(index), torch.cuda.stream(on):
-            captured = torch.cuda.is_current_stream_capturing()
-            if entry is not None and (not captured or entry[1] is None):
-                img, event, first = entry
-                if not captured:
-                    img.record_stream(on)
-                    if event is not None and event.query():
-                        self._images[index] = (img, None, first)
-                    elif event is not None:
-                        on.wait_event(event)
-                return img
-            nbytes = int(load_library().deft_kv_list_device_bytes(self._h))
-            img = torch.empty(nbytes, dtype=torch.uint8, device=torch.device("cuda", index))
-            _check(_lib.deft_kv_list_upload(self._h, img.data_ptr(), nbytes, raw), "deft_kv_list_upload")
-            if not captured:
-                event = torch.cuda.Event()
-                event.record(on)
-                self._images[index] = (img, event, raw)
-        return img
+        capture = _capture(raw) if raw else 0
+        image = self._images.of.get(index)
+        if image is not None and not capture and raw in image.streams:
+            return image.tensor
+
+        def upload(at, n):
+            _check(_lib.deft_kv_list_upload(self._h, at, n, raw), "deft_kv_list_upload")
+
+        return self._images.get(index, index, raw, capture, lambda: int(load_library().deft_kv_list_device_bytes(self._h)), upload)
 
 
 def deft_kv_rows(rows, n_pool_rows: int, block_rows: int = 32) -> KVList:
@@ -798,12 +810,11 @@ def deft_tree_attn_decode_q8(plan: Plan, q, cache: CacheQ8, out=None, scale: flo
         with torch.cuda.device(index):
             return deft_tree_attn_decode_q8(plan, q, cache, out, scale, None, workspace, stream)
     raw = _raw_stream(stream, index)
-    # an image that went out on this very stream, or that has landed, needs no ordering
-    entry = plan._images.get((Hq // Hkv, index))
-    img = entry[0] if entry is not None and (entry[2] == raw or entry[1] is None) else plan.image(Hq, Hkv, q.device, stream)
+    capture = _capture(raw) if raw else 0
+    image = plan._images.of.get((Hq // Hkv, index))
+    img = image.tensor if image is not None and not capture and raw in image.streams else plan._image(Hq, Hkv, index, raw, capture)
     ws = workspace
     if ws is None:
-        capture = _capture(raw) if raw else 0
         ws = plan._workspaces.get((Hq, Hkv, d, index, raw, capture))
         if ws is None:
             ws = plan._workspace(Hq, Hkv, d, index, raw, capture)

@@ -169,3 +169,84 @@ def test_two_graphs_of_one_stream_and_eager_calls_at_once(name):
             for x in o:
                 assert bool(((x.float() - want.float()).abs() <= 2.0 ** -7 * want.float().abs() + 2.0 ** -14).all())
         assert all(torch.equal(x, outs[0][0]) for o in outs for x in o)
+
+
+# ---- images ----
+
+@pytest.mark.parametrize("name", NAMES)
+def test_an_image_that_a_graph_uploads_is_not_used_before_its_replay(name):
+    # first use under capture; then eager calls on the very stream, before any replay; then replays of what two captures made
+    c = Calls()
+    want = c.call(name)
+    side = torch.cuda.Stream()
+    c.plan, c.rows = c.new_plan(), binding.deft_kv_rows(np.arange(c.t.ntok), c.t.ntok, 16)
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for _ in range(2):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=side):
+            outs.append([c.call(name) for _ in range(3)])
+    with torch.cuda.stream(side):
+        eager = c.call(name)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(eager, want))
+    for _ in range(4):
+        for o in outs:
+            for x in o:
+                for y in x:
+                    y.zero_()
+        torch.cuda.synchronize()
+        for g in graphs:
+            g.replay()
+        with torch.cuda.stream(side):
+            eager = c.call(name)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(eager, want))
+        for o in outs:
+            for x in o:
+                for a, b in zip(x, want):  # (two launches and one: as above)
+                    assert bool(((a.float() - b.float()).abs() <= 2.0 ** -7 * b.float().abs() + 2.0 ** -14).all())
+
+
+def test_a_capture_on_two_streams_uploads_its_image_once():
+    c = Calls()
+    want = c.call("q8_f32")[0]
+    side, fork = torch.cuda.Stream(), torch.cuda.Stream()
+    c.plan = c.new_plan()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        a = c.call("q8_f32")[0]
+        fork.wait_stream(side)
+        with torch.cuda.stream(fork):
+            b = c.call("q8_f32")[0]
+        side.wait_stream(fork)
+    assert len(c.plan._images.of) == 1 and len(c.plan._workspaces) == 2
+    for _ in range(4):
+        a.zero_()
+        b.zero_()
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        # sums of at most 50 fp32 terms in another order where the eager call took one launch
+        assert float((a - want).abs().max()) <= 2 * 50 * 2.0 ** -24 * 8 and torch.equal(a, b)
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_a_plan_or_list_that_is_dropped_leaves_its_memory_to_streams_that_still_use_it(name):
+    c = Calls()
+    want = c.call(name)
+    other = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        c.plan, c.rows = c.new_plan(), binding.deft_kv_rows(np.arange(c.t.ntok), c.t.ntok, 16)
+        c.call(name)  # uploads on the current stream
+        torch.cuda.synchronize()
+        sizes = [x.tensor.numel() for y in (c.plan, c.rows) for x in y._images.of.values()]
+        with torch.cuda.stream(other):
+            some_milliseconds()
+        got = c.call(name, other)
+        c.plan = c.rows = None
+        new = [torch.full((n,), 255, dtype=torch.uint8, device=dev()) for n in sizes for _ in range(4)]  # all bits, on the current stream
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)) and all(bool((x == 255).all()) for x in new)
