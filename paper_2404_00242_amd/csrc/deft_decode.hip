@@ -2475,14 +2475,19 @@ bool is_captured(hipStream_t st) {
 // one batch 8.8 -> 9.9, 10.0 -> 11.1, 10.1 -> 10.5 and 8.5 -> 11.0; three batches, 1.7 MB 11.4 -> 12.2, 5 MB 11.6 -> 13.0 or 10.1.
 // A captured call takes two: its replays have no host to spare and the GPU is the slower for it (0.4 MB 6.4 -> 6.9, 16 MB 6.8 ->
 // 7.5, 5 MB under 56 rows 7.5 -> 11.3), and their marks could hold the ticket from the replay before.
+// An 8-bit cache has more tokens in as many bytes, and lines of its own.  One row of one batch, 8 KV heads, 16 MB 11.5 -> 8.6, 33 MB
+// 10.8 -> 10.7, but 35 MB 11.3 -> 11.4 and with 32 KV heads 33 MB 10.2 -> 9.6, but 37 MB 13.7 -> 14.8; one of two 16.8 MB 10.5 -> 9.5,
+// at d = 64 16.8 MB 10.4 -> 9.8, but 17.4 MB 12.2 -> 14.9; two of half a batch 8.2 MB 10.5 -> 8.7, at d = 64 8.2 MB 10.4 -> 8.9, but
+// 9.2 MB 10.5 -> 11.5 (d = 128 breaks even at 13 MB).
 bool one_launch(const deft_plan_t *plan, const Call &call, int32_t Hq, int32_t Hkv, int32_t d) {
     constexpr int64_t kWavesOfRows = kWaves * kReduceGroups;
     const deft::TaskSet &T = whole_call(call, Hkv, d);
     if (!call.marks || plan->nq == 0 || T.n_items == 0) return false;
     const int64_t batch = d == 128 ? kReduceLoads * Stage2Row<128>::kRows : kReduceLoads * Stage2Row<64>::kRows;
     const int64_t rows = (int64_t)plan->nq * Hq, parts = T.max_parts, bytes = (int64_t)plan->n_flat * Hkv * d * (call.cache ? 2 : 4);
-    const bool pays = rows <= kWavesOfRows ? (parts <= batch && bytes <= (40 << 20)) || (parts <= 2 * batch && bytes <= (16 << 20))
-                                           : rows <= 2 * kWavesOfRows && 2 * parts <= batch && bytes <= (16 << 20);
+    const int64_t one_batch = (call.cache ? 32 : 40) << 20, two_batches = 16 << 20, two_rows = (call.cache ? 8 : 16) << 20;
+    const bool pays = rows <= kWavesOfRows ? (parts <= batch && bytes <= one_batch) || (parts <= 2 * batch && bytes <= two_batches)
+                                           : rows <= 2 * kWavesOfRows && 2 * parts <= batch && bytes <= two_rows;
     return pays && !is_captured(call.stream);
 }
 
