@@ -2674,10 +2674,16 @@ extern "C" int deft_tree_attn_decode(const deft_plan_t *plan, const void *dev_im
 
 extern "C" int deft_tree_attn_decode_q8(const deft_plan_t *plan, const void *dev_image, const void *q, const deft_cache_q8_t *cache, void *o,
                                         int32_t Hq, float scale, uint32_t flags, void *workspace, size_t workspace_bytes, void *stream) {
-    if (!plan || !deft::cache_ok(cache)) return DEFT_EINVAL;
+    return deft_decode_polls_q8(plan, dev_image, q, cache, o, Hq, scale, flags, workspace, workspace_bytes, stream, kMarkPolls);
+}
+
+extern "C" int deft_decode_polls_q8(const deft_plan_t *plan, const void *dev_image, const void *q, const deft_cache_q8_t *cache, void *o,
+                                    int32_t Hq, float scale, uint32_t flags, void *workspace, size_t workspace_bytes, void *stream,
+                                    int32_t polls) {
+    if (polls < 1 || polls > kMarkPolls || !plan || !deft::cache_ok(cache)) return DEFT_EINVAL;
     if (deft_plan_rows(plan) > cache->n_rows) return DEFT_EINVAL;
     return decode<E4m3Cache>(plan, dev_image, q, cache->k, cache->v, cache, o, Hq, cache->Hkv, cache->d, scale, flags, workspace,
-                             workspace_bytes, stream, kMarkPolls);
+                             workspace_bytes, stream, polls);
 }
 
 extern "C" uint64_t deft_capture_id(void *stream) {

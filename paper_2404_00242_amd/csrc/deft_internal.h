@@ -148,8 +148,11 @@ const Schedule *find_schedule(const deft_plan_t *plan, int32_t group);
 // of one graph share.
 extern "C" uint64_t deft_capture_id(void *stream);
 
-// deft_tree_attn_decode with another limit to the wait inside a call of one launch, 1 .. the library's: the result does not
+// deft_tree_attn_decode and deft_tree_attn_decode_q8 with another limit to the wait inside a call of one launch, 1 .. the library's: the result does not
 // depend on it.  Not part of the interface; the tests see with it that a wait which is given up costs no result.
 extern "C" int deft_decode_polls(const deft_plan_t *plan, const void *dev_image, const void *q, const void *k, const void *v, void *o,
                                  int32_t Hq, int32_t Hkv, int32_t d, float scale, uint32_t flags, void *workspace,
                                  size_t workspace_bytes, void *stream, int32_t polls);
+extern "C" int deft_decode_polls_q8(const deft_plan_t *plan, const void *dev_image, const void *q, const deft_cache_q8_t *cache, void *o,
+                                    int32_t Hq, float scale, uint32_t flags, void *workspace, size_t workspace_bytes, void *stream,
+                                    int32_t polls);

@@ -60,3 +60,35 @@ def test_which_calls_take_one_launch(t, chunk, one):
     got = binding.deft_tree_attn_decode_q8(plan, q, cache, out_dtype=torch.float32, workspace=ws)
     assert bool((marks(plan, t, ws) != -1).any()) == one
     close(got, two_launches(plan, t, q, cache), v)
+
+
+def call_with_polls(plan, t, q, cache, out, ws, polls):
+    """the call with another limit to the wait inside the kernel (deft_internal.h)"""
+    img, p = plan.image(t.Hq, t.Hkv, "cuda"), ctypes.c_void_p
+    flags = binding.DEFT_OUT_F32 if out.dtype == torch.float32 else binding.DEFT_OUT_BF16
+    assert binding.load_library().deft_decode_polls_q8(
+        plan.handle, p(img.data_ptr()), p(q.data_ptr()), binding._cache_args(cache, "")[0], p(out.data_ptr()), t.Hq, ctypes.c_float(0.0), flags,
+        p(ws.data_ptr()), ctypes.c_size_t(ws.numel()), p(torch.cuda.current_stream().cuda_stream), polls) == 0
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("t,chunk", [
+    (star(40, 0, 0, 4, 4, 128), 32),
+    (star(29 * 32, 0, 0, 2, 2, 64), 32),
+    (star(700, 3, 20, 7, 1, 128), 32),     # tasks of one tile, rows that do not fill it
+    (star(2048, 0, 0, 4, 1, 128), 32),     # two batches
+    (star(2000, 7, 40, 8, 2, 128), 256),   # 56 rows, tasks of two tiles
+    (star(900, 1, 100, 64, 8, 128), 128),  # 64 rows
+    (star(4000, 0, 0, 32, 4, 128), 1024),  # streaming tasks
+    (star(6000, 0, 0, 28, 2, 64), 512),
+])
+def test_rows_that_are_late_are_merged_by_stage_1(t, chunk, dtype):
+    plan, q, cache, _ = prepared(t, chunk)
+    ws = torch.zeros(plan.workspace_bytes(t.Hq, t.Hkv, t.d), dtype=torch.uint8, device="cuda")
+    want = binding.deft_tree_attn_decode_q8(plan, q, cache, out_dtype=dtype, workspace=ws)
+    assert bool((marks(plan, t, ws) != 0).any())  # made in one launch
+    for polls in (1, 1, 2, 3, 4, 6, 9, 14):  # from a wait that is given up at once to one that may just do
+        out = torch.full_like(want, float("nan"))
+        ws.zero_()
+        call_with_polls(plan, t, q, cache, out, ws, polls)
+        assert torch.equal(out, want), polls
