@@ -328,21 +328,32 @@ CacheArgs cache_args(const deft_cache_q8_t *c) {
             (uint32_t)c->Hkv, inverse((uint32_t)c->Hkv)};
 }
 
+// Threads of a launch of store and load at most (they are counted in 32 bits); longer lists take several launches.
+constexpr uint64_t kMaxThreads = 1u << 28;
+static_assert(kMaxThreads / 64 >= DEFT_MAX_Q8_HEADS, "a group's units go into one launch");
+
 template <int D, int BLOCK>
-void launch_store(const StoreArgs &a, hipStream_t st) {
+bool launch_store(StoreArgs a, uint32_t groups, hipStream_t st) {
     constexpr uint32_t lanes = D / 8 * BLOCK < 64 ? D / 8 * BLOCK : 64, units = 256 / lanes;
-    hipLaunchKernelGGL((deft_store_q8<D, BLOCK>), dim3((a.units + units - 1) / units), dim3(256), 0, st, a);
+    const uint32_t most = (uint32_t)(kMaxThreads / lanes / a.c.Hkv);
+    for (uint32_t n; groups > 0; groups -= n, a.groups += n) {
+        n = std::min(groups, most);
+        a.units = n * a.c.Hkv;
+        hipLaunchKernelGGL((deft_store_q8<D, BLOCK>), dim3((a.units + units - 1) / units), dim3(256), 0, st, a);
+        if (!deft::hip_ok(hipGetLastError(), "deft_store_q8 launch")) return false;
+    }
+    return true;
 }
 template <int D>
-void launch_store(const StoreArgs &a, int block_rows, hipStream_t st) {
+bool launch_store(const StoreArgs &a, uint32_t groups, int block_rows, hipStream_t st) {
     switch (block_rows) {
-        case 1: return launch_store<D, 1>(a, st);
-        case 2: return launch_store<D, 2>(a, st);
-        case 4: return launch_store<D, 4>(a, st);
-        case 8: return launch_store<D, 8>(a, st);
-        case 16: return launch_store<D, 16>(a, st);
-        case 32: return launch_store<D, 32>(a, st);
-        default: return launch_store<D, 64>(a, st);
+        case 1: return launch_store<D, 1>(a, groups, st);
+        case 2: return launch_store<D, 2>(a, groups, st);
+        case 4: return launch_store<D, 4>(a, groups, st);
+        case 8: return launch_store<D, 8>(a, groups, st);
+        case 16: return launch_store<D, 16>(a, groups, st);
+        case 32: return launch_store<D, 32>(a, groups, st);
+        default: return launch_store<D, 64>(a, groups, st);
     }
 }
 
@@ -368,8 +379,6 @@ extern "C" int deft_kv_store_q8(const deft_kv_list_t *list, const void *dev_imag
     const int64_t least = (int64_t)cache->Hkv * cache->d;
     if (!k || !v || !deft::aligned16(k) || !deft::aligned16(v)) return DEFT_EINVAL;
     if (k_stride < least || v_stride < least || (k_stride & 7) || (v_stride & 7)) return DEFT_EINVAL;
-    const int64_t units = (int64_t)list->heads * cache->Hkv;
-    if (units > INT32_MAX / 64) return DEFT_EINVAL;  // threads of a launch are counted in 32 bits
     const uint8_t *img = static_cast<const uint8_t *>(dev_image);
     StoreArgs a{};
     a.groups = reinterpret_cast<const u32x4 *>(img);
@@ -379,38 +388,40 @@ extern "C" int deft_kv_store_q8(const deft_kv_list_t *list, const void *dev_imag
     a.k_stride = k_stride;
     a.v_stride = v_stride;
     a.c = cache_args(cache);
-    a.units = (uint32_t)units;
-    if (cache->d == 128)
-        launch_store<128>(a, cache->block_rows, static_cast<hipStream_t>(stream));
-    else
-        launch_store<64>(a, cache->block_rows, static_cast<hipStream_t>(stream));
-    return deft::hip_ok(hipGetLastError(), "deft_store_q8 launch") ? DEFT_OK : DEFT_EHIP;
+    const uint32_t groups = (uint32_t)list->heads;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const bool ok = cache->d == 128 ? launch_store<128>(a, groups, cache->block_rows, st) : launch_store<64>(a, groups, cache->block_rows, st);
+    return ok ? DEFT_OK : DEFT_EHIP;
 }
 
 extern "C" int deft_kv_load_q8(const deft_kv_list_t *list, const void *dev_image, const deft_cache_q8_t *cache, void *k, void *v, void *stream) {
     if (!rows_fit(list, dev_image, cache)) return DEFT_EINVAL;
     if (list->entries == 0 || (!k && !v)) return DEFT_OK;
     if (!deft::aligned16(k) || !deft::aligned16(v) || k == v) return DEFT_EINVAL;
-    const int64_t per_row = (int64_t)cache->Hkv * cache->d / 16, threads = per_row * list->entries;
-    if (threads > INT32_MAX - 512) return DEFT_EINVAL;  // threads of a launch are counted in 32 bits, K's and V's together
+    const uint32_t per_row = (uint32_t)cache->Hkv * (uint32_t)cache->d / 16, both = k && v ? 2 : 1;
     const uint8_t *img = static_cast<const uint8_t *>(dev_image);
     LoadArgs a{};
     a.entries = reinterpret_cast<const u32x2 *>(img + list->off_entries);
     a.k = static_cast<uint16_t *>(k);
     a.v = static_cast<uint16_t *>(v);
     a.c = cache_args(cache);
-    a.per_row = (uint32_t)per_row;
-    a.inv_per_row = inverse(a.per_row);
-    a.threads = (uint32_t)threads;
+    a.per_row = per_row;
+    a.inv_per_row = inverse(per_row);
     a.shift = (uint32_t)__builtin_ctz((unsigned)cache->block_rows);
-    a.all = (uint32_t)((k && v ? 2 : 1) * threads);
-    const uint32_t groups = (a.all + 255) / 256;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (cache->d == 128)
-        hipLaunchKernelGGL((deft_load_q8<128>), dim3(groups), dim3(256), 0, st, a);
-    else
-        hipLaunchKernelGGL((deft_load_q8<64>), dim3(groups), dim3(256), 0, st, a);
-    return deft::hip_ok(hipGetLastError(), "deft_load_q8 launch") ? DEFT_OK : DEFT_EHIP;
+    const uint32_t most = (uint32_t)(kMaxThreads / both / per_row);
+    for (uint32_t left = (uint32_t)list->entries, n; left > 0; left -= n, a.entries += n) {
+        n = std::min(left, most);
+        a.threads = n * per_row;
+        a.all = both * a.threads;
+        const uint32_t groups = (a.all + 255) / 256;
+        if (cache->d == 128)
+            hipLaunchKernelGGL((deft_load_q8<128>), dim3(groups), dim3(256), 0, st, a);
+        else
+            hipLaunchKernelGGL((deft_load_q8<64>), dim3(groups), dim3(256), 0, st, a);
+        if (!deft::hip_ok(hipGetLastError(), "deft_load_q8 launch")) return DEFT_EHIP;
+    }
+    return DEFT_OK;
 }
 
 extern "C" int deft_kv_copy_pages(const deft_kv_list_t *list, const void *dev_image, void *const *pools, const int64_t *page_bytes,
