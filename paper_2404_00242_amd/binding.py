@@ -541,6 +541,7 @@ def deft_tree_attn_decode(plan: Plan, q, k, v, out=None, scale: float = 0.0, out
 # ---- the cache in 8 bits ----
 
 MAX_BLOCK_ROWS = 64
+_BLOCK_ROWS = (1, 2, 4, 8, 16, 32, 64)
 MIN_SCALE_BYTE = 10  # the smallest scale, 2^(10 - 127): of blocks that hold nothing yet
 
 
@@ -737,33 +738,55 @@ def deft_kv_load_q8(rows: KVList, cache: CacheQ8, k=None, v=None, stream=None):
     return k, v
 
 
-def deft_kv_copy_pages(copies: KVList, pools, stream=None) -> None:
-    """Makes the copies of the list in every pool, in place.  pools: contiguous device tensors of any type, each the
-    n_pool_pages pages of one K or V cache, or of an 8-bit cache's scales.  Asynchronous on `stream`."""
+def deft_kv_copy_pages(copies: KVList, pools, stream=None, page_size=None) -> None:
+    """Makes the copies of the list in every pool, in place.  pools: CacheQ8s, whose pages have to be whole blocks, and contiguous
+    device tensors of any type, each the n_pool_pages pages of one K or V cache, or of an 8-bit cache's scales.  How many rows a
+    page has follows from a pool's size; with page_size it is checked (a first dimension of n_pool_pages * page_size rows, or of their
+    blocks' scales).  Asynchronous on `stream`."""
     if copies.block_rows:
         raise DeftError(-1, "deft_kv_copy_pages: the list is one of rows, not of copies")
-    pools = list(pools)
+    pages, pools = copies.pool, list(pools)
+    if CacheQ8 in map(type, pools):
+        pools = [x for t in pools for x in (_pages_of_cache(t, pages, page_size) if type(t) is CacheQ8 else (t,))]
     if not pools:
         return
-    index, pages = pools[0].get_device(), copies.pool
-    at, sizes = array.array("Q"), array.array("q")
-    for t in pools:
-        if t.get_device() != index or not t.is_contiguous():
-            index = -1
-        nbytes = t.nbytes
+    e8m0 = (_torch or _get_torch()).float8_e8m0fnu
+    if page_size is not None or e8m0 in [t.dtype for t in pools]:
+        for t in pools:
+            _check_pool(t, pages, page_size, t.dtype is e8m0 and t.dim() == 2)
+    sizes = [t.nbytes for t in pools]
+    for nbytes in set(sizes):
         if pages == 0 or nbytes == 0 or nbytes % pages:
             raise DeftError(-1, "deft_kv_copy_pages: a pool is not a whole number of bytes for each of the list's pages")
-        at.append(t.data_ptr())
-        sizes.append(nbytes // pages)
-    if index < 0:
+    index, *others = {t.get_device() for t in pools}
+    if others or index < 0 or not all([t.is_contiguous() for t in pools]):
         raise DeftError(-1, "deft_kv_copy_pages: pools must be contiguous tensors on one device (there is no CPU path)")
     if _elsewhere(index):
         with (_torch or _get_torch()).cuda.device(index):
             return deft_kv_copy_pages(copies, pools, stream)
     raw = _raw_stream(stream, index)
-    rc = load_library().deft_kv_copy_pages(copies._h, copies._image(index, raw).data_ptr(), at.buffer_info()[0], sizes.buffer_info()[0], len(pools), raw)
+    at, per_page = array.array("Q", [t.data_ptr() for t in pools]), array.array("q", [n // pages for n in sizes])
+    rc = load_library().deft_kv_copy_pages(copies._h, copies._image(index, raw).data_ptr(), at.buffer_info()[0], per_page.buffer_info()[0], len(pools), raw)
     if rc != 0:
         _check(rc, "deft_kv_copy_pages")
+
+
+def _pages_of_cache(cache: CacheQ8, pages: int, page_size):
+    """A cache's four pools, where it is that many pages of whole blocks."""
+    rows = _cache_args(cache, "deft_kv_copy_pages")[2]
+    if pages == 0 or rows % pages or rows // pages % cache.block_rows or (page_size is not None and rows != pages * page_size):
+        raise DeftError(-1, "deft_kv_copy_pages: a cache is not a whole number of blocks for each of the list's pages, or of other pages")
+    return cache[:4]
+
+
+def _check_pool(t, pages: int, page_size, scales: bool):
+    rows = t.shape[0] if t.dim() else 0
+    if scales:  # [blocks, Hkv]
+        whole = pages > 0 and rows > 0 and rows % pages == 0
+        if not whole or (page_size is not None and (pages * page_size % rows or pages * page_size // rows not in _BLOCK_ROWS)):
+            raise DeftError(-1, "deft_kv_copy_pages: scales are not a whole number of blocks for each of the list's pages, or of other pages")
+    elif page_size is not None and rows != pages * page_size:
+        raise DeftError(-1, f"deft_kv_copy_pages: a pool's first dimension is not that of {pages} pages of {page_size} rows")
 
 
 def deft_tree_attn_decode_q8(plan: Plan, q, cache: CacheQ8, out=None, scale: float = 0.0, out_dtype=None, workspace=None, stream=None):
