@@ -407,8 +407,10 @@ int deft_kv_copy_pages(const deft_kv_list_t *list, const void *dev_image, void *
 /*
  * Which copies put a paged pool in order: every node's pages one after the other, nodes depth-first as deft_plan takes them,
  * from page 0 on.  All pages behind them are free then, and a plan has as few pieces as it can.  node_page_ptr, page_ids: as for
- * deft_plan_paged (n = node_page_ptr[n_nodes] pages); new_page_ids, src, dst: host int32[n], the new table and the copies to
- * make, *n_copies of them (for deft_kv_copies).  Host only, nothing is moved.  Errors: DEFT_EINVAL (as for deft_plan_paged).
+ * deft_plan_paged (n = node_page_ptr[n_nodes] pages), but every entry has to be a page of the node's own, those too that deft_plan_paged
+ * does not look at because the node's tokens do not reach them; new_page_ids (which may be page_ids), src, dst: host int32[n], the
+ * new table and the copies to make, *n_copies of them (for deft_kv_copies).  Host only, nothing is moved.  Errors: DEFT_EINVAL (null,
+ * a malformed tree or table, a page outside the pool or twice in the table, more pages than the pool's), DEFT_ENOMEM.
  */
 int deft_compact_pages(const int32_t *node_page_ptr, const int32_t *page_ids, int32_t n_pool_pages, const int32_t *node_parent,
                        int32_t n_nodes, int32_t *new_page_ids, int32_t *src, int32_t *dst, int32_t *n_copies);

@@ -206,9 +206,10 @@ extern "C" int deft_compact_pages(const int32_t *node_page_ptr, const int32_t *p
         int32_t at = 0, copies = 0;
         for (int32_t u : order)
             for (int32_t i = node_page_ptr[u]; i < node_page_ptr[u + 1]; ++i, ++at) {
+                const int32_t old = page_ids[i];  // (before the new number is written: the two tables may be one)
                 new_page_ids[i] = at;
-                if (page_ids[i] == at) continue;
-                src[copies] = page_ids[i];
+                if (old == at) continue;
+                src[copies] = old;
                 dst[copies++] = at;
             }
         *n_copies = copies;

@@ -175,3 +175,17 @@ def test_sizes_that_32_bits_do_not_hold():
         with pytest.raises(binding.DeftError) as e:
             call()
         assert e.value.status == EINVAL
+
+
+@pytest.mark.parametrize("seed", range(3))
+def test_the_new_table_may_be_the_old_one(seed):
+    t = wl.random_tree(seed, n_nodes=9, max_len=60, nq=5)
+    ptr, ids, n_pool, _ = wl.to_paged(t, 8, seed)
+    ptr, ids, par = (np.ascontiguousarray(x, dtype=np.int32) for x in (ptr, ids, t.node_parent))
+    want = binding.deft_compact_pages(ptr, ids, n_pool, par)
+    table, src, dst, n = ids.copy(), np.zeros_like(ids), np.zeros_like(ids), ctypes.c_int32()
+    at = lambda x: x.ctypes.data  # noqa: E731
+    assert binding.load_library().deft_compact_pages(at(ptr), at(table), n_pool, at(par), par.size, at(table), at(src), at(dst), ctypes.byref(n)) == 0
+    for got, x in zip((table, src[:n.value], dst[:n.value]), want):
+        assert np.array_equal(got, x)
+    assert n.value > 0
