@@ -329,8 +329,10 @@ int deft_tree_attn_decode_static(const deft_plan_t *plan, const void *dev_image,
  * k, v             : device, bytes [n_rows, Hkv, d], 16-byte aligned (these four may be NULL when n_rows == 0)
  * k_scale, v_scale : device, bytes [ceil(n_rows / block_rows), Hkv], 4-byte aligned and read in whole 4-byte words
  * Hkv, d           : at most DEFT_MAX_Q8_HEADS; 64 or 128
- * block_rows       : a power of two, 1 .. 64.  A block should belong to one node of the tree: choose a page size that is a
- *                    multiple of it, or with a contiguous cache begin nodes at multiples of it (block_rows = 1 suits any).
+ * block_rows       : a power of two, 1 .. 64.  A block's rows share a scale, and a store takes those behind the first one that it
+ *                    writes for empty (deft_kv_store_q8).  So a block must belong to one node of the tree, unless all of its rows
+ *                    are stored in ascending order: choose a page size that is a multiple of block_rows, or with a contiguous
+ *                    cache begin nodes at multiples of it (block_rows = 1 suits any).
  */
 #define DEFT_MAX_Q8_HEADS 65536
 typedef struct deft_cache_q8 {
@@ -379,7 +381,8 @@ void deft_kv_list_destroy(deft_kv_list_t *list);
  * k, v     : device bf16, token i at k + i * k_stride (elements), [Hkv, d] contiguous there; 16-byte aligned, strides multiples
  *            of 8 and at least Hkv * d (so slices of a fused projection's output can be stored as they are).
  * A block is filled from its first row on.  Of a block that is written to, the rows in front of the lowest one written are kept,
- * the others hold nothing yet: their bytes are left as they are and have no part in the scale.  The scale of (block, head) is
+ * the others hold nothing yet: their bytes are left as they are and have no part in the scale.  (A row behind the lowest one written
+ * that did hold a token, of another node for one, has another value afterwards wherever the scale changed.)  The scale of (block, head) is
  * the smallest that brings the largest magnitude written to 448 or below, or the block's old one if that is larger and rows are
  * kept; where it grows, the kept rows are rounded to it (only values below 2^-6 of it lose bits).  Values are rounded to
  * nearest, ties to even; what is above 448 * 2^119 becomes that.

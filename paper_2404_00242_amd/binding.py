@@ -557,8 +557,9 @@ class CacheQ8(NamedTuple):
 
 
 def alloc_kv_cache_q8(n_rows: int, Hkv: int, d: int, block_rows: int = 32, device="cuda") -> CacheQ8:
-    """An empty 8-bit cache.  `block_rows` is a power of two up to 64; with a paged pool choose pages of a multiple of it, so
-    that a block belongs to one node.  K and V come from one allocation and are staggered as in alloc_kv_cache."""
+    """An empty 8-bit cache.  `block_rows` is a power of two up to 64.  A block must belong to one node, since a store takes the
+    rows of a block behind those that it writes for empty and may change their scale: choose pages of a multiple of it, with a
+    contiguous cache begin nodes at multiples of it or take 1.  K and V come from one allocation and are staggered as in alloc_kv_cache."""
     import torch
 
     if block_rows < 1 or block_rows > MAX_BLOCK_ROWS or block_rows & (block_rows - 1):
@@ -684,7 +685,8 @@ def _rows_for(rows: KVList, cache: CacheQ8, what: str):
 
 def deft_kv_store_q8(rows: KVList, k, v, cache: CacheQ8, stream=None) -> None:
     """Stores the K and V of new tokens, bf16 [n, Hkv, d], into the rows of the list.  Tokens may lie apart (slices of a fused
-    projection's output), by a multiple of 16 bytes; the heads of one may not.  Asynchronous on `stream`."""
+    projection's output), by a multiple of 16 bytes; the heads of one may not.  A block is filled from its first row on: rows of it
+    behind the lowest one written, other than those of the list, hold nothing afterwards.  Asynchronous on `stream`."""
     torch = _torch or _get_torch()
     c, index, _, Hkv, d = _rows_for(rows, cache, "deft_kv_store_q8")
     n, bf16, strides = rows.n, torch.bfloat16, []
