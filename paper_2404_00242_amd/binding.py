@@ -365,37 +365,36 @@ def _capture(raw: int) -> int:
     return load_library().deft_capture_id(raw)
 
 
+_streams = {}  # (handle, device index) -> torch's object for it
+
+
 def _torch_stream(raw: int, index: int):
     """The stream of a handle, for torch."""
-    cuda = _get_torch().cuda
-    return cuda.ExternalStream(raw, device=index) if raw else cuda.default_stream(index)
-
-
-class _OnStream:
-    """What a call does on another stream than torch's current one: inside, that stream is the current one, so that memory which
-    the call makes goes to no tensor of the current stream, and from none whose work there is still to come.  The caller has the
-    results on the stream that it came from: `made` says so to the allocator."""
-
-    def __init__(self, raw: int, index: int):
+    stream = _streams.get((raw, index))
+    if stream is None:
         cuda = _get_torch().cuda
-        self._here, self._on = cuda.current_stream(index), cuda.stream(_torch_stream(raw, index))
-
-    def __enter__(self):
-        self._on.__enter__()
-        return self
-
-    def __exit__(self, *error):
-        return self._on.__exit__(*error)
-
-    def made(self, tensor):
-        tensor.record_stream(self._here)
-        return tensor
+        stream = _streams[raw, index] = cuda.ExternalStream(raw, device=index) if raw else cuda.default_stream(index)
+    return stream
 
 
-def _other_stream(stream, index: int):
-    """_OnStream where `stream` is not torch's current one, else None."""
-    raw = _raw_stream(stream, index)
-    return None if raw == _get_torch()._C._cuda_getCurrentRawStream(index) else _OnStream(raw, index)
+def _result(raw: int, index: int, shape, dtype):
+    """Memory for what a call writes on a stream that is not torch's current one: it goes to no tensor of the current stream, and
+    comes from none whose work there is still to come.  The caller has it on the current stream, and the allocator is told.  (4 us
+    of the host's; a call that is given its output does without.)"""
+    torch = _get_torch()
+    if _elsewhere(index):
+        with torch.cuda.device(index):
+            return _result(raw, index, shape, dtype)
+    on = _torch_stream(raw, index)
+    # (as torch.cuda.stream does it, 4 us less)
+    here, set_stream = torch._C._cuda_getCurrentStream(index), torch._C._cuda_setStream
+    set_stream(stream_id=on.stream_id, device_index=on.device_index, device_type=on.device_type)
+    try:
+        out = torch.empty(shape, dtype=dtype, device=on.device)
+    finally:
+        set_stream(stream_id=here[0], device_index=here[1], device_type=here[2])
+    out.record_stream(_torch_stream(torch._C._cuda_getCurrentRawStream(index), index))
+    return out
 
 
 def deft_suggest_chunk_size(node_tok_len, node_parent, query_node, Hq: int, Hkv: int, flags: int = 0) -> int:
@@ -497,12 +496,10 @@ def deft_tree_attn_decode(plan: Plan, q, k, v, out=None, scale: float = 0.0, out
         raise DeftError(-1, "deft_tree_attn_decode: the plan addresses rows beyond the KV cache")
     dev = q.device
     index = dev.index
-    other = None if stream is None else _other_stream(stream, index)
-    if other is not None:
-        with other:
-            got = deft_tree_attn_decode(plan, q, k, v, out, scale, out_dtype, workspace)
-        return other.made(got) if out is None else got
-    if out is None:
+    raw = _raw_stream(stream, index)
+    if out is None and stream is not None and raw != torch._C._cuda_getCurrentRawStream(index):
+        out = _result(raw, index, (nq, Hq, d), out_dtype or bf16)
+    elif out is None:
         # (empty_like costs half a microsecond less than naming shape, type and device; its format is named because a q of one
         # query, sliced from a wider tensor, is contiguous under strides that the output should not have; of a q that is a
         # subclass of Tensor it would make another)
@@ -521,7 +518,6 @@ def deft_tree_attn_decode(plan: Plan, q, k, v, out=None, scale: float = 0.0, out
         flags = DEFT_OUT_F32
     else:
         raise DeftError(-1, "deft_tree_attn_decode: out must be bf16 or float32")
-    raw = _raw_stream(stream, index)
     capture = _capture(raw) if raw else 0
     image = plan._images.of.get((Hq // Hkv, index))
     img = image.tensor if image is not None and not capture and raw in image.streams else plan._image(Hq, Hkv, index, raw, capture)
@@ -715,17 +711,14 @@ def deft_kv_load_q8(rows: KVList, cache: CacheQ8, k=None, v=None, stream=None):
     torch = _torch or _get_torch()
     c, index, _, Hkv, d = _rows_for(rows, cache, "deft_kv_load_q8")
     shape, bf16 = (rows.n, Hkv, d), torch.bfloat16
-    other = None if stream is None else _other_stream(stream, index)
-    if other is not None:
-        with other:
-            got = deft_kv_load_q8(rows, cache, k, v)
-        return tuple(other.made(x) if given is None else x for x, given in zip(got, (k, v)))
+    raw = _raw_stream(stream, index)
+    elsewhere = stream is not None and raw != torch._C._cuda_getCurrentRawStream(index)
     if k is None:
-        k = torch.empty(shape, dtype=bf16, device=cache.k.device)
+        k = _result(raw, index, shape, bf16) if elsewhere else torch.empty(shape, dtype=bf16, device=cache.k.device)
     elif k.dtype != bf16 or k.shape != shape or not k.is_contiguous() or k.get_device() != index:
         raise DeftError(-1, f"deft_kv_load_q8: k must be a contiguous bf16 [{rows.n}, {Hkv}, {d}] tensor on the cache's device")
     if v is None:
-        v = torch.empty(shape, dtype=bf16, device=cache.k.device)
+        v = _result(raw, index, shape, bf16) if elsewhere else torch.empty(shape, dtype=bf16, device=cache.k.device)
     elif v.dtype != bf16 or v.shape != shape or not v.is_contiguous() or v.get_device() != index:
         raise DeftError(-1, f"deft_kv_load_q8: v must be a contiguous bf16 [{rows.n}, {Hkv}, {d}] tensor on the cache's device")
     if rows.n == 0:
@@ -733,7 +726,6 @@ def deft_kv_load_q8(rows: KVList, cache: CacheQ8, k=None, v=None, stream=None):
     if _elsewhere(index):
         with torch.cuda.device(index):
             return deft_kv_load_q8(rows, cache, k, v, stream)
-    raw = _raw_stream(stream, index)
     rc = _lib.deft_kv_load_q8(rows._h, rows._image(index, raw).data_ptr(), c, k.data_ptr(), v.data_ptr(), raw)
     if rc != 0:
         _check(rc, "deft_kv_load_q8")
@@ -813,12 +805,10 @@ def deft_tree_attn_decode_q8(plan: Plan, q, cache: CacheQ8, out=None, scale: flo
         raise DeftError(-1, "deft_tree_attn_decode_q8: q has a different number of queries than the plan")
     if plan_rows > n_rows:
         raise DeftError(-1, "deft_tree_attn_decode_q8: the plan addresses rows beyond the KV cache")
-    other = None if stream is None else _other_stream(stream, index)
-    if other is not None:
-        with other:
-            got = deft_tree_attn_decode_q8(plan, q, cache, out, scale, out_dtype, workspace)
-        return other.made(got) if out is None else got
-    if out is None:  # (see deft_tree_attn_decode)
+    raw = _raw_stream(stream, index)
+    if out is None and stream is not None and raw != torch._C._cuda_getCurrentRawStream(index):
+        out = _result(raw, index, shape, out_dtype or bf16)
+    elif out is None:  # (see deft_tree_attn_decode)
         if type(q) is torch.Tensor and (out_dtype is None or out_dtype == bf16):
             out = torch.empty_like(q, memory_format=torch.contiguous_format)
         else:
@@ -834,7 +824,6 @@ def deft_tree_attn_decode_q8(plan: Plan, q, cache: CacheQ8, out=None, scale: flo
     if _elsewhere(index):
         with torch.cuda.device(index):
             return deft_tree_attn_decode_q8(plan, q, cache, out, scale, None, workspace, stream)
-    raw = _raw_stream(stream, index)
     capture = _capture(raw) if raw else 0
     image = plan._images.of.get((Hq // Hkv, index))
     img = image.tensor if image is not None and not capture and raw in image.streams else plan._image(Hq, Hkv, index, raw, capture)

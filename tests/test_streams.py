@@ -250,3 +250,41 @@ def test_a_plan_or_list_that_is_dropped_leaves_its_memory_to_streams_that_still_
         new = [torch.full((n,), 255, dtype=torch.uint8, device=dev()) for n in sizes for _ in range(4)]  # all bits, on the current stream
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want)) and all(bool((x == 255).all()) for x in new)
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_a_captured_call_on_a_stream_that_is_named(name):
+    c = Calls()
+    want = c.call(name)
+    side, fork = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        fork.wait_stream(side)
+        got = [c.call(name, fork) for _ in range(3)]
+        c.call(name, fork)  # dropped
+        after = c.call(name, fork)
+        side.wait_stream(fork)
+        copies = [[x.clone() for x in y] for y in (*got, after)]
+    for _ in range(4):
+        for y in copies:
+            for x in y:
+                x.zero_()
+        some_milliseconds()
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        for y in copies:
+            for a, b in zip(y, want):  # (two launches and one: as above)
+                assert bool(((a.float() - b.float()).abs() <= 2.0 ** -7 * b.float().abs() + 2.0 ** -14).all())
+
+
+def test_a_call_leaves_the_current_stream_as_it_was():
+    c = Calls()
+    other, side = torch.cuda.Stream(), torch.cuda.Stream()
+    for here in (torch.cuda.default_stream(), side):
+        with torch.cuda.stream(here):
+            for name in NAMES:
+                c.call(name, other)
+                assert torch.cuda.current_stream() == here and torch.cuda.current_device() == 0
+    torch.cuda.synchronize()
