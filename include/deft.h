@@ -346,7 +346,9 @@ typedef struct deft_cache_q8 {
  * that the cache holds.  The plan, its image, the workspace, o, scale, flags and the errors are those of deft_tree_attn_decode
  * (Hkv and d are the cache's); besides, a cache with fewer rows than the plan addresses is refused with DEFT_EINVAL.  (The ordinary
  * call that has to come before a captured one is one of this kind.)
- * A float result (DEFT_OUT_F32) is computed with two-term softmax weights in every group, whatever the plan says.
+ * Softmax weights are those that the plan's groups have with a bf16 cache: over long paths one bf16 term (error of a bf16 result
+ * 2.3e-3 in the 2-norm, 1.65e-3 of it the result's own rounding), with DEFT_PRECISE_WEIGHTS two (1.65e-3; 0 to 5 % slower over narrow
+ * groups, 21 % over wide ones).  A float result (DEFT_OUT_F32) is computed with two in every group, whatever the plan says (2.5e-6).
  * A NaN among the keys of a token makes the results NaN of exactly the queries that see it.  Values (V) must be finite, which
  * those that deft_kv_store_q8 writes are: a token with weight 0 that is not on a query's path still takes part in its products.
  */
