@@ -2693,7 +2693,7 @@ extern "C" uint64_t deft_capture_id(void *stream) {
         (void)hipGetLastError();
         return 0;
     }
-    return capture == hipStreamCaptureStatusActive ? id : 0;
+    return capture == hipStreamCaptureStatusActive ? id + 1 : 0;  // (the runtime may count from 0)
 }
 
 extern "C" int deft_decode_polls(const deft_plan_t *plan, const void *dev_image, const void *q, const void *k, const void *v, void *o,

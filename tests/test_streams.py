@@ -288,3 +288,23 @@ def test_a_call_leaves_the_current_stream_as_it_was():
                 c.call(name, other)
                 assert torch.cuda.current_stream() == here and torch.cuda.current_device() == 0
     torch.cuda.synchronize()
+
+
+def test_every_capture_has_a_number_of_its_own():
+    c, lib = Calls(), binding.load_library()
+    side, fork = torch.cuda.Stream(), torch.cuda.Stream()
+    seen = []
+    for _ in range(3):
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            seen.append(lib.deft_capture_id(side.cuda_stream))
+            assert lib.deft_capture_id(fork.cuda_stream) == 0
+            fork.wait_stream(side)
+            with torch.cuda.stream(fork):
+                c.call("q8")
+            assert lib.deft_capture_id(fork.cuda_stream) == seen[-1]
+            side.wait_stream(fork)
+        assert lib.deft_capture_id(side.cuda_stream) == 0
+    assert len(set(seen)) == 3 and 0 not in seen
+    assert {k[-1] for k in c.plan._workspaces} == set(seen) and len(c.plan._workspaces) == 3
