@@ -421,6 +421,80 @@ int deft_compact_pages(const int32_t *node_page_ptr, const int32_t *page_ids, in
                        int32_t n_nodes, int32_t *new_page_ids, int32_t *src, int32_t *dst, int32_t *n_copies);
 
 /*
+ * What happens to the heads of a projection's output before attention: norms, rotation by position, K and V into the cache.
+ *
+ * deft_heads_t: the queries', keys' or values' heads of the n tokens of a call.
+ *   x            : device bf16, head h of token i at x + i * token_stride + h * head_stride (elements): d contiguous elements.  Strides
+ *                  are multiples of 8, from 0 (one row for all) to 2^40, x is 16-byte aligned; slices of a fused projection's output
+ *                  need not be copied.
+ *   out          : device bf16 [n, heads, d], contiguous, 16-byte aligned; or x itself: the heads are then changed where they are.
+ *                  Otherwise what a call writes must not overlap what it reads, nor its other outputs.
+ *   weight       : NULL: no norm.  Otherwise device, 16-byte aligned, head h's d weights at weight + h * weight_stride (0: one for all
+ *                  heads, else a multiple of 8 up to 4096); bf16, or float where weight_f32 is set (the same for queries and keys).
+ *   heads        : 0 .. DEFT_MAX_Q8_HEADS
+ *
+ * A head x with a weight becomes x * (weight + weight_offset) / sqrt(mean(x^2) + eps).  Sums and products are fp32, and a result is
+ * rounded once, after the rotation (half a step of bf16, and at most 2^-19 of the pair's magnitude).
+ *
+ * deft_rope_t: how positions turn heads.  Pair i < rot / 2 of a head turns by positions[token] * frequency[i] radians, and the result
+ * is multiplied by factor: (a, b) becomes factor * (a cos - b sin, a sin + b cos).  The pair is elements (i, i + rot / 2) of the head
+ * (DEFT_ROPE_HALF) or (2i, 2i + 1) (DEFT_ROPE_INTERLEAVED); elements from rot on do not turn.  A rope is plain memory, made by
+ * deft_rope, copied at will; a call takes a copy of it.  Positions are device int32 [n], of any value: angles are right to 2^-31 of
+ * a turn, whatever the position.  Negative ones turn back.
+ *
+ * deft_rope: rot is a multiple of 16, 16 .. 128, at most d at the calls; frequency host double[rot / 2], of magnitude up to 1e6.
+ * deft_rope_frequencies writes the usual ones, base^(-2i / rot) (base > 1), slowed for contexts longer than a model was trained for:
+ *   DEFT_ROPE_PLAIN       as they are (scale and what follows it are not looked at)
+ *   DEFT_ROPE_LINEAR      all divided by scale
+ *   DEFT_ROPE_BASE        those of base * scale^(rot / (rot - 2)): the fastest stays, the slowest is divided by scale
+ *   DEFT_ROPE_DIMENSION   pairs of `high` turns and more within `original` positions stay, of `low` and less are divided by scale, between
+ *                         them the share of either is linear in i (from the floor of the one's real index to the ceiling of the
+ *                         other's); high, low default to 32, 1 where not above 0; *factor is 0.1 ln(scale) + 1 where scale > 1
+ *   DEFT_ROPE_WAVELENGTH  the same, linear in the turns themselves; 4, 1
+ * *factor is 1 otherwise.  Errors of both: DEFT_EINVAL (null, a number outside of what is said here or not finite).
+ */
+#define DEFT_ROPE_HALF 0
+#define DEFT_ROPE_INTERLEAVED 1
+#define DEFT_ROPE_PLAIN 0
+#define DEFT_ROPE_LINEAR 1
+#define DEFT_ROPE_BASE 2
+#define DEFT_ROPE_DIMENSION 3
+#define DEFT_ROPE_WAVELENGTH 4
+typedef struct deft_rope {
+    uint64_t turns[64]; /* what a position turns pair i, in 2^-64 of a turn, whole turns left out */
+    float factor;
+    int32_t rot, layout;
+} deft_rope_t;
+typedef struct deft_heads {
+    const void *x;
+    int64_t token_stride, head_stride;
+    void *out;
+    const void *weight;
+    int64_t weight_stride;
+    int32_t weight_f32, heads;
+} deft_heads_t;
+int deft_rope_frequencies(int32_t rot, double base, int32_t scaling, double scale, double original, double low, double high,
+                          double *frequency, double *factor);
+int deft_rope(const double *frequency, int32_t rot, int32_t layout, double factor, deft_rope_t *out);
+
+/*
+ * deft_rotate turns heads (which have no weight).  deft_qk_norm_rotate normalises those of q and k that have a weight and turns both;
+ * q or k may be NULL, and rope and positions both NULL: nothing is turned then.
+ *
+ * deft_qkv_store does the same and stores keys and values into a bf16 cache of n_rows rows, token i into row rows[i] of the list
+ * (deft_kv_rows; its blocks have no part in it): k->out and v->out are the K and V pools [n_rows, Hkv, d].  Values are copied bit for
+ * bit.  Other rows stay as they are.  q may be NULL; its out is as for the calls above.  n is the list's.
+ *
+ * d is 64 or 128.  Asynchronous on `stream`.  Errors: DEFT_EINVAL (null, misaligned, a stride, size, eps (finite, >= 0) or weight_offset
+ * outside of what is said here, a value with a weight, a list of copies or for a larger cache, memory that overlaps), DEFT_EHIP.
+ */
+int deft_rotate(const deft_heads_t *x, int32_t n, int32_t d, const int32_t *positions, const deft_rope_t *rope, void *stream);
+int deft_qk_norm_rotate(const deft_heads_t *q, const deft_heads_t *k, int32_t n, int32_t d, float eps, float weight_offset,
+                        const int32_t *positions, const deft_rope_t *rope, void *stream);
+int deft_qkv_store(const deft_kv_list_t *list, const void *dev_image, const deft_heads_t *q, const deft_heads_t *k, const deft_heads_t *v,
+                   int32_t n_rows, int32_t d, float eps, float weight_offset, const int32_t *positions, const deft_rope_t *rope, void *stream);
+
+/*
  * Benchmark aid, not part of the method (no decode call uses it; it exists so that the benchmark can state
  * the machine's read rate next to stage 1's).  Reads `bytes` bytes at dev_buf once with 128-bit loads from
  * every compute unit (DEFT_PROBE_SINK_BYTES / 4 workgroups, grid-stride) and stores, for each workgroup, the xor of the

@@ -42,6 +42,7 @@ EXPORTS = (
     "deft_tree_attn_decode", "deft_tree_attn_decode_static", "deft_stage1_partial_attention", "deft_stage2_global_reduction",
     "deft_tree_attn_decode_q8", "deft_kv_rows", "deft_kv_copies", "deft_kv_list_device_bytes", "deft_kv_list_upload", "deft_kv_list_destroy",
     "deft_kv_store_q8", "deft_kv_load_q8", "deft_kv_copy_pages", "deft_compact_pages",
+    "deft_rope_frequencies", "deft_rope", "deft_rotate", "deft_qk_norm_rotate", "deft_qkv_store",
     "deft_hbm_read_probe", "deft_plan_destroy", "deft_strerror", "deft_last_hip_error",
 )
 
@@ -158,6 +159,17 @@ def load_library():
     lib.deft_kv_copy_pages.argtypes = [vp, vp, vp, vp, c32, vp]
     lib.deft_compact_pages.restype = ctypes.c_int
     lib.deft_compact_pages.argtypes = [vp, vp, c32, vp, c32, vp, vp, vp, ctypes.POINTER(c32)]
+    rope, heads, f32, f64 = vp, vp, ctypes.c_float, ctypes.c_double  # (the bytes of a deft_rope_t, and of a deft_heads_t: _heads)
+    lib.deft_rope_frequencies.restype = ctypes.c_int
+    lib.deft_rope_frequencies.argtypes = [c32, f64, c32, f64, f64, f64, f64, vp, ctypes.POINTER(f64)]
+    lib.deft_rope.restype = ctypes.c_int
+    lib.deft_rope.argtypes = [vp, c32, c32, f64, vp]
+    lib.deft_rotate.restype = ctypes.c_int
+    lib.deft_rotate.argtypes = [heads, c32, c32, vp, rope, vp]
+    lib.deft_qk_norm_rotate.restype = ctypes.c_int
+    lib.deft_qk_norm_rotate.argtypes = [heads, heads, c32, c32, f32, f32, vp, rope, vp]
+    lib.deft_qkv_store.restype = ctypes.c_int
+    lib.deft_qkv_store.argtypes = [vp, vp, heads, heads, heads, c32, c32, f32, f32, vp, rope, vp]
     lib.deft_hbm_read_probe.restype = ctypes.c_int
     lib.deft_hbm_read_probe.argtypes = [vp, csz, vp, vp]
     lib.deft_plan_destroy.restype = None
@@ -837,3 +849,215 @@ def deft_tree_attn_decode_q8(plan: Plan, q, cache: CacheQ8, out=None, scale: flo
     if rc != 0:
         _check(rc, "deft_tree_attn_decode_q8")
     return out
+
+
+# ---- heads on their way to the attention: norms, rotation, rows of a bf16 cache ----
+
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "dimension": 3, "wavelength": 4}
+_ROPE_BYTES = 64 * 8 + 16  # deft_rope_t
+
+
+class Rope(NamedTuple):
+    """How positions turn heads; `deft_rope` makes one."""
+
+    packed: bytes  # a deft_rope_t
+    rot: int
+
+
+def deft_rope_frequencies(rot: int, base: float = 10000.0, scaling: str = "none", scale: float = 1.0, original: float = 0, low: float = 0,
+                          high: float = 0):
+    """(radians that a position turns each of the rot / 2 pairs, float64; the factor of the results): see include/deft.h for the ways
+    of scaling.  `original` is the context's length before it was stretched `scale` times."""
+    if scaling not in ROPE_SCALINGS:
+        raise DeftError(-1, f"deft_rope_frequencies: scaling is one of {', '.join(ROPE_SCALINGS)}")
+    f, factor = np.zeros(max(int(rot) // 2, 1)), ctypes.c_double()
+    _check(load_library().deft_rope_frequencies(_size(rot, "deft_rope_frequencies"), float(base), ROPE_SCALINGS[scaling], float(scale), float(original), float(low),
+                                                float(high), f.__array_interface__["data"][0], ctypes.byref(factor)), "deft_rope_frequencies")
+    return f, factor.value
+
+
+def deft_rope(rot: int, base: float = 10000.0, layout: str = "half", scaling: str = "none", scale: float = 1.0, original: float = 0,
+              low: float = 0, high: float = 0, factor=None, frequencies=None) -> Rope:
+    """A rotation of the first `rot` elements (a multiple of 16) of heads, in pairs (i, i + rot / 2) or, interleaved, (2i, 2i + 1).
+    Frequencies are those of deft_rope_frequencies, or the rot / 2 given (radians a position, then with factor 1); a factor given
+    takes the place of the scaling's."""
+    if layout not in ROPE_LAYOUTS:
+        raise DeftError(-1, f"deft_rope: layout is one of {', '.join(ROPE_LAYOUTS)}")
+    if frequencies is None:
+        f, own = deft_rope_frequencies(rot, base, scaling, scale, original, low, high)
+    else:
+        f, own = np.ascontiguousarray(np.asarray(frequencies, dtype=np.float64)).reshape(-1), 1.0
+        if 2 * f.size != rot:
+            raise DeftError(-1, "deft_rope: one frequency to each of the rot / 2 pairs")
+    out = ctypes.create_string_buffer(_ROPE_BYTES)
+    _check(load_library().deft_rope(f.__array_interface__["data"][0] if f.size else None, _size(rot, "deft_rope"), ROPE_LAYOUTS[layout],
+                                    float(own if factor is None else factor), out), "deft_rope")
+    return Rope(out.raw, int(rot))
+
+
+_pack_heads = struct.Struct("PqqPPqii").pack  # deft_heads_t
+
+
+def _heads(t, n, d, index, what: str, name: str):
+    """(address, strides, number of heads) of bf16 [n, heads, d]."""
+    if t.dtype != _torch.bfloat16 or t.dim() != 3 or t.get_device() != index:
+        raise DeftError(-1, f"{what}: {name} must be a 3-d bf16 tensor on one device with the others (there is no CPU path)")
+    n2, heads, d2 = t.shape
+    if n2 != n or d2 != d or heads >= 1 << 31:
+        raise DeftError(-1, f"{what}: {name} must be [{n}, heads, {d}]")
+    token, head, one = t.stride()
+    if one != 1 and n and heads:
+        raise DeftError(-1, f"{what}: the elements of {name}'s heads must be contiguous")
+    return t.data_ptr(), token if n > 1 else heads * d, head if heads > 1 else d, heads  # (one token's or head's stride says nothing)
+
+
+def _heads_out(out, t, at, raw, index, here, what: str, name: str):
+    """(a result for the heads t, made if none is given; its address)"""
+    shape = t.shape
+    if out is None:
+        out = _torch.empty(shape, dtype=_torch.bfloat16, device=t.device) if here else _result(raw, index, shape, _torch.bfloat16)
+        return out, out.data_ptr()
+    if out.dtype != _torch.bfloat16 or out.shape != shape or out.get_device() != index:
+        raise DeftError(-1, f"{what}: {name} must be bf16 {list(shape)}, on the input's device")
+    p = out.data_ptr()
+    if not out.is_contiguous() if p != at else not _alike(out, t):
+        raise DeftError(-1, f"{what}: {name} must be contiguous, or the input itself")
+    return out, p
+
+
+def _alike(a, b) -> bool:
+    """Whether two tensors of one shape and address are the same memory element by element."""
+    return a.numel() == 0 or all(n == 1 or x == y for n, x, y in zip(a.shape, a.stride(), b.stride()))
+
+
+def _head_weight(w, heads, d, index, what: str, name: str):
+    """(address, stride of heads, whether float) of a norm's weights, [d] or [heads, d]."""
+    if w is None:
+        return None, 0, 0
+    wide = w.dtype == _torch.float32
+    shape = w.shape
+    if not (wide or w.dtype == _torch.bfloat16) or w.get_device() != index or not w.is_contiguous() or (shape != (d,) and shape != (heads, d)):
+        raise DeftError(-1, f"{what}: {name} must be a contiguous bf16 or float32 [{d}] or [{heads}, {d}] tensor on the input's device")
+    return w.data_ptr(), 0 if len(shape) == 1 else d, wide
+
+
+def _positions(positions, n, rope, index, what: str):
+    """Address of the positions where there is a rope."""
+    if rope is None:
+        if positions is not None:
+            raise DeftError(-1, f"{what}: positions say nothing without a rope")
+        return None
+    if positions is None or positions.dtype != _torch.int32 or positions.shape != (n,) or positions.get_device() != index or not positions.is_contiguous():
+        raise DeftError(-1, f"{what}: positions must be a contiguous int32 [{n}] tensor on the input's device")
+    return positions.data_ptr() or 4  # (of none: anything)
+
+
+def deft_rotate(x, positions, rope: Rope, out=None, stream=None):
+    """Turns heads by their positions.  x: bf16 [n, H, d] whose tokens and heads may lie apart by multiples of 16 bytes; positions:
+    int32 [n].  Returns bf16 [n, H, d]; out=x turns them in place.  Asynchronous on `stream` (default: torch's current stream); the
+    current stream has to wait for another one before it reads the result."""
+    torch = _torch or _get_torch()
+    index = x.get_device()
+    if x.dim() != 3 or rope is None:
+        raise DeftError(-1, "deft_rotate: x must be a 3-d tensor, and a rope be given")
+    n, _, d = x.shape
+    at, token, head, H = _heads(x, n, d, index, "deft_rotate", "x")
+    if index < 0:
+        raise DeftError(-1, "deft_rotate: x must be a device tensor (there is no CPU path)")
+    pos = _positions(positions, n, rope, index, "deft_rotate")
+    raw = _raw_stream(stream, index)
+    out, to = _heads_out(out, x, at, raw, index, stream is None or raw == torch._C._cuda_getCurrentRawStream(index), "deft_rotate", "out")
+    if _elsewhere(index):
+        with torch.cuda.device(index):
+            return deft_rotate(x, positions, rope, out, raw)
+    rc = (_lib or load_library()).deft_rotate(_pack_heads(at, token, head, to, 0, 0, 0, H), n, d, pos, rope.packed, raw)
+    if rc != 0:
+        _check(rc, "deft_rotate")
+    return out
+
+
+def deft_qk_norm_rotate(q, k, q_weight=None, k_weight=None, positions=None, rope=None, eps: float = 1e-6, weight_offset: float = 0.0,
+                        q_out=None, k_out=None, stream=None):
+    """RMS norm of every head of q [n, Hq, d] and k [n, Hkv, d], and rotation by the tokens' positions, in one pass: a head becomes
+    head * (weight + weight_offset) / sqrt(mean(head^2) + eps), turned.  Weights: bf16 or float32 (both alike), [d] or a row for
+    every head; without one (None) there is no norm, without a rope no rotation.  Returns (q, k), bf16; q_out and k_out may be the
+    inputs themselves.  Otherwise as deft_rotate."""
+    torch = _torch or _get_torch()
+    what, index = "deft_qk_norm_rotate", q.get_device()
+    if q.dim() != 3 or index < 0:
+        raise DeftError(-1, "deft_qk_norm_rotate: q must be a 3-d device tensor (there is no CPU path)")
+    n, _, d = q.shape
+    q_at, q_token, q_head, Hq = _heads(q, n, d, index, what, "q")
+    k_at, k_token, k_head, Hkv = _heads(k, n, d, index, what, "k")
+    qw, qw_head, q_wide = _head_weight(q_weight, Hq, d, index, what, "q_weight")
+    kw, kw_head, k_wide = _head_weight(k_weight, Hkv, d, index, what, "k_weight")
+    if qw and kw and q_wide != k_wide:
+        raise DeftError(-1, "deft_qk_norm_rotate: weights must be of one type")
+    pos = _positions(positions, n, rope, index, what)
+    raw = _raw_stream(stream, index)
+    here = stream is None or raw == torch._C._cuda_getCurrentRawStream(index)
+    q_out, q_to = _heads_out(q_out, q, q_at, raw, index, here, what, "q_out")
+    k_out, k_to = _heads_out(k_out, k, k_at, raw, index, here, what, "k_out")
+    if _elsewhere(index):
+        with torch.cuda.device(index):
+            return deft_qk_norm_rotate(q, k, q_weight, k_weight, positions, rope, eps, weight_offset, q_out, k_out, raw)
+    rc = (_lib or load_library()).deft_qk_norm_rotate(
+        _pack_heads(q_at, q_token, q_head, q_to, qw or 0, qw_head, q_wide, Hq), _pack_heads(k_at, k_token, k_head, k_to, kw or 0, kw_head, k_wide, Hkv),
+        n, d, eps, weight_offset, pos, None if rope is None else rope.packed, raw)
+    if rc != 0:
+        _check(rc, what)
+    return q_out, k_out
+
+
+def deft_qkv_store(rows: KVList, q, k, v, cache, positions=None, rope=None, q_weight=None, k_weight=None, eps: float = 1e-6,
+                   weight_offset: float = 0.0, q_out=None, stream=None):
+    """What deft_qk_norm_rotate does to the heads of new tokens, keys and values put into a bf16 cache at once: token i into row
+    rows[i] of the list (deft_kv_rows, of any block_rows), values bit for bit.  cache: the K and V pools, contiguous bf16
+    [n_rows, Hkv, d].  q may be None.  Returns the queries, bf16 [n, Hq, d].  Otherwise as deft_qk_norm_rotate.  (An 8-bit cache
+    takes deft_qk_norm_rotate and deft_kv_store_q8.)"""
+    torch = _torch or _get_torch()
+    what, index = "deft_qkv_store", k.get_device()
+    if type(cache) is CacheQ8 or len(cache) != 2:
+        raise DeftError(-1, "deft_qkv_store: cache must be the K and V pools of a bf16 cache (deft_kv_store_q8 stores into one of 8 bits)")
+    if rows.block_rows == 0:
+        raise DeftError(-1, "deft_qkv_store: the list is one of copies, not of rows")
+    if k.dim() != 3 or index < 0:
+        raise DeftError(-1, "deft_qkv_store: k must be a 3-d device tensor (there is no CPU path)")
+    n, _, d = k.shape
+    if n != rows.n:
+        raise DeftError(-1, f"deft_qkv_store: the list has {rows.n} rows, not {n}")
+    k_at, k_token, k_head, Hkv = _heads(k, n, d, index, what, "k")
+    v_at, v_token, v_head, Hv = _heads(v, n, d, index, what, "v")
+    k_pool, v_pool = cache
+    shape, bf16 = k_pool.shape, torch.bfloat16
+    if (Hv != Hkv or len(shape) != 3 or shape[1] != Hkv or shape[2] != d or v_pool.shape != shape or not k_pool.dtype == v_pool.dtype == bf16
+            or not (k_pool.is_contiguous() and v_pool.is_contiguous()) or not k_pool.get_device() == v_pool.get_device() == index):
+        raise DeftError(-1, f"deft_qkv_store: the pools must both be contiguous bf16 [n_rows, {Hkv}, {d}] tensors on the heads' device")
+    n_rows = shape[0]
+    if rows.pool > n_rows or n_rows >= 1 << 31:
+        raise DeftError(-1, "deft_qkv_store: the list is for a larger cache, or the cache larger than 32 bits hold")
+    raw = _raw_stream(stream, index)
+    kw, kw_head, wide = _head_weight(k_weight, Hkv, d, index, what, "k_weight")
+    q_heads = None
+    if q is not None:
+        q_at, q_token, q_head, Hq = _heads(q, n, d, index, what, "q")
+        qw, qw_head, q_wide = _head_weight(q_weight, Hq, d, index, what, "q_weight")
+        if qw and kw and q_wide != wide:
+            raise DeftError(-1, "deft_qkv_store: weights must be of one type")
+        q_out, to = _heads_out(q_out, q, q_at, raw, index, stream is None or raw == torch._C._cuda_getCurrentRawStream(index), what, "q_out")
+        q_heads = _pack_heads(q_at, q_token, q_head, to, qw or 0, qw_head, q_wide, Hq)
+    elif q_weight is not None or q_out is not None:
+        raise DeftError(-1, "deft_qkv_store: without q it has neither weights nor a result")
+    pos = _positions(positions, n, rope, index, what)
+    if n == 0:
+        return q_out
+    if _elsewhere(index):
+        with torch.cuda.device(index):
+            return deft_qkv_store(rows, q, k, v, cache, positions, rope, q_weight, k_weight, eps, weight_offset, q_out, raw)
+    rc = (_lib or load_library()).deft_qkv_store(
+        rows._h, rows._image(index, raw).data_ptr(), q_heads, _pack_heads(k_at, k_token, k_head, k_pool.data_ptr(), kw or 0, kw_head, wide, Hkv),
+        _pack_heads(v_at, v_token, v_head, v_pool.data_ptr(), 0, 0, 0, Hkv), n_rows, d, eps, weight_offset, pos, None if rope is None else rope.packed, raw)
+    if rc != 0:
+        _check(rc, what)
+    return q_out
