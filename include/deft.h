@@ -495,6 +495,49 @@ int deft_qkv_store(const deft_kv_list_t *list, const void *dev_image, const deft
                    int32_t n_rows, int32_t d, float eps, float weight_offset, const int32_t *positions, const deft_rope_t *rope, void *stream);
 
 /*
+ * The logits of each query's next token, float or bf16, bent by what its path holds, by biases and by grammar masks.  For the logit x of
+ * token t of query j, with c_all the number of times that t stands on the tokens of j's path and c the same without prompt tokens:
+ *   x becomes x / repetition[j] where x > 0 and x * repetition[j] otherwise, if c_all > 0;
+ *   then x - (frequency[j] * c + presence[j]), if c > 0;  then x + bias[bias_row[j]][t];  then -inf where the mask's bit t is 0
+ * in fp32, rounded once to the type of the output.  What is NULL is left out.  A mask may leave nothing: the row is then all -inf.
+ *
+ * logits, out          : device [nq, vocab], queries (the caller's order) stride and out_stride elements apart, aligned as their type; the
+ *                        strides are at most 2^31, out_stride at least vocab.  float where logits_f32, out_f32 are set, else bf16; bf16 logits may
+ *                        become float ones.  out may be logits itself with its stride and type, otherwise they must not overlap.
+ * vocab                : 1 .. DEFT_MAX_VOCAB
+ * tokens               : device int32 [n_tokens], the token of every row of the KV cache that the plan is for (so a fork or a compaction copies
+ *                        its pages like any pool's); at least deft_plan_rows(plan) of them.  Prompt tokens may have DEFT_TOKEN_PROMPT or-ed
+ *                        to them: they count for the repetition penalty alone.  Negative numbers, and those from vocab on, are no token.
+ * repetition, frequency, presence : device float [nq], by query.  Any of them asks for tokens.
+ * bias                 : device float, rows bias_stride elements apart (at least vocab if there are two); bias_row: device int32 [nq], the row of each query,
+ *                        none where it is outside 0 .. n_bias - 1; NULL: row 0 for all
+ * mask, mask_row       : the same for masks: rows of (vocab + 31) / 32 words of 32 bits, mask_stride words apart, bit t % 32 of word t / 32 is
+ *                        set where token t is allowed
+ * dev_image, group     : with tokens, the image of the plan that deft_plan_upload made for group = Hq / Hkv (any will do); else not looked at
+ * Asynchronous on `stream`.  Errors: DEFT_EINVAL, DEFT_ENOTREADY, DEFT_EHIP as for deft_tree_attn_decode.
+ */
+#define DEFT_TOKEN_PROMPT 0x40000000
+#define DEFT_MAX_VOCAB (1 << 28)
+typedef struct deft_logits {
+    const void *logits;
+    void *out;
+    int64_t stride, out_stride;
+    int32_t vocab, logits_f32, out_f32;
+    int32_t n_bias, n_masks;
+    int32_t reserved; /* 0 */
+    const int32_t *tokens;
+    int64_t n_tokens;
+    const float *repetition, *frequency, *presence;
+    const float *bias;
+    const int32_t *bias_row;
+    int64_t bias_stride;
+    const void *mask;
+    const int32_t *mask_row;
+    int64_t mask_stride;
+} deft_logits_t;
+int deft_adjust_logits(const deft_plan_t *plan, const void *dev_image, int32_t group, const deft_logits_t *logits, void *stream);
+
+/*
  * Benchmark aid, not part of the method (no decode call uses it; it exists so that the benchmark can state
  * the machine's read rate next to stage 1's).  Reads `bytes` bytes at dev_buf once with 128-bit loads from
  * every compute unit (DEFT_PROBE_SINK_BYTES / 4 workgroups, grid-stride) and stores, for each workgroup, the xor of the

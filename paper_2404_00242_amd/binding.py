@@ -42,7 +42,7 @@ EXPORTS = (
     "deft_tree_attn_decode", "deft_tree_attn_decode_static", "deft_stage1_partial_attention", "deft_stage2_global_reduction",
     "deft_tree_attn_decode_q8", "deft_kv_rows", "deft_kv_copies", "deft_kv_list_device_bytes", "deft_kv_list_upload", "deft_kv_list_destroy",
     "deft_kv_store_q8", "deft_kv_load_q8", "deft_kv_copy_pages", "deft_compact_pages",
-    "deft_rope_frequencies", "deft_rope", "deft_rotate", "deft_qk_norm_rotate", "deft_qkv_store",
+    "deft_rope_frequencies", "deft_rope", "deft_rotate", "deft_qk_norm_rotate", "deft_qkv_store", "deft_adjust_logits",
     "deft_hbm_read_probe", "deft_plan_destroy", "deft_strerror", "deft_last_hip_error",
 )
 
@@ -170,6 +170,8 @@ def load_library():
     lib.deft_qk_norm_rotate.argtypes = [heads, heads, c32, c32, f32, f32, vp, rope, vp]
     lib.deft_qkv_store.restype = ctypes.c_int
     lib.deft_qkv_store.argtypes = [vp, vp, heads, heads, heads, c32, c32, f32, f32, vp, rope, vp]
+    lib.deft_adjust_logits.restype = ctypes.c_int
+    lib.deft_adjust_logits.argtypes = [vp, vp, c32, vp, vp]
     lib.deft_hbm_read_probe.restype = ctypes.c_int
     lib.deft_hbm_read_probe.argtypes = [vp, csz, vp, vp]
     lib.deft_plan_destroy.restype = None
@@ -339,6 +341,21 @@ class Plan:
             _check(_lib.deft_plan_upload(self._h, Hq, Hkv, at, n, raw), "deft_plan_upload")
 
         return self._images.get((Hq // Hkv, index), index, raw, capture, nbytes, upload)
+
+    def _any_image(self, index, raw, capture):
+        """(address, Hq / Hkv) of an image of any ratio: the tree is the same in all.  One that is there is taken and none made, since
+        the first image of a ratio decides how the attention's tasks are cut."""
+        ready = None
+        for key, image in list(self._images.of.items()):
+            if type(key[0]) is tuple:  # a capture's own
+                key = key[0]
+            elif key[1] == index and not capture and raw in image.streams:
+                return image.tensor.data_ptr(), key[0]
+            if ready is None or key[1] == index:
+                ready = key[0]
+        if ready is None:
+            raise DeftError(-5, "the plan has no device image yet: call an attention on it, or plan.image(Hq, Hkv, device), first [-5]")
+        return self._image(ready, 1, index, raw, capture).data_ptr(), ready
 
     def workspace(self, Hq: int, Hkv: int, d: int, device, stream=None):
         """The workspace of calls on a stream (default: torch's current stream).  Calls of two streams may overlap, and so may
@@ -1061,3 +1078,93 @@ def deft_qkv_store(rows: KVList, q, k, v, cache, positions=None, rope=None, q_we
     if rc != 0:
         _check(rc, what)
     return q_out
+
+
+# ---- logits ----
+
+DEFT_TOKEN_PROMPT = 0x40000000  # or-ed to the token ids of a prompt
+_pack_logits = struct.Struct("PPqqiiiiiiPqPPPPPqPPq").pack  # deft_logits_t
+
+
+def _per_query(t, nq, dtype, index, name: str):
+    if t is None:
+        return 0
+    if t.dtype != dtype or t.shape != (nq,) or t.get_device() != index or not t.is_contiguous():
+        raise DeftError(-1, f"deft_adjust_logits: {name} must be a contiguous {dtype} [{nq}] tensor on the logits' device")
+    return t.data_ptr()
+
+
+def _table(t, width, dtype, row, nq, index, name: str):
+    """(address, distance of rows, number of rows, address of the queries' row numbers) of a table of biases or masks."""
+    if t is None:
+        if row is not None:
+            raise DeftError(-1, f"deft_adjust_logits: {name}_row says nothing without a {name}")
+        return 0, 0, 0, 0
+    if t.dim() == 1:
+        t = t[None]
+    if t.dtype != dtype or t.dim() != 2 or t.shape[0] < 1 or t.shape[1] != width or t.get_device() != index or (width > 1 and t.stride(1) != 1):
+        raise DeftError(-1, f"deft_adjust_logits: {name} must be a {dtype} [rows, {width}] tensor of contiguous rows on the logits' device")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else 0, t.shape[0], _per_query(row, nq, _torch.int32, index, name + "_row")
+
+
+def deft_adjust_logits(plan: Plan, logits, tokens=None, repetition=None, frequency=None, presence=None, bias=None, bias_row=None, mask=None,
+                       mask_row=None, out=None, out_dtype=None, stream=None):
+    """The logits [nq, vocab] (float32 or bf16) of the plan's queries, bent by penalties for the tokens on each query's own path, by
+    biases and by grammar masks; see include/deft.h for the formula.
+
+    tokens: int32, the token of every row of the KV cache that the plan is for (or-ed with DEFT_TOKEN_PROMPT where a prompt's token
+    is to count for the repetition penalty alone; -1: none); repetition, frequency, presence: float32 [nq].  bias: float32
+    [rows, vocab], mask: int32 [rows, ceil(vocab / 32)] words of allowed tokens' bits; bias_row, mask_row: int32 [nq], the row of
+    each query, -1: none (without them row 0 is everyone's).  Returns a new tensor of the logits' type or out_dtype (float32), or
+    out, which may be the logits.  A plan that no attention call has used yet needs plan.image(Hq, Hkv, device) first.
+    Asynchronous on `stream` (default: torch's current stream); the current stream has to wait for another one before it reads the result."""
+    torch = _torch or _get_torch()
+    f32, index = torch.float32, logits.get_device()
+    wide = logits.dtype == f32
+    if index < 0 or logits.dim() != 2 or not (wide or logits.dtype == torch.bfloat16):
+        raise DeftError(-1, "deft_adjust_logits: logits must be a 2-d float32 or bf16 device tensor (there is no CPU path)")
+    nq, vocab = shape = logits.shape
+    stride, one = logits.stride()
+    if vocab > 1 and one != 1:
+        raise DeftError(-1, "deft_adjust_logits: a query's logits must be contiguous")
+    plan_nq, plan_rows = plan.limits()
+    if nq != plan_nq:
+        raise DeftError(-1, "deft_adjust_logits: logits are of a different number of queries than the plan")
+    if not 1 <= vocab <= 1 << 28:
+        raise DeftError(-1, "deft_adjust_logits: no vocabulary, or one of more than 2^28 tokens")
+    history = repetition is not None or frequency is not None or presence is not None
+    if history and tokens is None:
+        raise DeftError(-1, "deft_adjust_logits: penalties need the tokens")
+    if tokens is not None and (tokens.dtype != torch.int32 or tokens.dim() != 1 or tokens.get_device() != index or not tokens.is_contiguous()
+                               or tokens.numel() < plan_rows):
+        raise DeftError(-1, "deft_adjust_logits: tokens must be a contiguous int32 tensor with every row that the plan addresses")
+    penalties = [_per_query(t, nq, f32, index, name) for t, name in ((repetition, "repetition"), (frequency, "frequency"), (presence, "presence"))]
+    bias_at, bias_stride, n_bias, bias_row_at = _table(bias, vocab, f32, bias_row, nq, index, "bias")
+    mask_at, mask_stride, n_masks, mask_row_at = _table(mask, -(-vocab // 32), torch.int32, mask_row, nq, index, "mask")
+    raw = _raw_stream(stream, index)
+    if out is None:
+        dtype = out_dtype or logits.dtype
+        here = stream is None or raw == torch._C._cuda_getCurrentRawStream(index)
+        out = torch.empty(shape, dtype=dtype, device=logits.device) if here else _result(raw, index, shape, dtype)
+    elif out.shape != shape or out.get_device() != index or (vocab > 1 and out.stride(1) != 1):
+        raise DeftError(-1, "deft_adjust_logits: out must be like the logits, with contiguous rows")
+    out_wide = out.dtype == f32
+    if not out_wide and (wide or out.dtype != torch.bfloat16):
+        raise DeftError(-1, "deft_adjust_logits: out must be float32, or bf16 for bf16 logits")
+    if nq == 0:
+        return out
+    if _elsewhere(index):
+        with torch.cuda.device(index):
+            return deft_adjust_logits(plan, logits, tokens, repetition, frequency, presence, bias, bias_row, mask, mask_row, out, None, raw)
+    image, group = 0, 0
+    if history:
+        capture = _capture(raw) if raw else 0
+        image, group = plan._any_image(index, raw, capture)
+    rc = (_lib or load_library()).deft_adjust_logits(
+        plan._h, image, group,
+        _pack_logits(logits.data_ptr(), out.data_ptr(), stride if nq > 1 else vocab, out.stride(0) if nq > 1 else vocab, vocab, wide, out_wide, n_bias, n_masks, 0,
+                     tokens.data_ptr() if history else 0, tokens.numel() if history else 0, *penalties, bias_at, bias_row_at, bias_stride, mask_at,
+                     mask_row_at, mask_stride), raw)
+    if rc != 0:
+        _check(rc, "deft_adjust_logits")
+    return out

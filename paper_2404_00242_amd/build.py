@@ -9,7 +9,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libdeft.so")
-SOURCES = ["deft_plan.cpp", "deft_lists.cpp", "deft_rope.cpp", "deft_decode.hip", "deft_cache.hip", "deft_heads.hip"]
+SOURCES = ["deft_plan.cpp", "deft_lists.cpp", "deft_rope.cpp", "deft_decode.hip", "deft_cache.hip", "deft_heads.hip", "deft_logits.hip"]
 
 
 def hipcc_command(out: str = LIB, extra=()):

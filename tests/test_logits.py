@@ -1,0 +1,365 @@
+"""Logits bent by the tokens of each query's path, by biases and by masks: against the definition in 64 bits (oracle/logits.py)."""
+
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import logits as model
+from paper_2404_00242_amd import binding, workloads as wl
+
+EINVAL, ENOTREADY = -1, -5
+PROMPT = binding.DEFT_TOKEN_PROMPT
+
+
+def plan_of(t, chunk=0, flags=0, page=0, seed=0):
+    """(plan, pool row of every row of the contiguous cache, rows of the pool)"""
+    if not page:
+        return binding.deft_plan(t.node_tok_begin, t.node_tok_len, t.node_parent, t.query_node, t.ntok, chunk, flags), np.arange(t.ntok), t.ntok
+    pp, pg, npool, row_of = wl.to_paged(t, page, seed=seed)
+    return binding.deft_plan_paged(pp, pg, page, npool, t.node_tok_len, t.node_parent, t.query_node, chunk, flags), row_of, npool * page
+
+
+# ---- refusals (CPU: addresses that nothing reads) ----
+
+def test_calls_that_are_refused():
+    lib = binding.load_library()
+    t = wl.random_tree(3, n_nodes=5, nq=4)
+    plan = plan_of(t)[0]
+    rows = plan.limits()[1]
+
+    def call(plan=plan.handle, image=0, group=1, logits=1 << 20, out=1 << 24, stride=1000, out_stride=1000, vocab=1000, wide=1, out_wide=1, n_bias=0, n_masks=0,
+             tokens=0, n_tokens=0, repetition=0, frequency=0, presence=0, bias=0, bias_row=0, bias_stride=0, mask=0, mask_row=0, mask_stride=0):
+        packed = binding._pack_logits(logits, out, stride, out_stride, vocab, wide, out_wide, n_bias, n_masks, 0, tokens, n_tokens, repetition, frequency,
+                                      presence, bias, bias_row, bias_stride, mask, mask_row, mask_stride)
+        return lib.deft_adjust_logits(plan, image, group, packed, None)
+
+    at = 1 << 12
+    for bad in (dict(plan=None), dict(logits=0), dict(out=0), dict(vocab=0), dict(vocab=-5), dict(vocab=(1 << 28) + 1, stride=1 << 29, out_stride=1 << 29),
+                dict(out_stride=999), dict(stride=-1000), dict(stride=1 << 32), dict(out_stride=1 << 32), dict(logits=(1 << 20) + 2), dict(out=(1 << 24) + 2),
+                dict(wide=0, logits=(1 << 20) + 1), dict(wide=0, out_wide=0, out=(1 << 24) + 1), dict(out_wide=0),
+                dict(out=(1 << 20) + 4), dict(out=1 << 20, out_stride=1001), dict(out=1 << 20, wide=0), dict(out=(1 << 20) - 8000),
+                dict(bias=at), dict(bias=at + 2, n_bias=1), dict(bias=at, n_bias=-1), dict(bias=at, n_bias=2, bias_stride=999), dict(bias_row=at),
+                dict(bias=at, n_bias=1, bias_row=at + 1), dict(mask=at), dict(mask=at + 2, n_masks=1), dict(mask=at, n_masks=2, mask_stride=31), dict(mask_row=at),
+                dict(mask=at, n_masks=1, mask_row=at + 2),
+                dict(repetition=at), dict(frequency=at, tokens=at, n_tokens=rows - 1), dict(presence=at + 2, tokens=at, n_tokens=rows),
+                dict(presence=at, tokens=at + 2, n_tokens=rows), dict(repetition=at, tokens=at, n_tokens=rows), dict(repetition=at, tokens=at, n_tokens=rows, image=at + 8),
+                dict(repetition=at, tokens=at, n_tokens=rows, image=at, group=0)):
+        assert call(**bad) == EINVAL, bad
+    assert lib.deft_adjust_logits(plan.handle, None, 1, None, None) == EINVAL
+    assert call(repetition=at, tokens=at, n_tokens=rows, image=at, group=3) == ENOTREADY
+    nobody = binding.deft_plan(t.node_tok_begin, t.node_tok_len, t.node_parent, [], t.ntok)
+    assert call(plan=nobody.handle, logits=0, out=0) == 0
+    with pytest.raises(binding.DeftError):
+        binding.deft_adjust_logits(plan, torch.zeros((4, 10)))
+
+
+# ---- on the GPU ----
+
+def dev():
+    return torch.device("cuda:0")
+
+
+def gpu(x):
+    return None if x is None else torch.from_numpy(np.ascontiguousarray(x)).to(dev())
+
+
+class Inputs:
+    """Everything that a call can be given, on the host, for a tree whose rows lie in a pool as row_of says."""
+
+    def __init__(self, t, vocab, seed, wide, prompts=True):
+        rng = np.random.default_rng(seed)
+        self.t, self.vocab, self.rng = t, vocab, rng
+        x = torch.from_numpy(4.0 * rng.standard_normal((t.nq, vocab)).astype(np.float32))
+        self.x = x if wide else x.to(torch.bfloat16)
+        # few tokens often; tokens that are none, in every way
+        self.tokens = (vocab * rng.random(t.ntok) ** 4).astype(np.int32)
+        if prompts:
+            some = rng.random(t.ntok) < 0.4
+            self.tokens[some] |= PROMPT
+        odd = rng.random(t.ntok) < 0.05
+        self.tokens[odd] = rng.choice([-1, -(1 << 31), vocab, (1 << 31) - 1, vocab | PROMPT, -PROMPT], int(odd.sum()))
+        f32 = np.float32
+        self.repetition, self.frequency, self.presence = (f32(1) + rng.random(t.nq).astype(f32), rng.standard_normal(t.nq).astype(f32), rng.standard_normal(t.nq).astype(f32))
+        self.bias = np.where(rng.random((3, vocab)) < 0.1, 5 * rng.standard_normal((3, vocab)), 0).astype(f32)
+        self.mask = rng.integers(-(1 << 31), 1 << 31, (5, -(-vocab // 32))).astype(np.int32)
+        self.mask[3] = 0  # a state that allows nothing
+        self.mask[4] = -1
+        self.bias_row, self.mask_row = rng.integers(-1, 4, t.nq).astype(np.int32), rng.integers(-1, 6, t.nq).astype(np.int32)  # (3 and 5 are no rows)
+
+    def call(self, plan, row_of, pool, out_dtype=None, stream=None, x=None, **which):
+        tokens = None
+        if any(which.get(k) for k in ("repetition", "frequency", "presence")):
+            tokens = np.full(pool, 3, np.int32)  # (rows that no path holds)
+            owned = row_of >= 0
+            tokens[row_of[owned]] = self.tokens[owned]
+        args = {k: gpu(getattr(self, k)) for k in which if which[k]}
+        return binding.deft_adjust_logits(plan, self.x.to(dev()) if x is None else x, gpu(tokens), out_dtype=out_dtype, stream=stream, **args)
+
+    def want(self, **which):
+        return model.adjust(self.t, self.x.double().numpy(), self.tokens, **{k: getattr(self, k) for k in which if which[k]})
+
+
+def close(got, want, mag):
+    """Each of the at most six fp32 roundings (1 / repetition, the product; frequency * count + presence; two sums; 2^-24 each) is
+    relative to no more than `mag`; bf16 results are rounded once more, 2^-8."""
+    bf16 = got.dtype == torch.bfloat16
+    got = got.double().cpu().numpy()
+    assert (np.isnan(got) == np.isnan(want)).all()
+    inf = np.isinf(want)
+    assert (got[inf] == want[inf]).all()
+    with np.errstate(invalid="ignore"):
+        off = np.abs(got - want) - (6 * 2.0 ** -24 * mag * 1.001 + (2.0 ** -8 * 1.001 * np.abs(want) if bf16 else 0) + 2.0 ** -126)
+    bad = np.isfinite(want) & ~(off <= 0)
+    assert not bad.any(), (np.argwhere(bad)[:5], got[bad][:5], want[bad][:5])
+
+
+ALL = dict(repetition=True, frequency=True, presence=True, bias=True, bias_row=True, mask=True, mask_row=True)
+SOME = [dict(repetition=True), dict(presence=True), dict(frequency=True), dict(repetition=True, presence=True, mask=True, mask_row=True), dict(bias=True, bias_row=True),
+        dict(mask=True), dict(bias=True, mask=True, mask_row=True), ALL]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("which", SOME, ids=lambda w: "+".join(w))
+@pytest.mark.parametrize("vocab", [1, 31, 1024, 1027, 5003])
+@pytest.mark.parametrize("types", ["f32", "bf16", "bf16 f32"])
+def test_every_part_of_the_formula(which, vocab, types):
+    t = wl.random_tree(vocab, n_nodes=14, max_len=90, nq=11, n_roots=2)
+    s = Inputs(t, vocab, vocab, types == "f32")
+    plan, row_of, pool = plan_of(t)
+    plan.image(t.Hq, t.Hkv, dev())
+    got = s.call(plan, row_of, pool, out_dtype=torch.float32 if types == "bf16 f32" else None, **which)
+    assert got.dtype == (torch.bfloat16 if types == "bf16" else torch.float32)
+    close(got, *s.want(**which))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("mode", sorted(binding.SPLIT_MODES))
+@pytest.mark.parametrize("page", [0, 1, 16])
+@pytest.mark.parametrize("seed", range(4))
+def test_trees_of_any_kind(mode, page, seed):
+    t = wl.random_tree(900 + seed, n_nodes=3 + 17 * seed, max_len=[1, 40, 150, 90][seed], nq=[1, 9, 40, 100][seed], n_roots=1 + seed)
+    s = Inputs(t, 777, seed, True)
+    plan, row_of, pool = plan_of(t, 64, binding.SPLIT_MODES[mode], page, seed)
+    plan.image(t.Hq, t.Hkv, dev())
+    for which in (ALL, dict(repetition=True, presence=True)):
+        close(s.call(plan, row_of, pool, **which), *s.want(**which))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("counts", [False, True])
+def test_more_queries_than_a_workgroup_takes(counts):
+    t = wl.random_tree(77, n_nodes=300, max_len=12, nq=1100, n_roots=3)
+    s = Inputs(t, 30011, 5, True)
+    plan, row_of, pool = plan_of(t)
+    plan.image(t.Hq, t.Hkv, dev())
+    which = dict(repetition=True, presence=True, frequency=counts)
+    got = s.call(plan, row_of, pool, **which).cpu()
+    some = np.concatenate([np.arange(0, 1100, 13), [1099]])
+    t.query_node = t.query_node[some]
+    s.x = s.x[some]
+    for k in ("repetition", "presence", "frequency"):
+        setattr(s, k, getattr(s, k)[some])
+    close(got[some], *s.want(**which))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("counts", [False, True])
+@pytest.mark.parametrize("page", [0, 1, 16])
+def test_paths_of_many_pieces(counts, page):
+    # a long prompt, and branches behind it; of pages of one row every token is a piece
+    t = wl.config5_longcontext(root=6000, branches=9, lo=1, hi=700)
+    s = Inputs(t, 2500, page, False)
+    plan, row_of, pool = plan_of(t, 0, binding.DEFT_SPLIT_BALANCED | binding.rows_per_query(4), page, 1)
+    plan.image(t.Hq, t.Hkv, dev())
+    which = dict(repetition=True, presence=True, frequency=counts, mask=True, mask_row=True)
+    close(s.call(plan, row_of, pool, **which), *s.want(**which))
+
+
+@pytest.mark.gpu
+def test_one_token_more_often_than_sixteen_bits_hold():
+    t = wl.config2_fewshot(prefix=70000, branches=3, gen=5)
+    s = Inputs(t, 2000, 1, True, prompts=False)
+    s.tokens[:69000] = 1999
+    s.frequency[:] = [0.5, -0.001, 2.0 ** -12]
+    plan, row_of, pool = plan_of(t)
+    plan.image(t.Hq, t.Hkv, dev())
+    which = dict(frequency=True, repetition=True)
+    close(s.call(plan, row_of, pool, **which), *s.want(**which))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("wide", [False, True])
+def test_extreme_logits_and_tables(wide):
+    t = wl.random_tree(5, n_nodes=6, max_len=60, nq=7)
+    s = Inputs(t, 600, 2, wide)
+    for i, v in enumerate([math.inf, -math.inf, math.nan, 0.0, -0.0, 3e38, -3e38, 1e-40]):
+        s.x[:, 37 * i:37 * i + 20] = v
+    s.bias[0, ::7] = -math.inf
+    s.bias[1, ::5] = np.finfo(np.float32).min
+    s.bias[2, ::3] = math.nan
+    s.bias_row[:4], s.mask_row[:4] = [0, 1, 2, -1], [3, 4, 0, -1]
+    plan, row_of, pool = plan_of(t)
+    plan.image(t.Hq, t.Hkv, dev())
+    for which in (dict(repetition=True), dict(bias=True, bias_row=True), dict(mask=True, mask_row=True), ALL):
+        want, mag = s.want(**which)
+        # what leaves fp32 (and bf16, by rounding) on the way is an infinity
+        most = float(torch.finfo(s.x.dtype).max) * (1 + (2.0 ** -25 if wide else 2.0 ** -9))
+        want = np.where(np.abs(want) >= most, np.copysign(np.inf, want), want)
+        got = s.call(plan, row_of, pool, **which)
+        near = np.isinf(want) & (mag < 1.01 * most) & (mag > 0.99 * most)
+        keep = torch.from_numpy(~near)
+        assert keep.float().mean() > 0.8
+        close(got.cpu()[keep], want[~near], mag[~near])
+    assert torch.isinf(got[0]).all() and (got[0] < 0).all()  # a mask that leaves nothing
+
+
+@pytest.mark.gpu
+def test_in_place_and_rows_apart():
+    t = wl.random_tree(8, n_nodes=9, max_len=50, nq=6)
+    plan, row_of, pool = plan_of(t)
+    plan.image(t.Hq, t.Hkv, dev())
+    for wide in (True, False):
+        s = Inputs(t, 1501, 3, wide)
+        want = s.call(plan, row_of, pool, **ALL)
+        args = {k: gpu(getattr(s, k)) for k in ALL}
+        tokens = gpu(s.tokens)
+        base = torch.full((6, 1700), 9.0, dtype=s.x.dtype, device=dev())
+        x = base[:, 100:1601]
+        x.copy_(s.x)
+        assert torch.equal(binding.deft_adjust_logits(plan, x, tokens, **args), want)
+        out = torch.full((6, 1503), 7.0, dtype=s.x.dtype, device=dev())
+        assert torch.equal(binding.deft_adjust_logits(plan, x, tokens, out=out[:, 1:1502], **args), want)
+        assert (out[:, 0] == 7).all() and (out[:, 1502] == 7).all() and torch.equal(x, s.x.to(dev()))
+        assert binding.deft_adjust_logits(plan, x, tokens, out=x, **args) is x
+        assert torch.equal(x, want) and (base[:, :100] == 9).all() and (base[:, 1601:] == 9).all()
+        # one row of logits for every query, tables of one row
+        one = s.x[:1].to(dev())
+        same = {k: args[k] for k in ("repetition", "frequency", "presence")}
+        a = binding.deft_adjust_logits(plan, one.expand(6, 1501), tokens, bias=args["bias"][1], mask=args["mask"][1], **same)
+        b = binding.deft_adjust_logits(plan, one.repeat(6, 1), tokens, bias=args["bias"][1:2], mask=args["mask"][:, :][1:2], **same)
+        assert torch.equal(a, b)
+
+
+@pytest.mark.gpu
+def test_rows_behind_four_billion_elements():
+    t = wl.random_tree(9, n_nodes=4, max_len=30, nq=5)
+    s = Inputs(t, 1200, 4, False)
+    plan, row_of, pool = plan_of(t)
+    plan.image(t.Hq, t.Hkv, dev())
+    base = torch.empty((5, 1_100_000_000), dtype=torch.bfloat16, device=dev())
+    x = base[:, -1200:]
+    x.copy_(s.x)
+    want = s.call(plan, row_of, pool, **ALL)
+    assert torch.equal(s.call(plan, row_of, pool, x=x, **ALL), want)
+    args = {k: gpu(getattr(s, k)) for k in ALL}
+    binding.deft_adjust_logits(plan, s.x.to(dev()), gpu(s.tokens), out=base[:, 5:1205], **args)
+    assert torch.equal(base[:, 5:1205], want)
+    del base, x
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.gpu
+def test_gpu_refusals():
+    t = wl.random_tree(8, n_nodes=9, max_len=50, nq=6)
+    plan = plan_of(t)[0]
+    s = Inputs(t, 100, 3, True)
+    x, tokens = s.x.to(dev()), gpu(s.tokens)
+    f = gpu(s.frequency)
+    adjust = binding.deft_adjust_logits
+    with pytest.raises(binding.DeftError) as e:
+        adjust(plan, x, tokens, frequency=f)  # no image: it is not made here, that would choose how the attention is cut
+    assert e.value.status == ENOTREADY
+    plan.image(t.Hq, t.Hkv, dev())
+    bias, mask, row = gpu(s.bias), gpu(s.mask), gpu(s.bias_row)
+    bad = [
+        lambda: adjust(plan, x.half()), lambda: adjust(plan, x[0]), lambda: adjust(plan, x.cpu()), lambda: adjust(plan, x[:5]), lambda: adjust(plan, x[:, :0]),
+        lambda: adjust(plan, x[:, ::2]), lambda: adjust(plan, x, frequency=f), lambda: adjust(plan, x, tokens.long(), frequency=f), lambda: adjust(plan, x, tokens.cpu(), frequency=f),
+        lambda: adjust(plan, x, tokens[:5], frequency=f), lambda: adjust(plan, x, tokens, frequency=f[:5]), lambda: adjust(plan, x, tokens, frequency=f.double()),
+        lambda: adjust(plan, x, tokens, presence=f.cpu()), lambda: adjust(plan, x, tokens, repetition=f[None]), lambda: adjust(plan, x, bias=bias[:, :99]),
+        lambda: adjust(plan, x, bias=bias.double()), lambda: adjust(plan, x, bias=bias[:0]), lambda: adjust(plan, x, bias_row=row), lambda: adjust(plan, x, mask_row=row),
+        lambda: adjust(plan, x, bias=bias, bias_row=row.long()), lambda: adjust(plan, x, mask=mask, mask_row=row[:3]), lambda: adjust(plan, x, mask=mask[:, :3]),
+        lambda: adjust(plan, x, mask=mask.long()), lambda: adjust(plan, x, mask=mask.bool()), lambda: adjust(plan, x, out=x[:, :50]), lambda: adjust(plan, x, out=x.to(torch.bfloat16)),
+        lambda: adjust(plan, x, out_dtype=torch.bfloat16), lambda: adjust(plan, x, out=x.t().contiguous().t()), lambda: adjust(plan, x[:1].expand(6, 100), out=x),
+        lambda: adjust(plan, x.view(-1)[:594].view(6, 99), out=x.view(-1)[1:595].view(6, 99)), lambda: adjust(plan, x, bias=bias[:1].expand(3, 100)),
+    ]
+    for i, call in enumerate(bad):
+        with pytest.raises(binding.DeftError):
+            call()
+            pytest.fail(f"call {i}")
+    empty = binding.deft_plan(t.node_tok_begin, t.node_tok_len, t.node_parent, [], t.ntok)
+    assert adjust(empty, x[:0], tokens, frequency=f[:0]).shape == (0, 100)
+
+
+@pytest.mark.gpu
+def test_images_are_those_of_the_attention():
+    t = wl.random_tree(8, n_nodes=9, max_len=50, nq=6, Hq=8, Hkv=2)
+    s = Inputs(t, 300, 3, True)
+    plan, row_of, pool = plan_of(t)
+    Q, K, V = (x.to(dev()) for x in wl.make_qkv(t))
+    binding.deft_tree_attn_decode(plan, Q, K, V)
+    images = dict(plan._images.of)
+    got = s.call(plan, row_of, pool, **ALL)
+    assert plan._images.of.keys() == images.keys()
+    close(got, *s.want(**ALL))
+
+
+@pytest.mark.gpu
+def test_captured_and_replayed():
+    t = wl.random_tree(18, n_nodes=20, max_len=50, nq=30)
+    s = Inputs(t, 3001, 3, True)
+    plan, row_of, pool = plan_of(t)
+    plan.image(t.Hq, t.Hkv, dev())
+    x, tokens, args = s.x.to(dev()), gpu(s.tokens), {k: gpu(getattr(s, k)) for k in ALL}
+    binding.deft_adjust_logits(plan, x, tokens, **args)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = binding.deft_adjust_logits(plan, x, tokens, **args)
+        rest = binding.deft_adjust_logits(plan, x, tokens, repetition=args["repetition"])
+    for i in range(4):
+        n = Inputs(t, 3001, 20 + i, True)
+        x.copy_(n.x)
+        tokens.copy_(gpu(n.tokens))
+        for k in ALL:
+            args[k].copy_(gpu(getattr(n, k)))
+        graph.replay()
+        a, b = got.clone(), rest.clone()
+        assert torch.equal(a.nan_to_num(), binding.deft_adjust_logits(plan, x, tokens, **args).nan_to_num())
+        assert torch.equal(b, binding.deft_adjust_logits(plan, x, tokens, repetition=args["repetition"]))
+        close(a, *n.want(**ALL))
+        torch.cuda.synchronize()
+    # a plan whose image is first sent inside a graph
+    plan, _, _ = plan_of(t)
+    Q, K, V = (z.to(dev()) for z in wl.make_qkv(t))
+    binding.deft_tree_attn_decode(plan_of(t)[0], Q, K, V)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        binding.deft_tree_attn_decode(plan, Q, K, V)
+        got = binding.deft_adjust_logits(plan, x, tokens, **args)
+    for _ in range(2):
+        graph.replay()
+        close(got, *n.want(**ALL))
+        close(binding.deft_adjust_logits(plan, x, tokens, **args), *n.want(**ALL))
+
+
+@pytest.mark.gpu
+def test_two_streams_at_once():
+    t = wl.config5_longcontext(root=3000, branches=16, lo=10, hi=300)
+    s = Inputs(t, 20000, 3, True)
+    plan, row_of, pool = plan_of(t)
+    plan.image(t.Hq, t.Hkv, dev())
+    x, tokens, args = s.x.to(dev()), gpu(s.tokens), {k: gpu(getattr(s, k)) for k in ALL}
+    want = binding.deft_adjust_logits(plan, x, tokens, **args)
+    other = binding.deft_adjust_logits(plan, x, tokens, presence=args["presence"])
+    sides = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        got = []
+        for side in sides:
+            side.wait_stream(torch.cuda.current_stream())
+            got.append(binding.deft_adjust_logits(plan, x, tokens, stream=side, **args))
+            got.append(binding.deft_adjust_logits(plan, x, tokens, presence=args["presence"], stream=side.cuda_stream))
+        for side in sides:
+            torch.cuda.current_stream().wait_stream(side)
+        assert all(torch.equal(a, b) for a, b in zip(got, [want, other] * 2))
