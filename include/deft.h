@@ -514,7 +514,9 @@ int deft_qkv_store(const deft_kv_list_t *list, const void *dev_image, const deft
  * mask, mask_row       : the same for masks: rows of (vocab + 31) / 32 words of 32 bits, mask_stride words apart, bit t % 32 of word t / 32 is
  *                        set where token t is allowed
  * dev_image, group     : with tokens, the image of the plan that deft_plan_upload made for group = Hq / Hkv (any will do); else not looked at
- * Asynchronous on `stream`.  Errors: DEFT_EINVAL, DEFT_ENOTREADY, DEFT_EHIP as for deft_tree_attn_decode.
+ * workspace            : device, 16-byte aligned, deft_logits_workspace_bytes(plan, vocab) of them (0 where none is used); NULL is right too,
+ *                        and slow over many tokens.  Not looked at without tokens.
+ * Asynchronous on `stream`.  Errors: DEFT_EINVAL, DEFT_ENOTREADY, DEFT_EWORKSPACE, DEFT_EHIP as for deft_tree_attn_decode.
  */
 #define DEFT_TOKEN_PROMPT 0x40000000
 #define DEFT_MAX_VOCAB (1 << 28)
@@ -535,7 +537,9 @@ typedef struct deft_logits {
     const int32_t *mask_row;
     int64_t mask_stride;
 } deft_logits_t;
-int deft_adjust_logits(const deft_plan_t *plan, const void *dev_image, int32_t group, const deft_logits_t *logits, void *stream);
+size_t deft_logits_workspace_bytes(const deft_plan_t *plan, int32_t vocab);
+int deft_adjust_logits(const deft_plan_t *plan, const void *dev_image, int32_t group, const deft_logits_t *logits, void *workspace,
+                       size_t workspace_bytes, void *stream);
 
 /*
  * Benchmark aid, not part of the method (no decode call uses it; it exists so that the benchmark can state

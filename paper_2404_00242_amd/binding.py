@@ -42,7 +42,7 @@ EXPORTS = (
     "deft_tree_attn_decode", "deft_tree_attn_decode_static", "deft_stage1_partial_attention", "deft_stage2_global_reduction",
     "deft_tree_attn_decode_q8", "deft_kv_rows", "deft_kv_copies", "deft_kv_list_device_bytes", "deft_kv_list_upload", "deft_kv_list_destroy",
     "deft_kv_store_q8", "deft_kv_load_q8", "deft_kv_copy_pages", "deft_compact_pages",
-    "deft_rope_frequencies", "deft_rope", "deft_rotate", "deft_qk_norm_rotate", "deft_qkv_store", "deft_adjust_logits",
+    "deft_rope_frequencies", "deft_rope", "deft_rotate", "deft_qk_norm_rotate", "deft_qkv_store", "deft_logits_workspace_bytes", "deft_adjust_logits",
     "deft_hbm_read_probe", "deft_plan_destroy", "deft_strerror", "deft_last_hip_error",
 )
 
@@ -171,7 +171,9 @@ def load_library():
     lib.deft_qkv_store.restype = ctypes.c_int
     lib.deft_qkv_store.argtypes = [vp, vp, heads, heads, heads, c32, c32, f32, f32, vp, rope, vp]
     lib.deft_adjust_logits.restype = ctypes.c_int
-    lib.deft_adjust_logits.argtypes = [vp, vp, c32, vp, vp]
+    lib.deft_adjust_logits.argtypes = [vp, vp, c32, vp, vp, csz, vp]
+    lib.deft_logits_workspace_bytes.restype = csz
+    lib.deft_logits_workspace_bytes.argtypes = [vp, c32]
     lib.deft_hbm_read_probe.restype = ctypes.c_int
     lib.deft_hbm_read_probe.argtypes = [vp, csz, vp, vp]
     lib.deft_plan_destroy.restype = None
@@ -380,6 +382,19 @@ class Plan:
                 ws = torch.empty(nbytes, dtype=torch.uint8, device=torch.device("cuda", index))
             self._workspaces[key] = ws
         return ws
+
+
+    def _logits_workspace(self, vocab, index, raw, capture):
+        """(address, bytes) of the workspace of deft_adjust_logits, as `workspace`; (0, 0) where it uses none."""
+        key = ("logits", vocab, index, raw, capture)
+        ws = self._workspaces.get(key)
+        if ws is None:
+            torch = _get_torch()
+            nbytes = int(load_library().deft_logits_workspace_bytes(self._h, vocab))
+            with torch.cuda.stream(_torch_stream(raw, index)):
+                ws = torch.empty(nbytes, dtype=torch.uint8, device=torch.device("cuda", index))
+            self._workspaces[key] = ws
+        return ws.data_ptr(), ws.numel()
 
 
 def _raw_stream(stream, index: int) -> int:
@@ -1156,15 +1171,16 @@ def deft_adjust_logits(plan: Plan, logits, tokens=None, repetition=None, frequen
     if _elsewhere(index):
         with torch.cuda.device(index):
             return deft_adjust_logits(plan, logits, tokens, repetition, frequency, presence, bias, bias_row, mask, mask_row, out, None, raw)
-    image, group = 0, 0
+    image = group = ws = ws_bytes = 0
     if history:
         capture = _capture(raw) if raw else 0
         image, group = plan._any_image(index, raw, capture)
+        ws, ws_bytes = plan._logits_workspace(vocab, index, raw, capture)
     rc = (_lib or load_library()).deft_adjust_logits(
         plan._h, image, group,
         _pack_logits(logits.data_ptr(), out.data_ptr(), stride if nq > 1 else vocab, out.stride(0) if nq > 1 else vocab, vocab, wide, out_wide, n_bias, n_masks, 0,
                      tokens.data_ptr() if history else 0, tokens.numel() if history else 0, *penalties, bias_at, bias_row_at, bias_stride, mask_at,
-                     mask_row_at, mask_stride), raw)
+                     mask_row_at, mask_stride), ws, ws_bytes, raw)
     if rc != 0:
         _check(rc, "deft_adjust_logits")
     return out

@@ -127,6 +127,7 @@ struct deft_plan_s {
     int32_t n_slots() const { return chunk_slot_base.empty() ? 0 : chunk_slot_base.back(); }
 
     mutable std::atomic<int64_t> rows{-1};  // see deft_plan_rows; -1: not asked for yet
+    mutable std::atomic<int64_t> tokens{-1};  // of all segments; the same
 
     // schedules by G, built on demand (the canonical arrays above never change)
     mutable std::mutex mu;

@@ -10,15 +10,33 @@
 
 namespace {
 
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+
+// The pieces of the tree in its depth-first order, and the tokens that they hold.
+struct Pieces {
+    const int32_t *begin, *len, *qlo, *qhi;  // rows of the cache; queries that see them, in the plan's order
+    const int32_t *off;                      // tokens in front
+    const int32_t *tokens;
+    uint32_t n;
+};
+
+// Tokens by tile of the vocabulary, as deft_sort_tokens leaves them: of every kRun of them, group g, those of tile i are
+// events[g * kRun + table[i * groups + g]] up to where those of the next tile begin.
+struct Sorted {
+    u32x4 *events;  // {token, its queries, -}
+    uint32_t *table;
+    uint32_t groups;
+};
+
 struct LogitsArgs {
     const void *logits;
     void *out;
     int64_t stride, out_stride;
     uint32_t vocab, nq, block, tiles;  // block: queries of a workgroup
-    const int32_t *seg_begin, *seg_len, *seg_qlo, *seg_qhi;
+    Pieces pieces;
+    Sorted sorted;
+    uint32_t history;        // pieces or groups to look through
     const int32_t *q_order;  // null: queries in the caller's order (no tokens are looked at)
-    uint32_t n_segs;         // 0: none are
-    const int32_t *tokens;
     const float *repetition, *frequency, *presence;
     const float *bias;
     const uint32_t *mask;
@@ -30,7 +48,10 @@ struct LogitsArgs {
 constexpr int kThreads = 256, kEach = 4;     // logits of a row to a thread, side by side
 constexpr int kTile = kThreads * kEach;      // of a workgroup
 constexpr int kMost = 32, kMostCounted = 8;  // queries of a workgroup: bits of a word, and counters that LDS has room for
-constexpr int kStage = 1024;                 // pieces at a time
+constexpr int kStage = 1024;                 // pieces or groups at a time
+constexpr int kRun = 1024;                   // tokens that deft_sort_tokens takes to a workgroup
+constexpr int kMaxTiles = 2048;              // that it sorts by
+constexpr int kFewTokens = 4096;             // are looked through unsorted
 
 struct Query {
     int32_t row;
@@ -92,18 +113,134 @@ __device__ __forceinline__ void see(Seen<COUNTS> &seen, int32_t token, uint32_t 
     }
 }
 
+// Queries [qlo, qhi) as bits of a workgroup's that begin at q0.
+__device__ __forceinline__ uint32_t bits_of(int32_t qlo, int32_t qhi, uint32_t q0, uint32_t block) {
+    const int32_t lo = max(qlo - (int32_t)q0, 0), hi = min(qhi - (int32_t)q0, (int32_t)block);
+    return lo < hi ? (0xffffffffu >> (32 - hi)) & (0xffffffffu << lo) : 0;
+}
+
+// Sum over the threads in front of this one, and over all, of two numbers each.
+struct Sums {
+    uint32_t x, y, all_x, all_y;
+};
+__device__ __forceinline__ Sums sums_before(uint32_t x, uint32_t y, uint32_t (*part)[2]) {
+    const uint32_t t = threadIdx.x, lane = t & 63;
+    Sums s{x, y, 0, 0};
+#pragma unroll
+    for (uint32_t o = 1; o < 64; o <<= 1) {
+        const uint32_t u = __shfl_up(s.x, o), v = __shfl_up(s.y, o);
+        if (lane >= o) {
+            s.x += u;
+            s.y += v;
+        }
+    }
+    if (lane == 63) {
+        part[t / 64][0] = s.x;
+        part[t / 64][1] = s.y;
+    }
+    s.x -= x;
+    s.y -= y;
+    __syncthreads();
+#pragma unroll
+    for (uint32_t w = 0; w < kThreads / 64; ++w) {
+        const uint32_t u = part[w][0], v = part[w][1];
+        if (w < t / 64) {
+            s.x += u;
+            s.y += v;
+        }
+        s.all_x += u;
+        s.all_y += v;
+    }
+    return s;
+}
+
+// The last of n ascending numbers (n a power of two) that is not above f; the first is not.
+__device__ __forceinline__ uint32_t last_not_above(const uint32_t *x, uint32_t n, uint32_t f) {
+    uint32_t at = 0;
+    for (uint32_t step = n / 2; step > 0; step /= 2)
+        if (x[at + step] <= f) at += step;
+    return at;
+}
+
+// Every workgroup of deft_logits would look through all tokens of its queries' paths for the few that are its tile's.  Where those are
+// many they are sorted by tile first, kRun of them to a workgroup, in LDS.
+__global__ __launch_bounds__(kThreads) void deft_sort_tokens(Pieces p, Sorted to, uint32_t total, uint32_t tiles) {
+    constexpr uint32_t kMine = kRun / kThreads, kBins = kMaxTiles / kThreads;
+    __shared__ uint32_t off[kRun], bins[kMaxTiles], part[kThreads / 64][2];
+    const uint32_t t = threadIdx.x, f0 = blockIdx.x * kRun, end = min(f0 + kRun, total);
+    uint32_t lo = 0, hi = p.n;  // the first token's piece is one of [lo, hi)
+    while (hi - lo > 1) {
+        const uint32_t step = (hi - lo + kThreads - 1) / kThreads, probe = lo + (t + 1) * step;
+        lo += step * (uint32_t)__syncthreads_count(probe < hi && (uint32_t)p.off[probe] <= f0);
+        hi = min(hi, lo + step);
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kMine; ++i) {  // (a piece has a token at least: no more than kRun of them)
+        const uint32_t k = t + kThreads * i;
+        off[k] = lo + k < p.n ? (uint32_t)p.off[lo + k] : 0xffffffffu;
+    }
+    for (uint32_t i = t; i < tiles; i += kThreads) bins[i] = 0;
+    __syncthreads();
+    int32_t token[kMine], qlo[kMine], qhi[kMine];
+    uint32_t rank[kMine];
+#pragma unroll
+    for (uint32_t i = 0; i < kMine; ++i) {
+        const uint32_t f = f0 + t + kThreads * i;
+        token[i] = -1;
+        if (f >= end) continue;
+        const uint32_t k = last_not_above(off, kRun, f), s = lo + k;
+        token[i] = p.tokens[(int64_t)p.begin[s] + (f - off[k])];
+        qlo[i] = p.qlo[s];
+        qhi[i] = p.qhi[s];
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kMine; ++i) {
+        const uint32_t tile = ((uint32_t)token[i] & (DEFT_TOKEN_PROMPT - 1)) / kTile;
+        if (token[i] < 0 || tile >= tiles)
+            token[i] = -1;
+        else
+            rank[i] = atomicAdd(&bins[tile], 1);
+    }
+    __syncthreads();
+    uint32_t many[kBins], sum = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < kBins; ++i) {
+        const uint32_t k = kBins * t + i;
+        many[i] = k < tiles ? bins[k] : 0;
+        sum += many[i];
+    }
+    const Sums s = sums_before(sum, 0, part);
+    uint32_t at = s.x;
+#pragma unroll
+    for (uint32_t i = 0; i < kBins; ++i) {
+        const uint32_t k = kBins * t + i;
+        if (k < tiles) {
+            bins[k] = at;
+            to.table[(uint64_t)k * to.groups + blockIdx.x] = at;
+        }
+        at += many[i];
+    }
+    if (t == 0) to.table[(uint64_t)tiles * to.groups + blockIdx.x] = s.all_x;
+    __syncthreads();
+#pragma unroll
+    for (uint32_t i = 0; i < kMine; ++i)
+        if (token[i] >= 0) {
+            const uint32_t tile = ((uint32_t)token[i] & (DEFT_TOKEN_PROMPT - 1)) / kTile;
+            to.events[(uint64_t)f0 + bins[tile] + rank[i]] = u32x4{(uint32_t)token[i], (uint32_t)qlo[i], (uint32_t)qhi[i], 0};
+        }
+}
+
 // A workgroup has kTile logits of `block` queries.  It first looks which of those tokens stand on the queries' paths: pieces of the
-// tree that any of its queries sees are taken kStage at a time into LDS, with the sum of their lengths in front of each, and every
-// thread finds the piece of its next token there by bisection.
-template <typename I, typename O, bool COUNTS>
+// tree that any of its queries sees, or the sorted tokens of its tile, are taken kStage stretches at a time into LDS, with the sum
+// of their lengths in front of each, and every thread finds the stretch of its next token there by bisection.
+template <typename I, typename O, bool COUNTS, bool SORTED>
 __global__ __launch_bounds__(kThreads) void deft_logits(LogitsArgs a) {
     __shared__ Seen<COUNTS> seen;
-    __shared__ uint32_t before[kStage + 1], bits[kStage];
-    __shared__ int32_t begin[kStage];  // row of a piece's first token, less `before`
-    __shared__ uint32_t part[kThreads / 64];
+    __shared__ uint32_t before[kStage], bits[SORTED ? 1 : kStage], part[kThreads / 64][2];
+    __shared__ int32_t begin[kStage];  // of a stretch, less `before`
     __shared__ Query queries[kMost];
-    const uint32_t tile = blockIdx.x % a.tiles, q0 = blockIdx.x / a.tiles * a.block, block = min(a.block, a.nq - q0);
-    const uint32_t first = tile * kTile, t = threadIdx.x, lane = t & 63;
+    const uint32_t blocks = gridDim.x / a.tiles, tile = blockIdx.x / blocks, q0 = blockIdx.x % blocks * a.block, block = min(a.block, a.nq - q0);
+    const uint32_t first = tile * kTile, t = threadIdx.x;
     if (t < block) {
         Query q;
         q.row = a.q_order ? a.q_order[q0 + t] : (int32_t)(q0 + t);
@@ -118,7 +255,7 @@ __global__ __launch_bounds__(kThreads) void deft_logits(LogitsArgs a) {
         queries[t] = q;
     }
     for (uint32_t i = t; i < sizeof(seen) / 4; i += kThreads) reinterpret_cast<uint32_t *>(&seen)[i] = 0;
-    for (uint32_t s0 = 0; s0 < a.n_segs; s0 += kStage) {
+    for (uint32_t s0 = 0; s0 < a.history; s0 += kStage) {
         uint32_t len[4], on[4], sum = 0, many = 0;
         int32_t at[4];
 #pragma unroll
@@ -126,59 +263,43 @@ __global__ __launch_bounds__(kThreads) void deft_logits(LogitsArgs a) {
             const uint32_t s = s0 + 4 * t + i;
             len[i] = on[i] = 0;
             at[i] = 0;
-            if (s < a.n_segs) {
-                const int32_t lo = max(a.seg_qlo[s] - (int32_t)q0, 0), hi = min(a.seg_qhi[s] - (int32_t)q0, (int32_t)block);
-                if (lo < hi) {
-                    on[i] = (0xffffffffu >> (32 - hi)) & (0xffffffffu << lo);
-                    len[i] = (uint32_t)a.seg_len[s];
-                    at[i] = a.seg_begin[s];
+            if (s < a.history) {
+                if constexpr (SORTED) {
+                    const uint32_t *from = a.sorted.table + (uint64_t)tile * a.sorted.groups + s;
+                    const uint32_t lo = from[0];
+                    len[i] = on[i] = from[a.sorted.groups] - lo;
+                    at[i] = (int32_t)(s * kRun + lo);
+                } else {
+                    on[i] = bits_of(a.pieces.qlo[s], a.pieces.qhi[s], q0, block);
+                    len[i] = on[i] ? (uint32_t)a.pieces.len[s] : 0;
+                    at[i] = a.pieces.begin[s];
                 }
             }
             sum += len[i];
             many += on[i] != 0;
+            before[kStage / 4 * i + t] = 0xffffffffu;
         }
-        // sums over the threads in front, of lengths and of pieces; both are below 2^32 in all
-        uint32_t sums = sum, pieces = many;
-#pragma unroll
-        for (uint32_t o = 1; o < 64; o <<= 1) {
-            const uint32_t x = __shfl_up(sums, o), y = __shfl_up(pieces, o);
-            if (lane >= o) {
-                sums += x;
-                pieces += y;
-            }
-        }
-        __shared__ uint32_t part_pieces[kThreads / 64];
-        if (lane == 63) {
-            part[t / 64] = sums;
-            part_pieces[t / 64] = pieces;
-        }
-        __syncthreads();
-        uint32_t total = 0, all = 0, base = sums - sum, slot = pieces - many;
-#pragma unroll
-        for (uint32_t w = 0; w < kThreads / 64; ++w) {
-            if (w < t / 64) {
-                base += part[w];
-                slot += part_pieces[w];
-            }
-            total += part[w];
-            all += part_pieces[w];
-        }
+        Sums sums = sums_before(sum, many, part);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if (!on[i]) continue;
-            before[slot] = base;
-            begin[slot] = at[i] - (int32_t)base;
-            bits[slot++] = on[i];
-            base += len[i];
+            before[sums.y] = sums.x;
+            begin[sums.y] = at[i] - (int32_t)sums.x;
+            if constexpr (!SORTED) bits[sums.y] = on[i];
+            ++sums.y;
+            sums.x += len[i];
         }
         __syncthreads();
-        for (uint32_t f = t; f < total; f += kThreads) {
-            uint32_t lo = 0, hi = all;  // before[lo] <= f < before[hi]
-            while (hi - lo > 1) {
-                const uint32_t mid = (lo + hi) / 2;
-                (before[mid] <= f ? lo : hi) = mid;
+        const uint32_t steps = sums.all_y > 1 ? 1u << (32 - __builtin_clz(sums.all_y - 1)) : 1;
+        for (uint32_t f = t; f < sums.all_x; f += kThreads) {
+            const uint32_t k = last_not_above(before, steps, f);
+            if constexpr (SORTED) {
+                const u32x4 e = a.sorted.events[(uint32_t)(begin[k] + (int32_t)f)];
+                const uint32_t on = bits_of((int32_t)e[1], (int32_t)e[2], q0, block);
+                if (on) see(seen, (int32_t)e[0], first, on, block);
+            } else {
+                see(seen, a.pieces.tokens[(int64_t)begin[k] + f], first, bits[k], block);
             }
-            see(seen, a.tokens[(int64_t)begin[lo] + f], first, bits[lo], block);
         }
         __syncthreads();
     }
@@ -230,11 +351,35 @@ __global__ __launch_bounds__(kThreads) void deft_logits(LogitsArgs a) {
 }
 
 template <typename I, typename O>
-void launch(const LogitsArgs &a, bool counts, uint32_t groups, hipStream_t st) {
-    if (counts)
-        hipLaunchKernelGGL((deft_logits<I, O, true>), dim3(groups), dim3(kThreads), 0, st, a);
-    else
-        hipLaunchKernelGGL((deft_logits<I, O, false>), dim3(groups), dim3(kThreads), 0, st, a);
+void launch(const LogitsArgs &a, bool counts, bool sorted, uint32_t groups, hipStream_t st) {
+    auto *kernel = counts ? (sorted ? &deft_logits<I, O, true, true> : &deft_logits<I, O, true, false>)
+                          : (sorted ? &deft_logits<I, O, false, true> : &deft_logits<I, O, false, false>);
+    hipLaunchKernelGGL(kernel, dim3(groups), dim3(kThreads), 0, st, a);
+}
+
+// Tokens of all pieces, a query's own time and again where pieces are grouped by query.
+int64_t tokens_of(const deft_plan_t *plan) {
+    int64_t total = plan->tokens.load(std::memory_order_relaxed);
+    if (total < 0) {  // (a plan never changes)
+        total = 0;
+        for (const int32_t len : plan->seg_len) total += len;
+        plan->tokens.store(total, std::memory_order_relaxed);
+    }
+    return total;
+}
+// Whether they are sorted before they are looked for.
+bool sorts(const deft_plan_t *plan, int64_t total, uint32_t tiles) {
+    return tiles <= kMaxTiles && total < (int64_t(1) << 30) && (total > kFewTokens || plan->n_segs() > kStage);
+}
+struct Space {
+    uint64_t groups, table, bytes;  // the table's place
+};
+Space space_of(int64_t total, uint32_t tiles) {
+    Space s;
+    s.groups = (uint64_t)(total + kRun - 1) / kRun;
+    s.table = s.groups * kRun * sizeof(u32x4);
+    s.bytes = s.table + s.groups * (tiles + 1) * sizeof(uint32_t);
+    return s;
 }
 
 constexpr int64_t kMaxStride = int64_t(1) << 31;  // times 2^31 queries of 4 bytes: within 64 bits
@@ -243,7 +388,15 @@ bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0;
 
 }  // namespace
 
-extern "C" int deft_adjust_logits(const deft_plan_t *plan, const void *dev_image, int32_t group, const deft_logits_t *l, void *stream) {
+extern "C" size_t deft_logits_workspace_bytes(const deft_plan_t *plan, int32_t vocab) {
+    if (!plan || vocab < 1 || vocab > DEFT_MAX_VOCAB) return 0;
+    const uint32_t tiles = ((uint32_t)vocab + kTile - 1) / kTile;
+    const int64_t total = tokens_of(plan);
+    return sorts(plan, total, tiles) ? (size_t)space_of(total, tiles).bytes : 0;
+}
+
+extern "C" int deft_adjust_logits(const deft_plan_t *plan, const void *dev_image, int32_t group, const deft_logits_t *l, void *workspace,
+                                  size_t workspace_bytes, void *stream) {
     if (!plan || !l || l->vocab < 1 || l->vocab > DEFT_MAX_VOCAB) return DEFT_EINVAL;
     const int32_t nq = plan->nq;
     const bool history = l->repetition || l->frequency || l->presence;
@@ -288,27 +441,35 @@ extern "C" int deft_adjust_logits(const deft_plan_t *plan, const void *dev_image
     a.mask_row = l->mask_row;
     a.mask_stride = l->mask_stride;
     a.n_masks = (uint32_t)l->n_masks;
-    if (history) {
-        auto at = [&](size_t off) { return reinterpret_cast<const int32_t *>(static_cast<const uint8_t *>(dev_image) + off); };
-        a.seg_begin = at(S->off_seg_tok_begin);
-        a.seg_len = at(S->off_seg_len);
-        a.seg_qlo = at(S->off_seg_qlo);
-        a.seg_qhi = at(S->off_seg_qhi);
-        a.q_order = at(S->off_q_order);
-        a.n_segs = (uint32_t)plan->n_segs();
-        a.tokens = l->tokens;
-    }
     const bool counts = l->frequency != nullptr;
     const uint64_t work = (uint64_t)a.nq * a.tiles;
     a.block = (uint32_t)std::clamp<uint64_t>((work + 1023) / 1024, 1, counts ? kMostCounted : kMost);
     const uint64_t groups = (uint64_t)a.tiles * ((a.nq + a.block - 1) / a.block);
     if (groups * kThreads > UINT32_MAX) return DEFT_EINVAL;
     hipStream_t st = static_cast<hipStream_t>(stream);
+    bool sorted = false;
+    if (history && plan->n_segs() > 0) {
+        auto at = [&](size_t off) { return reinterpret_cast<const int32_t *>(static_cast<const uint8_t *>(dev_image) + off); };
+        a.pieces = {at(S->off_seg_tok_begin), at(S->off_seg_len), at(S->off_seg_qlo), at(S->off_seg_qhi), at(S->off_seg_off), l->tokens, (uint32_t)plan->n_segs()};
+        a.q_order = at(S->off_q_order);
+        a.history = a.pieces.n;
+        const int64_t total = tokens_of(plan);
+        sorted = workspace && sorts(plan, total, a.tiles);
+        if (sorted) {
+            const Space space = space_of(total, a.tiles);
+            if (!deft::aligned16(workspace)) return DEFT_EINVAL;
+            if (workspace_bytes < space.bytes) return DEFT_EWORKSPACE;
+            a.sorted = {static_cast<u32x4 *>(workspace), reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(workspace) + space.table), (uint32_t)space.groups};
+            a.history = a.sorted.groups;
+            hipLaunchKernelGGL(deft_sort_tokens, dim3(a.sorted.groups), dim3(kThreads), 0, st, a.pieces, a.sorted, (uint32_t)total, a.tiles);
+            if (!deft::hip_ok(hipGetLastError(), "deft_sort_tokens launch")) return DEFT_EHIP;
+        }
+    }
     if (l->logits_f32)
-        launch<float, float>(a, counts, (uint32_t)groups, st);
+        launch<float, float>(a, counts, sorted, (uint32_t)groups, st);
     else if (l->out_f32)
-        launch<__bf16, float>(a, counts, (uint32_t)groups, st);
+        launch<__bf16, float>(a, counts, sorted, (uint32_t)groups, st);
     else
-        launch<__bf16, __bf16>(a, counts, (uint32_t)groups, st);
+        launch<__bf16, __bf16>(a, counts, sorted, (uint32_t)groups, st);
     return deft::hip_ok(hipGetLastError(), "deft_logits launch") ? DEFT_OK : DEFT_EHIP;
 }

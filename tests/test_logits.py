@@ -33,7 +33,7 @@ def test_calls_that_are_refused():
              tokens=0, n_tokens=0, repetition=0, frequency=0, presence=0, bias=0, bias_row=0, bias_stride=0, mask=0, mask_row=0, mask_stride=0):
         packed = binding._pack_logits(logits, out, stride, out_stride, vocab, wide, out_wide, n_bias, n_masks, 0, tokens, n_tokens, repetition, frequency,
                                       presence, bias, bias_row, bias_stride, mask, mask_row, mask_stride)
-        return lib.deft_adjust_logits(plan, image, group, packed, None)
+        return lib.deft_adjust_logits(plan, image, group, packed, None, 0, None)
 
     at = 1 << 12
     for bad in (dict(plan=None), dict(logits=0), dict(out=0), dict(vocab=0), dict(vocab=-5), dict(vocab=(1 << 28) + 1, stride=1 << 29, out_stride=1 << 29),
@@ -47,7 +47,7 @@ def test_calls_that_are_refused():
                 dict(presence=at, tokens=at + 2, n_tokens=rows), dict(repetition=at, tokens=at, n_tokens=rows), dict(repetition=at, tokens=at, n_tokens=rows, image=at + 8),
                 dict(repetition=at, tokens=at, n_tokens=rows, image=at, group=0)):
         assert call(**bad) == EINVAL, bad
-    assert lib.deft_adjust_logits(plan.handle, None, 1, None, None) == EINVAL
+    assert lib.deft_adjust_logits(plan.handle, None, 1, None, None, 0, None) == EINVAL
     assert call(repetition=at, tokens=at, n_tokens=rows, image=at, group=3) == ENOTREADY
     nobody = binding.deft_plan(t.node_tok_begin, t.node_tok_len, t.node_parent, [], t.ntok)
     assert call(plan=nobody.handle, logits=0, out=0) == 0
