@@ -11,6 +11,8 @@
 namespace {
 
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+typedef __attribute__((ext_vector_type(2))) int32_t i32x2;
 
 // The pieces of the tree in its depth-first order, and the tokens that they hold.
 struct Pieces {
@@ -25,6 +27,7 @@ struct Pieces {
 struct Sorted {
     u32x4 *events;  // {token, its queries, -}
     uint32_t *table;
+    u32x2 *seen_by;  // of a group: queries that see any of its tokens lie in [x, y)
     uint32_t groups;
 };
 
@@ -45,48 +48,39 @@ struct LogitsArgs {
     uint32_t n_bias, n_masks;
 };
 
-constexpr int kThreads = 256, kEach = 4;     // logits of a row to a thread, side by side
-constexpr int kTile = kThreads * kEach;      // of a workgroup
-constexpr int kMost = 32, kMostCounted = 8;  // queries of a workgroup: bits of a word, and counters that LDS has room for
-constexpr int kStage = 1024;                 // pieces or groups at a time
-constexpr int kRun = 1024;                   // tokens that deft_sort_tokens takes to a workgroup
-constexpr int kMaxTiles = 2048;              // that it sorts by
-constexpr int kFewTokens = 4096;             // are looked through unsorted
+constexpr int kThreads = 512;
+constexpr int kTile = 1024;       // logits of a row to a workgroup
+constexpr int kMost = 8;          // rows to a workgroup: as many as a thread can have in flight in registers
+constexpr int kStage = 512;      // pieces or groups at a time
+constexpr uint32_t kEach = kTile / kThreads, kStretches = kStage / kThreads;  // to a thread
+constexpr int kSortThreads = 1024;
+constexpr int kRun = 1024;        // tokens that deft_sort_tokens takes to a workgroup
+constexpr int kMaxTiles = 2048;   // that it sorts by
+constexpr int kFewTokens = 5000;  // are looked through unsorted
+constexpr int kAhead = 2;         // tokens of a thread in flight
 
-struct Query {
-    int32_t row;
-    float repetition, inverse, frequency, presence;
-    int32_t bias, mask;  // rows of the tables, -1: none
-};
-
+// A value that is the same for all lanes, by a scalar load.
 template <typename T>
-struct Vec;
-template <>
-struct Vec<float> {
-    typedef __attribute__((ext_vector_type(4), aligned(4))) float type;  // (rows of odd length: any element can be a row's first)
-    static __device__ __forceinline__ float get(const float *p) { return *p; }
-    static __device__ __forceinline__ void get4(const float *p, float *x) {
-        const type v = *reinterpret_cast<const type *>(p);
+__device__ __forceinline__ T uniform(const T *p, uint32_t i) {
+    return *((const __attribute__((address_space(4))) T *)(uintptr_t)(p + i));
+}
+
+// `N` elements side by side, as floats.  (Rows may have odd lengths: any element can be a row's first.)
+template <typename T, int N>
+__device__ __forceinline__ void get(const T *p, float *x) {
+    typedef __attribute__((ext_vector_type(N), aligned(sizeof(T)))) T type;
+    const type v = *reinterpret_cast<const type *>(p);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = v[i];
-    }
-    static __device__ __forceinline__ void put(float *p, float x) { *p = x; }
-    static __device__ __forceinline__ void put4(float *p, const float *x) { *reinterpret_cast<type *>(p) = type{x[0], x[1], x[2], x[3]}; }
-};
-template <>
-struct Vec<__bf16> {
-    typedef __attribute__((ext_vector_type(4), aligned(2))) __bf16 type;
-    static __device__ __forceinline__ float get(const __bf16 *p) { return (float)*p; }
-    static __device__ __forceinline__ void get4(const __bf16 *p, float *x) {
-        const type v = *reinterpret_cast<const type *>(p);
+    for (int i = 0; i < N; ++i) x[i] = (float)v[i];
+}
+template <typename T, int N>
+__device__ __forceinline__ void put(T *p, const float *x) {
+    typedef __attribute__((ext_vector_type(N), aligned(sizeof(T)))) T type;
+    type v;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = (float)v[i];
-    }
-    static __device__ __forceinline__ void put(__bf16 *p, float x) { *p = (__bf16)x; }
-    static __device__ __forceinline__ void put4(__bf16 *p, const float *x) {
-        *reinterpret_cast<type *>(p) = type{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
-    }
-};
+    for (int i = 0; i < N; ++i) v[i] = (T)x[i];
+    *reinterpret_cast<type *>(p) = v;
+}
 
 // Queries are in the plan's depth-first order here, in which the queries whose path holds a token are neighbours: `bits` says which
 // of the workgroup's queries they are.  With COUNTS a token adds one at the first of them and takes one away behind the last, so
@@ -94,8 +88,8 @@ struct Vec<__bf16> {
 template <bool COUNTS>
 struct Seen {
     uint32_t any[kTile];                        // bit q: on the path of query q
-    uint32_t generated[COUNTS ? 1 : kTile];     // the same, prompt tokens left out
-    int32_t change[COUNTS ? kMostCounted : 1][COUNTS ? kTile : 1];
+    uint32_t generated[COUNTS ? 4 : kTile];     // the same, prompt tokens left out
+    int32_t change[COUNTS ? kMost : 1][COUNTS ? kTile : 4];
 };
 
 template <bool COUNTS>
@@ -123,6 +117,7 @@ __device__ __forceinline__ uint32_t bits_of(int32_t qlo, int32_t qhi, uint32_t q
 struct Sums {
     uint32_t x, y, all_x, all_y;
 };
+template <int THREADS>
 __device__ __forceinline__ Sums sums_before(uint32_t x, uint32_t y, uint32_t (*part)[2]) {
     const uint32_t t = threadIdx.x, lane = t & 63;
     Sums s{x, y, 0, 0};
@@ -142,7 +137,7 @@ __device__ __forceinline__ Sums sums_before(uint32_t x, uint32_t y, uint32_t (*p
     s.y -= y;
     __syncthreads();
 #pragma unroll
-    for (uint32_t w = 0; w < kThreads / 64; ++w) {
+    for (uint32_t w = 0; w < THREADS / 64; ++w) {
         const uint32_t u = part[w][0], v = part[w][1];
         if (w < t / 64) {
             s.x += u;
@@ -164,34 +159,42 @@ __device__ __forceinline__ uint32_t last_not_above(const uint32_t *x, uint32_t n
 
 // Every workgroup of deft_logits would look through all tokens of its queries' paths for the few that are its tile's.  Where those are
 // many they are sorted by tile first, kRun of them to a workgroup, in LDS.
-__global__ __launch_bounds__(kThreads) void deft_sort_tokens(Pieces p, Sorted to, uint32_t total, uint32_t tiles) {
-    constexpr uint32_t kMine = kRun / kThreads, kBins = kMaxTiles / kThreads;
-    __shared__ uint32_t off[kRun], bins[kMaxTiles], part[kThreads / 64][2];
+__global__ __launch_bounds__(kSortThreads) void deft_sort_tokens(Pieces p, Sorted to, uint32_t total, uint32_t tiles) {
+    constexpr uint32_t kMine = kRun / kSortThreads, kBins = kMaxTiles / kSortThreads;
+    __shared__ uint32_t off[kRun], bins[kMaxTiles], part[kSortThreads / 64][2];
+    __shared__ int32_t begin[kRun], least, most;
+    __shared__ i32x2 queries[kRun];
     const uint32_t t = threadIdx.x, f0 = blockIdx.x * kRun, end = min(f0 + kRun, total);
     uint32_t lo = 0, hi = p.n;  // the first token's piece is one of [lo, hi)
-    while (hi - lo > 1) {
-        const uint32_t step = (hi - lo + kThreads - 1) / kThreads, probe = lo + (t + 1) * step;
+    while (p.n > kRun && hi - lo > 1) {  // (of no more pieces than that, all are taken)
+        const uint32_t step = (hi - lo + kSortThreads - 1) / kSortThreads, probe = lo + (t + 1) * step;
         lo += step * (uint32_t)__syncthreads_count(probe < hi && (uint32_t)p.off[probe] <= f0);
         hi = min(hi, lo + step);
     }
 #pragma unroll
     for (uint32_t i = 0; i < kMine; ++i) {  // (a piece has a token at least: no more than kRun of them)
-        const uint32_t k = t + kThreads * i;
-        off[k] = lo + k < p.n ? (uint32_t)p.off[lo + k] : 0xffffffffu;
+        const uint32_t k = t + kSortThreads * i, s = min(lo + k, p.n - 1);
+        off[k] = lo + k < p.n ? (uint32_t)p.off[s] : 0xffffffffu;
+        begin[k] = p.begin[s];
+        queries[k] = i32x2{p.qlo[s], p.qhi[s]};
     }
-    for (uint32_t i = t; i < tiles; i += kThreads) bins[i] = 0;
+    for (uint32_t i = t; i < tiles; i += kSortThreads) bins[i] = 0;
+    if (t == 0) {
+        least = INT32_MAX;
+        most = 0;
+    }
     __syncthreads();
     int32_t token[kMine], qlo[kMine], qhi[kMine];
     uint32_t rank[kMine];
 #pragma unroll
     for (uint32_t i = 0; i < kMine; ++i) {
-        const uint32_t f = f0 + t + kThreads * i;
+        const uint32_t f = f0 + t + kSortThreads * i;
         token[i] = -1;
         if (f >= end) continue;
-        const uint32_t k = last_not_above(off, kRun, f), s = lo + k;
-        token[i] = p.tokens[(int64_t)p.begin[s] + (f - off[k])];
-        qlo[i] = p.qlo[s];
-        qhi[i] = p.qhi[s];
+        const uint32_t k = last_not_above(off, kRun, f);
+        token[i] = p.tokens[(int64_t)begin[k] + (f - off[k])];
+        qlo[i] = queries[k][0];
+        qhi[i] = queries[k][1];
     }
 #pragma unroll
     for (uint32_t i = 0; i < kMine; ++i) {
@@ -201,6 +204,22 @@ __global__ __launch_bounds__(kThreads) void deft_sort_tokens(Pieces p, Sorted to
         else
             rank[i] = atomicAdd(&bins[tile], 1);
     }
+    int32_t lowest = INT32_MAX, highest = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < kMine; ++i)
+        if (token[i] >= 0) {
+            lowest = min(lowest, qlo[i]);
+            highest = max(highest, qhi[i]);
+        }
+#pragma unroll
+    for (uint32_t o = 1; o < 64; o <<= 1) {
+        lowest = min(lowest, __shfl_xor(lowest, o));
+        highest = max(highest, __shfl_xor(highest, o));
+    }
+    if (t % 64 == 0) {
+        atomicMin(&least, lowest);
+        atomicMax(&most, highest);
+    }
     __syncthreads();
     uint32_t many[kBins], sum = 0;
 #pragma unroll
@@ -209,7 +228,7 @@ __global__ __launch_bounds__(kThreads) void deft_sort_tokens(Pieces p, Sorted to
         many[i] = k < tiles ? bins[k] : 0;
         sum += many[i];
     }
-    const Sums s = sums_before(sum, 0, part);
+    const Sums s = sums_before<kSortThreads>(sum, 0, part);
     uint32_t at = s.x;
 #pragma unroll
     for (uint32_t i = 0; i < kBins; ++i) {
@@ -220,7 +239,10 @@ __global__ __launch_bounds__(kThreads) void deft_sort_tokens(Pieces p, Sorted to
         }
         at += many[i];
     }
-    if (t == 0) to.table[(uint64_t)tiles * to.groups + blockIdx.x] = s.all_x;
+    if (t == 0) {
+        to.table[(uint64_t)tiles * to.groups + blockIdx.x] = s.all_x;
+        to.seen_by[blockIdx.x] = u32x2{(uint32_t)least, (uint32_t)most};
+    }
     __syncthreads();
 #pragma unroll
     for (uint32_t i = 0; i < kMine; ++i)
@@ -235,39 +257,65 @@ __global__ __launch_bounds__(kThreads) void deft_sort_tokens(Pieces p, Sorted to
 // of their lengths in front of each, and every thread finds the stretch of its next token there by bisection.
 template <typename I, typename O, bool COUNTS, bool SORTED>
 __global__ __launch_bounds__(kThreads) void deft_logits(LogitsArgs a) {
-    __shared__ Seen<COUNTS> seen;
+    __shared__ __align__(16) Seen<COUNTS> seen;
     __shared__ uint32_t before[kStage], bits[SORTED ? 1 : kStage], part[kThreads / 64][2];
     __shared__ int32_t begin[kStage];  // of a stretch, less `before`
-    __shared__ Query queries[kMost];
     const uint32_t blocks = gridDim.x / a.tiles, tile = blockIdx.x / blocks, q0 = blockIdx.x % blocks * a.block, block = min(a.block, a.nq - q0);
-    const uint32_t first = tile * kTile, t = threadIdx.x;
-    if (t < block) {
-        Query q;
-        q.row = a.q_order ? a.q_order[q0 + t] : (int32_t)(q0 + t);
-        q.repetition = a.repetition ? a.repetition[q.row] : 1.f;
-        q.inverse = 1.f / q.repetition;
-        q.frequency = a.frequency ? a.frequency[q.row] : 0.f;
-        q.presence = a.presence ? a.presence[q.row] : 0.f;
-        q.bias = a.bias ? (a.bias_row ? a.bias_row[q.row] : 0) : -1;
-        q.mask = a.mask ? (a.mask_row ? a.mask_row[q.row] : 0) : -1;
-        if ((uint32_t)q.bias >= a.n_bias) q.bias = -1;
-        if ((uint32_t)q.mask >= a.n_masks) q.mask = -1;
-        queries[t] = q;
-    }
-    for (uint32_t i = t; i < sizeof(seen) / 4; i += kThreads) reinterpret_cast<uint32_t *>(&seen)[i] = 0;
-    for (uint32_t s0 = 0; s0 < a.history; s0 += kStage) {
-        uint32_t len[4], on[4], sum = 0, many = 0;
-        int32_t at[4];
+    const uint32_t first = tile * kTile, t = threadIdx.x, mine = kEach * t, v = first + mine;
+    const uint32_t n = v < a.vocab ? min(a.vocab - v, kEach) : 0;
+    // Everything that does not wait for the tokens is asked for at once.  Queries behind the last are that one.
+    uint32_t row[kMost];
+    float repetition[kMost], frequency[kMost], presence[kMost];
+    int32_t bias[kMost], mask[kMost];  // rows of the tables
+    float x[kMost][kEach];
+    uint32_t word[kMost];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t s = s0 + 4 * t + i;
+    for (uint32_t q = 0; q < kMost; ++q) {
+        const uint32_t at = q0 + min(q, block - 1);
+        row[q] = a.q_order ? (uint32_t)uniform(a.q_order, at) : at;
+    }
+#pragma unroll
+    for (uint32_t q = 0; q < kMost; ++q) {
+        mask[q] = !a.mask ? -1 : a.mask_row ? uniform(a.mask_row, row[q]) : 0;
+        if ((uint32_t)mask[q] >= a.n_masks) mask[q] = -1;
+        bias[q] = !a.bias ? -1 : a.bias_row ? uniform(a.bias_row, row[q]) : 0;
+        if ((uint32_t)bias[q] >= a.n_bias) bias[q] = -1;
+        repetition[q] = a.repetition ? uniform(a.repetition, row[q]) : 1.f;
+        frequency[q] = COUNTS ? uniform(a.frequency, row[q]) : 0.f;
+        presence[q] = a.presence ? uniform(a.presence, row[q]) : 0.f;
+    }
+    if (n == kEach) {
+#pragma unroll
+        for (uint32_t q = 0; q < kMost; ++q) get<I, kEach>(static_cast<const I *>(a.logits) + (int64_t)row[q] * a.stride + v, x[q]);
+    } else {
+        for (uint32_t i = 0; i < n; ++i)
+#pragma unroll
+            for (uint32_t q = 0; q < kMost; ++q) {
+                const float y = (float)static_cast<const I *>(a.logits)[(int64_t)row[q] * a.stride + v + i];
+#pragma unroll
+                for (uint32_t k = 0; k < kEach; ++k) x[q][k] = k == i ? y : x[q][k];
+            }
+    }
+    if (a.mask && n) {
+#pragma unroll
+        for (uint32_t q = 0; q < kMost; ++q) word[q] = a.mask[(int64_t)max(mask[q], 0) * a.mask_stride + v / 32];
+    }
+    static_assert(sizeof(seen) % 16 == 0, "cleared in 128-bit words");
+    for (uint32_t i = t; i < sizeof(seen) / 16; i += kThreads) reinterpret_cast<u32x4 *>(&seen)[i] = u32x4{0, 0, 0, 0};
+    for (uint32_t s0 = 0; s0 < a.history; s0 += kStage) {
+        uint32_t len[kStretches], on[kStretches], sum = 0, many = 0;
+        int32_t at[kStretches];
+#pragma unroll
+        for (uint32_t i = 0; i < kStretches; ++i) {
+            const uint32_t s = s0 + kStretches * t + i;
             len[i] = on[i] = 0;
             at[i] = 0;
             if (s < a.history) {
                 if constexpr (SORTED) {
                     const uint32_t *from = a.sorted.table + (uint64_t)tile * a.sorted.groups + s;
-                    const uint32_t lo = from[0];
-                    len[i] = on[i] = from[a.sorted.groups] - lo;
+                    const u32x2 seen_by = a.sorted.seen_by[s];
+                    const uint32_t lo = from[0], many = from[a.sorted.groups] - lo;
+                    len[i] = on[i] = seen_by[0] < q0 + block && seen_by[1] > q0 ? many : 0;
                     at[i] = (int32_t)(s * kRun + lo);
                 } else {
                     on[i] = bits_of(a.pieces.qlo[s], a.pieces.qhi[s], q0, block);
@@ -277,11 +325,11 @@ __global__ __launch_bounds__(kThreads) void deft_logits(LogitsArgs a) {
             }
             sum += len[i];
             many += on[i] != 0;
-            before[kStage / 4 * i + t] = 0xffffffffu;
+            before[kThreads * i + t] = 0xffffffffu;
         }
-        Sums sums = sums_before(sum, many, part);
+        Sums sums = sums_before<kThreads>(sum, many, part);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (uint32_t i = 0; i < kStretches; ++i) {
             if (!on[i]) continue;
             before[sums.y] = sums.x;
             begin[sums.y] = at[i] - (int32_t)sums.x;
@@ -291,62 +339,77 @@ __global__ __launch_bounds__(kThreads) void deft_logits(LogitsArgs a) {
         }
         __syncthreads();
         const uint32_t steps = sums.all_y > 1 ? 1u << (32 - __builtin_clz(sums.all_y - 1)) : 1;
-        for (uint32_t f = t; f < sums.all_x; f += kThreads) {
-            const uint32_t k = last_not_above(before, steps, f);
-            if constexpr (SORTED) {
-                const u32x4 e = a.sorted.events[(uint32_t)(begin[k] + (int32_t)f)];
-                const uint32_t on = bits_of((int32_t)e[1], (int32_t)e[2], q0, block);
-                if (on) see(seen, (int32_t)e[0], first, on, block);
-            } else {
-                see(seen, a.pieces.tokens[(int64_t)begin[k] + f], first, bits[k], block);
+        for (uint32_t f0 = t; f0 < sums.all_x; f0 += kAhead * kThreads) {
+            uint32_t k[kAhead];
+            u32x4 e[kAhead];
+#pragma unroll
+            for (uint32_t u = 0; u < kAhead; ++u) {
+                const uint32_t f = min(f0 + u * kThreads, sums.all_x - 1);
+                k[u] = last_not_above(before, steps, f);
+                if constexpr (SORTED)
+                    e[u] = a.sorted.events[(uint32_t)(begin[k[u]] + (int32_t)f)];
+                else
+                    e[u][0] = (uint32_t)a.pieces.tokens[(int64_t)begin[k[u]] + f];
+            }
+#pragma unroll
+            for (uint32_t u = 0; u < kAhead; ++u) {
+                if (f0 + u * kThreads >= sums.all_x) break;
+                const uint32_t which = SORTED ? bits_of((int32_t)e[u][1], (int32_t)e[u][2], q0, block) : bits[k[u]];
+                if (which) see(seen, (int32_t)e[u][0], first, which, block);
             }
         }
         __syncthreads();
     }
     __syncthreads();
-    const uint32_t mine = kEach * t, v = first + mine;
-    if (v >= a.vocab) return;
-    const uint32_t n = min(a.vocab - v, (uint32_t)kEach);
+    if (n == 0) return;
     uint32_t any[kEach], generated[kEach];
     int32_t count[kEach] = {};
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
+    for (uint32_t i = 0; i < kEach; ++i) {
         any[i] = seen.any[mine + i];
         generated[i] = COUNTS ? 0 : seen.generated[mine + i];
     }
-    for (uint32_t q = 0; q < block; ++q) {
-        const Query &query = queries[q];
-        const I *from = static_cast<const I *>(a.logits) + (int64_t)query.row * a.stride + v;
-        O *to = static_cast<O *>(a.out) + (int64_t)query.row * a.out_stride + v;
-        float x[kEach] = {};
-        if (n == kEach)
-            Vec<I>::get4(from, x);
-        else
-            for (uint32_t i = 0; i < n; ++i) x[i] = Vec<I>::get(from + i);
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            if ((any[i] >> q) & 1) x[i] *= x[i] > 0 ? query.inverse : query.repetition;
+    for (uint32_t q = 0; q < kMost; ++q) {
+        if (q >= block) break;
+        const float inverse = 1.f / repetition[q];
+#pragma unroll
+        for (uint32_t i = 0; i < kEach; ++i) {
+            if ((any[i] >> q) & 1) x[q][i] *= x[q][i] > 0 ? inverse : repetition[q];
             if constexpr (COUNTS) {
                 count[i] += seen.change[q][mine + i];
-                if (count[i] > 0) x[i] -= query.frequency * (float)count[i] + query.presence;
+                if (count[i] > 0) x[q][i] -= frequency[q] * (float)count[i] + presence[q];
             } else {
-                if ((generated[i] >> q) & 1) x[i] -= query.presence;
+                if ((generated[i] >> q) & 1) x[q][i] -= presence[q];
             }
         }
-        if (query.bias >= 0) {
-            const float *b = a.bias + (int64_t)query.bias * a.bias_stride + v;
-            for (uint32_t i = 0; i < n; ++i) x[i] += b[i];
-        }
-        if (query.mask >= 0) {
-            const uint32_t word = a.mask[(int64_t)query.mask * a.mask_stride + v / 32] >> (v % 32);
+        if (bias[q] >= 0) {
+            const float *b = a.bias + (int64_t)bias[q] * a.bias_stride + v;
+            float y[kEach] = {};
+            if (n == kEach)
+                get<float, kEach>(b, y);
+            else
+                for (uint32_t i = 0; i < n; ++i) {
+                    const float z = b[i];
 #pragma unroll
-            for (int i = 0; i < kEach; ++i)
-                if (!((word >> i) & 1)) x[i] = -__builtin_inff();
+                    for (uint32_t k = 0; k < kEach; ++k) y[k] = k == i ? z : y[k];
+                }
+#pragma unroll
+            for (uint32_t i = 0; i < kEach; ++i) x[q][i] += y[i];
         }
-        if (n == kEach)
-            Vec<O>::put4(to, x);
-        else
-            for (uint32_t i = 0; i < n; ++i) Vec<O>::put(to + i, x[i]);
+        if (mask[q] >= 0) {
+#pragma unroll
+            for (uint32_t i = 0; i < kEach; ++i)
+                if (!((word[q] >> (v % 32 + i)) & 1)) x[q][i] = -__builtin_inff();
+        }
+        O *to = static_cast<O *>(a.out) + (int64_t)row[q] * a.out_stride + v;
+        if (n == kEach) {
+            put<O, kEach>(to, x[q]);
+        } else {
+#pragma unroll
+            for (uint32_t i = 0; i < kEach; ++i)
+                if (i < n) to[i] = (O)x[q][i];
+        }
     }
 }
 
@@ -372,13 +435,14 @@ bool sorts(const deft_plan_t *plan, int64_t total, uint32_t tiles) {
     return tiles <= kMaxTiles && total < (int64_t(1) << 30) && (total > kFewTokens || plan->n_segs() > kStage);
 }
 struct Space {
-    uint64_t groups, table, bytes;  // the table's place
+    uint64_t groups, table, seen_by, bytes;  // places
 };
 Space space_of(int64_t total, uint32_t tiles) {
     Space s;
     s.groups = (uint64_t)(total + kRun - 1) / kRun;
     s.table = s.groups * kRun * sizeof(u32x4);
-    s.bytes = s.table + s.groups * (tiles + 1) * sizeof(uint32_t);
+    s.seen_by = s.table + (s.groups * (tiles + 1) + 1) / 2 * 2 * sizeof(uint32_t);
+    s.bytes = s.seen_by + s.groups * sizeof(u32x2);
     return s;
 }
 
@@ -443,7 +507,7 @@ extern "C" int deft_adjust_logits(const deft_plan_t *plan, const void *dev_image
     a.n_masks = (uint32_t)l->n_masks;
     const bool counts = l->frequency != nullptr;
     const uint64_t work = (uint64_t)a.nq * a.tiles;
-    a.block = (uint32_t)std::clamp<uint64_t>((work + 1023) / 1024, 1, counts ? kMostCounted : kMost);
+    a.block = (uint32_t)std::clamp<uint64_t>((work + 511) / 512, 1, kMost);
     const uint64_t groups = (uint64_t)a.tiles * ((a.nq + a.block - 1) / a.block);
     if (groups * kThreads > UINT32_MAX) return DEFT_EINVAL;
     hipStream_t st = static_cast<hipStream_t>(stream);
@@ -459,9 +523,10 @@ extern "C" int deft_adjust_logits(const deft_plan_t *plan, const void *dev_image
             const Space space = space_of(total, a.tiles);
             if (!deft::aligned16(workspace)) return DEFT_EINVAL;
             if (workspace_bytes < space.bytes) return DEFT_EWORKSPACE;
-            a.sorted = {static_cast<u32x4 *>(workspace), reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(workspace) + space.table), (uint32_t)space.groups};
+            a.sorted = {static_cast<u32x4 *>(workspace), reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(workspace) + space.table),
+                        reinterpret_cast<u32x2 *>(static_cast<uint8_t *>(workspace) + space.seen_by), (uint32_t)space.groups};
             a.history = a.sorted.groups;
-            hipLaunchKernelGGL(deft_sort_tokens, dim3(a.sorted.groups), dim3(kThreads), 0, st, a.pieces, a.sorted, (uint32_t)total, a.tiles);
+            hipLaunchKernelGGL(deft_sort_tokens, dim3(a.sorted.groups), dim3(kSortThreads), 0, st, a.pieces, a.sorted, (uint32_t)total, a.tiles);
             if (!deft::hip_ok(hipGetLastError(), "deft_sort_tokens launch")) return DEFT_EHIP;
         }
     }
