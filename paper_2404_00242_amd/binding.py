@@ -931,11 +931,12 @@ def deft_rope(rot: int, base: float = 10000.0, layout: str = "half", scaling: st
 _pack_heads = struct.Struct("PqqPPqii").pack  # deft_heads_t
 
 
-def _heads(t, n, d, index, what: str, name: str):
+def _heads(t, n, d, index, bf16, what: str, name: str):
     """(address, strides, number of heads) of bf16 [n, heads, d]."""
-    if t.dtype != _torch.bfloat16 or t.dim() != 3 or t.get_device() != index:
-        raise DeftError(-1, f"{what}: {name} must be a 3-d bf16 tensor on one device with the others (there is no CPU path)")
-    n2, heads, d2 = t.shape
+    shape = t.shape
+    if t.dtype is not bf16 or len(shape) != 3 or t.get_device() != index or index < 0:
+        raise DeftError(-1, f"{what}: {name} must be a 3-d bf16 tensor, on one device with the others (there is no CPU path)")
+    n2, heads, d2 = shape
     if n2 != n or d2 != d or heads >= 1 << 31:
         raise DeftError(-1, f"{what}: {name} must be [{n}, heads, {d}]")
     token, head, one = t.stride()
@@ -944,14 +945,18 @@ def _heads(t, n, d, index, what: str, name: str):
     return t.data_ptr(), token if n > 1 else heads * d, head if heads > 1 else d, heads  # (one token's or head's stride says nothing)
 
 
-def _heads_out(out, t, at, raw, index, here, what: str, name: str):
+def _heads_out(out, t, at, bf16, raw, index, elsewhere, what: str, name: str):
     """(a result for the heads t, made if none is given; its address)"""
-    shape = t.shape
-    if out is None:
-        out = _torch.empty(shape, dtype=_torch.bfloat16, device=t.device) if here else _result(raw, index, shape, _torch.bfloat16)
+    if out is None:  # (see deft_tree_attn_decode)
+        if elsewhere:
+            out = _result(raw, index, t.shape, bf16)
+        elif type(t) is _torch.Tensor:
+            out = _torch.empty_like(t, memory_format=_torch.contiguous_format)
+        else:
+            out = _torch.empty(t.shape, dtype=bf16, device=t.device)
         return out, out.data_ptr()
-    if out.dtype != _torch.bfloat16 or out.shape != shape or out.get_device() != index:
-        raise DeftError(-1, f"{what}: {name} must be bf16 {list(shape)}, on the input's device")
+    if out.dtype is not bf16 or out.shape != t.shape or out.get_device() != index:
+        raise DeftError(-1, f"{what}: {name} must be bf16 {list(t.shape)}, on the input's device")
     p = out.data_ptr()
     if not out.is_contiguous() if p != at else not _alike(out, t):
         raise DeftError(-1, f"{what}: {name} must be contiguous, or the input itself")
@@ -963,26 +968,26 @@ def _alike(a, b) -> bool:
     return a.numel() == 0 or all(n == 1 or x == y for n, x, y in zip(a.shape, a.stride(), b.stride()))
 
 
-def _head_weight(w, heads, d, index, what: str, name: str):
+def _head_weight(w, heads, d, index, bf16, what: str, name: str):
     """(address, stride of heads, whether float) of a norm's weights, [d] or [heads, d]."""
-    if w is None:
-        return None, 0, 0
-    wide = w.dtype == _torch.float32
-    shape = w.shape
-    if not (wide or w.dtype == _torch.bfloat16) or w.get_device() != index or not w.is_contiguous() or (shape != (d,) and shape != (heads, d)):
+    dtype, shape = w.dtype, w.shape
+    if (dtype is not bf16 and dtype is not _torch.float32) or w.get_device() != index or not w.is_contiguous() or (shape != (d,) and shape != (heads, d)):
         raise DeftError(-1, f"{what}: {name} must be a contiguous bf16 or float32 [{d}] or [{heads}, {d}] tensor on the input's device")
-    return w.data_ptr(), 0 if len(shape) == 1 else d, wide
+    return w.data_ptr(), 0 if len(shape) == 1 else d, dtype is not bf16
 
 
-def _positions(positions, n, rope, index, what: str):
-    """Address of the positions where there is a rope."""
+_NO_WEIGHT = 0, 0, 0
+
+
+def _turn(positions, rope, n, index, what: str):
+    """(address of the positions, a deft_rope_t), or twice None without a rope."""
     if rope is None:
         if positions is not None:
             raise DeftError(-1, f"{what}: positions say nothing without a rope")
-        return None
-    if positions is None or positions.dtype != _torch.int32 or positions.shape != (n,) or positions.get_device() != index or not positions.is_contiguous():
+        return None, None
+    if positions is None or positions.dtype is not _torch.int32 or positions.shape != (n,) or positions.get_device() != index or not positions.is_contiguous():
         raise DeftError(-1, f"{what}: positions must be a contiguous int32 [{n}] tensor on the input's device")
-    return positions.data_ptr() or 4  # (of none: anything)
+    return positions.data_ptr() or 4, rope.packed  # (of none: anything)
 
 
 def deft_rotate(x, positions, rope: Rope, out=None, stream=None):
@@ -990,20 +995,19 @@ def deft_rotate(x, positions, rope: Rope, out=None, stream=None):
     int32 [n].  Returns bf16 [n, H, d]; out=x turns them in place.  Asynchronous on `stream` (default: torch's current stream); the
     current stream has to wait for another one before it reads the result."""
     torch = _torch or _get_torch()
-    index = x.get_device()
+    index, bf16 = x.get_device(), torch.bfloat16
     if x.dim() != 3 or rope is None:
         raise DeftError(-1, "deft_rotate: x must be a 3-d tensor, and a rope be given")
     n, _, d = x.shape
-    at, token, head, H = _heads(x, n, d, index, "deft_rotate", "x")
-    if index < 0:
-        raise DeftError(-1, "deft_rotate: x must be a device tensor (there is no CPU path)")
-    pos = _positions(positions, n, rope, index, "deft_rotate")
+    at, token, head, H = _heads(x, n, d, index, bf16, "deft_rotate", "x")
+    pos, packed = _turn(positions, rope, n, index, "deft_rotate")
     raw = _raw_stream(stream, index)
-    out, to = _heads_out(out, x, at, raw, index, stream is None or raw == torch._C._cuda_getCurrentRawStream(index), "deft_rotate", "out")
-    if _elsewhere(index):
+    elsewhere = stream is not None and raw != torch._C._cuda_getCurrentRawStream(index)
+    out, to = _heads_out(out, x, at, bf16, raw, index, elsewhere, "deft_rotate", "out")
+    if torch._C._cuda_getDevice() != index:
         with torch.cuda.device(index):
             return deft_rotate(x, positions, rope, out, raw)
-    rc = (_lib or load_library()).deft_rotate(_pack_heads(at, token, head, to, 0, 0, 0, H), n, d, pos, rope.packed, raw)
+    rc = (_lib or load_library()).deft_rotate(_pack_heads(at, token, head, to, 0, 0, 0, H), n, d, pos, packed, raw)
     if rc != 0:
         _check(rc, "deft_rotate")
     return out
@@ -1016,27 +1020,27 @@ def deft_qk_norm_rotate(q, k, q_weight=None, k_weight=None, positions=None, rope
     every head; without one (None) there is no norm, without a rope no rotation.  Returns (q, k), bf16; q_out and k_out may be the
     inputs themselves.  Otherwise as deft_rotate."""
     torch = _torch or _get_torch()
-    what, index = "deft_qk_norm_rotate", q.get_device()
-    if q.dim() != 3 or index < 0:
-        raise DeftError(-1, "deft_qk_norm_rotate: q must be a 3-d device tensor (there is no CPU path)")
+    what, index, bf16 = "deft_qk_norm_rotate", q.get_device(), torch.bfloat16
+    if q.dim() != 3:
+        raise DeftError(-1, "deft_qk_norm_rotate: q must be a 3-d tensor")
     n, _, d = q.shape
-    q_at, q_token, q_head, Hq = _heads(q, n, d, index, what, "q")
-    k_at, k_token, k_head, Hkv = _heads(k, n, d, index, what, "k")
-    qw, qw_head, q_wide = _head_weight(q_weight, Hq, d, index, what, "q_weight")
-    kw, kw_head, k_wide = _head_weight(k_weight, Hkv, d, index, what, "k_weight")
-    if qw and kw and q_wide != k_wide:
+    q_at, q_token, q_head, Hq = _heads(q, n, d, index, bf16, what, "q")
+    k_at, k_token, k_head, Hkv = _heads(k, n, d, index, bf16, what, "k")
+    qw, qw_head, q_wide = _NO_WEIGHT if q_weight is None else _head_weight(q_weight, Hq, d, index, bf16, what, "q_weight")
+    kw, kw_head, k_wide = _NO_WEIGHT if k_weight is None else _head_weight(k_weight, Hkv, d, index, bf16, what, "k_weight")
+    if q_wide != k_wide and qw and kw:
         raise DeftError(-1, "deft_qk_norm_rotate: weights must be of one type")
-    pos = _positions(positions, n, rope, index, what)
+    pos, packed = _turn(positions, rope, n, index, what)
     raw = _raw_stream(stream, index)
-    here = stream is None or raw == torch._C._cuda_getCurrentRawStream(index)
-    q_out, q_to = _heads_out(q_out, q, q_at, raw, index, here, what, "q_out")
-    k_out, k_to = _heads_out(k_out, k, k_at, raw, index, here, what, "k_out")
-    if _elsewhere(index):
+    elsewhere = stream is not None and raw != torch._C._cuda_getCurrentRawStream(index)
+    q_out, q_to = _heads_out(q_out, q, q_at, bf16, raw, index, elsewhere, what, "q_out")
+    k_out, k_to = _heads_out(k_out, k, k_at, bf16, raw, index, elsewhere, what, "k_out")
+    if torch._C._cuda_getDevice() != index:
         with torch.cuda.device(index):
             return deft_qk_norm_rotate(q, k, q_weight, k_weight, positions, rope, eps, weight_offset, q_out, k_out, raw)
     rc = (_lib or load_library()).deft_qk_norm_rotate(
-        _pack_heads(q_at, q_token, q_head, q_to, qw or 0, qw_head, q_wide, Hq), _pack_heads(k_at, k_token, k_head, k_to, kw or 0, kw_head, k_wide, Hkv),
-        n, d, eps, weight_offset, pos, None if rope is None else rope.packed, raw)
+        _pack_heads(q_at, q_token, q_head, q_to, qw, qw_head, q_wide, Hq), _pack_heads(k_at, k_token, k_head, k_to, kw, kw_head, k_wide, Hkv), n, d, eps,
+        weight_offset, pos, packed, raw)
     if rc != 0:
         _check(rc, what)
     return q_out, k_out
@@ -1049,47 +1053,48 @@ def deft_qkv_store(rows: KVList, q, k, v, cache, positions=None, rope=None, q_we
     [n_rows, Hkv, d].  q may be None.  Returns the queries, bf16 [n, Hq, d].  Otherwise as deft_qk_norm_rotate.  (An 8-bit cache
     takes deft_qk_norm_rotate and deft_kv_store_q8.)"""
     torch = _torch or _get_torch()
-    what, index = "deft_qkv_store", k.get_device()
-    if type(cache) is CacheQ8 or len(cache) != 2:
+    what, index, bf16 = "deft_qkv_store", k.get_device(), torch.bfloat16
+    if len(cache) != 2:
         raise DeftError(-1, "deft_qkv_store: cache must be the K and V pools of a bf16 cache (deft_kv_store_q8 stores into one of 8 bits)")
     if rows.block_rows == 0:
         raise DeftError(-1, "deft_qkv_store: the list is one of copies, not of rows")
-    if k.dim() != 3 or index < 0:
-        raise DeftError(-1, "deft_qkv_store: k must be a 3-d device tensor (there is no CPU path)")
+    if k.dim() != 3:
+        raise DeftError(-1, "deft_qkv_store: k must be a 3-d tensor")
     n, _, d = k.shape
     if n != rows.n:
         raise DeftError(-1, f"deft_qkv_store: the list has {rows.n} rows, not {n}")
-    k_at, k_token, k_head, Hkv = _heads(k, n, d, index, what, "k")
-    v_at, v_token, v_head, Hv = _heads(v, n, d, index, what, "v")
+    k_at, k_token, k_head, Hkv = _heads(k, n, d, index, bf16, what, "k")
+    v_at, v_token, v_head, Hv = _heads(v, n, d, index, bf16, what, "v")
     k_pool, v_pool = cache
-    shape, bf16 = k_pool.shape, torch.bfloat16
-    if (Hv != Hkv or len(shape) != 3 or shape[1] != Hkv or shape[2] != d or v_pool.shape != shape or not k_pool.dtype == v_pool.dtype == bf16
-            or not (k_pool.is_contiguous() and v_pool.is_contiguous()) or not k_pool.get_device() == v_pool.get_device() == index):
+    shape = k_pool.shape
+    if (Hv != Hkv or len(shape) != 3 or shape[1] != Hkv or shape[2] != d or v_pool.shape != shape or k_pool.dtype is not bf16 or v_pool.dtype is not bf16
+            or not (k_pool.is_contiguous() and v_pool.is_contiguous()) or k_pool.get_device() != index or v_pool.get_device() != index):
         raise DeftError(-1, f"deft_qkv_store: the pools must both be contiguous bf16 [n_rows, {Hkv}, {d}] tensors on the heads' device")
     n_rows = shape[0]
     if rows.pool > n_rows or n_rows >= 1 << 31:
         raise DeftError(-1, "deft_qkv_store: the list is for a larger cache, or the cache larger than 32 bits hold")
     raw = _raw_stream(stream, index)
-    kw, kw_head, wide = _head_weight(k_weight, Hkv, d, index, what, "k_weight")
+    kw, kw_head, wide = _NO_WEIGHT if k_weight is None else _head_weight(k_weight, Hkv, d, index, bf16, what, "k_weight")
     q_heads = None
     if q is not None:
-        q_at, q_token, q_head, Hq = _heads(q, n, d, index, what, "q")
-        qw, qw_head, q_wide = _head_weight(q_weight, Hq, d, index, what, "q_weight")
-        if qw and kw and q_wide != wide:
+        q_at, q_token, q_head, Hq = _heads(q, n, d, index, bf16, what, "q")
+        qw, qw_head, q_wide = _NO_WEIGHT if q_weight is None else _head_weight(q_weight, Hq, d, index, bf16, what, "q_weight")
+        if q_wide != wide and qw and kw:
             raise DeftError(-1, "deft_qkv_store: weights must be of one type")
-        q_out, to = _heads_out(q_out, q, q_at, raw, index, stream is None or raw == torch._C._cuda_getCurrentRawStream(index), what, "q_out")
-        q_heads = _pack_heads(q_at, q_token, q_head, to, qw or 0, qw_head, q_wide, Hq)
+        elsewhere = stream is not None and raw != torch._C._cuda_getCurrentRawStream(index)
+        q_out, to = _heads_out(q_out, q, q_at, bf16, raw, index, elsewhere, what, "q_out")
+        q_heads = _pack_heads(q_at, q_token, q_head, to, qw, qw_head, q_wide, Hq)
     elif q_weight is not None or q_out is not None:
         raise DeftError(-1, "deft_qkv_store: without q it has neither weights nor a result")
-    pos = _positions(positions, n, rope, index, what)
+    pos, packed = _turn(positions, rope, n, index, what)
     if n == 0:
         return q_out
-    if _elsewhere(index):
+    if torch._C._cuda_getDevice() != index:
         with torch.cuda.device(index):
             return deft_qkv_store(rows, q, k, v, cache, positions, rope, q_weight, k_weight, eps, weight_offset, q_out, raw)
     rc = (_lib or load_library()).deft_qkv_store(
-        rows._h, rows._image(index, raw).data_ptr(), q_heads, _pack_heads(k_at, k_token, k_head, k_pool.data_ptr(), kw or 0, kw_head, wide, Hkv),
-        _pack_heads(v_at, v_token, v_head, v_pool.data_ptr(), 0, 0, 0, Hkv), n_rows, d, eps, weight_offset, pos, None if rope is None else rope.packed, raw)
+        rows._h, rows._image(index, raw).data_ptr(), q_heads, _pack_heads(k_at, k_token, k_head, k_pool.data_ptr(), kw, kw_head, wide, Hkv),
+        _pack_heads(v_at, v_token, v_head, v_pool.data_ptr(), 0, 0, 0, Hkv), n_rows, d, eps, weight_offset, pos, packed, raw)
     if rc != 0:
         _check(rc, what)
     return q_out
@@ -1159,8 +1164,12 @@ def deft_adjust_logits(plan: Plan, logits, tokens=None, repetition=None, frequen
     raw = _raw_stream(stream, index)
     if out is None:
         dtype = out_dtype or logits.dtype
-        here = stream is None or raw == torch._C._cuda_getCurrentRawStream(index)
-        out = torch.empty(shape, dtype=dtype, device=logits.device) if here else _result(raw, index, shape, dtype)
+        if stream is not None and raw != torch._C._cuda_getCurrentRawStream(index):
+            out = _result(raw, index, shape, dtype)
+        elif out_dtype is None and type(logits) is torch.Tensor:  # (see deft_tree_attn_decode)
+            out = torch.empty_like(logits, memory_format=torch.contiguous_format)
+        else:
+            out = torch.empty(shape, dtype=dtype, device=logits.device)
     elif out.shape != shape or out.get_device() != index or (vocab > 1 and out.stride(1) != 1):
         raise DeftError(-1, "deft_adjust_logits: out must be like the logits, with contiguous rows")
     out_wide = out.dtype == f32

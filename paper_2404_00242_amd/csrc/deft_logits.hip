@@ -53,6 +53,7 @@ constexpr int kTile = 1024;       // logits of a row to a workgroup
 constexpr int kMost = 8;          // rows to a workgroup: as many as a thread can have in flight in registers
 constexpr int kStage = 512;      // pieces or groups at a time
 constexpr uint32_t kEach = kTile / kThreads, kStretches = kStage / kThreads;  // to a thread
+static_assert(kEach == 2, "a row ends behind a thread's logits, or behind the first of them");
 constexpr int kSortThreads = 1024;
 constexpr int kRun = 1024;        // tokens that deft_sort_tokens takes to a workgroup
 constexpr int kMaxTiles = 2048;   // that it sorts by
@@ -85,15 +86,15 @@ __device__ __forceinline__ void put(T *p, const float *x) {
 // Queries are in the plan's depth-first order here, in which the queries whose path holds a token are neighbours: `bits` says which
 // of the workgroup's queries they are.  With COUNTS a token adds one at the first of them and takes one away behind the last, so
 // that the sum over the queries up to one is how often the token stands on that one's path.
-template <bool COUNTS>
+template <bool COUNTS, int MOST>
 struct Seen {
     uint32_t any[kTile];                        // bit q: on the path of query q
     uint32_t generated[COUNTS ? 4 : kTile];     // the same, prompt tokens left out
-    int32_t change[COUNTS ? kMost : 1][COUNTS ? kTile : 4];
+    int32_t change[COUNTS ? MOST : 1][COUNTS ? kTile : 4];
 };
 
-template <bool COUNTS>
-__device__ __forceinline__ void see(Seen<COUNTS> &seen, int32_t token, uint32_t first, uint32_t bits, uint32_t block) {
+template <bool COUNTS, int MOST>
+__device__ __forceinline__ void see(Seen<COUNTS, MOST> &seen, int32_t token, uint32_t first, uint32_t bits, uint32_t block) {
     const uint32_t at = ((uint32_t)token & (DEFT_TOKEN_PROMPT - 1)) - first;
     if (token < 0 || at >= kTile) return;
     if ((seen.any[at] & bits) != bits) atomicOr(&seen.any[at], bits);
@@ -255,27 +256,41 @@ __global__ __launch_bounds__(kSortThreads) void deft_sort_tokens(Pieces p, Sorte
 // A workgroup has kTile logits of `block` queries.  It first looks which of those tokens stand on the queries' paths: pieces of the
 // tree that any of its queries sees, or the sorted tokens of its tile, are taken kStage stretches at a time into LDS, with the sum
 // of their lengths in front of each, and every thread finds the stretch of its next token there by bisection.
-template <typename I, typename O, bool COUNTS, bool SORTED>
+template <typename I, typename O, bool COUNTS, bool SORTED, int MOST>
 __global__ __launch_bounds__(kThreads) void deft_logits(LogitsArgs a) {
-    __shared__ __align__(16) Seen<COUNTS> seen;
+    __shared__ __align__(16) Seen<COUNTS, MOST> seen;
     __shared__ uint32_t before[kStage], bits[SORTED ? 1 : kStage], part[kThreads / 64][2];
     __shared__ int32_t begin[kStage];  // of a stretch, less `before`
     const uint32_t blocks = gridDim.x / a.tiles, tile = blockIdx.x / blocks, q0 = blockIdx.x % blocks * a.block, block = min(a.block, a.nq - q0);
     const uint32_t first = tile * kTile, t = threadIdx.x, mine = kEach * t, v = first + mine;
     const uint32_t n = v < a.vocab ? min(a.vocab - v, kEach) : 0;
-    // Everything that does not wait for the tokens is asked for at once.  Queries behind the last are that one.
-    uint32_t row[kMost];
-    float repetition[kMost], frequency[kMost], presence[kMost];
-    int32_t bias[kMost], mask[kMost];  // rows of the tables
-    float x[kMost][kEach];
-    uint32_t word[kMost];
+    // What the first look at the tokens waits for is asked for first, and behind it all that does not wait for them.
+    u32x4 stretch[kStretches];  // its length, where it begins, and the queries that see it
+    auto look = [&](uint32_t s0) {
 #pragma unroll
-    for (uint32_t q = 0; q < kMost; ++q) {
+        for (uint32_t i = 0; i < kStretches; ++i) {
+            const uint32_t s = min(s0 + kStretches * t + i, a.history - 1);
+            if constexpr (SORTED) {
+                const uint32_t *from = a.sorted.table + (uint64_t)tile * a.sorted.groups + s;
+                const u32x2 seen_by = a.sorted.seen_by[s];
+                stretch[i] = u32x4{from[a.sorted.groups], from[0], seen_by[0], seen_by[1]};
+            } else {
+                stretch[i] = u32x4{(uint32_t)a.pieces.len[s], (uint32_t)a.pieces.begin[s], (uint32_t)a.pieces.qlo[s], (uint32_t)a.pieces.qhi[s]};
+            }
+        }
+    };
+    if (a.history) look(0);
+    // Queries behind the last are that one.
+    uint32_t row[MOST];
+    float repetition[MOST], frequency[MOST], presence[MOST];
+    int32_t bias[MOST], mask[MOST];  // rows of the tables
+#pragma unroll
+    for (uint32_t q = 0; q < MOST; ++q) {
         const uint32_t at = q0 + min(q, block - 1);
         row[q] = a.q_order ? (uint32_t)uniform(a.q_order, at) : at;
     }
 #pragma unroll
-    for (uint32_t q = 0; q < kMost; ++q) {
+    for (uint32_t q = 0; q < MOST; ++q) {
         mask[q] = !a.mask ? -1 : a.mask_row ? uniform(a.mask_row, row[q]) : 0;
         if ((uint32_t)mask[q] >= a.n_masks) mask[q] = -1;
         bias[q] = !a.bias ? -1 : a.bias_row ? uniform(a.bias_row, row[q]) : 0;
@@ -284,45 +299,34 @@ __global__ __launch_bounds__(kThreads) void deft_logits(LogitsArgs a) {
         frequency[q] = COUNTS ? uniform(a.frequency, row[q]) : 0.f;
         presence[q] = a.presence ? uniform(a.presence, row[q]) : 0.f;
     }
+    float x[MOST][kEach];
+    uint32_t word[MOST];
+    const I *logits = static_cast<const I *>(a.logits) + v;
     if (n == kEach) {
 #pragma unroll
-        for (uint32_t q = 0; q < kMost; ++q) get<I, kEach>(static_cast<const I *>(a.logits) + (int64_t)row[q] * a.stride + v, x[q]);
-    } else {
-        for (uint32_t i = 0; i < n; ++i)
+        for (uint32_t q = 0; q < MOST; ++q) get<I, kEach>(logits + (int64_t)row[q] * a.stride, x[q]);
+    } else if (n) {
 #pragma unroll
-            for (uint32_t q = 0; q < kMost; ++q) {
-                const float y = (float)static_cast<const I *>(a.logits)[(int64_t)row[q] * a.stride + v + i];
-#pragma unroll
-                for (uint32_t k = 0; k < kEach; ++k) x[q][k] = k == i ? y : x[q][k];
-            }
+        for (uint32_t q = 0; q < MOST; ++q) get<I, 1>(logits + (int64_t)row[q] * a.stride, x[q]);
     }
     if (a.mask && n) {
 #pragma unroll
-        for (uint32_t q = 0; q < kMost; ++q) word[q] = a.mask[(int64_t)max(mask[q], 0) * a.mask_stride + v / 32];
+        for (uint32_t q = 0; q < MOST; ++q) word[q] = a.mask[(int64_t)max(mask[q], 0) * a.mask_stride + v / 32] >> (v % 32);
     }
     static_assert(sizeof(seen) % 16 == 0, "cleared in 128-bit words");
     for (uint32_t i = t; i < sizeof(seen) / 16; i += kThreads) reinterpret_cast<u32x4 *>(&seen)[i] = u32x4{0, 0, 0, 0};
     for (uint32_t s0 = 0; s0 < a.history; s0 += kStage) {
+        if (s0) look(s0);
         uint32_t len[kStretches], on[kStretches], sum = 0, many = 0;
         int32_t at[kStretches];
 #pragma unroll
         for (uint32_t i = 0; i < kStretches; ++i) {
             const uint32_t s = s0 + kStretches * t + i;
-            len[i] = on[i] = 0;
-            at[i] = 0;
-            if (s < a.history) {
-                if constexpr (SORTED) {
-                    const uint32_t *from = a.sorted.table + (uint64_t)tile * a.sorted.groups + s;
-                    const u32x2 seen_by = a.sorted.seen_by[s];
-                    const uint32_t lo = from[0], many = from[a.sorted.groups] - lo;
-                    len[i] = on[i] = seen_by[0] < q0 + block && seen_by[1] > q0 ? many : 0;
-                    at[i] = (int32_t)(s * kRun + lo);
-                } else {
-                    on[i] = bits_of(a.pieces.qlo[s], a.pieces.qhi[s], q0, block);
-                    len[i] = on[i] ? (uint32_t)a.pieces.len[s] : 0;
-                    at[i] = a.pieces.begin[s];
-                }
-            }
+            on[i] = s < a.history ? bits_of((int32_t)stretch[i][2], (int32_t)stretch[i][3], q0, block) : 0;
+            len[i] = SORTED ? stretch[i][0] - stretch[i][1] : stretch[i][0];
+            if (SORTED && len[i] == 0) on[i] = 0;
+            if (!on[i]) len[i] = 0;
+            at[i] = (int32_t)(SORTED ? s * kRun + stretch[i][1] : stretch[i][1]);
             sum += len[i];
             many += on[i] != 0;
             before[kThreads * i + t] = 0xffffffffu;
@@ -370,7 +374,7 @@ __global__ __launch_bounds__(kThreads) void deft_logits(LogitsArgs a) {
         generated[i] = COUNTS ? 0 : seen.generated[mine + i];
     }
 #pragma unroll
-    for (uint32_t q = 0; q < kMost; ++q) {
+    for (uint32_t q = 0; q < MOST; ++q) {
         if (q >= block) break;
         const float inverse = 1.f / repetition[q];
 #pragma unroll
@@ -384,40 +388,42 @@ __global__ __launch_bounds__(kThreads) void deft_logits(LogitsArgs a) {
             }
         }
         if (bias[q] >= 0) {
-            const float *b = a.bias + (int64_t)bias[q] * a.bias_stride + v;
-            float y[kEach] = {};
+            const float *from = a.bias + (int64_t)bias[q] * a.bias_stride + v;
+            float y[kEach];
             if (n == kEach)
-                get<float, kEach>(b, y);
+                get<float, kEach>(from, y);
             else
-                for (uint32_t i = 0; i < n; ++i) {
-                    const float z = b[i];
-#pragma unroll
-                    for (uint32_t k = 0; k < kEach; ++k) y[k] = k == i ? z : y[k];
-                }
+                get<float, 1>(from, y);
 #pragma unroll
             for (uint32_t i = 0; i < kEach; ++i) x[q][i] += y[i];
         }
         if (mask[q] >= 0) {
 #pragma unroll
             for (uint32_t i = 0; i < kEach; ++i)
-                if (!((word[q] >> (v % 32 + i)) & 1)) x[q][i] = -__builtin_inff();
+                if (!((word[q] >> i) & 1)) x[q][i] = -__builtin_inff();
         }
         O *to = static_cast<O *>(a.out) + (int64_t)row[q] * a.out_stride + v;
-        if (n == kEach) {
+        if (n == kEach)
             put<O, kEach>(to, x[q]);
-        } else {
-#pragma unroll
-            for (uint32_t i = 0; i < kEach; ++i)
-                if (i < n) to[i] = (O)x[q][i];
-        }
+        else
+            put<O, 1>(to, x[q]);
     }
 }
 
+template <typename I, typename O, int MOST>
+void launch(const LogitsArgs &a, bool counts, bool sorted, uint32_t groups, hipStream_t st) {
+    auto *kernel = counts ? (sorted ? &deft_logits<I, O, true, true, MOST> : &deft_logits<I, O, true, false, MOST>)
+                          : (sorted ? &deft_logits<I, O, false, true, MOST> : &deft_logits<I, O, false, false, MOST>);
+    hipLaunchKernelGGL(kernel, dim3(groups), dim3(kThreads), 0, st, a);
+}
 template <typename I, typename O>
 void launch(const LogitsArgs &a, bool counts, bool sorted, uint32_t groups, hipStream_t st) {
-    auto *kernel = counts ? (sorted ? &deft_logits<I, O, true, true> : &deft_logits<I, O, true, false>)
-                          : (sorted ? &deft_logits<I, O, false, true> : &deft_logits<I, O, false, false>);
-    hipLaunchKernelGGL(kernel, dim3(groups), dim3(kThreads), 0, st, a);
+    if (a.block == 1)
+        launch<I, O, 1>(a, counts, sorted, groups, st);
+    else if (a.block <= kMost / 2)
+        launch<I, O, kMost / 2>(a, counts, sorted, groups, st);
+    else
+        launch<I, O, kMost>(a, counts, sorted, groups, st);
 }
 
 // Tokens of all pieces, a query's own time and again where pieces are grouped by query.
