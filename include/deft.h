@@ -479,7 +479,7 @@ int deft_rope(const double *frequency, int32_t rot, int32_t layout, double facto
 
 /*
  * deft_rotate turns heads (which have no weight).  deft_qk_norm_rotate normalises those of q and k that have a weight and turns both;
- * q or k may be NULL, and rope and positions both NULL: nothing is turned then.
+ * q or k may be NULL, and so may rope: nothing is turned then, and positions are not looked at.
  *
  * deft_qkv_store does the same and stores keys and values into a bf16 cache of n_rows rows, token i into row rows[i] of the list
  * (deft_kv_rows; its blocks have no part in it): k->out and v->out are the K and V pools [n_rows, Hkv, d].  Values are copied bit for

@@ -980,10 +980,8 @@ _NO_WEIGHT = 0, 0, 0
 
 
 def _turn(positions, rope, n, index, what: str):
-    """(address of the positions, a deft_rope_t), or twice None without a rope."""
+    """(address of the positions, a deft_rope_t), or twice None without a rope: positions are not looked at then."""
     if rope is None:
-        if positions is not None:
-            raise DeftError(-1, f"{what}: positions say nothing without a rope")
         return None, None
     if positions is None or positions.dtype is not _torch.int32 or positions.shape != (n,) or positions.get_device() != index or not positions.is_contiguous():
         raise DeftError(-1, f"{what}: positions must be a contiguous int32 [{n}] tensor on the input's device")
@@ -1017,7 +1015,7 @@ def deft_qk_norm_rotate(q, k, q_weight=None, k_weight=None, positions=None, rope
                         q_out=None, k_out=None, stream=None):
     """RMS norm of every head of q [n, Hq, d] and k [n, Hkv, d], and rotation by the tokens' positions, in one pass: a head becomes
     head * (weight + weight_offset) / sqrt(mean(head^2) + eps), turned.  Weights: bf16 or float32 (both alike), [d] or a row for
-    every head; without one (None) there is no norm, without a rope no rotation.  Returns (q, k), bf16; q_out and k_out may be the
+    every head; without one (None) there is no norm, without a rope no rotation (of some layers: positions may be given all the same).  Returns (q, k), bf16; q_out and k_out may be the
     inputs themselves.  Otherwise as deft_rotate."""
     torch = _torch or _get_torch()
     what, index, bf16 = "deft_qk_norm_rotate", q.get_device(), torch.bfloat16

@@ -87,9 +87,9 @@ __device__ __forceinline__ void load8(const void *p, uint32_t at, bool wide, flo
     }
 }
 
-// A wave has one token and 64 / (D / 16) of its heads, sixteen elements of a head to a lane: two groups of eight that are partners of
-// one another in the half layout, so that no lane needs another's elements (interleaved pairs lie within a group).  The angles of a
-// token are the same for all its heads: a lane makes one pair's cosine and sine, and the wave's LDS hands them round.
+// A wave has one token and 64 / (D / 16) of its heads, sixteen elements of a head to a lane: two groups of eight that in the half layout
+// are partners of one another, so that no lane needs another's elements.  The angles of a token are the same for all its heads: a
+// lane makes one pair's cosine and sine, and the wave's LDS hands them round.
 template <int D, int TURN, bool NORM>
 __global__ __launch_bounds__(256) void deft_heads(HeadsArgs a) {
     constexpr uint32_t kLanes = D / 16, kHeads = 64 / kLanes;
@@ -108,8 +108,11 @@ __global__ __launch_bounds__(256) void deft_heads(HeadsArgs a) {
     const int kind = at >= a.v_begin ? kV : at >= a.k_begin ? kK : kQ;
     const Part &p = a.part[kind];
     const uint32_t head = at - (kind == kV ? a.v_begin : kind == kK ? a.k_begin : 0);
-    const bool turned = TURN != kNoTurn && kind != kV && 16 * j < a.rot;
-    const uint32_t first = turned ? 8 * j : 16 * j, second = turned ? a.rot / 2 + 8 * j : 16 * j + 8;
+    // the lane's two groups: interleaved anywhere in the head, in the half layout partners, and of the elements that do not turn the same
+    const bool turned = TURN == kHalf && kind != kV && 16 * j < a.rot;
+    const uint32_t begin = turned || TURN != kHalf || kind == kV ? 0 : a.rot, width = turned ? a.rot : D - begin;
+    const uint32_t first = begin + 8 * (j - begin / 16), second = first + width / 2;
+    const bool turned0 = TURN == kInterleaved ? kind != kV && first < a.rot : turned, turned1 = TURN == kInterleaved ? kind != kV && second < a.rot : turned;
     const uint16_t *x = p.x + ((int64_t)token * p.token + (int64_t)head * p.head);
     const u32x4 x0 = *reinterpret_cast<const u32x4 *>(x + first), x1 = *reinterpret_cast<const u32x4 *>(x + second);
     float (*cs)[64] = table[wave];
@@ -162,31 +165,36 @@ __global__ __launch_bounds__(256) void deft_heads(HeadsArgs a) {
             }
         }
     }
-    if (turned) {
-        const uint32_t i0 = TURN == kHalf ? 8 * j : 4 * j, i1 = TURN == kHalf ? 8 * j + 4 : a.rot / 4 + 4 * j;
-        const f32x4 c0 = *reinterpret_cast<const f32x4 *>(&cs[0][i0]), c1 = *reinterpret_cast<const f32x4 *>(&cs[0][i1]);
-        const f32x4 s0 = *reinterpret_cast<const f32x4 *>(&cs[1][i0]), s1 = *reinterpret_cast<const f32x4 *>(&cs[1][i1]);
-        auto turn = [](float &u, float &v, float c, float s) {
-            const float t = u * c - v * s;
-            v = v * c + u * s;
-            u = t;
-        };
+    auto turn = [](float &u, float &v, float c, float s) {
+        const float t = u * c - v * s;
+        v = v * c + u * s;
+        u = t;
+    };
+    auto cosines = [&](uint32_t i) { return *reinterpret_cast<const f32x4 *>(&cs[0][i]); };
+    auto sines = [&](uint32_t i) { return *reinterpret_cast<const f32x4 *>(&cs[1][i]); };
+    if (TURN == kHalf && turned) {
+        const f32x4 c0 = cosines(first), c1 = cosines(first + 4), s0 = sines(first), s1 = sines(first + 4);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            if (TURN == kHalf) {
-                turn(y0[i], y1[i], c0[i], s0[i]);
-                turn(y0[4 + i], y1[4 + i], c1[i], s1[i]);
-            } else {
-                turn(y0[2 * i], y0[2 * i + 1], c0[i], s0[i]);
-                turn(y1[2 * i], y1[2 * i + 1], c1[i], s1[i]);
-            }
+            turn(y0[i], y1[i], c0[i], s0[i]);
+            turn(y0[4 + i], y1[4 + i], c1[i], s1[i]);
         }
     }
+    if (TURN == kInterleaved && turned0) {
+        const f32x4 c = cosines(first / 2), s = sines(first / 2);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) turn(y0[2 * i], y0[2 * i + 1], c[i], s[i]);
+    }
+    if (TURN == kInterleaved && turned1) {
+        const f32x4 c = cosines(second / 2), s = sines(second / 2);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) turn(y1[2 * i], y1[2 * i + 1], c[i], s[i]);
+    }
     if (asked >= a.heads) return;
-    const bool same = !turned && !normed;  // bits as they are
     uint16_t *out = p.out + ((int64_t)(kind == kQ ? token : row) * p.out_token + (int64_t)head * p.out_head);
-    *reinterpret_cast<u32x4 *>(out + first) = same ? x0 : pack8(y0);
-    *reinterpret_cast<u32x4 *>(out + second) = same ? x1 : pack8(y1);
+    // bits as they are where nothing is done to them; none of it is read again here
+    __builtin_nontemporal_store(turned0 || normed ? pack8(y0) : x0, reinterpret_cast<u32x4 *>(out + first));
+    __builtin_nontemporal_store(turned1 || normed ? pack8(y1) : x1, reinterpret_cast<u32x4 *>(out + second));
 }
 
 // ---- host ----
@@ -248,8 +256,7 @@ int run(const deft_heads_t *const (&parts)[kParts], int64_t n, int32_t d, float 
     if (n < 0 || (d != 64 && d != 128)) return DEFT_EINVAL;
     if (rope && (rope->rot < 16 || rope->rot > d || rope->rot % 16 || (rope->layout != DEFT_ROPE_HALF && rope->layout != DEFT_ROPE_INTERLEAVED)))
         return DEFT_EINVAL;
-    if ((rope != nullptr) != (positions != nullptr) && n > 0) return DEFT_EINVAL;
-    if (reinterpret_cast<uintptr_t>(positions) & 3) return DEFT_EINVAL;
+    if (rope && ((!positions && n > 0) || (reinterpret_cast<uintptr_t>(positions) & 3))) return DEFT_EINVAL;
     HeadsArgs a{};
     Area in[kParts], out[kParts];
     uint32_t begin[kParts + 1] = {};

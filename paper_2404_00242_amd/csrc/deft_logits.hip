@@ -58,7 +58,7 @@ constexpr int kSortThreads = 1024;
 constexpr int kRun = 1024;        // tokens that deft_sort_tokens takes to a workgroup
 constexpr int kMaxTiles = 2048;   // that it sorts by
 constexpr int kFewTokens = 5000;  // are looked through unsorted
-constexpr int kAhead = 2;         // tokens of a thread in flight
+constexpr int kAhead = 2;         // tokens of a thread at a time, side by side
 
 // A value that is the same for all lanes, by a scalar load.
 template <typename T>
@@ -259,7 +259,7 @@ __global__ __launch_bounds__(kSortThreads) void deft_sort_tokens(Pieces p, Sorte
 template <typename I, typename O, bool COUNTS, bool SORTED, int MOST>
 __global__ __launch_bounds__(kThreads) void deft_logits(LogitsArgs a) {
     __shared__ __align__(16) Seen<COUNTS, MOST> seen;
-    __shared__ uint32_t before[kStage], bits[SORTED ? 1 : kStage], part[kThreads / 64][2];
+    __shared__ uint32_t before[kStage + 1], bits[SORTED ? 1 : kStage], part[kThreads / 64][2];
     __shared__ int32_t begin[kStage];  // of a stretch, less `before`
     const uint32_t blocks = gridDim.x / a.tiles, tile = blockIdx.x / blocks, q0 = blockIdx.x % blocks * a.block, block = min(a.block, a.nq - q0);
     const uint32_t first = tile * kTile, t = threadIdx.x, mine = kEach * t, v = first + mine;
@@ -331,6 +331,7 @@ __global__ __launch_bounds__(kThreads) void deft_logits(LogitsArgs a) {
             many += on[i] != 0;
             before[kThreads * i + t] = 0xffffffffu;
         }
+        if (t == 0) before[kStage] = 0xffffffffu;
         Sums sums = sums_before<kThreads>(sum, many, part);
 #pragma unroll
         for (uint32_t i = 0; i < kStretches; ++i) {
@@ -343,21 +344,22 @@ __global__ __launch_bounds__(kThreads) void deft_logits(LogitsArgs a) {
         }
         __syncthreads();
         const uint32_t steps = sums.all_y > 1 ? 1u << (32 - __builtin_clz(sums.all_y - 1)) : 1;
-        for (uint32_t f0 = t; f0 < sums.all_x; f0 += kAhead * kThreads) {
+        for (uint32_t f = kAhead * t; f < sums.all_x; f += kAhead * kThreads) {
             uint32_t k[kAhead];
             u32x4 e[kAhead];
 #pragma unroll
-            for (uint32_t u = 0; u < kAhead; ++u) {
-                const uint32_t f = min(f0 + u * kThreads, sums.all_x - 1);
-                k[u] = last_not_above(before, steps, f);
+            for (uint32_t u = 0; u < kAhead; ++u) {  // (a stretch has a token at least)
+                k[u] = u == 0 ? last_not_above(before, steps, f) : k[u - 1] + (before[k[u - 1] + 1] <= f + u);
+                k[u] = min(k[u], sums.all_y - 1);
+                const uint32_t g = min(f + u, sums.all_x - 1);
                 if constexpr (SORTED)
-                    e[u] = a.sorted.events[(uint32_t)(begin[k[u]] + (int32_t)f)];
+                    e[u] = a.sorted.events[(uint32_t)(begin[k[u]] + (int32_t)g)];
                 else
-                    e[u][0] = (uint32_t)a.pieces.tokens[(int64_t)begin[k[u]] + f];
+                    e[u][0] = (uint32_t)a.pieces.tokens[(int64_t)begin[k[u]] + g];
             }
 #pragma unroll
             for (uint32_t u = 0; u < kAhead; ++u) {
-                if (f0 + u * kThreads >= sums.all_x) break;
+                if (f + u >= sums.all_x) break;
                 const uint32_t which = SORTED ? bits_of((int32_t)e[u][1], (int32_t)e[u][2], q0, block) : bits[k[u]];
                 if (which) see(seen, (int32_t)e[u][0], first, which, block);
             }

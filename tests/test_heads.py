@@ -104,7 +104,7 @@ def test_calls_that_are_refused():
         return lib.deft_qk_norm_rotate(q, k, n, d, eps, offset, positions, rope, None)
 
     q = _part(weight=1 << 12)
-    for bad in (dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf")), dict(offset=float("nan")), dict(rope=None), dict(positions=None), dict(d=32)):
+    for bad in (dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf")), dict(offset=float("nan")), dict(positions=None), dict(d=32)):
         assert norm(q, None, **bad) == EINVAL, bad
     for bad in (dict(weight=(1 << 12) + 4), dict(weight=1 << 12, step=4), dict(weight=1 << 12, step=-64), dict(weight=1 << 12, step=8192),
                 dict(weight=1 << 12, wide=1), dict(out=1 << 20), dict(out=(1 << 24) + 1024), dict(out=(1 << 20) + 1024)):
@@ -329,6 +329,15 @@ def test_store_puts_heads_into_their_rows(n, Hq, Hkv, d, rows, block, norm, asce
 
 
 @pytest.mark.gpu
+def test_positions_say_nothing_without_a_rope():
+    x, p = values(5, 6, 64, 1).to(dev()), on_gpu(positions(5))
+    w = torch.rand(64, device=dev())
+    for a, b in zip(binding.deft_qk_norm_rotate(x[:, :4], x[:, 4:], w, None, p), binding.deft_qk_norm_rotate(x[:, :4], x[:, 4:], w, None)):
+        assert torch.equal(a, b)
+    assert torch.equal(b, x[:, 4:])
+
+
+@pytest.mark.gpu
 def test_nothing_to_do():
     rope, x = binding.deft_rope(64), torch.zeros((0, 4, 64), dtype=torch.bfloat16, device=dev())
     p = torch.zeros(0, dtype=torch.int32, device=dev())
@@ -379,7 +388,7 @@ def test_gpu_refusals():
         lambda: rotate(q, p, rope, out=k), lambda: rotate(q, p, rope, out=x.view(-1)[:n * 2 * d].view(n, 2, d)), lambda: rotate(q, p, rope, out=x.view(-1)[64:64 + n * 2 * d].view(n, 2, d)),
         lambda: rotate(x.view(-1)[4:4 + 2 * d].view(1, 2, d), p[:1], rope), lambda: rotate(x[:, :1].expand(n, 3, d), p, rope, out=x[:, :1].expand(n, 3, d)),
         lambda: norm(q, k, w, wide, p, rope), lambda: norm(q, k, w[:32], None, p, rope), lambda: norm(q, k, w.half(), None, p, rope), lambda: norm(q, k, w.cpu(), None, p, rope),
-        lambda: norm(q, k, w, w, p, None), lambda: norm(q, k, w, w, None, rope), lambda: norm(q, k, w, w, p, rope, eps=-1.0), lambda: norm(q, k, w.expand(3, d), w, p, rope),
+        lambda: norm(q, k, w, w, None, rope), lambda: norm(q, k, w, w, p, rope, eps=-1.0), lambda: norm(q, k, w.expand(3, d), w, p, rope),
         lambda: norm(q, k[:3], w, w, p, rope), lambda: norm(q, k.cpu(), w, w, p, rope), lambda: norm(q, q, w, w, p, rope, q_out=q, k_out=q),
         lambda: norm(q, k, w, w, p, rope, q_out=dense, k_out=dense), lambda: norm(dense, k, w, w, p, rope, k_out=dense),
         lambda: store(rows, q, k, v, cache, p, rope), lambda: store(rows, q, k, v, pools[:1], p, rope), lambda: store(rows, q, k, v, (pools[0], pools[0]), p, rope),
