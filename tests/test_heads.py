@@ -10,6 +10,7 @@ import torch
 
 from oracle import heads as model
 from paper_2404_00242_amd import binding
+from tests.test_upload_errors import fake, needs_gxx, run  # noqa: F401 (fake is a fixture)
 
 EINVAL = -1
 SCALINGS = [dict(), dict(scaling="linear", scale=4.0), dict(scaling="base", scale=8.0, base=500000.0),
@@ -134,6 +135,50 @@ def test_cpu_tensors_are_refused():
     for call in (lambda: binding.deft_rotate(x, p, rope), lambda: binding.deft_qk_norm_rotate(x, x), lambda: binding.deft_qkv_store(rows, x, x, x, (x, x))):
         with pytest.raises(binding.DeftError):
             call()
+
+
+# ---- many heads: more than a launch holds ----
+
+WAVES = 1 << 22  # of a launch, kMaxWaves in deft_heads.hip
+
+
+@needs_gxx
+@pytest.mark.parametrize("heads,d", [((65536, 65536, 65536), 128), ((65536, 1, 1), 64), ((40, 8, 8), 128)])
+def test_calls_of_any_length(fake, heads, d):  # noqa: F811
+    run(fake, f"""
+class Fake(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in names] + [("grid", ctypes.c_int32 * 16), ("kernel", ctypes.c_void_p * 16)]
+fake = Fake.in_dll(fake_lib, "fake")
+H, d = {heads}, {d}
+def part(i, out, heads):
+    return binding._pack_heads(1 << 50 + i, heads * d, d, out, 0, 0, 0, heads)
+def launched(n):
+    fake.launches = 0
+    pools = [part(i, (1 << 55) + (i << 53), H[i]) for i in range(3)]
+    lst = binding.deft_kv_rows(np.arange(n), n, 1)
+    assert lib.deft_qkv_store(lst.handle, 4096, *pools, n, d, 0.0, 0.0, 4096, binding.deft_rope(64).packed, 1 << 12) == 0
+    return list(fake.grid[:fake.launches])
+H = (H[0], H[1], H[1])
+chunks = -(-sum(H) // (64 // (d // 16)))
+most = {WAVES} // chunks
+for n, want in ((1, [1]), (most, [most]), (most + 1, [most, 1]), (2 * most + 3, [most, most, 3])):
+    if n < 1 << 20:
+        assert launched(n) == [-(-x * chunks // 4) for x in want], n
+""")
+
+
+@pytest.mark.gpu
+def test_heads_of_two_launches():
+    # beside the same tokens in calls of one launch each
+    n, H, d = 1100, 65536, 64
+    x = torch.empty((n, H, d), dtype=torch.bfloat16, device=dev())
+    x.view(torch.int16).random_(0, 0x4000)
+    p, rope = on_gpu(positions(n)), binding.deft_rope(32)
+    whole = binding.deft_rotate(x, p, rope)
+    for a in range(0, n, 100):
+        assert torch.equal(whole[a:a + 100], binding.deft_rotate(x[a:a + 100], p[a:a + 100], rope))
+    del whole, x
+    torch.cuda.empty_cache()
 
 
 # ---- on the GPU ----

@@ -178,6 +178,27 @@ def test_paths_of_many_pieces(counts, page):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("counts", [False, True])
+@pytest.mark.parametrize("page", [0, 16])
+def test_without_a_workspace_and_with_a_large_vocabulary(counts, page):
+    # the tokens are then looked through as they are
+    t = wl.config5_longcontext(root=6000, branches=9, lo=1, hi=700)
+    s = Inputs(t, 3000, 1, True)
+    plan, row_of, pool = plan_of(t, 0, 0, page, 1)
+    plan.image(t.Hq, t.Hkv, dev())
+    which = dict(repetition=True, presence=True, frequency=counts)
+    want = s.call(plan, row_of, pool, **which)
+    plan._logits_workspace = lambda *args: (0, 0)
+    assert torch.equal(s.call(plan, row_of, pool, **which), want)
+    s = Inputs(t, 2_200_000, 1, False)
+    plan, row_of, pool = plan_of(t, 0, 0, page, 1)
+    plan.image(t.Hq, t.Hkv, dev())
+    room = binding.load_library().deft_logits_workspace_bytes
+    assert room(plan.handle, 2_200_000) == 0 < room(plan.handle, 2_000_000)
+    close(s.call(plan, row_of, pool, **which), *s.want(**which))
+
+
+@pytest.mark.gpu
 def test_one_token_more_often_than_sixteen_bits_hold():
     t = wl.config2_fewshot(prefix=70000, branches=3, gen=5)
     s = Inputs(t, 2000, 1, True, prompts=False)
