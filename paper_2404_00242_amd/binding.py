@@ -348,7 +348,7 @@ class Plan:
         """(address, Hq / Hkv) of an image of any ratio: the tree is the same in all.  One that is there is taken and none made, since
         the first image of a ratio decides how the attention's tasks are cut."""
         ready = None
-        for key, image in list(self._images.of.items()):
+        for key, image in self._images.of.items():
             if type(key[0]) is tuple:  # a capture's own
                 key = key[0]
             elif key[1] == index and not capture and raw in image.streams:
@@ -393,8 +393,8 @@ class Plan:
             nbytes = int(load_library().deft_logits_workspace_bytes(self._h, vocab))
             with torch.cuda.stream(_torch_stream(raw, index)):
                 ws = torch.empty(nbytes, dtype=torch.uint8, device=torch.device("cuda", index))
-            self._workspaces[key] = ws
-        return ws.data_ptr(), ws.numel()
+            ws = self._workspaces[key] = ws.data_ptr(), nbytes, ws
+        return ws[:2]
 
 
 def _raw_stream(stream, index: int) -> int:
@@ -937,12 +937,14 @@ def _heads(t, n, d, index, bf16, what: str, name: str):
     if t.dtype is not bf16 or len(shape) != 3 or t.get_device() != index or index < 0:
         raise DeftError(-1, f"{what}: {name} must be a 3-d bf16 tensor, on one device with the others (there is no CPU path)")
     n2, heads, d2 = shape
-    if n2 != n or d2 != d or heads >= 1 << 31:
-        raise DeftError(-1, f"{what}: {name} must be [{n}, heads, {d}]")
     token, head, one = t.stride()
-    if one != 1 and n and heads:
-        raise DeftError(-1, f"{what}: the elements of {name}'s heads must be contiguous")
-    return t.data_ptr(), token if n > 1 else heads * d, head if heads > 1 else d, heads  # (one token's or head's stride says nothing)
+    if n2 != n or d2 != d or heads >= 1 << 31 or (one != 1 and n and heads):
+        raise DeftError(-1, f"{what}: {name} must be [{n}, heads, {d}], the elements of a head contiguous")
+    if n < 2:  # (one token's or head's stride says nothing)
+        token = heads * d
+    if heads < 2:
+        head = d
+    return t.data_ptr(), token, head, heads
 
 
 def _heads_out(out, t, at, bf16, raw, index, elsewhere, what: str, name: str):
@@ -1104,25 +1106,21 @@ DEFT_TOKEN_PROMPT = 0x40000000  # or-ed to the token ids of a prompt
 _pack_logits = struct.Struct("PPqqiiiiiiPqPPPPPqPPq").pack  # deft_logits_t
 
 
-def _per_query(t, nq, dtype, index, name: str):
-    if t is None:
-        return 0
-    if t.dtype != dtype or t.shape != (nq,) or t.get_device() != index or not t.is_contiguous():
-        raise DeftError(-1, f"deft_adjust_logits: {name} must be a contiguous {dtype} [{nq}] tensor on the logits' device")
+def _per_query(t, shape, dtype, index, name: str):
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index or not t.is_contiguous():
+        raise DeftError(-1, f"deft_adjust_logits: {name} must be a contiguous {dtype} {list(shape)} tensor on the logits' device")
     return t.data_ptr()
 
 
-def _table(t, width, dtype, row, nq, index, name: str):
+def _table(t, width, dtype, row, of_nq, index, name: str):
     """(address, distance of rows, number of rows, address of the queries' row numbers) of a table of biases or masks."""
-    if t is None:
-        if row is not None:
-            raise DeftError(-1, f"deft_adjust_logits: {name}_row says nothing without a {name}")
-        return 0, 0, 0, 0
-    if t.dim() == 1:
-        t = t[None]
-    if t.dtype != dtype or t.dim() != 2 or t.shape[0] < 1 or t.shape[1] != width or t.get_device() != index or (width > 1 and t.stride(1) != 1):
+    rows, *one = shape = t.shape if t.dim() != 1 else (1, t.shape[0])
+    if t.dtype is not dtype or len(shape) != 2 or rows < 1 or one[0] != width or t.get_device() != index or (width > 1 and t.stride(-1) != 1):
         raise DeftError(-1, f"deft_adjust_logits: {name} must be a {dtype} [rows, {width}] tensor of contiguous rows on the logits' device")
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else 0, t.shape[0], _per_query(row, nq, _torch.int32, index, name + "_row")
+    return t.data_ptr(), t.stride(0) if rows > 1 else 0, rows, 0 if row is None else _per_query(row, of_nq, _torch.int32, index, name + "_row")
+
+
+_NO_TABLE = 0, 0, 0, 0
 
 
 def deft_adjust_logits(plan: Plan, logits, tokens=None, repetition=None, frequency=None, presence=None, bias=None, bias_row=None, mask=None,
@@ -1137,45 +1135,55 @@ def deft_adjust_logits(plan: Plan, logits, tokens=None, repetition=None, frequen
     out, which may be the logits.  A plan that no attention call has used yet needs plan.image(Hq, Hkv, device) first.
     Asynchronous on `stream` (default: torch's current stream); the current stream has to wait for another one before it reads the result."""
     torch = _torch or _get_torch()
-    f32, index = torch.float32, logits.get_device()
-    wide = logits.dtype == f32
-    if index < 0 or logits.dim() != 2 or not (wide or logits.dtype == torch.bfloat16):
+    f32, i32, index, dtype = torch.float32, torch.int32, logits.get_device(), logits.dtype
+    wide, shape = dtype is f32, logits.shape
+    if index < 0 or len(shape) != 2 or not (wide or dtype is torch.bfloat16):
         raise DeftError(-1, "deft_adjust_logits: logits must be a 2-d float32 or bf16 device tensor (there is no CPU path)")
-    nq, vocab = shape = logits.shape
+    nq, vocab = shape
     stride, one = logits.stride()
-    if vocab > 1 and one != 1:
+    if one != 1 and vocab > 1:
         raise DeftError(-1, "deft_adjust_logits: a query's logits must be contiguous")
     plan_nq, plan_rows = plan.limits()
     if nq != plan_nq:
         raise DeftError(-1, "deft_adjust_logits: logits are of a different number of queries than the plan")
     if not 1 <= vocab <= 1 << 28:
         raise DeftError(-1, "deft_adjust_logits: no vocabulary, or one of more than 2^28 tokens")
+    of_nq = (nq,)
     history = repetition is not None or frequency is not None or presence is not None
-    if history and tokens is None:
+    tokens_at = n_tokens = repetition_at = frequency_at = presence_at = 0
+    if tokens is not None:
+        n_tokens = tokens.numel()
+        if tokens.dtype is not i32 or tokens.dim() != 1 or tokens.get_device() != index or not tokens.is_contiguous() or n_tokens < plan_rows:
+            raise DeftError(-1, "deft_adjust_logits: tokens must be a contiguous int32 tensor with every row that the plan addresses")
+        tokens_at = tokens.data_ptr() or 4  # (of none: anything)
+    elif history:
         raise DeftError(-1, "deft_adjust_logits: penalties need the tokens")
-    if tokens is not None and (tokens.dtype != torch.int32 or tokens.dim() != 1 or tokens.get_device() != index or not tokens.is_contiguous()
-                               or tokens.numel() < plan_rows):
-        raise DeftError(-1, "deft_adjust_logits: tokens must be a contiguous int32 tensor with every row that the plan addresses")
-    penalties = [_per_query(t, nq, f32, index, name) for t, name in ((repetition, "repetition"), (frequency, "frequency"), (presence, "presence"))]
-    bias_at, bias_stride, n_bias, bias_row_at = _table(bias, vocab, f32, bias_row, nq, index, "bias")
-    mask_at, mask_stride, n_masks, mask_row_at = _table(mask, -(-vocab // 32), torch.int32, mask_row, nq, index, "mask")
+    if repetition is not None:
+        repetition_at = _per_query(repetition, of_nq, f32, index, "repetition")
+    if frequency is not None:
+        frequency_at = _per_query(frequency, of_nq, f32, index, "frequency")
+    if presence is not None:
+        presence_at = _per_query(presence, of_nq, f32, index, "presence")
+    if (bias is None and bias_row is not None) or (mask is None and mask_row is not None):
+        raise DeftError(-1, "deft_adjust_logits: rows say nothing without their table")
+    bias_at, bias_stride, n_bias, bias_row_at = _NO_TABLE if bias is None else _table(bias, vocab, f32, bias_row, of_nq, index, "bias")
+    mask_at, mask_stride, n_masks, mask_row_at = _NO_TABLE if mask is None else _table(mask, -(-vocab // 32), i32, mask_row, of_nq, index, "mask")
     raw = _raw_stream(stream, index)
     if out is None:
-        dtype = out_dtype or logits.dtype
         if stream is not None and raw != torch._C._cuda_getCurrentRawStream(index):
-            out = _result(raw, index, shape, dtype)
+            out = _result(raw, index, shape, out_dtype or dtype)
         elif out_dtype is None and type(logits) is torch.Tensor:  # (see deft_tree_attn_decode)
             out = torch.empty_like(logits, memory_format=torch.contiguous_format)
         else:
-            out = torch.empty(shape, dtype=dtype, device=logits.device)
+            out = torch.empty(shape, dtype=out_dtype or dtype, device=logits.device)
     elif out.shape != shape or out.get_device() != index or (vocab > 1 and out.stride(1) != 1):
         raise DeftError(-1, "deft_adjust_logits: out must be like the logits, with contiguous rows")
-    out_wide = out.dtype == f32
-    if not out_wide and (wide or out.dtype != torch.bfloat16):
+    out_wide = out.dtype is f32
+    if not out_wide and (wide or out.dtype is not torch.bfloat16):
         raise DeftError(-1, "deft_adjust_logits: out must be float32, or bf16 for bf16 logits")
     if nq == 0:
         return out
-    if _elsewhere(index):
+    if torch._C._cuda_getDevice() != index:
         with torch.cuda.device(index):
             return deft_adjust_logits(plan, logits, tokens, repetition, frequency, presence, bias, bias_row, mask, mask_row, out, None, raw)
     image = group = ws = ws_bytes = 0
@@ -1183,11 +1191,13 @@ def deft_adjust_logits(plan: Plan, logits, tokens=None, repetition=None, frequen
         capture = _capture(raw) if raw else 0
         image, group = plan._any_image(index, raw, capture)
         ws, ws_bytes = plan._logits_workspace(vocab, index, raw, capture)
+    out_stride = out.stride(0)
+    if nq == 1:  # (one row's stride says nothing)
+        stride = out_stride = vocab
     rc = (_lib or load_library()).deft_adjust_logits(
         plan._h, image, group,
-        _pack_logits(logits.data_ptr(), out.data_ptr(), stride if nq > 1 else vocab, out.stride(0) if nq > 1 else vocab, vocab, wide, out_wide, n_bias, n_masks, 0,
-                     tokens.data_ptr() if history else 0, tokens.numel() if history else 0, *penalties, bias_at, bias_row_at, bias_stride, mask_at,
-                     mask_row_at, mask_stride), ws, ws_bytes, raw)
+        _pack_logits(logits.data_ptr(), out.data_ptr(), stride, out_stride, vocab, wide, out_wide, n_bias, n_masks, 0, tokens_at, n_tokens, repetition_at,
+                     frequency_at, presence_at, bias_at, bias_row_at, bias_stride, mask_at, mask_row_at, mask_stride), ws, ws_bytes, raw)
     if rc != 0:
         _check(rc, "deft_adjust_logits")
     return out
