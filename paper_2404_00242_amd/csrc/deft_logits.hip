@@ -51,8 +51,9 @@ struct LogitsArgs {
 constexpr int kThreads = 512;
 constexpr int kTile = 1024;       // logits of a row to a workgroup
 constexpr int kMost = 8;          // rows to a workgroup: as many as a thread can have in flight in registers
-constexpr int kStage = 512;      // pieces or groups at a time
-constexpr uint32_t kEach = kTile / kThreads, kStretches = kStage / kThreads;  // to a thread
+constexpr uint32_t kEach = kTile / kThreads;  // to a thread
+constexpr int kPieces = 512;      // at a time
+constexpr int kGroups = 256;      // at a time: the less LDS, the more workgroups to a compute unit
 static_assert(kEach == 2, "a row ends behind a thread's logits, or behind the first of them");
 constexpr int kSortThreads = 1024;
 constexpr int kRun = 1024;        // tokens that deft_sort_tokens takes to a workgroup
@@ -65,6 +66,21 @@ template <typename T>
 __device__ __forceinline__ T uniform(const T *p, uint32_t i) {
     return *((const __attribute__((address_space(4))) T *)(uintptr_t)(p + i));
 }
+
+// Element i of what begins at a place that is the same for all lanes (so it stays in scalar registers); i * sizeof(T) is below 2^32.
+template <typename T>
+__device__ __forceinline__ T *element(T *p, uint32_t i) {
+    return (T *)((char *)p + i * (uint32_t)sizeof(T));
+}
+template <typename T>
+__device__ __forceinline__ const T *element(const T *p, uint32_t i) {
+    return (const T *)((const char *)p + i * (uint32_t)sizeof(T));
+}
+
+struct Query {
+    float repetition, inverse, frequency, presence;
+    int32_t bias, mask;  // rows of the tables, -1: none
+};
 
 // `N` elements side by side, as floats.  (Rows may have odd lengths: any element can be a row's first.)
 template <typename T, int N>
@@ -254,93 +270,84 @@ __global__ __launch_bounds__(kSortThreads) void deft_sort_tokens(Pieces p, Sorte
 }
 
 // A workgroup has kTile logits of `block` queries.  It first looks which of those tokens stand on the queries' paths: pieces of the
-// tree that any of its queries sees, or the sorted tokens of its tile, are taken kStage stretches at a time into LDS, with the sum
+// tree that any of its queries sees, or the sorted tokens of its tile, are taken hundreds of stretches at a time into LDS, with the sum
 // of their lengths in front of each, and every thread finds the stretch of its next token there by bisection.
 template <typename I, typename O, bool COUNTS, bool SORTED, int MOST>
 __global__ __launch_bounds__(kThreads) void deft_logits(LogitsArgs a) {
     __shared__ __align__(16) Seen<COUNTS, MOST> seen;
+    constexpr uint32_t kStage = SORTED ? kGroups : kPieces;  // stretches at a time
+    static_assert(kStage <= kThreads, "one to a thread");
     __shared__ uint32_t before[kStage + 1], bits[SORTED ? 1 : kStage], part[kThreads / 64][2];
     __shared__ int32_t begin[kStage];  // of a stretch, less `before`
+    __shared__ Query queries[MOST];
     const uint32_t blocks = gridDim.x / a.tiles, tile = blockIdx.x / blocks, q0 = blockIdx.x % blocks * a.block, block = min(a.block, a.nq - q0);
     const uint32_t first = tile * kTile, t = threadIdx.x, mine = kEach * t, v = first + mine;
     const uint32_t n = v < a.vocab ? min(a.vocab - v, kEach) : 0;
     // What the first look at the tokens waits for is asked for first, and behind it all that does not wait for them.
-    u32x4 stretch[kStretches];  // its length, where it begins, and the queries that see it
+    u32x4 stretch{};  // its length, where it begins, and the queries that see it
     auto look = [&](uint32_t s0) {
-#pragma unroll
-        for (uint32_t i = 0; i < kStretches; ++i) {
-            const uint32_t s = min(s0 + kStretches * t + i, a.history - 1);
-            if constexpr (SORTED) {
-                const uint32_t *from = a.sorted.table + (uint64_t)tile * a.sorted.groups + s;
-                const u32x2 seen_by = a.sorted.seen_by[s];
-                stretch[i] = u32x4{from[a.sorted.groups], from[0], seen_by[0], seen_by[1]};
-            } else {
-                stretch[i] = u32x4{(uint32_t)a.pieces.len[s], (uint32_t)a.pieces.begin[s], (uint32_t)a.pieces.qlo[s], (uint32_t)a.pieces.qhi[s]};
-            }
+        const uint32_t s = min(s0 + t, a.history - 1);
+        if constexpr (SORTED) {
+            const uint32_t *from = a.sorted.table + (uint64_t)tile * a.sorted.groups + s;
+            const u32x2 seen_by = a.sorted.seen_by[s];
+            stretch = u32x4{from[a.sorted.groups], from[0], seen_by[0], seen_by[1]};
+        } else {
+            stretch = u32x4{(uint32_t)a.pieces.len[s], (uint32_t)a.pieces.begin[s], (uint32_t)a.pieces.qlo[s], (uint32_t)a.pieces.qhi[s]};
         }
     };
     if (a.history) look(0);
     // Queries behind the last are that one.
     uint32_t row[MOST];
-    float repetition[MOST], frequency[MOST], presence[MOST];
-    int32_t bias[MOST], mask[MOST];  // rows of the tables
 #pragma unroll
     for (uint32_t q = 0; q < MOST; ++q) {
         const uint32_t at = q0 + min(q, block - 1);
         row[q] = a.q_order ? (uint32_t)uniform(a.q_order, at) : at;
     }
+    if (t < MOST) {
+        uint32_t r = row[0];
 #pragma unroll
-    for (uint32_t q = 0; q < MOST; ++q) {
-        mask[q] = !a.mask ? -1 : a.mask_row ? uniform(a.mask_row, row[q]) : 0;
-        if ((uint32_t)mask[q] >= a.n_masks) mask[q] = -1;
-        bias[q] = !a.bias ? -1 : a.bias_row ? uniform(a.bias_row, row[q]) : 0;
-        if ((uint32_t)bias[q] >= a.n_bias) bias[q] = -1;
-        repetition[q] = a.repetition ? uniform(a.repetition, row[q]) : 1.f;
-        frequency[q] = COUNTS ? uniform(a.frequency, row[q]) : 0.f;
-        presence[q] = a.presence ? uniform(a.presence, row[q]) : 0.f;
+        for (uint32_t q = 1; q < MOST; ++q) r = t == q ? row[q] : r;
+        Query q;
+        q.repetition = a.repetition ? a.repetition[r] : 1.f;
+        q.frequency = COUNTS ? a.frequency[r] : 0.f;
+        q.presence = a.presence ? a.presence[r] : 0.f;
+        q.bias = !a.bias ? -1 : a.bias_row ? a.bias_row[r] : 0;
+        q.mask = !a.mask ? -1 : a.mask_row ? a.mask_row[r] : 0;
+        if ((uint32_t)q.bias >= a.n_bias) q.bias = -1;
+        if ((uint32_t)q.mask >= a.n_masks) q.mask = -1;
+        q.inverse = 1.f / q.repetition;
+        queries[t] = q;
     }
     float x[MOST][kEach];
     uint32_t word[MOST];
-    const I *logits = static_cast<const I *>(a.logits) + v;
+    const I *logits = static_cast<const I *>(a.logits);
     if (n == kEach) {
 #pragma unroll
-        for (uint32_t q = 0; q < MOST; ++q) get<I, kEach>(logits + (int64_t)row[q] * a.stride, x[q]);
+        for (uint32_t q = 0; q < MOST; ++q) get<I, kEach>(element(logits + (int64_t)row[q] * a.stride, v), x[q]);
     } else if (n) {
 #pragma unroll
-        for (uint32_t q = 0; q < MOST; ++q) get<I, 1>(logits + (int64_t)row[q] * a.stride, x[q]);
+        for (uint32_t q = 0; q < MOST; ++q) get<I, 1>(element(logits + (int64_t)row[q] * a.stride, v), x[q]);
     }
     if (a.mask && n) {
 #pragma unroll
-        for (uint32_t q = 0; q < MOST; ++q) word[q] = a.mask[(int64_t)max(mask[q], 0) * a.mask_stride + v / 32] >> (v % 32);
+        for (uint32_t q = 0; q < MOST; ++q) {
+            const uint32_t m = a.mask_row ? (uint32_t)uniform(a.mask_row, row[q]) : 0;
+            word[q] = *element(a.mask + (int64_t)(m < a.n_masks ? m : 0) * a.mask_stride, v / 32) >> (v % 32);
+        }
     }
     static_assert(sizeof(seen) % 16 == 0, "cleared in 128-bit words");
     for (uint32_t i = t; i < sizeof(seen) / 16; i += kThreads) reinterpret_cast<u32x4 *>(&seen)[i] = u32x4{0, 0, 0, 0};
     for (uint32_t s0 = 0; s0 < a.history; s0 += kStage) {
         if (s0) look(s0);
-        uint32_t len[kStretches], on[kStretches], sum = 0, many = 0;
-        int32_t at[kStretches];
-#pragma unroll
-        for (uint32_t i = 0; i < kStretches; ++i) {
-            const uint32_t s = s0 + kStretches * t + i;
-            on[i] = s < a.history ? bits_of((int32_t)stretch[i][2], (int32_t)stretch[i][3], q0, block) : 0;
-            len[i] = SORTED ? stretch[i][0] - stretch[i][1] : stretch[i][0];
-            if (SORTED && len[i] == 0) on[i] = 0;
-            if (!on[i]) len[i] = 0;
-            at[i] = (int32_t)(SORTED ? s * kRun + stretch[i][1] : stretch[i][1]);
-            sum += len[i];
-            many += on[i] != 0;
-            before[kThreads * i + t] = 0xffffffffu;
-        }
-        if (t == 0) before[kStage] = 0xffffffffu;
-        Sums sums = sums_before<kThreads>(sum, many, part);
-#pragma unroll
-        for (uint32_t i = 0; i < kStretches; ++i) {
-            if (!on[i]) continue;
+        uint32_t on = t < kStage && s0 + t < a.history ? bits_of((int32_t)stretch[2], (int32_t)stretch[3], q0, block) : 0;
+        if (SORTED && stretch[0] == stretch[1]) on = 0;
+        const uint32_t len = !on ? 0 : SORTED ? stretch[0] - stretch[1] : stretch[0];
+        for (uint32_t i = t; i <= kStage; i += kThreads) before[i] = 0xffffffffu;
+        const Sums sums = sums_before<kThreads>(len, on != 0, part);
+        if (on) {
             before[sums.y] = sums.x;
-            begin[sums.y] = at[i] - (int32_t)sums.x;
-            if constexpr (!SORTED) bits[sums.y] = on[i];
-            ++sums.y;
-            sums.x += len[i];
+            begin[sums.y] = (int32_t)((SORTED ? (s0 + t) * kRun : 0) + stretch[1] - sums.x);
+            if constexpr (!SORTED) bits[sums.y] = on;
         }
         __syncthreads();
         const uint32_t steps = sums.all_y > 1 ? 1u << (32 - __builtin_clz(sums.all_y - 1)) : 1;
@@ -378,19 +385,19 @@ __global__ __launch_bounds__(kThreads) void deft_logits(LogitsArgs a) {
 #pragma unroll
     for (uint32_t q = 0; q < MOST; ++q) {
         if (q >= block) break;
-        const float inverse = 1.f / repetition[q];
+        const Query query = queries[q];
 #pragma unroll
         for (uint32_t i = 0; i < kEach; ++i) {
-            if ((any[i] >> q) & 1) x[q][i] *= x[q][i] > 0 ? inverse : repetition[q];
+            if ((any[i] >> q) & 1) x[q][i] *= x[q][i] > 0 ? query.inverse : query.repetition;
             if constexpr (COUNTS) {
                 count[i] += seen.change[q][mine + i];
-                if (count[i] > 0) x[q][i] -= frequency[q] * (float)count[i] + presence[q];
+                if (count[i] > 0) x[q][i] -= query.frequency * (float)count[i] + query.presence;
             } else {
-                if ((generated[i] >> q) & 1) x[q][i] -= presence[q];
+                if ((generated[i] >> q) & 1) x[q][i] -= query.presence;
             }
         }
-        if (bias[q] >= 0) {
-            const float *from = a.bias + (int64_t)bias[q] * a.bias_stride + v;
+        if (query.bias >= 0) {
+            const float *from = element(a.bias + (int64_t)__builtin_amdgcn_readfirstlane(query.bias) * a.bias_stride, v);
             float y[kEach];
             if (n == kEach)
                 get<float, kEach>(from, y);
@@ -399,12 +406,12 @@ __global__ __launch_bounds__(kThreads) void deft_logits(LogitsArgs a) {
 #pragma unroll
             for (uint32_t i = 0; i < kEach; ++i) x[q][i] += y[i];
         }
-        if (mask[q] >= 0) {
+        if (query.mask >= 0) {
 #pragma unroll
             for (uint32_t i = 0; i < kEach; ++i)
                 if (!((word[q] >> i) & 1)) x[q][i] = -__builtin_inff();
         }
-        O *to = static_cast<O *>(a.out) + (int64_t)row[q] * a.out_stride + v;
+        O *to = element(static_cast<O *>(a.out) + (int64_t)row[q] * a.out_stride, v);
         if (n == kEach)
             put<O, kEach>(to, x[q]);
         else
@@ -440,7 +447,7 @@ int64_t tokens_of(const deft_plan_t *plan) {
 }
 // Whether they are sorted before they are looked for.
 bool sorts(const deft_plan_t *plan, int64_t total, uint32_t tiles) {
-    return tiles <= kMaxTiles && total < (int64_t(1) << 30) && (total > kFewTokens || plan->n_segs() > kStage);
+    return tiles <= kMaxTiles && total < (int64_t(1) << 30) && (total > kFewTokens || plan->n_segs() > kPieces);
 }
 struct Space {
     uint64_t groups, table, seen_by, bytes;  // places
