@@ -1,5 +1,8 @@
 // The next token's logits, bent by what each query's path holds (penalties for repeated tokens), by biases and by grammar masks.
-// Every logit is read once and written once.
+// Every logit is read once and written once; which tokens stand on which path is worked out in LDS, never as a table of queries by
+// vocabulary.  Bound by HBM where there are many queries (120 x 128000 float over a tree of 107000 tokens in 16-row pages 37 us, 8 of
+// them to sort; the logits alone with a mask 22, a copy of them 25), by a chain of a few dependent loads where there are few (4 x
+// 32000 4.3 us).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -48,9 +51,13 @@ struct LogitsArgs {
     uint32_t n_bias, n_masks;
 };
 
+// A thread has two logits side by side of every row of its workgroup, all in flight from the beginning: up to eight rows, since with
+// more the counters of their tokens leave LDS for one workgroup to a compute unit (16 rows: 120 x 128000 40 -> 110 us) and with fewer
+// the tokens are looked for more often (4: 50 us).  Kernels for one and for four rows have fewer loads and counters (one query, 8191
+// tokens 12.4 -> 11.1 us).  256 or 1024 threads with four logits or one: 60 and 86 us where 512 took 47.
 constexpr int kThreads = 512;
 constexpr int kTile = 1024;       // logits of a row to a workgroup
-constexpr int kMost = 8;          // rows to a workgroup: as many as a thread can have in flight in registers
+constexpr int kMost = 8;          // rows
 constexpr uint32_t kEach = kTile / kThreads;  // to a thread
 constexpr int kPieces = 512;      // at a time
 constexpr int kGroups = 256;      // at a time: the less LDS, the more workgroups to a compute unit
@@ -58,7 +65,8 @@ static_assert(kEach == 2, "a row ends behind a thread's logits, or behind the fi
 constexpr int kSortThreads = 1024;
 constexpr int kRun = 1024;        // tokens that deft_sort_tokens takes to a workgroup
 constexpr int kMaxTiles = 2048;   // that it sorts by
-constexpr int kFewTokens = 5000;  // are looked through unsorted
+constexpr int kFill = 512;        // workgroups that the chip holds with no trouble: two to a compute unit
+constexpr int kFewTokens = 7500;  // are looked through unsorted by as many workgroups, see sorts
 constexpr int kAhead = 2;         // tokens of a thread at a time, side by side
 
 // A value that is the same for all lanes, by a scalar load.
@@ -96,7 +104,7 @@ __device__ __forceinline__ void put(T *p, const float *x) {
     type v;
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = (T)x[i];
-    *reinterpret_cast<type *>(p) = v;
+    __builtin_nontemporal_store(v, reinterpret_cast<type *>(p));  // (not read again here)
 }
 
 // Queries are in the plan's depth-first order here, in which the queries whose path holds a token are neighbours: `bits` says which
@@ -175,7 +183,9 @@ __device__ __forceinline__ uint32_t last_not_above(const uint32_t *x, uint32_t n
 }
 
 // Every workgroup of deft_logits would look through all tokens of its queries' paths for the few that are its tile's.  Where those are
-// many they are sorted by tile first, kRun of them to a workgroup, in LDS.
+// many they are sorted by tile first, kRun of them to a workgroup, in LDS: a counting sort, whose order within a tile is any, since
+// what becomes of a tile's tokens (bits set, whole numbers added) does not depend on it.  Bound by latency: 5 us for 8000 tokens of 512
+// pieces, 8 us for 107000 of 6700, whose first piece has to be searched for.
 __global__ __launch_bounds__(kSortThreads) void deft_sort_tokens(Pieces p, Sorted to, uint32_t total, uint32_t tiles) {
     constexpr uint32_t kMine = kRun / kSortThreads, kBins = kMaxTiles / kSortThreads;
     __shared__ uint32_t off[kRun], bins[kMaxTiles], part[kSortThreads / 64][2];
@@ -445,9 +455,24 @@ int64_t tokens_of(const deft_plan_t *plan) {
     }
     return total;
 }
-// Whether they are sorted before they are looked for.
-bool sorts(const deft_plan_t *plan, int64_t total, uint32_t tiles) {
-    return tiles <= kMaxTiles && total < (int64_t(1) << 30) && (total > kFewTokens || plan->n_segs() > kPieces);
+// A row is cut into tiles, and as many rows to a workgroup as still leave kFill of them.
+struct Shape {
+    uint32_t tiles, block;
+    uint64_t groups;
+};
+Shape shape_of(uint32_t nq, uint32_t vocab) {
+    Shape s;
+    s.tiles = (vocab + kTile - 1) / kTile;
+    s.block = (uint32_t)std::clamp<uint64_t>(((uint64_t)nq * s.tiles + kFill - 1) / kFill, 1, kMost);
+    s.groups = (uint64_t)s.tiles * ((nq + s.block - 1) / s.block);
+    return s;
+}
+// Whether tokens are sorted before they are looked for.  us, unsorted -> sorted: one query x 128000, 125 workgroups, 6000 tokens 9.5 ->
+// 9.6, 8000 11.5 -> 10.4; 64 x 50001, 490 workgroups, 7000 tokens 14.1 -> 14.5, 8000 15.5 -> 15.0; 80 x 128000, 1250 workgroups, 2000
+// tokens 16.4 -> 19.0, 4000 19.9 -> 19.1; 200 x 128000, 3125 workgroups, 1200 tokens 30.5 -> 33.3, 2200 34.4 -> 33.9.
+bool sorts(const deft_plan_t *plan, int64_t total, const Shape &s) {
+    if (s.tiles > kMaxTiles || total >= (int64_t(1) << 30)) return false;
+    return plan->n_segs() > kPieces || total * (int64_t)std::max<uint64_t>(s.groups, kFill) > (int64_t)kFewTokens * kFill;
 }
 struct Space {
     uint64_t groups, table, seen_by, bytes;  // places
@@ -461,7 +486,7 @@ Space space_of(int64_t total, uint32_t tiles) {
     return s;
 }
 
-constexpr int64_t kMaxStride = int64_t(1) << 31;  // times 2^31 queries of 4 bytes: within 64 bits
+constexpr int64_t kMaxStride = int64_t(1) << 31;
 
 bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0; }
 
@@ -469,9 +494,9 @@ bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0;
 
 extern "C" size_t deft_logits_workspace_bytes(const deft_plan_t *plan, int32_t vocab) {
     if (!plan || vocab < 1 || vocab > DEFT_MAX_VOCAB) return 0;
-    const uint32_t tiles = ((uint32_t)vocab + kTile - 1) / kTile;
+    const Shape shape = shape_of((uint32_t)plan->nq, (uint32_t)vocab);
     const int64_t total = tokens_of(plan);
-    return sorts(plan, total, tiles) ? (size_t)space_of(total, tiles).bytes : 0;
+    return sorts(plan, total, shape) ? (size_t)space_of(total, shape.tiles).bytes : 0;
 }
 
 extern "C" int deft_adjust_logits(const deft_plan_t *plan, const void *dev_image, int32_t group, const deft_logits_t *l, void *workspace,
@@ -497,6 +522,7 @@ extern "C" int deft_adjust_logits(const deft_plan_t *plan, const void *dev_image
     const int in_bytes = l->logits_f32 ? 4 : 2, out_bytes = l->out_f32 ? 4 : 2;
     if (reinterpret_cast<uintptr_t>(l->logits) % in_bytes || reinterpret_cast<uintptr_t>(l->out) % out_bytes) return DEFT_EINVAL;
     if (nq > 1 && (l->stride < 0 || l->out_stride < l->vocab || l->stride > kMaxStride || l->out_stride > kMaxStride)) return DEFT_EINVAL;
+    if (nq > 1 && (double)nq * (double)std::max(l->stride, l->out_stride) > 0x1p60) return DEFT_EINVAL;
     const bool in_place = l->out == l->logits && in_bytes == out_bytes && (nq == 1 || l->stride == l->out_stride);
     const uintptr_t in = reinterpret_cast<uintptr_t>(l->logits), out = reinterpret_cast<uintptr_t>(l->out);
     const uint64_t in_size = in_bytes * ((uint64_t)(nq - 1) * (uint64_t)l->stride + l->vocab), out_size = out_bytes * ((uint64_t)(nq - 1) * (uint64_t)l->out_stride + l->vocab);
@@ -508,7 +534,9 @@ extern "C" int deft_adjust_logits(const deft_plan_t *plan, const void *dev_image
     a.out_stride = l->out_stride;
     a.vocab = (uint32_t)l->vocab;
     a.nq = (uint32_t)nq;
-    a.tiles = (a.vocab + kTile - 1) / kTile;
+    const Shape shape = shape_of(a.nq, a.vocab);
+    a.tiles = shape.tiles;
+    a.block = shape.block;
     a.repetition = l->repetition;
     a.frequency = l->frequency;
     a.presence = l->presence;
@@ -521,10 +549,7 @@ extern "C" int deft_adjust_logits(const deft_plan_t *plan, const void *dev_image
     a.mask_stride = l->mask_stride;
     a.n_masks = (uint32_t)l->n_masks;
     const bool counts = l->frequency != nullptr;
-    const uint64_t work = (uint64_t)a.nq * a.tiles;
-    a.block = (uint32_t)std::clamp<uint64_t>((work + 511) / 512, 1, kMost);
-    const uint64_t groups = (uint64_t)a.tiles * ((a.nq + a.block - 1) / a.block);
-    if (groups * kThreads > UINT32_MAX) return DEFT_EINVAL;
+    if (shape.groups * kThreads > UINT32_MAX) return DEFT_EINVAL;
     hipStream_t st = static_cast<hipStream_t>(stream);
     bool sorted = false;
     if (history && plan->n_segs() > 0) {
@@ -533,7 +558,7 @@ extern "C" int deft_adjust_logits(const deft_plan_t *plan, const void *dev_image
         a.q_order = at(S->off_q_order);
         a.history = a.pieces.n;
         const int64_t total = tokens_of(plan);
-        sorted = workspace && sorts(plan, total, a.tiles);
+        sorted = workspace && sorts(plan, total, shape);
         if (sorted) {
             const Space space = space_of(total, a.tiles);
             if (!deft::aligned16(workspace)) return DEFT_EINVAL;
@@ -546,10 +571,10 @@ extern "C" int deft_adjust_logits(const deft_plan_t *plan, const void *dev_image
         }
     }
     if (l->logits_f32)
-        launch<float, float>(a, counts, sorted, (uint32_t)groups, st);
+        launch<float, float>(a, counts, sorted, (uint32_t)shape.groups, st);
     else if (l->out_f32)
-        launch<__bf16, float>(a, counts, sorted, (uint32_t)groups, st);
+        launch<__bf16, float>(a, counts, sorted, (uint32_t)shape.groups, st);
     else
-        launch<__bf16, __bf16>(a, counts, sorted, (uint32_t)groups, st);
+        launch<__bf16, __bf16>(a, counts, sorted, (uint32_t)shape.groups, st);
     return deft::hip_ok(hipGetLastError(), "deft_logits launch") ? DEFT_OK : DEFT_EHIP;
 }
