@@ -7,6 +7,7 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <type_traits>
 
 #include "deft_device.h"
 #include "deft_internal.h"
@@ -52,7 +53,7 @@ struct LogitsArgs {
 };
 
 // A thread has two logits side by side of every row of its workgroup, all in flight from the beginning: up to eight rows, since with
-// more the counters of their tokens leave LDS for one workgroup to a compute unit (16 rows: 120 x 128000 40 -> 110 us) and with fewer
+// more the counters of their tokens leave LDS for one workgroup to a compute unit (16 rows: 120 x 128000 44 -> 112 us) and with fewer
 // the tokens are looked for more often (4: 50 us).  Kernels for one and for four rows have fewer loads and counters (one query, 8191
 // tokens 12.4 -> 11.1 us).  256 or 1024 threads with four logits or one: 60 and 86 us where 512 took 47.
 constexpr int kThreads = 512;
@@ -66,8 +67,7 @@ constexpr int kSortThreads = 1024;
 constexpr int kRun = 1024;        // tokens that deft_sort_tokens takes to a workgroup
 constexpr int kMaxTiles = 2048;   // that it sorts by
 constexpr int kFill = 512;        // workgroups that the chip holds with no trouble: two to a compute unit
-constexpr int kFewTokens = 7500;  // are looked through unsorted by as many workgroups, see sorts
-constexpr int kAhead = 2;         // tokens of a thread at a time, side by side
+constexpr int kFewTokens = 9000;  // are looked through unsorted by as many workgroups, see sorts
 
 // A value that is the same for all lanes, by a scalar load.
 template <typename T>
@@ -361,26 +361,37 @@ __global__ __launch_bounds__(kThreads) void deft_logits(LogitsArgs a) {
         }
         __syncthreads();
         const uint32_t steps = sums.all_y > 1 ? 1u << (32 - __builtin_clz(sums.all_y - 1)) : 1;
-        for (uint32_t f = kAhead * t; f < sums.all_x; f += kAhead * kThreads) {
-            uint32_t k[kAhead];
-            u32x4 e[kAhead];
+        auto take = [&](auto ahead) {
+            constexpr uint32_t kAhead = decltype(ahead)::value;
+            for (uint32_t f = kAhead * t; f < sums.all_x; f += kAhead * kThreads) {
+                uint32_t k[kAhead];
+                u32x4 e[kAhead];
 #pragma unroll
-            for (uint32_t u = 0; u < kAhead; ++u) {  // (a stretch has a token at least)
-                k[u] = u == 0 ? last_not_above(before, steps, f) : k[u - 1] + (before[k[u - 1] + 1] <= f + u);
-                k[u] = min(k[u], sums.all_y - 1);
-                const uint32_t g = min(f + u, sums.all_x - 1);
-                if constexpr (SORTED)
-                    e[u] = a.sorted.events[(uint32_t)(begin[k[u]] + (int32_t)g)];
-                else
-                    e[u][0] = (uint32_t)a.pieces.tokens[(int64_t)begin[k[u]] + g];
-            }
+                for (uint32_t u = 0; u < kAhead; ++u) {  // (a stretch has a token at least)
+                    k[u] = u == 0 ? last_not_above(before, steps, f) : k[u - 1] + (before[k[u - 1] + 1] <= f + u);
+                    k[u] = min(k[u], sums.all_y - 1);
+                    const uint32_t g = min(f + u, sums.all_x - 1);
+                    if constexpr (SORTED)
+                        e[u] = a.sorted.events[(uint32_t)(begin[k[u]] + (int32_t)g)];
+                    else
+                        e[u][0] = (uint32_t)a.pieces.tokens[(int64_t)begin[k[u]] + g];
+                }
 #pragma unroll
-            for (uint32_t u = 0; u < kAhead; ++u) {
-                if (f + u >= sums.all_x) break;
-                const uint32_t which = SORTED ? bits_of((int32_t)e[u][1], (int32_t)e[u][2], q0, block) : bits[k[u]];
-                if (which) see(seen, (int32_t)e[u][0], first, which, block);
+                for (uint32_t u = 0; u < kAhead; ++u) {
+                    if (f + u >= sums.all_x) break;
+                    const uint32_t which = SORTED ? bits_of((int32_t)e[u][1], (int32_t)e[u][2], q0, block) : bits[k[u]];
+                    if (which) see(seen, (int32_t)e[u][0], first, which, block);
+                }
             }
-        }
+        };
+        // a thread's tokens side by side, one bisection for all: as many as still leave work for every thread (8000 tokens of one query
+        // two by two 11.1 us, four by four 9.8; 1000 tokens 4.5 and 4.9); sorted ones are larger, and two by two is best throughout
+        if (sums.all_x <= kThreads)
+            take(std::integral_constant<uint32_t, 1>{});
+        else if (SORTED || sums.all_x <= 2 * kThreads)
+            take(std::integral_constant<uint32_t, 2>{});
+        else
+            take(std::integral_constant<uint32_t, 4>{});
         __syncthreads();
     }
     __syncthreads();
@@ -469,7 +480,8 @@ Shape shape_of(uint32_t nq, uint32_t vocab) {
 }
 // Whether tokens are sorted before they are looked for.  us, unsorted -> sorted: one query x 128000, 125 workgroups, 6000 tokens 9.5 ->
 // 9.6, 8000 11.5 -> 10.4; 64 x 50001, 490 workgroups, 7000 tokens 14.1 -> 14.5, 8000 15.5 -> 15.0; 80 x 128000, 1250 workgroups, 2000
-// tokens 16.4 -> 19.0, 4000 19.9 -> 19.1; 200 x 128000, 3125 workgroups, 1200 tokens 30.5 -> 33.3, 2200 34.4 -> 33.9.
+// tokens 16.4 -> 19.0, 4000 19.9 -> 19.1; 200 x 128000, 3125 workgroups, 1200 tokens 30.5 -> 33.3, 2200 34.4 -> 33.9.  That is in a graph;
+// otherwise the host has a second launch to make, 3 us (one query, 8191 tokens, 11.6 -> 13.4), so the line is drawn somewhat later.
 bool sorts(const deft_plan_t *plan, int64_t total, const Shape &s) {
     if (s.tiles > kMaxTiles || total >= (int64_t(1) << 30)) return false;
     return plan->n_segs() > kPieces || total * (int64_t)std::max<uint64_t>(s.groups, kFill) > (int64_t)kFewTokens * kFill;
