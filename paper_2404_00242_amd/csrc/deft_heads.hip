@@ -31,6 +31,7 @@ struct Part {
     uint16_t *out;
     const void *weight;  // null: not normalised
     int64_t token, head, out_token, out_head, weight_head;
+    uint32_t heads, chunk;  // a token's first wave for them
 };
 
 struct HeadsArgs {
@@ -38,7 +39,6 @@ struct HeadsArgs {
     const int32_t *positions;
     const u32x2 *entries;  // {row of k's and v's out, token}; null: every token, and its row is its own number
     uint32_t waves, chunks, inv_chunks;  // of the launch; of a token
-    uint32_t k_begin, v_begin, heads;    // of a token's heads, q's before k's before v's
     uint32_t rot, wide;                  // wide: weights are float
     float eps, offset, factor;
     uint64_t turns[64];  // of a turn a position, in 2^-64
@@ -73,23 +73,49 @@ __device__ __forceinline__ void unpack8(const u32x4 &x, float *y) {
     }
 }
 __device__ __forceinline__ u32x4 pack8(const float *y) { return u32x4{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7])}; }
-__device__ __forceinline__ void load8(const void *p, uint32_t at, bool wide, float *y) {
+
+// Eight weights as they lie in memory, and as floats.
+struct Weights {
+    u32x4 a, b;  // b: the second four floats
+};
+__device__ __forceinline__ Weights weights_at(const void *p, uint32_t at, bool wide) {
+    Weights w;
     if (wide) {
-        const f32x4 *w = reinterpret_cast<const f32x4 *>(static_cast<const float *>(p) + at);
-        const f32x4 a = w[0], b = w[1];
+        const u32x4 *x = reinterpret_cast<const u32x4 *>(static_cast<const float *>(p) + at);
+        w.a = x[0];
+        w.b = x[1];
+    } else {
+        w.a = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(p) + at);
+    }
+    return w;
+}
+__device__ __forceinline__ void unpack_weights(const Weights &w, bool wide, float offset, float *y) {
+    if (wide) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            y[i] = a[i];
-            y[4 + i] = b[i];
+            y[i] = __builtin_bit_cast(float, (uint32_t)w.a[i]);
+            y[4 + i] = __builtin_bit_cast(float, (uint32_t)w.b[i]);
         }
     } else {
-        unpack8(*reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(p) + at), y);
+        unpack8(w.a, y);
     }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] += offset;
 }
 
-// A wave has one token and 64 / (D / 16) of its heads, sixteen elements of a head to a lane: two groups of eight that in the half layout
-// are partners of one another, so that no lane needs another's elements.  The angles of a token are the same for all its heads: a
-// lane makes one pair's cosine and sine, and the wave's LDS hands them round.
+// A value that is the same for all lanes, by a scalar load.
+template <typename T>
+__device__ __forceinline__ T uniform(const T *p, uint32_t i) {
+    return *((const __attribute__((address_space(4))) T *)(uintptr_t)(p + i));
+}
+
+// A wave has one token and 64 / (D / 16) of its heads of one kind (what tells queries, keys and values apart is then in scalar registers:
+// 8192 tokens x 40 heads normalised and turned 32.0 -> 28.1 us), sixteen elements of a head to a lane: two groups of eight that in the
+// half layout are partners of one another, so that no lane needs another's elements.  The angles of a token are the same for all its
+// heads: a lane makes one pair's cosine and sine, and the wave's LDS hands them round.
+// Bound by HBM where calls are large: 8192 tokens x 40 heads of 128, us: copied by this kernel 26.8, turned 27.1, normalised 27.1, both
+// 28.0 (6.0 TB/s); by the host's call, and 3 to 4 us of launch and dependent loads, where they are a decode iteration's.  Two or more
+// batches of heads to a wave, 8192 x 32 turned: 21.0 -> 21.8.  Stores that stay in the caches: 8192 x 32 20.7 -> 25.1.
 template <int D, int TURN, bool NORM>
 __global__ __launch_bounds__(256) void deft_heads(HeadsArgs a) {
     constexpr uint32_t kLanes = D / 16, kHeads = 64 / kLanes;
@@ -97,28 +123,43 @@ __global__ __launch_bounds__(256) void deft_heads(HeadsArgs a) {
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const uint32_t unit = blockIdx.x * 4 + wave;
     if (unit >= a.waves) return;
-    const uint32_t entry = divide(unit, a.chunks, a.inv_chunks);
+    const uint32_t entry = divide(unit, a.chunks, a.inv_chunks), chunk = unit - entry * a.chunks;
+    const int kind = chunk >= a.part[kV].chunk ? kV : chunk >= a.part[kK].chunk ? kK : kQ;
+    const Part &p = a.part[kind];
     uint32_t token = entry, row = entry;
     if (a.entries) {
-        const u32x2 e = a.entries[entry];
-        row = e[0];
+        const u32x2 e = uniform(a.entries, entry);
+        row = kind == kQ ? e[1] : e[0];
         token = e[1];
     }
-    const uint32_t j = lane % kLanes, asked = (unit - entry * a.chunks) * kHeads + lane / kLanes, at = min(asked, a.heads - 1);
-    const int kind = at >= a.v_begin ? kV : at >= a.k_begin ? kK : kQ;
-    const Part &p = a.part[kind];
-    const uint32_t head = at - (kind == kV ? a.v_begin : kind == kK ? a.k_begin : 0);
     // the lane's two groups: interleaved anywhere in the head, in the half layout partners, and of the elements that do not turn the same
-    const bool turned = TURN == kHalf && kind != kV && 16 * j < a.rot;
-    const uint32_t begin = turned || TURN != kHalf || kind == kV ? 0 : a.rot, width = turned ? a.rot : D - begin;
+    const uint32_t j = lane % kLanes, rot = kind == kV ? 0 : a.rot;
+    const bool turned = TURN == kHalf && 16 * j < rot;
+    const uint32_t begin = turned || TURN != kHalf ? 0 : rot, width = turned ? rot : D - begin;
     const uint32_t first = begin + 8 * (j - begin / 16), second = first + width / 2;
-    const bool turned0 = TURN == kInterleaved ? kind != kV && first < a.rot : turned, turned1 = TURN == kInterleaved ? kind != kV && second < a.rot : turned;
-    const uint16_t *x = p.x + ((int64_t)token * p.token + (int64_t)head * p.head);
+    const bool turned0 = TURN == kInterleaved ? first < rot : turned, turned1 = TURN == kInterleaved ? second < rot : turned;
+    const uint32_t head = (chunk - p.chunk) * kHeads + lane / kLanes, at = min(head, p.heads - 1);  // (heads behind the last are that one)
+    const uint16_t *x = p.x + ((int64_t)token * p.token + (int64_t)at * p.head);
+    // What the angles and the norm wait for is asked for in front of the heads, by vector loads: those come back in order, and a scalar
+    // load of the position would hold up everything behind the next wait for any scalar load.
+    int32_t position = 0;
+    uint64_t turns = 0;
+    if (TURN != kNoTurn && 2 * lane < rot) {
+        uint32_t of = token;
+        asm("" : "+v"(of));
+        position = a.positions[of];
+        turns = a.turns[lane];
+    }
+    const bool normed = NORM && p.weight;
+    Weights v0, v1;
+    if (normed) {
+        const uint32_t w = at * (uint32_t)p.weight_head;
+        v0 = weights_at(p.weight, w + first, a.wide);
+        v1 = weights_at(p.weight, w + second, a.wide);
+    }
     const u32x4 x0 = *reinterpret_cast<const u32x4 *>(x + first), x1 = *reinterpret_cast<const u32x4 *>(x + second);
     float (*cs)[64] = table[wave];
-    if (TURN != kNoTurn && 2 * lane < a.rot) {
-        const int32_t position = a.positions[token];
-        const uint64_t turns = a.turns[lane];
+    if (TURN != kNoTurn && 2 * lane < rot) {
         const uint32_t low = (uint32_t)turns, high = (uint32_t)(turns >> 32);
         uint32_t phase = __umulhi((uint32_t)position, low) + (uint32_t)position * high;
         if (position < 0) phase -= low;
@@ -130,14 +171,10 @@ __global__ __launch_bounds__(256) void deft_heads(HeadsArgs a) {
     float y0[8], y1[8];
     unpack8(x0, y0);
     unpack8(x1, y1);
-    const bool normed = NORM && p.weight;
-    if (NORM) {
+    if (normed) {
         float w0[8], w1[8];
-        if (normed) {
-            const uint32_t w = (uint32_t)(head * p.weight_head);
-            load8(p.weight, w + first, a.wide, w0);
-            load8(p.weight, w + second, a.wide, w1);
-        }
+        unpack_weights(v0, a.wide, a.offset, w0);
+        unpack_weights(v1, a.wide, a.offset, w1);
         auto mean = [&](float eps) {
             float sum = 0;
 #pragma unroll
@@ -147,7 +184,7 @@ __global__ __launch_bounds__(256) void deft_heads(HeadsArgs a) {
             return fmaf(sum, 1.f / D, eps);
         };
         float m = mean(a.eps);
-        if (normed && (m > 0x1p100f || m < 0x1p-80f)) {  // squares near the ends of fp32: the head is taken by a power of two of itself
+        if (m > 0x1p100f || m < 0x1p-80f) {  // squares near the ends of fp32: the head is taken by a power of two of itself
             const float by = m > 1.f ? 0x1p-70f : 0x1p90f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -157,12 +194,10 @@ __global__ __launch_bounds__(256) void deft_heads(HeadsArgs a) {
             m = mean(a.eps * by * by);
         }
         const float r = __builtin_amdgcn_rsqf(m);
-        if (normed) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                y0[i] *= r * (w0[i] + a.offset);
-                y1[i] *= r * (w1[i] + a.offset);
-            }
+        for (int i = 0; i < 8; ++i) {
+            y0[i] *= r * w0[i];
+            y1[i] *= r * w1[i];
         }
     }
     auto turn = [](float &u, float &v, float c, float s) {
@@ -190,8 +225,8 @@ __global__ __launch_bounds__(256) void deft_heads(HeadsArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) turn(y1[2 * i], y1[2 * i + 1], c[i], s[i]);
     }
-    if (asked >= a.heads) return;
-    uint16_t *out = p.out + ((int64_t)(kind == kQ ? token : row) * p.out_token + (int64_t)head * p.out_head);
+    if (head >= p.heads) return;
+    uint16_t *out = p.out + ((int64_t)row * p.out_token + (int64_t)head * p.out_head);
     // bits as they are where nothing is done to them; none of it is read again here
     __builtin_nontemporal_store(turned0 || normed ? pack8(y0) : x0, reinterpret_cast<u32x4 *>(out + first));
     __builtin_nontemporal_store(turned1 || normed ? pack8(y1) : x1, reinterpret_cast<u32x4 *>(out + second));
@@ -201,13 +236,10 @@ __global__ __launch_bounds__(256) void deft_heads(HeadsArgs a) {
 
 constexpr uint64_t kMaxWaves = 1u << 22;  // of a launch
 
-template <int D, int TURN, bool NORM>
-void launch(const HeadsArgs &a, hipStream_t st) {
-    hipLaunchKernelGGL((deft_heads<D, TURN, NORM>), dim3((a.waves + 3) / 4), dim3(256), 0, st, a);
-}
 template <int D, int TURN>
 void launch(const HeadsArgs &a, bool norm, hipStream_t st) {
-    norm ? launch<D, TURN, true>(a, st) : launch<D, TURN, false>(a, st);
+    auto *kernel = norm ? &deft_heads<D, TURN, true> : &deft_heads<D, TURN, false>;
+    hipLaunchKernelGGL(kernel, dim3((a.waves + 3) / 4), dim3(256), 0, st, a);
 }
 template <int D>
 void launch(const HeadsArgs &a, int turn, bool norm, hipStream_t st) {
@@ -259,12 +291,11 @@ int run(const deft_heads_t *const (&parts)[kParts], int64_t n, int32_t d, float 
     if (rope && ((!positions && n > 0) || (reinterpret_cast<uintptr_t>(positions) & 3))) return DEFT_EINVAL;
     HeadsArgs a{};
     Area in[kParts], out[kParts];
-    uint32_t begin[kParts + 1] = {};
+    uint32_t heads = 0;
     bool norm = false, wide = false;
     for (int i = 0; i < kParts; ++i) {
         const deft_heads_t *p = parts[i];
         in[i] = out[i] = Area{};
-        begin[i + 1] = begin[i];
         if (!p || p->heads == 0) continue;
         if (p->heads < 0 || p->heads > DEFT_MAX_Q8_HEADS) return DEFT_EINVAL;
         if (p->weight) {
@@ -292,7 +323,8 @@ int run(const deft_heads_t *const (&parts)[kParts], int64_t n, int32_t d, float 
         t.out_head = in_place ? t.head : d;
         in[i] = area(p->x, n, p->heads, d, t.token, t.head);
         out[i] = area(p->out, stored ? pool : n, p->heads, d, t.out_token, t.out_head);
-        begin[i + 1] += (uint32_t)p->heads;
+        t.heads = (uint32_t)p->heads;
+        heads += t.heads;
     }
     for (int i = 0; i < kParts; ++i)
         for (int j = 0; j < kParts; ++j) {
@@ -300,11 +332,12 @@ int run(const deft_heads_t *const (&parts)[kParts], int64_t n, int32_t d, float 
             if (!(i == j && out[i].same(in[i])) && !apart(out[i], in[j])) return DEFT_EINVAL;
             if (j < i && !apart(out[i], out[j])) return DEFT_EINVAL;
         }
-    if (n == 0 || begin[kParts] == 0) return DEFT_OK;
-    a.k_begin = begin[kK];
-    a.v_begin = begin[kV];
-    a.heads = begin[kParts];
-    a.chunks = (a.heads + 64 / (d / 16) - 1) / (64 / (d / 16));
+    if (n == 0 || heads == 0) return DEFT_OK;
+    const uint32_t at_once = 64 / ((uint32_t)d / 16);  // heads of a wave
+    for (Part &p : a.part) {
+        p.chunk = a.chunks;
+        a.chunks += (p.heads + at_once - 1) / at_once;
+    }
     a.inv_chunks = inverse(a.chunks);
     a.positions = positions;
     a.entries = entries;

@@ -159,7 +159,7 @@ def launched(n):
     assert lib.deft_qkv_store(lst.handle, 4096, *pools, n, d, 0.0, 0.0, 4096, binding.deft_rope(64).packed, 1 << 12) == 0
     return list(fake.grid[:fake.launches])
 H = (H[0], H[1], H[1])
-chunks = -(-sum(H) // (64 // (d // 16)))
+chunks = sum(-(-h // (64 // (d // 16))) for h in H)  # a wave has heads of one kind
 most = {WAVES} // chunks
 for n, want in ((1, [1]), (most, [most]), (most + 1, [most, 1]), (2 * most + 3, [most, most, 3])):
     if n < 1 << 20:
