@@ -428,7 +428,7 @@ int deft_compact_pages(const int32_t *node_page_ptr, const int32_t *page_ids, in
  *                  are multiples of 8, from 0 (one row for all) to 2^40, x is 16-byte aligned; slices of a fused projection's output
  *                  need not be copied.
  *   out          : device bf16 [n, heads, d], contiguous, 16-byte aligned; or x itself: the heads are then changed where they are.
- *                  Otherwise what a call writes must not overlap what it reads, nor its other outputs.
+ *                  Otherwise what a call writes must not overlap anything it reads, nor its other outputs.
  *   weight       : NULL: no norm.  Otherwise device, 16-byte aligned, head h's d weights at weight + h * weight_stride (0: one for all
  *                  heads, else a multiple of 8 up to 4096); bf16, or float where weight_f32 is set (the same for queries and keys).
  *   heads        : 0 .. DEFT_MAX_Q8_HEADS
@@ -503,13 +503,14 @@ int deft_qkv_store(const deft_kv_list_t *list, const void *dev_image, const deft
  *
  * logits, out          : device [nq, vocab], queries (the caller's order) stride and out_stride elements apart, aligned as their type; the
  *                        strides are at most 2^31, out_stride at least vocab.  float where logits_f32, out_f32 are set, else bf16; bf16 logits may
- *                        become float ones.  out may be logits itself with its stride and type, otherwise they must not overlap.
+ *                        become float ones.  out may be logits itself with its stride and type, otherwise it
+ *                        must not overlap anything that the call reads.
  * vocab                : 1 .. DEFT_MAX_VOCAB
  * tokens               : device int32 [n_tokens], the token of every row of the KV cache that the plan is for (so a fork or a compaction copies
  *                        its pages like any pool's); at least deft_plan_rows(plan) of them.  Prompt tokens may have DEFT_TOKEN_PROMPT or-ed
  *                        to them: they count for the repetition penalty alone.  Negative numbers, and those from vocab on, are no token.
  * repetition, frequency, presence : device float [nq], by query.  Any of them asks for tokens.
- * bias                 : device float, rows bias_stride elements apart (at least vocab if there are two); bias_row: device int32 [nq], the row of each query,
+ * bias                 : device float, rows bias_stride elements apart (at least vocab if there are two, at most 2^31); bias_row: device int32 [nq], the row of each query,
  *                        none where it is outside 0 .. n_bias - 1; NULL: row 0 for all
  * mask, mask_row       : the same for masks: rows of (vocab + 31) / 32 words of 32 bits, mask_stride words apart, bit t % 32 of word t / 32 is
  *                        set where token t is allowed

@@ -326,12 +326,22 @@ int run(const deft_heads_t *const (&parts)[kParts], int64_t n, int32_t d, float 
         t.heads = (uint32_t)p->heads;
         heads += t.heads;
     }
-    for (int i = 0; i < kParts; ++i)
+    for (int i = 0; i < kParts; ++i)  // what is written is nobody else's, and nobody's input but the part's own, in place
         for (int j = 0; j < kParts; ++j) {
             if (out[i].begin == out[i].end) continue;
             if (!(i == j && out[i].same(in[i])) && !apart(out[i], in[j])) return DEFT_EINVAL;
             if (j < i && !apart(out[i], out[j])) return DEFT_EINVAL;
         }
+    for (int i = 0; i < kParts; ++i) {  // nor a weight or position
+        auto meets = [&](const void *p, int64_t bytes) {
+            const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+            return p && at < out[i].end && out[i].begin < at + (uint64_t)bytes;
+        };
+        if (out[i].begin == out[i].end) continue;
+        if (rope && meets(positions, 4 * n)) return DEFT_EINVAL;
+        for (int j = 0; j < kParts; ++j)
+            if (parts[j] && meets(parts[j]->weight, ((parts[j]->heads - 1) * parts[j]->weight_stride + d) * (wide ? 4 : 2))) return DEFT_EINVAL;
+    }
     if (n == 0 || heads == 0) return DEFT_OK;
     const uint32_t at_once = 64 / ((uint32_t)d / 16);  // heads of a wave
     for (Part &p : a.part) {

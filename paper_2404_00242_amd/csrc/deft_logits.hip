@@ -520,8 +520,9 @@ extern "C" int deft_adjust_logits(const deft_plan_t *plan, const void *dev_image
     if (!aligned4(l->repetition) || !aligned4(l->frequency) || !aligned4(l->presence) || !aligned4(l->bias) || !aligned4(l->mask) ||
         !aligned4(l->bias_row) || !aligned4(l->mask_row))
         return DEFT_EINVAL;
-    if (l->bias && (l->n_bias < 1 || l->bias_stride < (l->n_bias > 1 ? l->vocab : 0))) return DEFT_EINVAL;
-    if (l->mask && (l->n_masks < 1 || l->mask_stride < (l->n_masks > 1 ? (l->vocab + 31) / 32 : 0))) return DEFT_EINVAL;
+    if (l->reserved != 0) return DEFT_EINVAL;
+    if (l->bias && (l->n_bias < 1 || l->bias_stride < (l->n_bias > 1 ? l->vocab : 0) || l->bias_stride > kMaxStride)) return DEFT_EINVAL;
+    if (l->mask && (l->n_masks < 1 || l->mask_stride < (l->n_masks > 1 ? (l->vocab + 31) / 32 : 0) || l->mask_stride > kMaxStride)) return DEFT_EINVAL;
     if ((l->bias_row && !l->bias) || (l->mask_row && !l->mask)) return DEFT_EINVAL;
     const deft::Schedule *S = nullptr;
     if (history) {
@@ -535,10 +536,21 @@ extern "C" int deft_adjust_logits(const deft_plan_t *plan, const void *dev_image
     if (reinterpret_cast<uintptr_t>(l->logits) % in_bytes || reinterpret_cast<uintptr_t>(l->out) % out_bytes) return DEFT_EINVAL;
     if (nq > 1 && (l->stride < 0 || l->out_stride < l->vocab || l->stride > kMaxStride || l->out_stride > kMaxStride)) return DEFT_EINVAL;
     if (nq > 1 && (double)nq * (double)std::max(l->stride, l->out_stride) > 0x1p60) return DEFT_EINVAL;
+    if ((double)l->n_bias * (double)l->bias_stride > 0x1p60 || (double)l->n_masks * (double)l->mask_stride > 0x1p60) return DEFT_EINVAL;
     const bool in_place = l->out == l->logits && in_bytes == out_bytes && (nq == 1 || l->stride == l->out_stride);
     const uintptr_t in = reinterpret_cast<uintptr_t>(l->logits), out = reinterpret_cast<uintptr_t>(l->out);
     const uint64_t in_size = in_bytes * ((uint64_t)(nq - 1) * (uint64_t)l->stride + l->vocab), out_size = out_bytes * ((uint64_t)(nq - 1) * (uint64_t)l->out_stride + l->vocab);
+    auto meets = [&](const void *p, uint64_t bytes) {  // what is written
+        const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+        return p && at < out + out_size && out < at + bytes;
+    };
     if (!in_place && in < out + out_size && out < in + in_size) return DEFT_EINVAL;
+    const uint64_t words = ((uint64_t)l->vocab + 31) / 32, of_queries = 4 * (uint64_t)nq;
+    if (meets(l->bias, 4 * ((uint64_t)(l->n_bias - 1) * (uint64_t)l->bias_stride + l->vocab)) || meets(l->bias_row, of_queries) ||
+        meets(l->mask, 4 * ((uint64_t)(l->n_masks - 1) * (uint64_t)l->mask_stride + words)) || meets(l->mask_row, of_queries) ||
+        meets(l->repetition, of_queries) || meets(l->frequency, of_queries) || meets(l->presence, of_queries) ||
+        (history && meets(l->tokens, 4 * (uint64_t)l->n_tokens)))
+        return DEFT_EINVAL;
     LogitsArgs a{};
     a.logits = l->logits;
     a.out = l->out;

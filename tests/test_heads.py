@@ -110,6 +110,10 @@ def test_calls_that_are_refused():
     for bad in (dict(weight=(1 << 12) + 4), dict(weight=1 << 12, step=4), dict(weight=1 << 12, step=-64), dict(weight=1 << 12, step=8192),
                 dict(weight=1 << 12, wide=1), dict(out=1 << 20), dict(out=(1 << 24) + 1024), dict(out=(1 << 20) + 1024)):
         assert norm(q, _part(x=1 << 21, **{"out": 1 << 25, **bad})) == EINVAL, bad
+    # what is written meets a weight or the positions
+    for out in ((1 << 12) - 1000, (1 << 12) - 4080):
+        assert norm(_part(weight=1 << 16, out=out & ~15), None) == EINVAL
+    assert norm(_part(weight=(1 << 24) + 2048), None) == norm(_part(), _part(x=1 << 21, out=1 << 25, weight=(1 << 24) - 16)) == EINVAL
     # one tensor twice, in place
     assert norm(_part(out=1 << 20), _part(out=1 << 20)) == EINVAL
     assert norm(None, None, n=0) == 0

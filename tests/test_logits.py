@@ -9,7 +9,7 @@ import torch
 from oracle import logits as model
 from paper_2404_00242_amd import binding, workloads as wl
 
-EINVAL, ENOTREADY = -1, -5
+EINVAL, EWORKSPACE, ENOTREADY = -1, -3, -5
 PROMPT = binding.DEFT_TOKEN_PROMPT
 
 
@@ -29,9 +29,9 @@ def test_calls_that_are_refused():
     plan = plan_of(t)[0]
     rows = plan.limits()[1]
 
-    def call(plan=plan.handle, image=0, group=1, logits=1 << 20, out=1 << 24, stride=1000, out_stride=1000, vocab=1000, wide=1, out_wide=1, n_bias=0, n_masks=0,
+    def call(plan=plan.handle, image=0, group=1, logits=1 << 20, out=1 << 24, stride=1000, out_stride=1000, vocab=1000, wide=1, out_wide=1, n_bias=0, n_masks=0, reserved=0,
              tokens=0, n_tokens=0, repetition=0, frequency=0, presence=0, bias=0, bias_row=0, bias_stride=0, mask=0, mask_row=0, mask_stride=0):
-        packed = binding._pack_logits(logits, out, stride, out_stride, vocab, wide, out_wide, n_bias, n_masks, 0, tokens, n_tokens, repetition, frequency,
+        packed = binding._pack_logits(logits, out, stride, out_stride, vocab, wide, out_wide, n_bias, n_masks, reserved, tokens, n_tokens, repetition, frequency,
                                       presence, bias, bias_row, bias_stride, mask, mask_row, mask_stride)
         return lib.deft_adjust_logits(plan, image, group, packed, None, 0, None)
 
@@ -42,13 +42,20 @@ def test_calls_that_are_refused():
                 dict(out=(1 << 20) + 4), dict(out=1 << 20, out_stride=1001), dict(out=1 << 20, wide=0), dict(out=(1 << 20) - 8000),
                 dict(bias=at), dict(bias=at + 2, n_bias=1), dict(bias=at, n_bias=-1), dict(bias=at, n_bias=2, bias_stride=999), dict(bias_row=at),
                 dict(bias=at, n_bias=1, bias_row=at + 1), dict(mask=at), dict(mask=at + 2, n_masks=1), dict(mask=at, n_masks=2, mask_stride=31), dict(mask_row=at),
-                dict(mask=at, n_masks=1, mask_row=at + 2),
+                dict(mask=at, n_masks=1, mask_row=at + 2), dict(reserved=1), dict(bias=at, n_bias=2, bias_stride=1 << 32), dict(mask=at, n_masks=2, mask_stride=1 << 32),
+                # what is written meets what is read
+                dict(bias=(1 << 24) + 12000, n_bias=1), dict(bias=(1 << 24) - 4000, n_bias=3, bias_stride=1000), dict(bias=at, n_bias=1, bias_row=(1 << 24) + 4),
+                dict(mask=(1 << 24) - 4, n_masks=1), dict(mask=at, n_masks=1, mask_row=(1 << 24) + 15996),
                 dict(repetition=at), dict(frequency=at, tokens=at, n_tokens=rows - 1), dict(presence=at + 2, tokens=at, n_tokens=rows),
                 dict(presence=at, tokens=at + 2, n_tokens=rows), dict(repetition=at, tokens=at, n_tokens=rows), dict(repetition=at, tokens=at, n_tokens=rows, image=at + 8),
                 dict(repetition=at, tokens=at, n_tokens=rows, image=at, group=0)):
         assert call(**bad) == EINVAL, bad
     assert lib.deft_adjust_logits(plan.handle, None, 1, None, None, 0, None) == EINVAL
-    assert call(repetition=at, tokens=at, n_tokens=rows, image=at, group=3) == ENOTREADY
+    history = dict(tokens=at, n_tokens=rows, image=1 << 16, group=3)
+    assert call(repetition=at, **history) == ENOTREADY
+    assert lib.deft_plan_upload(plan.handle, 3, 1, 1 << 16, 0, None) == EWORKSPACE  # (the schedule is made, nothing is copied)
+    for bad in (dict(repetition=(1 << 24) + 8), dict(presence=(1 << 24) - 12), dict(frequency=1 << 24), dict(repetition=at, tokens=(1 << 24) - 4)):
+        assert call(**{**history, **bad}) == EINVAL, bad
     nobody = binding.deft_plan(t.node_tok_begin, t.node_tok_len, t.node_parent, [], t.ntok)
     assert call(plan=nobody.handle, logits=0, out=0) == 0
     with pytest.raises(binding.DeftError):
