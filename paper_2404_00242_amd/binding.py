@@ -931,31 +931,23 @@ def deft_rope(rot: int, base: float = 10000.0, layout: str = "half", scaling: st
 _pack_heads = struct.Struct("PqqPPqii").pack  # deft_heads_t
 
 
-def _heads(t, n, d, index, bf16, what: str, name: str):
-    """(address, strides, number of heads) of bf16 [n, heads, d]."""
-    shape = t.shape
-    if t.dtype is not bf16 or len(shape) != 3 or t.get_device() != index or index < 0:
-        raise DeftError(-1, f"{what}: {name} must be a 3-d bf16 tensor, on one device with the others (there is no CPU path)")
-    n2, heads, d2 = shape
-    token, head, one = t.stride()
-    if n2 != n or d2 != d or heads >= 1 << 31 or (one != 1 and n and heads):
-        raise DeftError(-1, f"{what}: {name} must be [{n}, heads, {d}], the elements of a head contiguous")
-    if n < 2:  # (one token's or head's stride says nothing)
-        token = heads * d
-    if heads < 2:
-        head = d
-    return t.data_ptr(), token, head, heads
+# The checks of the three calls below stand in line: of a decode iteration's call, whose kernel takes 4 us, the host's part is what is
+# waited for, and every helper called is 0.1 us more.  (Strides of one token or one head say nothing and are put right.)
+
+def _heads_error(what: str, tensors, n=None, d=None):
+    """What is wrong with heads that were refused."""
+    for name, t in tensors:
+        if t.dtype != _torch.bfloat16 or t.dim() != 3 or t.get_device() < 0:
+            return DeftError(-1, f"{what}: {name} must be a 3-d bf16 device tensor (there is no CPU path)")
+    first = tensors[0][1].shape
+    n, d = first[0] if n is None else n, first[2] if d is None else d
+    return DeftError(-1, f"{what}: {', '.join(name for name, _ in tensors)} must be [{n}, heads, {d}] on one device, the elements of a head contiguous")
 
 
 def _heads_out(out, t, at, bf16, raw, index, elsewhere, what: str, name: str):
     """(a result for the heads t, made if none is given; its address)"""
-    if out is None:  # (see deft_tree_attn_decode)
-        if elsewhere:
-            out = _result(raw, index, t.shape, bf16)
-        elif type(t) is _torch.Tensor:
-            out = _torch.empty_like(t, memory_format=_torch.contiguous_format)
-        else:
-            out = _torch.empty(t.shape, dtype=bf16, device=t.device)
+    if out is None:
+        out = _result(raw, index, t.shape, bf16) if elsewhere else _torch.empty(t.shape, dtype=bf16, device=t.device)
         return out, out.data_ptr()
     if out.dtype is not bf16 or out.shape != t.shape or out.get_device() != index:
         raise DeftError(-1, f"{what}: {name} must be bf16 {list(t.shape)}, on the input's device")
@@ -981,13 +973,8 @@ def _head_weight(w, heads, d, index, bf16, what: str, name: str):
 _NO_WEIGHT = 0, 0, 0
 
 
-def _turn(positions, rope, n, index, what: str):
-    """(address of the positions, a deft_rope_t), or twice None without a rope: positions are not looked at then."""
-    if rope is None:
-        return None, None
-    if positions is None or positions.dtype is not _torch.int32 or positions.shape != (n,) or positions.get_device() != index or not positions.is_contiguous():
-        raise DeftError(-1, f"{what}: positions must be a contiguous int32 [{n}] tensor on the input's device")
-    return positions.data_ptr() or 4, rope.packed  # (of none: anything)
+def _positions_error(what: str, n):
+    return DeftError(-1, f"{what}: positions must be a contiguous int32 [{n}] tensor on the input's device")
 
 
 def deft_rotate(x, positions, rope: Rope, out=None, stream=None):
@@ -995,19 +982,32 @@ def deft_rotate(x, positions, rope: Rope, out=None, stream=None):
     int32 [n].  Returns bf16 [n, H, d]; out=x turns them in place.  Asynchronous on `stream` (default: torch's current stream); the
     current stream has to wait for another one before it reads the result."""
     torch = _torch or _get_torch()
-    index, bf16 = x.get_device(), torch.bfloat16
-    if x.dim() != 3 or rope is None:
-        raise DeftError(-1, "deft_rotate: x must be a 3-d tensor, and a rope be given")
-    n, _, d = x.shape
-    at, token, head, H = _heads(x, n, d, index, bf16, "deft_rotate", "x")
-    pos, packed = _turn(positions, rope, n, index, "deft_rotate")
-    raw = _raw_stream(stream, index)
-    elsewhere = stream is not None and raw != torch._C._cuda_getCurrentRawStream(index)
-    out, to = _heads_out(out, x, at, bf16, raw, index, elsewhere, "deft_rotate", "out")
+    index, bf16, shape = x.get_device(), torch.bfloat16, x.shape
+    if x.dtype is not bf16 or len(shape) != 3 or index < 0:
+        raise _heads_error("deft_rotate", [("x", x)])
+    n, H, d = shape
+    token, head, one = x.stride()
+    if (one != 1 and n and H) or H >= 1 << 31:
+        raise _heads_error("deft_rotate", [("x", x)])
+    if n < 2:
+        token = H * d
+    if H < 2:
+        head = d
+    if rope is None or positions is None or positions.dtype is not torch.int32 or positions.shape != (n,) or positions.get_device() != index or not positions.is_contiguous():
+        raise DeftError(-1, "deft_rotate: a rope is needed") if rope is None else _positions_error("deft_rotate", n)
+    at = x.data_ptr()
+    if out is None and stream is None and type(x) is torch.Tensor:  # (see deft_tree_attn_decode)
+        raw = torch._C._cuda_getCurrentRawStream(index)
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+        to = out.data_ptr()
+    else:
+        raw = _raw_stream(stream, index)
+        elsewhere = stream is not None and raw != torch._C._cuda_getCurrentRawStream(index)
+        out, to = _heads_out(out, x, at, bf16, raw, index, elsewhere, "deft_rotate", "out")
     if torch._C._cuda_getDevice() != index:
         with torch.cuda.device(index):
             return deft_rotate(x, positions, rope, out, raw)
-    rc = (_lib or load_library()).deft_rotate(_pack_heads(at, token, head, to, 0, 0, 0, H), n, d, pos, packed, raw)
+    rc = (_lib or load_library()).deft_rotate(_pack_heads(at, token, head, to, 0, 0, 0, H), n, d, positions.data_ptr() or 4, rope.packed, raw)
     if rc != 0:
         _check(rc, "deft_rotate")
     return out
@@ -1021,20 +1021,40 @@ def deft_qk_norm_rotate(q, k, q_weight=None, k_weight=None, positions=None, rope
     inputs themselves.  Otherwise as deft_rotate."""
     torch = _torch or _get_torch()
     what, index, bf16 = "deft_qk_norm_rotate", q.get_device(), torch.bfloat16
-    if q.dim() != 3:
-        raise DeftError(-1, "deft_qk_norm_rotate: q must be a 3-d tensor")
-    n, _, d = q.shape
-    q_at, q_token, q_head, Hq = _heads(q, n, d, index, bf16, what, "q")
-    k_at, k_token, k_head, Hkv = _heads(k, n, d, index, bf16, what, "k")
+    shape, k_shape = q.shape, k.shape
+    if q.dtype is not bf16 or k.dtype is not bf16 or len(shape) != 3 or len(k_shape) != 3 or index < 0 or k.get_device() != index:
+        raise _heads_error(what, [("q", q), ("k", k)])
+    n, Hq, d = shape
+    k_n, Hkv, k_d = k_shape
+    q_token, q_head, q_one = q.stride()
+    k_token, k_head, k_one = k.stride()
+    if k_n != n or k_d != d or (q_one != 1 and n and Hq) or (k_one != 1 and n and Hkv) or Hq >= 1 << 31 or Hkv >= 1 << 31:
+        raise _heads_error(what, [("q", q), ("k", k)])
+    if n < 2:
+        q_token, k_token = Hq * d, Hkv * d
+    if Hq < 2:
+        q_head = d
+    if Hkv < 2:
+        k_head = d
+    q_at, k_at = q.data_ptr(), k.data_ptr()
     qw, qw_head, q_wide = _NO_WEIGHT if q_weight is None else _head_weight(q_weight, Hq, d, index, bf16, what, "q_weight")
     kw, kw_head, k_wide = _NO_WEIGHT if k_weight is None else _head_weight(k_weight, Hkv, d, index, bf16, what, "k_weight")
     if q_wide != k_wide and qw and kw:
         raise DeftError(-1, "deft_qk_norm_rotate: weights must be of one type")
-    pos, packed = _turn(positions, rope, n, index, what)
-    raw = _raw_stream(stream, index)
-    elsewhere = stream is not None and raw != torch._C._cuda_getCurrentRawStream(index)
-    q_out, q_to = _heads_out(q_out, q, q_at, bf16, raw, index, elsewhere, what, "q_out")
-    k_out, k_to = _heads_out(k_out, k, k_at, bf16, raw, index, elsewhere, what, "k_out")
+    packed = pos = None
+    if rope is not None:
+        if positions is None or positions.dtype is not torch.int32 or positions.shape != (n,) or positions.get_device() != index or not positions.is_contiguous():
+            raise _positions_error(what, n)
+        pos, packed = positions.data_ptr() or 4, rope.packed  # (of none: anything)
+    if q_out is None and k_out is None and stream is None and type(q) is type(k) is torch.Tensor:
+        raw, dense = torch._C._cuda_getCurrentRawStream(index), torch.contiguous_format
+        q_out, k_out = torch.empty_like(q, memory_format=dense), torch.empty_like(k, memory_format=dense)
+        q_to, k_to = q_out.data_ptr(), k_out.data_ptr()
+    else:
+        raw = _raw_stream(stream, index)
+        elsewhere = stream is not None and raw != torch._C._cuda_getCurrentRawStream(index)
+        q_out, q_to = _heads_out(q_out, q, q_at, bf16, raw, index, elsewhere, what, "q_out")
+        k_out, k_to = _heads_out(k_out, k, k_at, bf16, raw, index, elsewhere, what, "k_out")
     if torch._C._cuda_getDevice() != index:
         with torch.cuda.device(index):
             return deft_qk_norm_rotate(q, k, q_weight, k_weight, positions, rope, eps, weight_offset, q_out, k_out, raw)
@@ -1058,43 +1078,71 @@ def deft_qkv_store(rows: KVList, q, k, v, cache, positions=None, rope=None, q_we
         raise DeftError(-1, "deft_qkv_store: cache must be the K and V pools of a bf16 cache (deft_kv_store_q8 stores into one of 8 bits)")
     if rows.block_rows == 0:
         raise DeftError(-1, "deft_qkv_store: the list is one of copies, not of rows")
-    if k.dim() != 3:
-        raise DeftError(-1, "deft_qkv_store: k must be a 3-d tensor")
-    n, _, d = k.shape
+    shape = k.shape
+    if k.dtype is not bf16 or v.dtype is not bf16 or v.shape != shape or len(shape) != 3 or index < 0 or v.get_device() != index:
+        raise _heads_error(what, [("k", k), ("v", v)])
+    n, Hkv, d = shape
     if n != rows.n:
         raise DeftError(-1, f"deft_qkv_store: the list has {rows.n} rows, not {n}")
-    k_at, k_token, k_head, Hkv = _heads(k, n, d, index, bf16, what, "k")
-    v_at, v_token, v_head, Hv = _heads(v, n, d, index, bf16, what, "v")
+    k_token, k_head, k_one = k.stride()
+    v_token, v_head, v_one = v.stride()
+    if ((k_one != 1 or v_one != 1) and n and Hkv) or Hkv >= 1 << 31:
+        raise _heads_error(what, [("k", k), ("v", v)])
+    if n < 2:
+        k_token = v_token = Hkv * d
+    if Hkv < 2:
+        k_head = v_head = d
     k_pool, v_pool = cache
-    shape = k_pool.shape
-    if (Hv != Hkv or len(shape) != 3 or shape[1] != Hkv or shape[2] != d or v_pool.shape != shape or k_pool.dtype is not bf16 or v_pool.dtype is not bf16
+    pool = k_pool.shape
+    if (len(pool) != 3 or pool[1] != Hkv or pool[2] != d or v_pool.shape != pool or k_pool.dtype is not bf16 or v_pool.dtype is not bf16
             or not (k_pool.is_contiguous() and v_pool.is_contiguous()) or k_pool.get_device() != index or v_pool.get_device() != index):
         raise DeftError(-1, f"deft_qkv_store: the pools must both be contiguous bf16 [n_rows, {Hkv}, {d}] tensors on the heads' device")
-    n_rows = shape[0]
+    n_rows = pool[0]
     if rows.pool > n_rows or n_rows >= 1 << 31:
         raise DeftError(-1, "deft_qkv_store: the list is for a larger cache, or the cache larger than 32 bits hold")
-    raw = _raw_stream(stream, index)
+    raw = torch._C._cuda_getCurrentRawStream(index) if stream is None else _raw_stream(stream, index)
     kw, kw_head, wide = _NO_WEIGHT if k_weight is None else _head_weight(k_weight, Hkv, d, index, bf16, what, "k_weight")
     q_heads = None
     if q is not None:
-        q_at, q_token, q_head, Hq = _heads(q, n, d, index, bf16, what, "q")
+        shape = q.shape
+        if q.dtype is not bf16 or len(shape) != 3 or shape[0] != n or shape[2] != d or q.get_device() != index:
+            raise _heads_error(what, [("q", q)], n, d)
+        Hq = shape[1]
+        q_token, q_head, q_one = q.stride()
+        if (q_one != 1 and n and Hq) or Hq >= 1 << 31:
+            raise _heads_error(what, [("q", q)], n, d)
+        if n < 2:
+            q_token = Hq * d
+        if Hq < 2:
+            q_head = d
         qw, qw_head, q_wide = _NO_WEIGHT if q_weight is None else _head_weight(q_weight, Hq, d, index, bf16, what, "q_weight")
         if q_wide != wide and qw and kw:
             raise DeftError(-1, "deft_qkv_store: weights must be of one type")
-        elsewhere = stream is not None and raw != torch._C._cuda_getCurrentRawStream(index)
-        q_out, to = _heads_out(q_out, q, q_at, bf16, raw, index, elsewhere, what, "q_out")
+        q_at = q.data_ptr()
+        if q_out is None and stream is None and type(q) is torch.Tensor:
+            q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            to = q_out.data_ptr()
+        else:
+            elsewhere = stream is not None and raw != torch._C._cuda_getCurrentRawStream(index)
+            q_out, to = _heads_out(q_out, q, q_at, bf16, raw, index, elsewhere, what, "q_out")
         q_heads = _pack_heads(q_at, q_token, q_head, to, qw, qw_head, q_wide, Hq)
     elif q_weight is not None or q_out is not None:
         raise DeftError(-1, "deft_qkv_store: without q it has neither weights nor a result")
-    pos, packed = _turn(positions, rope, n, index, what)
+    packed = pos = None
+    if rope is not None:
+        if positions is None or positions.dtype is not torch.int32 or positions.shape != (n,) or positions.get_device() != index or not positions.is_contiguous():
+            raise _positions_error(what, n)
+        pos, packed = positions.data_ptr() or 4, rope.packed  # (of none: anything)
     if n == 0:
         return q_out
     if torch._C._cuda_getDevice() != index:
         with torch.cuda.device(index):
             return deft_qkv_store(rows, q, k, v, cache, positions, rope, q_weight, k_weight, eps, weight_offset, q_out, raw)
+    image = rows._images.of.get(index) if raw == 0 else None  # (the null stream is in no capture)
+    image = image.tensor if image is not None and raw in image.streams else rows._image(index, raw)
     rc = (_lib or load_library()).deft_qkv_store(
-        rows._h, rows._image(index, raw).data_ptr(), q_heads, _pack_heads(k_at, k_token, k_head, k_pool.data_ptr(), kw, kw_head, wide, Hkv),
-        _pack_heads(v_at, v_token, v_head, v_pool.data_ptr(), 0, 0, 0, Hkv), n_rows, d, eps, weight_offset, pos, packed, raw)
+        rows._h, image.data_ptr(), q_heads, _pack_heads(k.data_ptr(), k_token, k_head, k_pool.data_ptr(), kw, kw_head, wide, Hkv),
+        _pack_heads(v.data_ptr(), v_token, v_head, v_pool.data_ptr(), 0, 0, 0, Hkv), n_rows, d, eps, weight_offset, pos, packed, raw)
     if rc != 0:
         _check(rc, what)
     return q_out

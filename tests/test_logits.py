@@ -206,6 +206,22 @@ def test_without_a_workspace_and_with_a_large_vocabulary(counts, page):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("counts", [False, True])
+@pytest.mark.parametrize("page", [0, 64])
+def test_more_tokens_than_are_taken_at_a_time(counts, page):
+    # sorted tokens come in groups of 1024, of which 256 are looked at together; unsorted pieces 512 together
+    t = wl.config2_fewshot(prefix=290_000, branches=3, gen=20_000)
+    s = Inputs(t, 5000, page, True)
+    plan, row_of, pool = plan_of(t, 1024, 0, page, 1)
+    plan.image(t.Hq, t.Hkv, dev())
+    which = dict(repetition=True, presence=True, frequency=counts)
+    got = s.call(plan, row_of, pool, **which)
+    close(got, *s.want(**which))
+    plan._logits_workspace = lambda *args: (0, 0)
+    assert torch.equal(s.call(plan, row_of, pool, **which), got)
+
+
+@pytest.mark.gpu
 def test_one_token_more_often_than_sixteen_bits_hold():
     t = wl.config2_fewshot(prefix=70000, branches=3, gen=5)
     s = Inputs(t, 2000, 1, True, prompts=False)
