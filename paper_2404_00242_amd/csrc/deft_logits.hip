@@ -60,8 +60,8 @@ constexpr int kThreads = 512;
 constexpr int kTile = 1024;       // logits of a row to a workgroup
 constexpr int kMost = 8;          // rows
 constexpr uint32_t kEach = kTile / kThreads;  // to a thread
-constexpr int kPieces = 512;      // at a time
-constexpr int kGroups = 256;      // at a time: the less LDS, the more workgroups to a compute unit
+constexpr int kPieces = 512;      // of the tree that are looked at together
+constexpr int kGroups = 256;      // of sorted tokens that are
 static_assert(kEach == 2, "a row ends behind a thread's logits, or behind the first of them");
 constexpr int kSortThreads = 1024;
 constexpr int kRun = 1024;        // tokens that deft_sort_tokens takes to a workgroup
@@ -466,7 +466,8 @@ int64_t tokens_of(const deft_plan_t *plan) {
     }
     return total;
 }
-// A row is cut into tiles, and as many rows to a workgroup as still leave kFill of them.
+// A row is cut into tiles, and as many rows to a workgroup as still leave kFill of them (us with 256, 512, 768 and 1024 of them: 20 x
+// 128000 12.0, 11.3, 10.9, 13.9, 64 x 50001 14.0, 14.2, 16.1, 18.8, one query the same with all).
 struct Shape {
     uint32_t tiles, block;
     uint64_t groups;
