@@ -118,18 +118,18 @@ def test_calls_that_are_refused():
     assert norm(_part(out=1 << 20), _part(out=1 << 20)) == EINVAL
     assert norm(None, None, n=0) == 0
 
-    rows = binding.deft_kv_rows([3, 1], 8, 4)
+    rows, none, copies = binding.deft_kv_rows([3, 1], 8, 4), binding.deft_kv_rows([], 8, 4), binding.deft_kv_copies([0], [1], 8)
     k, v = _part(), _part(x=1 << 21, out=1 << 25)
 
     def store(lst=rows.handle, image=1 << 16, q=None, k=k, v=v, n_rows=8, d=64, eps=0.0, positions=pos, rope=rope):
         return lib.deft_qkv_store(lst, image, q, k, v, n_rows, d, eps, 0.0, positions, rope, None)
 
-    for bad in (dict(lst=None), dict(lst=binding.deft_kv_copies([0], [1], 8).handle), dict(image=None), dict(image=24), dict(k=None), dict(v=None), dict(n_rows=7),
+    for bad in (dict(lst=None), dict(lst=copies.handle), dict(image=None), dict(image=24), dict(k=None), dict(v=None), dict(n_rows=7),
                 dict(n_rows=-1), dict(v=_part(x=1 << 21, out=1 << 25, heads=3)), dict(k=_part(heads=0), v=_part(heads=0)),
                 dict(v=_part(x=1 << 21, out=1 << 25, weight=1 << 12)), dict(v=_part(x=1 << 21)), dict(v=_part(x=1 << 21, out=(1 << 24) + 8 * 512 - 16)),
                 dict(k=_part(out=1 << 20)), dict(q=_part(x=1 << 22, out=1 << 24)), dict(q=_part(x=(1 << 25) + 16, out=1 << 26)), dict(d=256)):
         assert store(**bad) == EINVAL, bad
-    assert store(lst=binding.deft_kv_rows([], 8, 4).handle, rope=None, positions=None) == 0
+    assert store(lst=none.handle, rope=None, positions=None) == 0
 
 
 def test_cpu_tensors_are_refused():
