@@ -485,6 +485,10 @@ int deft_rope(const double *frequency, int32_t rot, int32_t layout, double facto
  * (deft_kv_rows; its blocks have no part in it): k->out and v->out are the K and V pools [n_rows, Hkv, d].  Values are copied bit for
  * bit.  Other rows stay as they are.  q may be NULL; its out is as for the calls above.  n is the list's.
  *
+ * deft_qkv_store_q8 stores them into an 8-bit cache, and leaves it as deft_qk_norm_rotate (into bf16 keys) and deft_kv_store_q8 after it
+ * would, byte for byte: the scales, the rows kept of a block and those behind them, infinities and NaN as there.  The out of k and v
+ * is not looked at; both have the cache's Hkv heads of its d elements.
+ *
  * d is 64 or 128.  Asynchronous on `stream`.  Errors: DEFT_EINVAL (null, misaligned, a stride, size, eps (finite, >= 0) or weight_offset
  * outside of what is said here, a value with a weight, a list of copies or for a larger cache, memory that overlaps), DEFT_EHIP.
  */
@@ -493,6 +497,9 @@ int deft_qk_norm_rotate(const deft_heads_t *q, const deft_heads_t *k, int32_t n,
                         const int32_t *positions, const deft_rope_t *rope, void *stream);
 int deft_qkv_store(const deft_kv_list_t *list, const void *dev_image, const deft_heads_t *q, const deft_heads_t *k, const deft_heads_t *v,
                    int32_t n_rows, int32_t d, float eps, float weight_offset, const int32_t *positions, const deft_rope_t *rope, void *stream);
+int deft_qkv_store_q8(const deft_kv_list_t *list, const void *dev_image, const deft_heads_t *q, const deft_heads_t *k, const deft_heads_t *v,
+                      const deft_cache_q8_t *cache, float eps, float weight_offset, const int32_t *positions, const deft_rope_t *rope,
+                      void *stream);
 
 /*
  * The logits of each query's next token, float or bf16, bent by what its path holds, by biases and by grammar masks.  For the logit x of

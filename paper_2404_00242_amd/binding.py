@@ -42,7 +42,8 @@ EXPORTS = (
     "deft_tree_attn_decode", "deft_tree_attn_decode_static", "deft_stage1_partial_attention", "deft_stage2_global_reduction",
     "deft_tree_attn_decode_q8", "deft_kv_rows", "deft_kv_copies", "deft_kv_list_device_bytes", "deft_kv_list_upload", "deft_kv_list_destroy",
     "deft_kv_store_q8", "deft_kv_load_q8", "deft_kv_copy_pages", "deft_compact_pages",
-    "deft_rope_frequencies", "deft_rope", "deft_rotate", "deft_qk_norm_rotate", "deft_qkv_store", "deft_logits_workspace_bytes", "deft_adjust_logits",
+    "deft_rope_frequencies", "deft_rope", "deft_rotate", "deft_qk_norm_rotate", "deft_qkv_store", "deft_qkv_store_q8", "deft_logits_workspace_bytes",
+    "deft_adjust_logits",
     "deft_hbm_read_probe", "deft_plan_destroy", "deft_strerror", "deft_last_hip_error",
 )
 
@@ -170,6 +171,8 @@ def load_library():
     lib.deft_qk_norm_rotate.argtypes = [heads, heads, c32, c32, f32, f32, vp, rope, vp]
     lib.deft_qkv_store.restype = ctypes.c_int
     lib.deft_qkv_store.argtypes = [vp, vp, heads, heads, heads, c32, c32, f32, f32, vp, rope, vp]
+    lib.deft_qkv_store_q8.restype = ctypes.c_int
+    lib.deft_qkv_store_q8.argtypes = [vp, vp, heads, heads, heads, cache, f32, f32, vp, rope, vp]
     lib.deft_adjust_logits.restype = ctypes.c_int
     lib.deft_adjust_logits.argtypes = [vp, vp, c32, vp, vp, csz, vp]
     lib.deft_logits_workspace_bytes.restype = csz
@@ -1070,20 +1073,36 @@ def deft_qkv_store(rows: KVList, q, k, v, cache, positions=None, rope=None, q_we
                    weight_offset: float = 0.0, q_out=None, stream=None):
     """What deft_qk_norm_rotate does to the heads of new tokens, keys and values put into a bf16 cache at once: token i into row
     rows[i] of the list (deft_kv_rows, of any block_rows), values bit for bit.  cache: the K and V pools, contiguous bf16
-    [n_rows, Hkv, d].  q may be None.  Returns the queries, bf16 [n, Hq, d].  Otherwise as deft_qk_norm_rotate.  (An 8-bit cache
-    takes deft_qk_norm_rotate and deft_kv_store_q8.)"""
+    [n_rows, Hkv, d].  q may be None.  Returns the queries, bf16 [n, Hq, d].  Otherwise as deft_qk_norm_rotate."""
+    return _qkv_store(False, rows, q, k, v, cache, positions, rope, q_weight, k_weight, eps, weight_offset, q_out, stream)
+
+
+def deft_qkv_store_q8(rows: KVList, q, k, v, cache: CacheQ8, positions=None, rope=None, q_weight=None, k_weight=None, eps: float = 1e-6,
+                      weight_offset: float = 0.0, q_out=None, stream=None):
+    """What deft_qk_norm_rotate does to the heads of new tokens, keys and values put into an 8-bit cache at once as by deft_kv_store_q8,
+    with the same bytes: the keys that are rounded to 8 bits are those that deft_qk_norm_rotate returns.  q may be None.  Returns the
+    queries, bf16 [n, Hq, d].  Otherwise as the two."""
+    return _qkv_store(True, rows, q, k, v, cache, positions, rope, q_weight, k_weight, eps, weight_offset, q_out, stream)
+
+
+def _qkv_store(q8, rows, q, k, v, cache, positions, rope, q_weight, k_weight, eps, weight_offset, q_out, stream):
     torch = _torch or _get_torch()
-    what, index, bf16 = "deft_qkv_store", k.get_device(), torch.bfloat16
-    if len(cache) != 2:
-        raise DeftError(-1, "deft_qkv_store: cache must be the K and V pools of a bf16 cache (deft_kv_store_q8 stores into one of 8 bits)")
-    if rows.block_rows == 0:
-        raise DeftError(-1, "deft_qkv_store: the list is one of copies, not of rows")
+    index, bf16 = k.get_device(), torch.bfloat16
+    if q8:
+        what = "deft_qkv_store_q8"
+        c, cache_index, _, cache_heads, cache_d = _rows_for(rows, cache, what)
+    else:
+        what = "deft_qkv_store"
+        if len(cache) != 2:
+            raise DeftError(-1, "deft_qkv_store: cache must be the K and V pools of a bf16 cache (deft_qkv_store_q8 stores into one of 8 bits)")
+        if rows.block_rows == 0:
+            raise DeftError(-1, "deft_qkv_store: the list is one of copies, not of rows")
     shape = k.shape
     if k.dtype is not bf16 or v.dtype is not bf16 or v.shape != shape or len(shape) != 3 or index < 0 or v.get_device() != index:
         raise _heads_error(what, [("k", k), ("v", v)])
     n, Hkv, d = shape
     if n != rows.n:
-        raise DeftError(-1, f"deft_qkv_store: the list has {rows.n} rows, not {n}")
+        raise DeftError(-1, f"{what}: the list has {rows.n} rows, not {n}")
     k_token, k_head, k_one = k.stride()
     v_token, v_head, v_one = v.stride()
     if ((k_one != 1 or v_one != 1) and n and Hkv) or Hkv >= 1 << 31:
@@ -1092,14 +1111,20 @@ def deft_qkv_store(rows: KVList, q, k, v, cache, positions=None, rope=None, q_we
         k_token = v_token = Hkv * d
     if Hkv < 2:
         k_head = v_head = d
-    k_pool, v_pool = cache
-    pool = k_pool.shape
-    if (len(pool) != 3 or pool[1] != Hkv or pool[2] != d or v_pool.shape != pool or k_pool.dtype is not bf16 or v_pool.dtype is not bf16
-            or not (k_pool.is_contiguous() and v_pool.is_contiguous()) or k_pool.get_device() != index or v_pool.get_device() != index):
-        raise DeftError(-1, f"deft_qkv_store: the pools must both be contiguous bf16 [n_rows, {Hkv}, {d}] tensors on the heads' device")
-    n_rows = pool[0]
-    if rows.pool > n_rows or n_rows >= 1 << 31:
-        raise DeftError(-1, "deft_qkv_store: the list is for a larger cache, or the cache larger than 32 bits hold")
+    if q8:
+        if Hkv != cache_heads or d != cache_d or index != cache_index:
+            raise DeftError(-1, f"{what}: k and v must have the cache's {cache_heads} heads of {cache_d}, on its device")
+        k_pool = v_pool = 0
+    else:
+        k_pool, v_pool = cache
+        pool = k_pool.shape
+        if (len(pool) != 3 or pool[1] != Hkv or pool[2] != d or v_pool.shape != pool or k_pool.dtype is not bf16 or v_pool.dtype is not bf16
+                or not (k_pool.is_contiguous() and v_pool.is_contiguous()) or k_pool.get_device() != index or v_pool.get_device() != index):
+            raise DeftError(-1, f"deft_qkv_store: the pools must both be contiguous bf16 [n_rows, {Hkv}, {d}] tensors on the heads' device")
+        n_rows = pool[0]
+        if rows.pool > n_rows or n_rows >= 1 << 31:
+            raise DeftError(-1, "deft_qkv_store: the list is for a larger cache, or the cache larger than 32 bits hold")
+        k_pool, v_pool = k_pool.data_ptr(), v_pool.data_ptr()
     raw = torch._C._cuda_getCurrentRawStream(index) if stream is None else _raw_stream(stream, index)
     kw, kw_head, wide = _NO_WEIGHT if k_weight is None else _head_weight(k_weight, Hkv, d, index, bf16, what, "k_weight")
     q_heads = None
@@ -1117,7 +1142,7 @@ def deft_qkv_store(rows: KVList, q, k, v, cache, positions=None, rope=None, q_we
             q_head = d
         qw, qw_head, q_wide = _NO_WEIGHT if q_weight is None else _head_weight(q_weight, Hq, d, index, bf16, what, "q_weight")
         if q_wide != wide and qw and kw:
-            raise DeftError(-1, "deft_qkv_store: weights must be of one type")
+            raise DeftError(-1, f"{what}: weights must be of one type")
         q_at = q.data_ptr()
         if q_out is None and stream is None and type(q) is torch.Tensor:
             q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
@@ -1127,7 +1152,7 @@ def deft_qkv_store(rows: KVList, q, k, v, cache, positions=None, rope=None, q_we
             q_out, to = _heads_out(q_out, q, q_at, bf16, raw, index, elsewhere, what, "q_out")
         q_heads = _pack_heads(q_at, q_token, q_head, to, qw, qw_head, q_wide, Hq)
     elif q_weight is not None or q_out is not None:
-        raise DeftError(-1, "deft_qkv_store: without q it has neither weights nor a result")
+        raise DeftError(-1, f"{what}: without q it has neither weights nor a result")
     packed = pos = None
     if rope is not None:
         if positions is None or positions.dtype is not torch.int32 or positions.shape != (n,) or positions.get_device() != index or not positions.is_contiguous():
@@ -1137,12 +1162,15 @@ def deft_qkv_store(rows: KVList, q, k, v, cache, positions=None, rope=None, q_we
         return q_out
     if torch._C._cuda_getDevice() != index:
         with torch.cuda.device(index):
-            return deft_qkv_store(rows, q, k, v, cache, positions, rope, q_weight, k_weight, eps, weight_offset, q_out, raw)
+            return _qkv_store(q8, rows, q, k, v, cache, positions, rope, q_weight, k_weight, eps, weight_offset, q_out, raw)
     image = rows._images.of.get(index) if raw == 0 else None  # (the null stream is in no capture)
     image = image.tensor if image is not None and raw in image.streams else rows._image(index, raw)
-    rc = (_lib or load_library()).deft_qkv_store(
-        rows._h, image.data_ptr(), q_heads, _pack_heads(k.data_ptr(), k_token, k_head, k_pool.data_ptr(), kw, kw_head, wide, Hkv),
-        _pack_heads(v.data_ptr(), v_token, v_head, v_pool.data_ptr(), 0, 0, 0, Hkv), n_rows, d, eps, weight_offset, pos, packed, raw)
+    k_heads = _pack_heads(k.data_ptr(), k_token, k_head, k_pool, kw, kw_head, wide, Hkv)
+    v_heads = _pack_heads(v.data_ptr(), v_token, v_head, v_pool, 0, 0, 0, Hkv)
+    if q8:
+        rc = _lib.deft_qkv_store_q8(rows._h, image.data_ptr(), q_heads, k_heads, v_heads, c, eps, weight_offset, pos, packed, raw)
+    else:
+        rc = (_lib or load_library()).deft_qkv_store(rows._h, image.data_ptr(), q_heads, k_heads, v_heads, n_rows, d, eps, weight_offset, pos, packed, raw)
     if rc != 0:
         _check(rc, what)
     return q_out

@@ -8,22 +8,14 @@
 
 #include "deft_device.h"
 #include "deft_lists.h"
+#include "deft_q8_device.h"
 
 namespace {
 
-typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
-typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 
-// floor(n / d), given inverse(d)
-uint32_t inverse(uint32_t d) { return d == 1 ? 0xffffffffu : (uint32_t)((uint64_t(1) << 32) / d); }
-__device__ __forceinline__ uint32_t divide(uint32_t n, uint32_t d, uint32_t inv) {
-    const uint32_t q = __umulhi(n, inv);  // floor(n / d) or one less
-    return n - q * d >= d ? q + 1 : q;
-}
-
 enum { kQ, kK, kV, kParts };
-enum Turn { kNoTurn, kHalf, kInterleaved };
+enum Turn { kNoTurn, kHalf, kInterleaved, kAny };  // kAny: as the arguments say
 
 // Heads of one kind.  Strides in elements.
 struct Part {
@@ -39,10 +31,17 @@ struct HeadsArgs {
     const int32_t *positions;
     const u32x2 *entries;  // {row of k's and v's out, token}; null: every token, and its row is its own number
     uint32_t waves, chunks, inv_chunks;  // of the launch; of a token
-    uint32_t rot, wide;                  // wide: weights are float
+    uint32_t rot, wide, turn;            // wide: weights are float; turn: a Turn
     float eps, offset, factor;
     uint64_t turns[64];  // of a turn a position, in 2^-64
 };
+
+// The upper half of position x turns modulo 2^64.
+__device__ __forceinline__ uint32_t phase_of(int32_t position, uint64_t turns) {
+    const uint32_t low = (uint32_t)turns, high = (uint32_t)(turns >> 32);
+    const uint32_t phase = __umulhi((uint32_t)position, low) + (uint32_t)position * high;
+    return position < 0 ? phase - low : phase;
+}
 
 // cos and sin of 2 pi phase / 2^32: the nearest quarter turn is taken off exactly, and what is left, at most pi / 4, goes through the
 // Taylor polynomials of degree 8 and 9 (their first term left out is below 3e-8; with the roundings 1.5e-7 all in all).
@@ -103,6 +102,59 @@ __device__ __forceinline__ void unpack_weights(const Weights &w, bool wide, floa
     for (int i = 0; i < 8; ++i) y[i] += offset;
 }
 
+// A head whose elements D / 16 neighbouring lanes have, sixteen each.
+template <int D>
+__device__ __forceinline__ void normalise(float *y0, float *y1, const float *w0, const float *w1, float eps) {
+    auto mean = [&](float eps) {
+        float sum = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum = fmaf(y0[i], y0[i], fmaf(y1[i], y1[i], sum));
+#pragma unroll
+        for (uint32_t o = 1; o < D / 16; o <<= 1) sum += __shfl_xor(sum, o);
+        return fmaf(sum, 1.f / D, eps);
+    };
+    float m = mean(eps);
+    if (m > 0x1p100f || m < 0x1p-80f) {  // squares near the ends of fp32: the head is taken by a power of two of itself
+        const float by = m > 1.f ? 0x1p-70f : 0x1p90f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            y0[i] *= by;
+            y1[i] *= by;
+        }
+        m = mean(eps * by * by);
+    }
+    const float r = __builtin_amdgcn_rsqf(m);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        y0[i] *= r * w0[i];
+        y1[i] *= r * w1[i];
+    }
+}
+// (which of the products is rounded by itself is said here, so that every kernel gives the same bits)
+__device__ __forceinline__ void turn(float &u, float &v, float c, float s) {
+    const float t = fmaf(u, c, -(v * s));
+    v = fmaf(v, c, u * s);
+    u = t;
+}
+
+// A lane's two groups of eight elements: interleaved anywhere in the head, in the half layout partners, and of the elements that do not
+// turn the same.
+struct Groups {
+    uint32_t first, second;
+    bool turned0, turned1;
+};
+template <int D>
+__device__ __forceinline__ Groups groups_of(uint32_t j, int turn, uint32_t rot) {
+    const bool turned = turn == kHalf && 16 * j < rot;
+    const uint32_t begin = turned || turn != kHalf ? 0 : rot, width = turned ? rot : D - begin;
+    Groups g;
+    g.first = begin + 8 * (j - begin / 16);
+    g.second = g.first + width / 2;
+    g.turned0 = turn == kInterleaved ? g.first < rot : turned;
+    g.turned1 = turn == kInterleaved ? g.second < rot : turned;
+    return g;
+}
+
 // A value that is the same for all lanes, by a scalar load.
 template <typename T>
 __device__ __forceinline__ T uniform(const T *p, uint32_t i) {
@@ -117,12 +169,9 @@ __device__ __forceinline__ T uniform(const T *p, uint32_t i) {
 // 28.0 (6.0 TB/s); by the host's call, and 3 to 4 us of launch and dependent loads, where they are a decode iteration's.  Two or more
 // batches of heads to a wave, 8192 x 32 turned: 21.0 -> 21.8.  Stores that stay in the caches: 8192 x 32 20.7 -> 25.1.
 template <int D, int TURN, bool NORM>
-__global__ __launch_bounds__(256) void deft_heads(HeadsArgs a) {
+__device__ __forceinline__ void heads_of_wave(const HeadsArgs &a, uint32_t unit, float (*cs)[64]) {
     constexpr uint32_t kLanes = D / 16, kHeads = 64 / kLanes;
-    __shared__ float table[4][2][64];
-    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const uint32_t unit = blockIdx.x * 4 + wave;
-    if (unit >= a.waves) return;
+    const uint32_t lane = threadIdx.x & 63;
     const uint32_t entry = divide(unit, a.chunks, a.inv_chunks), chunk = unit - entry * a.chunks;
     const int kind = chunk >= a.part[kV].chunk ? kV : chunk >= a.part[kK].chunk ? kK : kQ;
     const Part &p = a.part[kind];
@@ -132,19 +181,17 @@ __global__ __launch_bounds__(256) void deft_heads(HeadsArgs a) {
         row = kind == kQ ? e[1] : e[0];
         token = e[1];
     }
-    // the lane's two groups: interleaved anywhere in the head, in the half layout partners, and of the elements that do not turn the same
-    const uint32_t j = lane % kLanes, rot = kind == kV ? 0 : a.rot;
-    const bool turned = TURN == kHalf && 16 * j < rot;
-    const uint32_t begin = turned || TURN != kHalf ? 0 : rot, width = turned ? rot : D - begin;
-    const uint32_t first = begin + 8 * (j - begin / 16), second = first + width / 2;
-    const bool turned0 = TURN == kInterleaved ? first < rot : turned, turned1 = TURN == kInterleaved ? second < rot : turned;
+    const int how = TURN == kAny ? (int)a.turn : TURN;
+    const uint32_t j = lane % kLanes, rot = how == kNoTurn || kind == kV ? 0 : a.rot;
+    const Groups g = groups_of<D>(j, how, rot);
+    const uint32_t first = g.first, second = g.second;
     const uint32_t head = (chunk - p.chunk) * kHeads + lane / kLanes, at = min(head, p.heads - 1);  // (heads behind the last are that one)
     const uint16_t *x = p.x + ((int64_t)token * p.token + (int64_t)at * p.head);
     // What the angles and the norm wait for is asked for in front of the heads, by vector loads: those come back in order, and a scalar
     // load of the position would hold up everything behind the next wait for any scalar load.
     int32_t position = 0;
     uint64_t turns = 0;
-    if (TURN != kNoTurn && 2 * lane < rot) {
+    if (2 * lane < rot) {
         uint32_t of = token;
         asm("" : "+v"(of));
         position = a.positions[of];
@@ -158,13 +205,9 @@ __global__ __launch_bounds__(256) void deft_heads(HeadsArgs a) {
         v1 = weights_at(p.weight, w + second, a.wide);
     }
     const u32x4 x0 = *reinterpret_cast<const u32x4 *>(x + first), x1 = *reinterpret_cast<const u32x4 *>(x + second);
-    float (*cs)[64] = table[wave];
-    if (TURN != kNoTurn && 2 * lane < rot) {
-        const uint32_t low = (uint32_t)turns, high = (uint32_t)(turns >> 32);
-        uint32_t phase = __umulhi((uint32_t)position, low) + (uint32_t)position * high;
-        if (position < 0) phase -= low;
+    if (2 * lane < rot) {
         float c, s;
-        cos_sin(phase, c, s);
+        cos_sin(phase_of(position, turns), c, s);
         cs[0][lane] = c * a.factor;
         cs[1][lane] = s * a.factor;
     }
@@ -175,39 +218,11 @@ __global__ __launch_bounds__(256) void deft_heads(HeadsArgs a) {
         float w0[8], w1[8];
         unpack_weights(v0, a.wide, a.offset, w0);
         unpack_weights(v1, a.wide, a.offset, w1);
-        auto mean = [&](float eps) {
-            float sum = 0;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum = fmaf(y0[i], y0[i], fmaf(y1[i], y1[i], sum));
-#pragma unroll
-            for (uint32_t o = 1; o < kLanes; o <<= 1) sum += __shfl_xor(sum, o);
-            return fmaf(sum, 1.f / D, eps);
-        };
-        float m = mean(a.eps);
-        if (m > 0x1p100f || m < 0x1p-80f) {  // squares near the ends of fp32: the head is taken by a power of two of itself
-            const float by = m > 1.f ? 0x1p-70f : 0x1p90f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                y0[i] *= by;
-                y1[i] *= by;
-            }
-            m = mean(a.eps * by * by);
-        }
-        const float r = __builtin_amdgcn_rsqf(m);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            y0[i] *= r * w0[i];
-            y1[i] *= r * w1[i];
-        }
+        normalise<D>(y0, y1, w0, w1, a.eps);
     }
-    auto turn = [](float &u, float &v, float c, float s) {
-        const float t = u * c - v * s;
-        v = v * c + u * s;
-        u = t;
-    };
     auto cosines = [&](uint32_t i) { return *reinterpret_cast<const f32x4 *>(&cs[0][i]); };
     auto sines = [&](uint32_t i) { return *reinterpret_cast<const f32x4 *>(&cs[1][i]); };
-    if (TURN == kHalf && turned) {
+    if (how == kHalf && g.turned0) {
         const f32x4 c0 = cosines(first), c1 = cosines(first + 4), s0 = sines(first), s1 = sines(first + 4);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -215,12 +230,12 @@ __global__ __launch_bounds__(256) void deft_heads(HeadsArgs a) {
             turn(y0[4 + i], y1[4 + i], c1[i], s1[i]);
         }
     }
-    if (TURN == kInterleaved && turned0) {
+    if (how == kInterleaved && g.turned0) {
         const f32x4 c = cosines(first / 2), s = sines(first / 2);
 #pragma unroll
         for (int i = 0; i < 4; ++i) turn(y0[2 * i], y0[2 * i + 1], c[i], s[i]);
     }
-    if (TURN == kInterleaved && turned1) {
+    if (how == kInterleaved && g.turned1) {
         const f32x4 c = cosines(second / 2), s = sines(second / 2);
 #pragma unroll
         for (int i = 0; i < 4; ++i) turn(y1[2 * i], y1[2 * i + 1], c[i], s[i]);
@@ -228,8 +243,219 @@ __global__ __launch_bounds__(256) void deft_heads(HeadsArgs a) {
     if (head >= p.heads) return;
     uint16_t *out = p.out + ((int64_t)row * p.out_token + (int64_t)head * p.out_head);
     // bits as they are where nothing is done to them; none of it is read again here
-    __builtin_nontemporal_store(turned0 || normed ? pack8(y0) : x0, reinterpret_cast<u32x4 *>(out + first));
-    __builtin_nontemporal_store(turned1 || normed ? pack8(y1) : x1, reinterpret_cast<u32x4 *>(out + second));
+    __builtin_nontemporal_store(g.turned0 || normed ? pack8(y0) : x0, reinterpret_cast<u32x4 *>(out + first));
+    __builtin_nontemporal_store(g.turned1 || normed ? pack8(y1) : x1, reinterpret_cast<u32x4 *>(out + second));
+}
+
+template <int D, int TURN, bool NORM>
+__global__ __launch_bounds__(256) void deft_heads(HeadsArgs a) {
+    __shared__ float table[4][2][64];
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), unit = blockIdx.x * 4 + wave;
+    if (unit < a.waves) heads_of_wave<D, TURN, NORM>(a, unit, table[wave]);
+}
+
+// ---- into an 8-bit cache ----
+
+struct StoreArgs {
+    HeadsArgs h;            // its entries are null; k's and v's parts have no out
+    const u32x4 *groups;    // {block, first, count, low}, see deft::RowGroup
+    const u32x2 *entries;   // {row, token}
+    CacheArgs c;
+    uint32_t units, parts, inv_parts, workgroups;  // the queries' workgroups come behind the others
+};
+
+// How a launch is cut: a row takes D / 16 lanes, so that a lane has a key's partners, and a unit, the new rows of a block and head, as many
+// waves as that makes or a part of one.
+template <int D, int BLOCK>
+struct Cut {
+    static constexpr int kRowLanes = D / 16, kWaveRows = 64 / kRowLanes;
+    static constexpr bool kWhole = BLOCK >= kWaveRows;  // whole waves: a workgroup has heads of one block; otherwise units in order
+    static constexpr int kUnitLanes = kWhole ? 64 : kRowLanes * BLOCK;  // of a wave
+    static constexpr int kThreads = kWhole ? 512 : 256, kWaves = kThreads / 64;
+    static constexpr int kUnitWaves = kWhole ? BLOCK / kWaveRows : 1;
+    static constexpr int kHeads = kWhole ? kWaves / kUnitWaves : 0;  // of a workgroup
+    static constexpr int kPitch = 68;                                // floats of a row of angles, so that rows begin in different banks
+    static constexpr int kTable = kWhole && 2 * BLOCK * kPitch > kWaves * 128 ? 2 * BLOCK * kPitch : kWaves * 128;
+};
+
+// Keys normalised and turned as by deft_heads and then, with the values, stored as by deft_store_q8, byte for byte what the two do one after
+// the other; the queries in the same launch.
+template <int D, int BLOCK>
+__global__ __launch_bounds__((Cut<D, BLOCK>::kThreads)) void deft_store_heads_q8(StoreArgs a) {
+    using C = Cut<D, BLOCK>;
+    constexpr int kRowLanes = C::kRowLanes, kPitch = C::kPitch;
+    __shared__ __attribute__((aligned(16))) float table[C::kTable];
+    __shared__ uint32_t scales[C::kWaves];
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (blockIdx.x >= a.workgroups) {
+        const uint32_t unit = (blockIdx.x - a.workgroups) * C::kWaves + wave;
+        if (unit < a.h.waves) heads_of_wave<D, kAny, true>(a.h, unit, reinterpret_cast<float (*)[64]>(table + wave * 128));
+        return;
+    }
+    uint32_t group, h, sub = lane % C::kUnitLanes / kRowLanes;  // sub: which of the unit's rows
+    if (C::kWhole) {
+        group = divide(blockIdx.x, a.parts, a.inv_parts);
+        h = (blockIdx.x - group * a.parts) * C::kHeads + wave / C::kUnitWaves;
+        sub += wave % C::kUnitWaves * C::kWaveRows;
+    } else {
+        const uint32_t unit = (blockIdx.x * C::kThreads + threadIdx.x) / C::kUnitLanes;
+        if (unit >= a.units) return;  // (whole units, and all lanes that exchange values below belong to one)
+        group = divide(unit, a.c.Hkv, a.c.inv_Hkv);
+        h = unit - group * a.c.Hkv;
+    }
+    const uint32_t j = lane % kRowLanes;
+    const int how = (int)a.h.turn;
+    const uint32_t rot = how == kNoTurn ? 0 : a.h.rot;
+    const Groups g = groups_of<D>(j, how, rot);
+    const uint32_t v_first = 8 * j, v_second = D / 2 + 8 * j;
+    const Part &kp = a.h.part[kK], &vp = a.h.part[kV];
+    const bool normed = kp.weight;
+    const u32x4 head = a.groups[group];
+    const uint32_t block = head[0], first = head[1], count = head[2], low = head[3];
+    // Waves behind the last head or the last row make angles all the same, and wait with the others.
+    const bool ours = !C::kWhole || h < a.c.Hkv, live = !C::kWhole || (ours && wave % C::kUnitWaves * C::kWaveRows < __builtin_amdgcn_readfirstlane(count));
+    const size_t scale_at = (size_t)block * a.c.Hkv + h;
+    int ek = kScaleMin, ev = kScaleMin;
+    const bool kept = low > 0 && ours;
+    if (kept) {
+        ek = a.c.k_scale[scale_at];
+        ev = a.c.v_scale[scale_at];
+    }
+    // A lane's pairs: those of its first group, or of its first four and its second group's.
+    const uint32_t pair0 = how == kHalf ? g.first : g.first / 2, pair1 = how == kHalf ? g.first + 4 : g.second / 2;
+    uint64_t turns[8] = {};
+    int32_t position = 0;
+    Weights w0, w1;
+    uint32_t row = 0;
+    u32x4 k0, k1, v0, v1;
+    if (C::kWhole && rot) {
+        if (2 * lane < rot) turns[0] = a.h.turns[lane];
+        position = a.h.positions[a.entries[first + min(lane, count - 1)][1]];  // of row `lane`
+    }
+    if (live) {
+        const u32x2 e = a.entries[first + min(sub, count - 1)];  // rows past the last repeat it
+        row = e[0];
+        if (normed) {
+            const uint32_t w = h * (uint32_t)kp.weight_head;
+            w0 = weights_at(kp.weight, w + g.first, a.h.wide);
+            w1 = weights_at(kp.weight, w + g.second, a.h.wide);
+        }
+        if (!C::kWhole && rot) {
+            position = a.h.positions[e[1]];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (g.turned0) turns[i] = a.h.turns[pair0 + i];
+                if (g.turned1) turns[4 + i] = a.h.turns[pair1 + i];
+            }
+        }
+        const uint16_t *k = kp.x + ((int64_t)e[1] * kp.token + (int64_t)h * kp.head), *v = vp.x + ((int64_t)e[1] * vp.token + (int64_t)h * vp.head);
+        k0 = load_once(reinterpret_cast<const u32x4 *>(k + g.first));
+        k1 = load_once(reinterpret_cast<const u32x4 *>(k + g.second));
+        v0 = load_once(reinterpret_cast<const u32x4 *>(v + v_first));
+        v1 = load_once(reinterpret_cast<const u32x4 *>(v + v_second));
+    }
+    if (C::kWhole && rot) {  // the angles of the block's rows, once for all its heads here: a wave makes a row's, a lane one pair's
+        const uint32_t rows = __builtin_amdgcn_readfirstlane(count);
+        for (uint32_t r = wave; r < rows; r += C::kWaves) {
+            float c, s;
+            cos_sin(phase_of(__builtin_amdgcn_readlane(position, r), turns[0]), c, s);
+            table[2 * r * kPitch + lane] = c * a.h.factor;
+            table[(2 * r + 1) * kPitch + lane] = s * a.h.factor;
+        }
+        __syncthreads();
+    }
+    const int old_k = ek, old_v = ev;
+    bool spoiled = false;  // an infinity or a NaN in the row
+    if (live) {
+        if (normed || rot) {
+            float y0[8], y1[8];
+            unpack8(k0, y0);
+            unpack8(k1, y1);
+            if (normed) {
+                float f0[8], f1[8];
+                unpack_weights(w0, a.h.wide, a.h.offset, f0);
+                unpack_weights(w1, a.h.wide, a.h.offset, f1);
+                normalise<D>(y0, y1, f0, f1, a.h.eps);
+            }
+            f32x4 c[2], s[2];
+            if (C::kWhole) {
+                const float *of = table + 2 * min(sub, count - 1) * kPitch;
+                if (g.turned0) {
+                    c[0] = *reinterpret_cast<const f32x4 *>(of + pair0);
+                    s[0] = *reinterpret_cast<const f32x4 *>(of + kPitch + pair0);
+                }
+                if (g.turned1) {
+                    c[1] = *reinterpret_cast<const f32x4 *>(of + pair1);
+                    s[1] = *reinterpret_cast<const f32x4 *>(of + kPitch + pair1);
+                }
+            } else if (g.turned0 || g.turned1) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    float cs, sn;
+                    cos_sin(phase_of(position, turns[i]), cs, sn);
+                    c[i / 4][i % 4] = cs * a.h.factor;
+                    s[i / 4][i % 4] = sn * a.h.factor;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (how == kHalf && g.turned0) {
+                    turn(y0[i], y1[i], c[0][i], s[0][i]);
+                    turn(y0[4 + i], y1[4 + i], c[1][i], s[1][i]);
+                }
+                if (how == kInterleaved && g.turned0) turn(y0[2 * i], y0[2 * i + 1], c[0][i], s[0][i]);
+                if (how == kInterleaved && g.turned1) turn(y1[2 * i], y1[2 * i + 1], c[1][i], s[1][i]);
+            }
+            if (g.turned0 || normed) k0 = pack8(y0);
+            if (g.turned1 || normed) k1 = pack8(y1);
+        }
+        uint32_t mk = 0, mv = 0;  // magnitudes as pairs of bf16 bits
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            mk = pk_max(pk_max(mk, k0[i] & 0x7fff7fffu), k1[i] & 0x7fff7fffu);
+            mv = pk_max(pk_max(mv, v0[i] & 0x7fff7fffu), v1[i] & 0x7fff7fffu);
+        }
+        const uint32_t both = pk_max(mk, mv);
+        const uint64_t bad = __ballot(max(both & 0xffffu, both >> 16) >= 0x7f80u);
+        spoiled = ((bad >> (lane / kRowLanes * kRowLanes)) & ((uint64_t(1) << kRowLanes) - 1)) != 0;
+        uint32_t top = spoiled ? 0u : max(mk & 0xffffu, mk >> 16) | max(mv & 0xffffu, mv >> 16) << 16;
+#pragma unroll
+        for (int o = C::kUnitLanes / 2; o > 0; o >>= 1) top = pk_max(top, (uint32_t)__shfl_xor((int)top, o));
+        ek = max(ek, scale_byte(top & 0xffffu));
+        ev = max(ev, scale_byte(top >> 16));
+    }
+    if (C::kUnitWaves > 1) {
+        if (lane == 0) scales[wave] = (uint32_t)ek | (uint32_t)ev << 16;
+        __syncthreads();
+        uint32_t most = 0;
+#pragma unroll
+        for (int i = 0; i < C::kUnitWaves; ++i) most = pk_max(most, scales[wave / C::kUnitWaves * C::kUnitWaves + i]);
+        ek = (int)(most & 0xffffu);
+        ev = (int)(most >> 16);
+    }
+    const size_t pitch = (size_t)a.c.Hkv * D;
+    if (kept) {
+        const size_t begin = (size_t)block * BLOCK * pitch + h * D;
+        constexpr uint32_t step = C::kWhole ? BLOCK : C::kUnitLanes / kRowLanes;  // (of the unit's rows a lane has one)
+        for (const uint32_t col : {v_first, v_second}) {
+            if (ek > old_k) rescale_kept(a.c.k + begin + col, sub, step, low, pitch, power(max(127 + old_k - ek, 0)));
+            if (ev > old_v) rescale_kept(a.c.v + begin + col, sub, step, low, pitch, power(max(127 + old_v - ev, 0)));
+        }
+    }
+    if (!ours) return;
+    if (sub < count) {
+        const float inv_k = power(254 - ek), inv_v = power(254 - ev);
+        const u32x2 nan = {0x7f7f7f7fu, 0x7f7f7f7fu}, zero = {0u, 0u};
+        const size_t at = row * pitch + h * D;
+        *reinterpret_cast<u32x2 *>(a.c.k + at + g.first) = spoiled ? nan : round8(k0, inv_k);
+        *reinterpret_cast<u32x2 *>(a.c.k + at + g.second) = spoiled ? nan : round8(k1, inv_k);
+        *reinterpret_cast<u32x2 *>(a.c.v + at + v_first) = spoiled ? zero : round8(v0, inv_v);
+        *reinterpret_cast<u32x2 *>(a.c.v + at + v_second) = spoiled ? zero : round8(v1, inv_v);
+    }
+    if (sub == 0 && j == 0) {
+        a.c.k_scale[scale_at] = (uint8_t)ek;
+        a.c.v_scale[scale_at] = (uint8_t)ev;
+    }
 }
 
 // ---- host ----
@@ -282,35 +508,44 @@ bool plain(int64_t n, const deft_heads_t &p, int64_t d) {
 
 constexpr int64_t kMaxStride = int64_t(1) << 40;
 
-// One call.  parts: q, k, v, each may be null; pool: rows of k's and v's out where the call has a list.
-int run(const deft_heads_t *const (&parts)[kParts], int64_t n, int32_t d, float eps, float offset, const int32_t *positions,
-        const deft_rope_t *rope, const u32x2 *entries, int64_t pool, void *stream) {
+// A call as it was checked.
+struct Call {
+    HeadsArgs a{};
+    uint32_t heads = 0;
+    bool norm = false;
+    Area in[kParts]{}, out[kParts]{};
+};
+enum Where { kOwnOut, kPool, kCache };  // where keys and values go: as queries do, into rows of a bf16 cache, or elsewhere
+
+// parts: q, k, v, each may be null; pool: rows of k's and v's out where they are a bf16 cache's.
+int check(const deft_heads_t *const (&parts)[kParts], int64_t n, int32_t d, float eps, float offset, const int32_t *positions,
+          const deft_rope_t *rope, Where where, int64_t pool, Call &call) {
     if (n < 0 || (d != 64 && d != 128)) return DEFT_EINVAL;
     if (rope && (rope->rot < 16 || rope->rot > d || rope->rot % 16 || (rope->layout != DEFT_ROPE_HALF && rope->layout != DEFT_ROPE_INTERLEAVED)))
         return DEFT_EINVAL;
     if (rope && ((!positions && n > 0) || (reinterpret_cast<uintptr_t>(positions) & 3))) return DEFT_EINVAL;
-    HeadsArgs a{};
-    Area in[kParts], out[kParts];
-    uint32_t heads = 0;
-    bool norm = false, wide = false;
+    HeadsArgs &a = call.a;
+    auto &in = call.in;
+    auto &out = call.out;
+    bool wide = false;
     for (int i = 0; i < kParts; ++i) {
         const deft_heads_t *p = parts[i];
-        in[i] = out[i] = Area{};
+        const bool stored = where != kOwnOut && i != kQ, writes = where != kCache || i == kQ;
         if (!p || p->heads == 0) continue;
         if (p->heads < 0 || p->heads > DEFT_MAX_Q8_HEADS) return DEFT_EINVAL;
         if (p->weight) {
             if (i == kV || !(eps >= 0) || !std::isfinite(eps) || !std::isfinite(offset)) return DEFT_EINVAL;
             if (!deft::aligned16(p->weight) || p->weight_stride < 0 || p->weight_stride % 8 || p->weight_stride > 4096) return DEFT_EINVAL;
-            if (norm && wide != (p->weight_f32 != 0)) return DEFT_EINVAL;
-            norm = true;
+            if (call.norm && wide != (p->weight_f32 != 0)) return DEFT_EINVAL;
+            call.norm = true;
             wide = p->weight_f32 != 0;
         }
         if (n == 0) continue;
-        if (!p->x || !p->out || !deft::aligned16(p->x) || !deft::aligned16(p->out)) return DEFT_EINVAL;
+        if (!p->x || !deft::aligned16(p->x) || (writes && (!p->out || !deft::aligned16(p->out)))) return DEFT_EINVAL;
         if ((p->token_stride | p->head_stride) & 7) return DEFT_EINVAL;
         if (p->token_stride < 0 || p->head_stride < 0 || p->token_stride > kMaxStride || p->head_stride > kMaxStride) return DEFT_EINVAL;
         if ((double)n * (double)p->token_stride + (double)p->heads * (double)p->head_stride > 0x1p60) return DEFT_EINVAL;
-        const bool stored = entries && i != kQ, in_place = !stored && p->out == p->x;
+        const bool in_place = !stored && p->out == p->x;
         if (in_place && !plain(n, *p, d)) return DEFT_EINVAL;
         Part &t = a.part[i];
         t.x = static_cast<const uint16_t *>(p->x);
@@ -322,9 +557,9 @@ int run(const deft_heads_t *const (&parts)[kParts], int64_t n, int32_t d, float 
         t.out_token = in_place ? t.token : (int64_t)p->heads * d;
         t.out_head = in_place ? t.head : d;
         in[i] = area(p->x, n, p->heads, d, t.token, t.head);
-        out[i] = area(p->out, stored ? pool : n, p->heads, d, t.out_token, t.out_head);
+        if (writes) out[i] = area(p->out, stored ? pool : n, p->heads, d, t.out_token, t.out_head);
         t.heads = (uint32_t)p->heads;
-        heads += t.heads;
+        call.heads += t.heads;
     }
     for (int i = 0; i < kParts; ++i)  // what is written is nobody else's, and nobody's input but the part's own, in place
         for (int j = 0; j < kParts; ++j) {
@@ -342,29 +577,34 @@ int run(const deft_heads_t *const (&parts)[kParts], int64_t n, int32_t d, float 
         for (int j = 0; j < kParts; ++j)
             if (parts[j] && meets(parts[j]->weight, ((parts[j]->heads - 1) * parts[j]->weight_stride + d) * (wide ? 4 : 2))) return DEFT_EINVAL;
     }
-    if (n == 0 || heads == 0) return DEFT_OK;
     const uint32_t at_once = 64 / ((uint32_t)d / 16);  // heads of a wave
-    for (Part &p : a.part) {
-        p.chunk = a.chunks;
-        a.chunks += (p.heads + at_once - 1) / at_once;
+    for (int i = 0; i < kParts; ++i) {
+        a.part[i].chunk = a.chunks;
+        if (where != kCache || i == kQ) a.chunks += (a.part[i].heads + at_once - 1) / at_once;
     }
-    a.inv_chunks = inverse(a.chunks);
+    if (a.chunks) a.inv_chunks = inverse(a.chunks);
     a.positions = positions;
-    a.entries = entries;
     a.eps = eps;
     a.offset = offset;
     a.wide = wide;
+    a.turn = !rope ? kNoTurn : rope->layout == DEFT_ROPE_HALF ? kHalf : kInterleaved;
     if (rope) {
         a.rot = (uint32_t)rope->rot;
         a.factor = rope->factor;
         std::copy(rope->turns, rope->turns + rope->rot / 2, a.turns);
     }
-    const int turn = !rope ? kNoTurn : rope->layout == DEFT_ROPE_HALF ? kHalf : kInterleaved;
+    return DEFT_OK;
+}
+
+// The waves of a call, in launches.
+int launch_waves(HeadsArgs a, bool norm, int64_t n, int32_t d, hipStream_t st) {
+    if (n == 0 || a.chunks == 0) return DEFT_OK;
+    const int turn = (int)a.turn;
     const int64_t most = (int64_t)(kMaxWaves / a.chunks);
     for (int64_t left = n, now; left > 0; left -= now) {
         now = std::min(left, most);
         a.waves = (uint32_t)now * a.chunks;
-        d == 128 ? launch<128>(a, turn, norm, static_cast<hipStream_t>(stream)) : launch<64>(a, turn, norm, static_cast<hipStream_t>(stream));
+        d == 128 ? launch<128>(a, turn, norm, st) : launch<64>(a, turn, norm, st);
         if (!deft::hip_ok(hipGetLastError(), "deft_heads launch")) return DEFT_EHIP;
         if (a.entries) {
             a.entries += now;
@@ -377,6 +617,49 @@ int run(const deft_heads_t *const (&parts)[kParts], int64_t n, int32_t d, float 
         }
     }
     return DEFT_OK;
+}
+
+int run(const deft_heads_t *const (&parts)[kParts], int64_t n, int32_t d, float eps, float offset, const int32_t *positions,
+        const deft_rope_t *rope, const u32x2 *entries, int64_t pool, void *stream) {
+    Call call;
+    const int rc = check(parts, n, d, eps, offset, positions, rope, entries ? kPool : kOwnOut, pool, call);
+    if (rc != DEFT_OK || call.heads == 0) return rc;
+    call.a.entries = entries;
+    return launch_waves(call.a, call.norm, n, d, static_cast<hipStream_t>(stream));
+}
+
+// Threads of a launch of stores at most (they are counted in 32 bits); longer lists take several launches.
+constexpr uint64_t kMaxThreads = 1u << 28;
+
+template <int D, int BLOCK>
+bool launch_store(StoreArgs a, uint32_t groups, hipStream_t st) {
+    using C = Cut<D, BLOCK>;
+    constexpr uint32_t units = C::kThreads / C::kUnitLanes;
+    a.parts = C::kWhole ? (a.c.Hkv + C::kHeads - 1) / std::max(C::kHeads, 1) : 0;
+    if (C::kWhole) a.inv_parts = inverse(a.parts);
+    const uint32_t most = (uint32_t)(C::kWhole ? kMaxThreads / C::kThreads / a.parts : kMaxThreads / C::kUnitLanes / a.c.Hkv);
+    for (uint32_t n; groups > 0; groups -= n, a.groups += n) {
+        n = std::min(groups, most);
+        a.units = n * a.c.Hkv;
+        a.workgroups = C::kWhole ? n * a.parts : (a.units + units - 1) / units;
+        const uint32_t queries = (a.h.waves + C::kWaves - 1) / C::kWaves;
+        hipLaunchKernelGGL((deft_store_heads_q8<D, BLOCK>), dim3(a.workgroups + queries), dim3(C::kThreads), 0, st, a);
+        if (!deft::hip_ok(hipGetLastError(), "deft_store_heads_q8 launch")) return false;
+        a.h.waves = 0;
+    }
+    return true;
+}
+template <int D>
+bool launch_store(const StoreArgs &a, uint32_t groups, int block_rows, hipStream_t st) {
+    switch (block_rows) {
+        case 1: return launch_store<D, 1>(a, groups, st);
+        case 2: return launch_store<D, 2>(a, groups, st);
+        case 4: return launch_store<D, 4>(a, groups, st);
+        case 8: return launch_store<D, 8>(a, groups, st);
+        case 16: return launch_store<D, 16>(a, groups, st);
+        case 32: return launch_store<D, 32>(a, groups, st);
+        default: return launch_store<D, 64>(a, groups, st);
+    }
 }
 
 }  // namespace
@@ -398,4 +681,48 @@ extern "C" int deft_qkv_store(const deft_kv_list_t *list, const void *dev_image,
     if (n_rows < 0 || list->pool > n_rows) return DEFT_EINVAL;
     const u32x2 *entries = reinterpret_cast<const u32x2 *>(static_cast<const uint8_t *>(dev_image) + list->off_entries);
     return run({q, k, v}, list->entries, d, eps, weight_offset, positions, rope, entries, n_rows, stream);
+}
+
+extern "C" int deft_qkv_store_q8(const deft_kv_list_t *list, const void *dev_image, const deft_heads_t *q, const deft_heads_t *k, const deft_heads_t *v,
+                                 const deft_cache_q8_t *cache, float eps, float weight_offset, const int32_t *positions, const deft_rope_t *rope,
+                                 void *stream) {
+    if (!rows_fit(list, dev_image, cache) || !k || !v || k->heads != cache->Hkv || v->heads != cache->Hkv) return DEFT_EINVAL;
+    if (cache->n_rows > 0 && (cache->k == cache->v || cache->k_scale == cache->v_scale)) return DEFT_EINVAL;
+    const int64_t n = list->entries, d = cache->d;
+    Call call;
+    const int rc = check({q, k, v}, n, (int32_t)d, eps, weight_offset, positions, rope, kCache, 0, call);
+    if (rc != DEFT_OK || n == 0) return rc;
+    // what the cache is made of is nobody's input, nor the queries' output
+    const int64_t bytes = (int64_t)cache->n_rows * cache->Hkv * d, scales = ((int64_t)cache->n_rows + cache->block_rows - 1) / cache->block_rows * cache->Hkv;
+    const struct { const void *p; int64_t bytes; } own[] = {{cache->k, bytes}, {cache->v, bytes}, {cache->k_scale, scales}, {cache->v_scale, scales}};
+    auto meets = [&](uintptr_t begin, uintptr_t end) {
+        for (const auto &o : own) {
+            const uintptr_t at = reinterpret_cast<uintptr_t>(o.p);
+            if (begin < at + (uint64_t)o.bytes && at < end) return true;
+        }
+        return false;
+    };
+    for (int i = 0; i < kParts; ++i) {
+        if (meets(call.in[i].begin, call.in[i].end) || meets(call.out[i].begin, call.out[i].end)) return DEFT_EINVAL;
+        const Part &p = call.a.part[i];
+        const uintptr_t w = reinterpret_cast<uintptr_t>(p.weight);
+        if (w && meets(w, w + (uint64_t)((p.heads - 1) * p.weight_head + d) * (call.a.wide ? 4 : 2))) return DEFT_EINVAL;
+    }
+    const uintptr_t at = reinterpret_cast<uintptr_t>(positions);
+    if (rope && meets(at, at + 4 * (uint64_t)n)) return DEFT_EINVAL;
+    StoreArgs a{};
+    a.h = call.a;
+    a.groups = static_cast<const u32x4 *>(dev_image);
+    a.entries = reinterpret_cast<const u32x2 *>(static_cast<const uint8_t *>(dev_image) + list->off_entries);
+    a.c = cache_args(cache);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const uint64_t waves = (uint64_t)n * call.a.chunks;
+    if (waves > kMaxWaves) {
+        const int done = launch_waves(call.a, call.norm, n, (int32_t)d, st);
+        if (done != DEFT_OK) return done;
+    } else {
+        a.h.waves = (uint32_t)waves;
+    }
+    const bool ok = d == 128 ? launch_store<128>(a, (uint32_t)list->heads, cache->block_rows, st) : launch_store<64>(a, (uint32_t)list->heads, cache->block_rows, st);
+    return ok ? DEFT_OK : DEFT_EHIP;
 }
