@@ -265,21 +265,28 @@ struct StoreArgs {
 };
 
 // How a launch is cut: a row takes D / 16 lanes, so that a lane has a key's partners, and a unit, the new rows of a block and head, as many
-// waves as that makes or a part of one.
+// waves as that makes or a part of one.  Eight waves to a workgroup everywhere, us (32 + 8 heads of 128): a token in each of 20 blocks
+// of 32 rows 4.6 -> 5.1, 1024 tokens in blocks of 16 6.4 -> 6.9, 8192 in blocks of 32 33.1 -> 32.9.
 template <int D, int BLOCK>
 struct Cut {
     static constexpr int kRowLanes = D / 16, kWaveRows = 64 / kRowLanes;
     static constexpr bool kWhole = BLOCK >= kWaveRows;  // whole waves: a workgroup has heads of one block; otherwise units in order
     static constexpr int kUnitLanes = kWhole ? 64 : kRowLanes * BLOCK;  // of a wave
-    static constexpr int kThreads = kWhole ? 512 : 256, kWaves = kThreads / 64;
     static constexpr int kUnitWaves = kWhole ? BLOCK / kWaveRows : 1;
+    static constexpr int kWaves = kUnitWaves > 4 ? kUnitWaves : 4, kThreads = 64 * kWaves;  // of a workgroup
     static constexpr int kHeads = kWhole ? kWaves / kUnitWaves : 0;  // of a workgroup
     static constexpr int kPitch = 68;                                // floats of a row of angles, so that rows begin in different banks
     static constexpr int kTable = kWhole && 2 * BLOCK * kPitch > kWaves * 128 ? 2 * BLOCK * kPitch : kWaves * 128;
 };
 
 // Keys normalised and turned as by deft_heads and then, with the values, stored as by deft_store_q8, byte for byte what the two do one after
-// the other; the queries in the same launch.
+// the other; the queries in the same launch.  Each lane has one row's sixteen elements of K and of V: a wave that has all rows of a block
+// of 32 one step after the other, as that kernel's have, takes three times the registers here and its steps wait for one another
+// (32 + 8 heads of 128, 300 tokens 9.7 -> 5.9 us, 8192 37.3 -> 33.1).  So the waves of a unit tell each other their scales, and those of
+// a workgroup make the angles of a block's rows together (8192 tokens, 32 heads: 5 % of the time is theirs).
+// Bound by HBM where calls are large: 8192 tokens, 32 + 8 heads of 128, 184 MB: 33.1 us, 5.6 TB/s, where deft_heads and deft_store_q8 need
+// 38.5; by the launch and dependent loads where they are an iteration's: 20 tokens 4.6 us, 6.5 by the two.  Queries by a launch of their
+// own in front, 8192 tokens: 36.6 -> 39.5 (2048: 13.1 -> 17.6).
 template <int D, int BLOCK>
 __global__ __launch_bounds__((Cut<D, BLOCK>::kThreads)) void deft_store_heads_q8(StoreArgs a) {
     using C = Cut<D, BLOCK>;

@@ -62,9 +62,9 @@ WAVES = 1 << 22  # of queries that share a launch, kMaxWaves in deft_heads.hip
 @needs_gxx
 @pytest.mark.parametrize("heads,d,block,n", [(65536, 128, 64, 640), (65536, 128, 64, 4200), (65536, 64, 1, 4097), (8, 128, 32, 500), (3, 64, 2, 5), (1, 128, 8, 1), (5, 128, 16, 100), (65533, 64, 32, 1500)])
 def test_calls_of_any_length(fake, heads, d, block, n):  # noqa: F811
-    # a block's rows of one head have lanes of sixteen elements: waves of them, and then a workgroup of eight waves has heads of one block,
-    # or a part of one, four waves to a workgroup; queries share the first launch, or have launches of their own in front if they
-    # are too many for it
+    # a block's rows of one head have lanes of sixteen elements: waves of them, and then a workgroup has heads of one block, or a part
+    # of a wave; a workgroup has four waves, or eight where one head's are that many; queries share the first launch, or have launches
+    # of their own in front if they are too many for it
     run(fake, f"""
 class Fake(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in names] + [("grid", ctypes.c_int32 * 16), ("kernel", ctypes.c_void_p * 16)]
@@ -80,8 +80,9 @@ def launched(q):
     return list(fake.grid[:fake.launches])
 lanes = d // 16 * block
 whole = lanes >= 64
-parts = -(-heads // (512 // lanes)) if whole else 0
-groups, most = -(-n // block), (1 << 28) // 512 // parts if whole else (1 << 28) // lanes // heads
+threads = max(lanes, 256)
+parts = -(-heads // (threads // lanes)) if whole else 0
+groups, most = -(-n // block), (1 << 28) // threads // parts if whole else (1 << 28) // lanes // heads
 want = []
 while groups:
     now = min(groups, most)
@@ -92,7 +93,7 @@ for Hq in (8, 65536):
     chunks = -(-Hq // (64 // (d // 16)))
     waves, most = n * chunks, {WAVES} // chunks
     if waves <= {WAVES}:
-        expected = [want[0] + -(-waves // (8 if whole else 4))] + want[1:]
+        expected = [want[0] + -(-waves // (threads // 64))] + want[1:]
     else:
         expected = [-(-min(most, n - i) * chunks // 4) for i in range(0, n, most)] + want
     if len(expected) <= 16:
