@@ -990,7 +990,7 @@ def deft_rotate(x, positions, rope: Rope, out=None, stream=None):
         raise _heads_error("deft_rotate", [("x", x)])
     n, H, d = shape
     token, head, one = x.stride()
-    if (one != 1 and n and H) or H >= 1 << 31:
+    if (one != 1 and n and H) or H | d >= 1 << 31:
         raise _heads_error("deft_rotate", [("x", x)])
     if n < 2:
         token = H * d
@@ -1031,7 +1031,7 @@ def deft_qk_norm_rotate(q, k, q_weight=None, k_weight=None, positions=None, rope
     k_n, Hkv, k_d = k_shape
     q_token, q_head, q_one = q.stride()
     k_token, k_head, k_one = k.stride()
-    if k_n != n or k_d != d or (q_one != 1 and n and Hq) or (k_one != 1 and n and Hkv) or Hq >= 1 << 31 or Hkv >= 1 << 31:
+    if k_n != n or k_d != d or (q_one != 1 and n and Hq) or (k_one != 1 and n and Hkv) or Hq | Hkv | d >= 1 << 31:
         raise _heads_error(what, [("q", q), ("k", k)])
     if n < 2:
         q_token, k_token = Hq * d, Hkv * d
@@ -1105,7 +1105,7 @@ def _qkv_store(q8, rows, q, k, v, cache, positions, rope, q_weight, k_weight, ep
         raise DeftError(-1, f"{what}: the list has {rows.n} rows, not {n}")
     k_token, k_head, k_one = k.stride()
     v_token, v_head, v_one = v.stride()
-    if ((k_one != 1 or v_one != 1) and n and Hkv) or Hkv >= 1 << 31:
+    if ((k_one != 1 or v_one != 1) and n and Hkv) or Hkv | d >= 1 << 31:
         raise _heads_error(what, [("k", k), ("v", v)])
     if n < 2:
         k_token = v_token = Hkv * d

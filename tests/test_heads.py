@@ -455,6 +455,18 @@ def test_gpu_refusals():
 
 
 @pytest.mark.gpu
+def test_heads_longer_than_thirty_two_bits_say_are_refused():
+    x = torch.empty((1, 1, (1 << 32) + 64), dtype=torch.bfloat16, device=dev())
+    p, rope, rows = torch.zeros(1, dtype=torch.int32, device=dev()), binding.deft_rope(64), binding.deft_kv_rows([0], 1, 1)
+    for call in (lambda: binding.deft_rotate(x, p, rope, out=x), lambda: binding.deft_qk_norm_rotate(x, x, None, None, p, rope, q_out=x, k_out=x),
+                 lambda: binding.deft_qkv_store(rows, None, x, x, (x, x), p, rope)):
+        with pytest.raises(binding.DeftError, match="must be"):
+            call()
+    del x
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.gpu
 def test_captured_and_replayed():
     n, Hq, Hkv, d = 40, 8, 2, 128
     rope, rng = binding.deft_rope(64, layout="interleaved"), np.random.default_rng(0)

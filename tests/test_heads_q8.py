@@ -211,6 +211,27 @@ def test_what_is_stored_is_near_the_definition(layout):
 
 
 @pytest.mark.gpu
+def test_rows_behind_four_billion_elements():
+    # beside the same tokens in the first rows of a small cache
+    n, Hkv, d, block = 70, 64, 128, 32
+    rows = (1 << 32) // (Hkv * d) + 2 * n
+    first = rows // block * block - 3 * block
+    big, small = (binding.alloc_kv_cache_q8(r, Hkv, d, block, dev()) for r in (rows, 96))
+    at = np.random.default_rng(1).permutation(n)
+    q, k, v = fresh(n, 4, Hkv, d, 3)
+    p, rope, w = on_gpu(positions(n)), binding.deft_rope(d), torch.rand(d, device=dev())
+    got = binding.deft_qkv_store_q8(binding.deft_kv_rows(at + first, rows, block), q, k, v, big, p, rope, k_weight=w)
+    want = by_two_calls(binding.deft_kv_rows(at, 96, block), q, k, v, small, p, rope, None, w)
+    assert torch.equal(got, want)
+    for a, b in zip(big[:2], small[:2]):
+        assert torch.equal(a[first:first + n].view(torch.uint8), b[:n].view(torch.uint8))
+    for a, b in zip(big[2:4], small[2:4]):
+        assert torch.equal(a.view(torch.uint8)[first // block:first // block + 3], b.view(torch.uint8))
+    del big
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.gpu
 def test_nothing_to_do():
     cache, _ = new_cache(64, 2, 64, 8)
     before = [t.view(torch.uint8).clone() for t in cache[:4]]
