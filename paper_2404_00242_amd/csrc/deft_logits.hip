@@ -385,13 +385,17 @@ __global__ __launch_bounds__(kThreads) void deft_logits(LogitsArgs a) {
             }
         };
         // a thread's tokens side by side, one bisection for all: as many as still leave work for every thread (8000 tokens of one query
-        // two by two 11.1 us, four by four 9.8; 1000 tokens 4.5 and 4.9); sorted ones are larger, and two by two is best throughout
+        // two by two 11.1 us, four by four 9.8, eight by eight 9.1; 1000 tokens 4.5 and 4.9 by two and four); with eight rows, whose
+        // logits are in registers, no more than four (64 x 50001, 4000 tokens, 11.1 -> 12.3 with eight); sorted ones are larger, and
+        // two by two is best throughout
         if (sums.all_x <= kThreads)
             take(std::integral_constant<uint32_t, 1>{});
         else if (SORTED || sums.all_x <= 2 * kThreads)
             take(std::integral_constant<uint32_t, 2>{});
-        else
+        else if (MOST == kMost || sums.all_x <= 4 * kThreads)
             take(std::integral_constant<uint32_t, 4>{});
+        else
+            take(std::integral_constant<uint32_t, MOST == kMost ? 4 : 8>{});
         __syncthreads();
     }
     __syncthreads();
