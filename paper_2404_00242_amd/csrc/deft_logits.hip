@@ -67,7 +67,7 @@ constexpr int kSortThreads = 1024;
 constexpr int kRun = 1024;        // tokens that deft_sort_tokens takes to a workgroup
 constexpr int kMaxTiles = 2048;   // that it sorts by
 constexpr int kFill = 512;        // workgroups that the chip holds with no trouble: two to a compute unit
-constexpr int kFewTokens = 9000;  // are looked through unsorted by as many workgroups, see sorts
+constexpr int kFewTokens = 11000;  // are looked through unsorted by as many workgroups, see sorts
 
 // A value that is the same for all lanes, by a scalar load.
 template <typename T>
@@ -483,10 +483,11 @@ Shape shape_of(uint32_t nq, uint32_t vocab) {
     s.groups = (uint64_t)s.tiles * ((nq + s.block - 1) / s.block);
     return s;
 }
-// Whether tokens are sorted before they are looked for.  us, unsorted -> sorted: one query x 128000, 125 workgroups, 6000 tokens 9.5 ->
-// 9.6, 8000 11.5 -> 10.4; 64 x 50001, 490 workgroups, 7000 tokens 14.1 -> 14.5, 8000 15.5 -> 15.0; 80 x 128000, 1250 workgroups, 2000
-// tokens 16.4 -> 19.0, 4000 19.9 -> 19.1; 200 x 128000, 3125 workgroups, 1200 tokens 30.5 -> 33.3, 2200 34.4 -> 33.9.  That is in a graph;
-// otherwise the host has a second launch to make, 3 us (one query, 8191 tokens, 11.6 -> 13.4), so the line is drawn somewhat later.
+// Whether tokens are sorted before they are looked for.  us, unsorted -> sorted: one query x 128000, 125 workgroups, 9500 tokens 11.1 ->
+// 10.9, 13000 13.2 -> 11.6; 4 x 32000 9500 tokens 11.3 -> 12.6, 13000 13.5 -> 13.6; 64 x 50001, 490 workgroups, 9500 tokens 13.9 -> 14.8,
+// 13000 16.3 -> 15.9; 80 x 128000, 1250 workgroups, 2000 tokens 16.4 -> 19.0, 4000 19.9 -> 19.1; 200 x 128000, 3125 workgroups, 1200
+// tokens 30.5 -> 33.3, 2200 34.4 -> 33.9.  That is in a graph; otherwise the host has a second launch to make, 3 us, so the line is
+// drawn somewhat later.
 bool sorts(const deft_plan_t *plan, int64_t total, const Shape &s) {
     if (s.tiles > kMaxTiles || total >= (int64_t(1) << 30)) return false;
     return plan->n_segs() > kPieces || total * (int64_t)std::max<uint64_t>(s.groups, kFill) > (int64_t)kFewTokens * kFill;
