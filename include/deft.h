@@ -482,8 +482,8 @@ int deft_rope(const double *frequency, int32_t rot, int32_t layout, double facto
  * q or k may be NULL, and so may rope: nothing is turned then, and positions are not looked at.
  *
  * deft_qkv_store does the same and stores keys and values into a bf16 cache of n_rows rows, token i into row rows[i] of the list
- * (deft_kv_rows; its blocks have no part in it): k->out and v->out are the K and V pools [n_rows, Hkv, d].  Values are copied bit for
- * bit.  Other rows stay as they are.  q may be NULL; its out is as for the calls above.  n is the list's.
+ * (deft_kv_rows; its blocks have no part in it): k->out and v->out are the K and V pools [n_rows, Hkv, d], which none of the call's
+ * inputs lies in, k->x and v->x neither.  Values are copied bit for bit.  Other rows stay as they are.  q may be NULL; its out is as for the calls above.  n is the list's.
  *
  * deft_qkv_store_q8 stores them into an 8-bit cache, and leaves it as deft_qk_norm_rotate (into bf16 keys) and deft_kv_store_q8 after it
  * would, byte for byte: the scales, the rows kept of a block and those behind them, infinities and NaN as there.  The out of k and v

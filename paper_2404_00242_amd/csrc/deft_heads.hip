@@ -568,10 +568,11 @@ int check(const deft_heads_t *const (&parts)[kParts], int64_t n, int32_t d, floa
         t.heads = (uint32_t)p->heads;
         call.heads += t.heads;
     }
-    for (int i = 0; i < kParts; ++i)  // what is written is nobody else's, and nobody's input but the part's own, in place
-        for (int j = 0; j < kParts; ++j) {
+    for (int i = 0; i < kParts; ++i)  // what is written is nobody else's, and nobody's input but the part's own, in place (not in a pool,
+        for (int j = 0; j < kParts; ++j) {  // whose rows are others than the tokens')
             if (out[i].begin == out[i].end) continue;
-            if (!(i == j && out[i].same(in[i])) && !apart(out[i], in[j])) return DEFT_EINVAL;
+            const bool own = i == j && (where == kOwnOut || i == kQ) && out[i].same(in[i]);
+            if (!own && !apart(out[i], in[j])) return DEFT_EINVAL;
             if (j < i && !apart(out[i], out[j])) return DEFT_EINVAL;
         }
     for (int i = 0; i < kParts; ++i) {  // nor a weight or position

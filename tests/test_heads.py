@@ -132,6 +132,23 @@ def test_calls_that_are_refused():
     assert store(lst=none.handle, rope=None, positions=None) == 0
 
 
+def test_keys_and_values_in_their_own_pool_are_refused():
+    # token i goes to row rows[i]: where the heads are the pool's own rows another wave has yet to read that one
+    lib, rope = binding.load_library(), binding.deft_rope(64).packed
+    for at in ([7, 6, 5, 4, 3, 2, 1, 0], [1, 0], [0, 1, 2], [0]):
+        n = len(at)
+        rows = binding.deft_kv_rows(at, n, 4)
+
+        def store(k, v, q=None):
+            return lib.deft_qkv_store(rows.handle, 1 << 16, q, k, v, n, 64, 1e-6, 0.0, 1 << 12, rope, None)
+
+        here, there = _part(out=1 << 20), _part(x=1 << 21, out=1 << 25)
+        assert store(here, there) == store(there, here) == EINVAL, at
+        assert store(here, _part(x=1 << 22, out=1 << 22)) == store(_part(x=1 << 20, weight=1 << 12, out=1 << 20), there) == EINVAL, at
+        # nor is a pool the other's heads, or the queries
+        assert store(_part(out=1 << 21), there) == store(there, _part(x=1 << 20, out=1 << 26), _part(x=1 << 26, out=1 << 27)) == EINVAL, at
+
+
 def test_cpu_tensors_are_refused():
     x = torch.zeros((2, 4, 64), dtype=torch.bfloat16)
     p, rope = torch.zeros(2, dtype=torch.int32), binding.deft_rope(64)
