@@ -351,7 +351,7 @@ class Plan:
         """(address, Hq / Hkv) of an image of any ratio: the tree is the same in all.  One that is there is taken and none made, since
         the first image of a ratio decides how the attention's tasks are cut."""
         ready = None
-        for key, image in self._images.of.items():
+        for key, image in self._images.of.copy().items():  # (another thread may add one meanwhile)
             if type(key[0]) is tuple:  # a capture's own
                 key = key[0]
             elif key[1] == index and not capture and raw in image.streams:

@@ -62,6 +62,24 @@ def test_calls_that_are_refused():
         binding.deft_adjust_logits(plan, torch.zeros((4, 10)))
 
 
+def test_an_image_is_looked_for_while_another_thread_adds_one():
+    t = wl.random_tree(3, n_nodes=5, nq=4)
+    plan = plan_of(t)[0]
+
+    class Index(int):  # a device's number; while it is compared, another thread makes an image
+        def __eq__(self, other):
+            plan._images.of[(len(plan._images.of) + 10, 7)] = image
+            return int(self) == other
+
+        __hash__ = int.__hash__
+
+    image = binding._Images._Image()
+    image.tensor, image.event, image.first, image.streams = torch.zeros(1), None, 5, {5}
+    plan._images.of.update({(4, Index(1)): image, (2, Index(1)): image, (3, Index(0)): image})
+    assert plan._any_image(0, 5, 0) == (image.tensor.data_ptr(), 3)
+    assert len(plan._images.of) > 3
+
+
 # ---- on the GPU ----
 
 def dev():
