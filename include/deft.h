@@ -451,7 +451,8 @@ int deft_compact_pages(const int32_t *node_page_ptr, const int32_t *page_ids, in
  *                         them the share of either is linear in i (from the floor of the one's real index to the ceiling of the
  *                         other's); high, low default to 32, 1 where not above 0; *factor is 0.1 ln(scale) + 1 where scale > 1
  *   DEFT_ROPE_WAVELENGTH  the same, linear in the turns themselves; 4, 1
- * *factor is 1 otherwise.  Errors of both: DEFT_EINVAL (null, a number outside of what is said here or not finite).
+ * *factor is 1 otherwise.  Errors of both: DEFT_EINVAL (null, a number outside of what is said here or not finite, the scaled base and
+ * the frequencies that come of it among them).  Nothing is written then.
  */
 #define DEFT_ROPE_HALF 0
 #define DEFT_ROPE_INTERLEAVED 1

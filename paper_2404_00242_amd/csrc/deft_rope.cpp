@@ -7,6 +7,7 @@
 
 namespace {
 constexpr int kMaxRot = 128;
+constexpr double kMaxFrequency = 1e6;  // radians a position
 bool rot_ok(int32_t rot) { return rot >= 16 && rot <= kMaxRot && rot % 16 == 0; }
 constexpr long double kTurn = 6.283185307179586476925286766559005768L;
 }  // namespace
@@ -23,6 +24,7 @@ extern "C" int deft_rope_frequencies(int32_t rot, double base, int32_t scaling, 
         if (!std::isfinite(original) || original <= 0 || !std::isfinite(high) || low >= high) return DEFT_EINVAL;
     }
     if (scaling == DEFT_ROPE_BASE) base *= std::pow(scale, rot / (rot - 2.0));
+    if (!std::isfinite(base) || base <= 1) return DEFT_EINVAL;
     // the dimension that makes `turns` turns within the original length, as a real number
     auto dimension = [&](double turns) { return rot * std::log(original / (turns * (double)kTurn)) / (2 * std::log(base)); };
     double first = 0, width = 1;
@@ -30,14 +32,17 @@ extern "C" int deft_rope_frequencies(int32_t rot, double base, int32_t scaling, 
         first = std::max(std::floor(dimension(high)), 0.0);
         width = std::max(std::min(std::ceil(dimension(low)), rot - 1.0) - first, 0.001);
     }
+    double out[kMaxRot / 2];
     for (int32_t i = 0; i < rot / 2; ++i) {
         const double f = std::pow(base, -2.0 * i / rot);
         double keep = 1;  // share of f that stays f; the rest becomes f / scale
         if (scaling == DEFT_ROPE_LINEAR) keep = 0;
         if (scaling == DEFT_ROPE_DIMENSION) keep = 1 - std::clamp((i - first) / width, 0.0, 1.0);
         if (scaling == DEFT_ROPE_WAVELENGTH) keep = std::clamp((original * f / (double)kTurn - low) / (high - low), 0.0, 1.0);
-        frequency[i] = f * keep + (keep < 1 ? f / scale * (1 - keep) : 0);
+        out[i] = f * keep + (keep < 1 ? f / scale * (1 - keep) : 0);
+        if (!(out[i] <= kMaxFrequency)) return DEFT_EINVAL;
     }
+    std::copy(out, out + rot / 2, frequency);
     *factor = scaling == DEFT_ROPE_DIMENSION && scale > 1 ? 0.1 * std::log(scale) + 1 : 1;
     return DEFT_OK;
 }
@@ -53,7 +58,7 @@ extern "C" int deft_rope(const double *frequency, int32_t rot, int32_t layout, d
     rope.layout = layout;
     rope.factor = (float)factor;
     for (int32_t i = 0; i < rot / 2; ++i) {
-        if (!std::isfinite(frequency[i]) || std::fabs(frequency[i]) > 1e6) return DEFT_EINVAL;
+        if (!std::isfinite(frequency[i]) || std::fabs(frequency[i]) > kMaxFrequency) return DEFT_EINVAL;
         const long double turns = std::fabs((long double)frequency[i]) / kTurn, part = std::ldexp(turns - std::floor(turns), 64);
         const long double bits = std::round(part);  // 0 .. 2^64
         rope.turns[i] = bits >= std::ldexp(1.0L, 64) ? 0 : (uint64_t)bits;

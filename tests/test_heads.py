@@ -75,6 +75,30 @@ def test_ropes_that_are_refused():
     assert lib.deft_rope_frequencies(64, 1e4, 0, 1, 1, 1, 1, None, one) == EINVAL
 
 
+@pytest.mark.parametrize("bad", [
+    dict(scaling="base", base=1e300, scale=1e30),  # the base leaves 64 bits: all pairs but the first would stand still
+    dict(scaling="base", scale=1e-9), dict(scaling="base", base=2.0, scale=0.5),  # a base of one or less
+    dict(scaling="linear", scale=5e-324), dict(scaling="linear", scale=1e-7),  # infinite, and more than a rope takes
+    dict(scaling="dimension", scale=1e-300, original=4096), dict(scaling="wavelength", scale=1e-300, original=4096)], ids=str)
+def test_scalings_that_lead_out_of_a_ropes_range_are_refused(bad):
+    for rot in (16, 128):
+        with pytest.raises(binding.DeftError):
+            binding.deft_rope_frequencies(rot, **bad)
+        with pytest.raises(binding.DeftError):
+            binding.deft_rope(rot, **bad)
+
+
+@pytest.mark.parametrize("good", [dict(scaling="linear", scale=1.1e-6), dict(scaling="base", scale=0.9, base=2.0), dict(scaling="base", base=1e200, scale=1e30),
+                                  dict(base=1e300), dict(base=1 + 1e-9), dict(scaling="linear", scale=1e300)], ids=str)
+def test_scalings_at_the_ends_of_a_ropes_range(good):
+    for rot in (16, 128):
+        f, factor = binding.deft_rope_frequencies(rot, **good)
+        want, _ = model.frequencies(rot, **good)
+        # the power's argument is off by a few roundings, times the base's logarithm: at most 1100 of them
+        assert np.allclose(f, want, rtol=4096 * 2.0 ** -53, atol=0) and factor == 1 and np.isfinite(f).all()
+        binding.deft_rope(rot, **good)
+
+
 # ---- refusals (CPU: addresses that nothing reads) ----
 
 def _part(x=1 << 20, token=256, head=64, out=1 << 24, weight=0, step=0, wide=0, heads=4):
