@@ -906,8 +906,9 @@ def deft_rope_frequencies(rot: int, base: float = 10000.0, scaling: str = "none"
     of scaling.  `original` is the context's length before it was stretched `scale` times."""
     if scaling not in ROPE_SCALINGS:
         raise DeftError(-1, f"deft_rope_frequencies: scaling is one of {', '.join(ROPE_SCALINGS)}")
-    f, factor = np.zeros(max(int(rot) // 2, 1)), ctypes.c_double()
-    _check(load_library().deft_rope_frequencies(_size(rot, "deft_rope_frequencies"), float(base), ROPE_SCALINGS[scaling], float(scale), float(original), float(low),
+    rot = _size(rot, "deft_rope_frequencies")
+    f, factor = np.zeros(min(max(rot // 2, 1), 64)), ctypes.c_double()  # (a rope has no more pairs)
+    _check(load_library().deft_rope_frequencies(rot, float(base), ROPE_SCALINGS[scaling], float(scale), float(original), float(low),
                                                 float(high), f.__array_interface__["data"][0], ctypes.byref(factor)), "deft_rope_frequencies")
     return f, factor.value
 

@@ -43,6 +43,13 @@ def _pi():
     return 4 * (4 * arctan(5) - arctan(239))
 
 
+@pytest.mark.parametrize("rot", [1 << 62, 1 << 45, -(1 << 62), 1 << 30, 130])
+def test_sizes_of_ropes_are_looked_at_before_memory_is_taken_for_them(rot):
+    for call in (lambda: binding.deft_rope_frequencies(rot), lambda: binding.deft_rope(rot)):
+        with pytest.raises(binding.DeftError):
+            call()
+
+
 def test_turns_are_the_frequencies_to_sixty_four_bits():
     rng = np.random.default_rng(1)
     f = np.concatenate([10000.0 ** (-np.arange(32) / 32), rng.uniform(-1e6, 1e6, 16), [0.0, -1e-9, 2 * math.pi, 1e6], rng.uniform(-7, 7, 12)])
