@@ -211,6 +211,8 @@ __device__ __forceinline__ void heads_of_wave(const HeadsArgs &a, uint32_t unit,
         cs[0][lane] = c * a.factor;
         cs[1][lane] = s * a.factor;
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // other lanes' angles are read from here on (a wave's LDS operations stay in
+    __builtin_amdgcn_wave_barrier();                        // order: neither costs an instruction)
     float y0[8], y1[8];
     unpack8(x0, y0);
     unpack8(x1, y1);

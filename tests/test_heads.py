@@ -370,6 +370,29 @@ def test_extreme_heads(d, rot):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("d,H", [(128, 9), (64, 17)])
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_every_pair_has_its_own_angle_in_every_wave(d, H, layout):
+    # a lane makes one pair's angle and the others of its wave read it: frequencies and positions that are all different, waves of
+    # several batches of heads, and the same tokens in other waves and workgroups
+    n = 2000
+    rng = np.random.default_rng(d)
+    f = rng.uniform(-3, 3, d // 2)
+    rope = binding.deft_rope(d, layout=layout, frequencies=f)
+    p = rng.permutation(1 << 20)[:n].astype(np.int32)
+    x = values(n, H, d, 3)
+    got = binding.deft_rotate(x.to(dev()), on_gpu(p), rope)
+    close(got, *model.heads(x.double().numpy(), p, f, 1.0, layout == "interleaved"))
+    for _ in range(3):
+        at = torch.from_numpy(rng.permutation(n)[:n - 7])
+        assert torch.equal(binding.deft_rotate(x[at].to(dev()), on_gpu(p)[at.to(dev())], rope), got[at.to(dev())])
+    # the waves of the queries in a store into an 8-bit cache
+    cache = binding.alloc_kv_cache_q8(n, 2, d, 16, dev())
+    q = binding.deft_qkv_store_q8(binding.deft_kv_rows(np.arange(n), n, 16), x.to(dev()), x[:, :2].to(dev()), x[:, 2:4].to(dev()), cache, on_gpu(p), rope)
+    assert torch.equal(q, got)
+
+
+@pytest.mark.gpu
 def test_turning_back_and_relative_positions():
     rope = binding.deft_rope(128)
     x = values(64, 8, 128, 1, 0.0).to(dev())
