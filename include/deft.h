@@ -507,7 +507,9 @@ int deft_qkv_store_q8(const deft_kv_list_t *list, const void *dev_image, const d
  * token t of query j, with c_all the number of times that t stands on the tokens of j's path and c the same without prompt tokens:
  *   x becomes x / repetition[j] where x > 0 and x * repetition[j] otherwise, if c_all > 0;
  *   then x - (frequency[j] * c + presence[j]), if c > 0;  then x + bias[bias_row[j]][t];  then -inf where the mask's bit t is 0
- * in fp32, rounded once to the type of the output.  What is NULL is left out.  A mask may leave nothing: the row is then all -inf.
+ * in fp32, rounded once to the type of the output.  (x / repetition[j] is the fp32 product x * (1 / repetition[j]), whose two roundings are
+ * half a step each; penalties outside 2^-126 .. 2^126, whose reciprocal fp32 does not hold, divide.)  What is NULL is left out.  A mask may
+ * leave nothing: the row is then all -inf.
  *
  * logits, out          : device [nq, vocab], queries (the caller's order) stride and out_stride elements apart, aligned as their type; the
  *                        strides are at most 2^31, out_stride at least vocab.  float where logits_f32, out_f32 are set, else bf16; bf16 logits may

@@ -278,6 +278,36 @@ def test_extreme_logits_and_tables(wide):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("wide", [False, True])
+def test_the_repetition_penalty_is_a_quotient(wide):
+    # two roundings of fp32, the reciprocal's and the product's, also where the reciprocal would leave fp32 or its normal numbers
+    r = np.array([1.1, 1.3, 3.0, 0.7, 3e38, 1e-39, 2e-45, 2.0 ** 127, 1e-30], np.float32)
+    t = wl.random_tree(6, n_nodes=9, max_len=200, nq=len(r))
+    s = Inputs(t, 700, 8, wide)
+    s.x[:, ::3] *= 2.0 ** -80
+    s.x[:, 1::3] *= 2.0 ** 110
+    s.x[:, 1::17] = 2.0 ** -126
+    s.repetition = r
+    plan, row_of, pool = plan_of(t)
+    plan.image(t.Hq, t.Hkv, dev())
+    got = s.call(plan, row_of, pool, out_dtype=torch.float32, repetition=True).cpu().numpy()
+    x = s.x.float().numpy()
+    some = 0
+    for j in range(t.nq):
+        on = s.tokens[model.path(t, j)].astype(np.int64)
+        on = np.bincount(on[(on >= 0) & (on % PROMPT < 700)] % PROMPT, minlength=700) > 0
+        y = x[j].astype(np.float64)
+        want = np.where(on, np.where(y > 0, y / float(r[j]), y * float(r[j])), y)
+        # half a step each, 2^-24, and their product; below fp32's normal numbers half of their step, 2^-150
+        out = np.abs(want) >= 2.0 ** 128 * (1 - 2.0 ** -24)
+        assert (got[j][out] == np.copysign(np.inf, want[out])).all()
+        off = np.abs(got[j][~out] - want[~out]) - (2.0 ** -23 * (1 + 2.0 ** -20) * np.abs(want[~out]) + 2.0 ** -150)
+        assert (off <= 0).all(), (j, off.max())
+        some += (on & (x[j] > 0)).sum()
+    assert some > 500
+
+
+@pytest.mark.gpu
 def test_in_place_and_rows_apart():
     t = wl.random_tree(8, n_nodes=9, max_len=50, nq=6)
     plan, row_of, pool = plan_of(t)
