@@ -80,6 +80,30 @@ def test_an_image_is_looked_for_while_another_thread_adds_one():
     assert len(plan._images.of) > 3
 
 
+def _tree(kind, **sizes):
+    return getattr(wl, kind)(**sizes)
+
+
+@pytest.mark.parametrize("sorts,vocab,tree,plan", [
+    (False, 5003, ("random_tree", dict(seed=5003, n_nodes=14, max_len=90, nq=11, n_roots=2)), {}),
+    (False, 777, ("random_tree", dict(seed=902, n_nodes=37, max_len=150, nq=40, n_roots=3)), dict(chunk=64, page=16)),
+    (True, 777, ("random_tree", dict(seed=902, n_nodes=37, max_len=150, nq=40, n_roots=3)), dict(chunk=64, page=1)),
+    (True, 777, ("random_tree", dict(seed=903, n_nodes=54, max_len=90, nq=100, n_roots=4)), dict(chunk=64, flags=binding.SPLIT_MODES["query"])),
+    (True, 30011, ("random_tree", dict(seed=77, n_nodes=300, max_len=12, nq=1100, n_roots=3)), {}),
+    (True, 2500, ("config5_longcontext", dict(root=6000, branches=9, lo=1, hi=700)), dict(flags=binding.DEFT_SPLIT_BALANCED | binding.rows_per_query(4))),
+    (True, 2500, ("config5_longcontext", dict(root=6000, branches=9, lo=1, hi=700)), dict(page=1)),
+    (True, 3000, ("config5_longcontext", dict(root=6000, branches=9, lo=1, hi=700)), dict(page=16)),
+    (True, 5000, ("config2_fewshot", dict(prefix=290_000, branches=3, gen=20_000)), dict(chunk=1024)),
+    (True, 2000, ("config2_fewshot", dict(prefix=70000, branches=3, gen=5)), {}),
+    (False, 3001, ("random_tree", dict(seed=18, n_nodes=20, max_len=50, nq=30)), {}),
+    (True, 20000, ("config5_longcontext", dict(root=3000, branches=16, lo=10, hi=300)), {}),
+], ids=str)
+def test_trees_of_the_tests_below_take_the_form_that_is_meant(sorts, vocab, tree, plan):
+    # both forms are tested below, by these trees: where the line between them moves, they have to move with it
+    plan = plan_of(_tree(tree[0], **tree[1]), **plan)[0]
+    assert (binding.load_library().deft_logits_workspace_bytes(plan.handle, vocab) > 0) == sorts
+
+
 # ---- on the GPU ----
 
 def dev():
@@ -455,3 +479,47 @@ def test_two_streams_at_once():
         for side in sides:
             torch.cuda.current_stream().wait_stream(side)
         assert all(torch.equal(a, b) for a, b in zip(got, [want, other] * 2))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("counts", [False, True])
+def test_sorted_tokens_captured_and_replayed(counts):
+    # two launches and a workspace of the graph's own, taken while it is captured; tokens, logits and tables change between replays,
+    # and eager calls with other tokens, in workspaces of theirs, stand in between
+    t, vocab = wl.config5_longcontext(root=3000, branches=16, lo=10, hi=300), 20000
+    which = {k: v for k, v in ALL.items() if counts or k != "frequency"}
+    s = Inputs(t, vocab, 3, True)
+    plan, row_of, pool = plan_of(t)
+    assert binding.load_library().deft_logits_workspace_bytes(plan.handle, vocab) > 0
+    plan.image(t.Hq, t.Hkv, dev())
+    x, tokens, args = s.x.to(dev()), gpu(s.tokens), {k: gpu(getattr(s, k)) for k in which}
+    torch.cuda.synchronize()
+    graphs, results = [], []
+    for _ in range(2):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            results.append((binding.deft_adjust_logits(plan, x, tokens, **args), binding.deft_adjust_logits(plan, x, tokens, presence=args["presence"])))
+    spaces = [w[0] for k, w in plan._workspaces.items() if k[0] == "logits"]
+    assert len(spaces) == len(set(spaces)) == 2
+    other_tokens = gpu(Inputs(t, vocab, 99, True).tokens)
+    side = torch.cuda.Stream()
+    for i in range(4):
+        n = Inputs(t, vocab, 20 + i, True)
+        x.copy_(n.x)
+        tokens.copy_(gpu(n.tokens))
+        for k in which:
+            args[k].copy_(gpu(getattr(n, k)))
+        torch.cuda.synchronize()
+        for graph, (a, b) in zip(graphs, results):
+            graph.replay()
+            # at the same time, on another stream
+            with torch.cuda.stream(side):
+                between = binding.deft_adjust_logits(plan, x, other_tokens, presence=args["presence"])
+            eager = binding.deft_adjust_logits(plan, x, tokens, **args)
+            assert torch.equal(a.nan_to_num(), eager.nan_to_num())
+            assert torch.equal(b, binding.deft_adjust_logits(plan, x, tokens, presence=args["presence"]))
+            side.synchronize()
+            assert torch.equal(between, binding.deft_adjust_logits(plan, x, other_tokens, presence=args["presence"]))
+        if i in (0, 3):
+            close(results[0][0], *n.want(**which))
+        torch.cuda.synchronize()
