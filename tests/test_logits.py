@@ -523,3 +523,50 @@ def test_sorted_tokens_captured_and_replayed(counts):
         if i in (0, 3):
             close(results[0][0], *n.want(**which))
         torch.cuda.synchronize()
+
+
+@pytest.mark.gpu
+def test_two_host_threads():
+    # each on a stream of its own, with the same plan and lists: logits of both forms, and heads
+    import threading
+    from concurrent.futures import ThreadPoolExecutor
+
+    big, small = wl.config5_longcontext(root=3000, branches=16, lo=10, hi=300), wl.random_tree(18, n_nodes=20, max_len=50, nq=30)
+    room = binding.load_library().deft_logits_workspace_bytes
+    work = []
+    for t, vocab in ((big, 20000), (small, 3001)):
+        s = Inputs(t, vocab, 3, True)
+        plan = plan_of(t)[0]
+        assert (room(plan.handle, vocab) > 0) == (t is big)
+        plan.image(t.Hq, t.Hkv, dev())
+        work.append((plan, s.x.to(dev()), gpu(s.tokens), {k: gpu(getattr(s, k)) for k in ALL}))
+    want = [binding.deft_adjust_logits(p, x, tokens, **a) for p, x, tokens, a in work]
+    n, Hq, Hkv, d = 500, 8, 2, 128
+    heads = torch.randn((n, Hq + 2 * Hkv, d), device=dev()).to(torch.bfloat16)
+    rope, p = binding.deft_rope(d), torch.arange(n, dtype=torch.int32, device=dev())
+    rows = binding.deft_kv_rows(np.random.default_rng(1).permutation(n), n, 1)
+
+    def store(pools):
+        return binding.deft_qkv_store(rows, heads[:, :Hq], heads[:, Hq:Hq + Hkv], heads[:, Hq + Hkv:], pools, p, rope)
+
+    def pools():
+        return [torch.zeros((n, Hkv, d), dtype=torch.bfloat16, device=dev()) for _ in range(2)]
+
+    kept = pools()
+    q = store(kept)
+    torch.cuda.synchronize()
+    start = threading.Barrier(2)
+
+    def one():
+        with torch.cuda.stream(torch.cuda.Stream()):
+            mine = pools()
+            start.wait(30)
+            for _ in range(30):
+                got = [binding.deft_adjust_logits(p, x, tokens, **a) for p, x, tokens, a in work]
+                mine_q = store(mine)
+            torch.cuda.current_stream().synchronize()
+            return all(torch.equal(a.nan_to_num(), b.nan_to_num()) for a, b in zip(got, want)) and torch.equal(mine_q, q) and all(torch.equal(a, b) for a, b in zip(mine, kept))
+
+    with ThreadPoolExecutor(2) as pool:
+        done = [pool.submit(one) for _ in range(2)]
+        assert [f.result(60) for f in done] == [True, True]
