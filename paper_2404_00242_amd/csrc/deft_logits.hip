@@ -68,6 +68,7 @@ constexpr int kRun = 1024;        // tokens that deft_sort_tokens takes to a wor
 constexpr int kMaxTiles = 2048;   // that it sorts by
 constexpr int kFill = 512;        // workgroups that the chip holds with no trouble: two to a compute unit
 constexpr int kFewTokens = 11000;  // are looked through unsorted by as many workgroups, see sorts
+constexpr int kStepTokens = 3500;
 
 // A value that is the same for all lanes, by a scalar load.
 template <typename T>
@@ -512,9 +513,16 @@ Shape shape_of(uint32_t nq, uint32_t vocab) {
 // 13000 16.3 -> 15.9; 80 x 128000, 1250 workgroups, 2000 tokens 16.4 -> 19.0, 4000 19.9 -> 19.1; 200 x 128000, 3125 workgroups, 1200
 // tokens 30.5 -> 33.3, 2200 34.4 -> 33.9.  That is in a graph; otherwise the host has a second launch to make, 3 us, so the line is
 // drawn somewhat later.
+// Pieces beyond the first kPieces are looked through in further steps, each of which costs as much as 2000 tokens where there are few
+// workgroups and 4000 where there are 500, and counts as kStepTokens.  In pages of one row: one query x 128000, 600 tokens 6.4 -> 8.4, 1000 6.5 ->
+// 8.8, 1500 8.3 -> 9.9, 2000 10.0 -> 10.2, 4000 17.2 -> 11.0; 20 x 128000, 1160 11.0 -> 12.4, 1660 13.3 -> 12.4, 2160 15.4 -> 12.6; 64 x 50001, 1512 12.1 -> 13.6,
+// 2012 14.2 -> 13.7; 120 x 128000, 1360 28.7 -> 25.1.  In pages of 16 rows: one query x 128000, 8000 tokens (500 pieces) 9.4 -> 10.9, 8193 (513) 10.5 -> 10.9,
+// 8400 11.8 -> 11.1; 4 x 32000, 8225 11.0 -> 12.2, 12000 13.5 -> 13.9; 20 x 128000, 8353 14.5 -> 12.9; 64 x 50001, 8912 16.0 -> 14.6.  In pages of 64, one
+// query x 128000: 8400 11.2 -> 11.0, 12000 12.7 -> 11.9.
 bool sorts(const deft_plan_t *plan, int64_t total, const Shape &s) {
     if (s.tiles > kMaxTiles || total >= (int64_t(1) << 30)) return false;
-    return plan->n_segs() > kPieces || total * (int64_t)std::max<uint64_t>(s.groups, kFill) > (int64_t)kFewTokens * kFill;
+    const int64_t steps = (plan->n_segs() + kPieces - 1) / kPieces, cost = total + kStepTokens * std::max<int64_t>(steps - 1, 0);
+    return cost * (int64_t)std::max<uint64_t>(s.groups, kFill) > (int64_t)kFewTokens * kFill;
 }
 struct Space {
     uint64_t groups, table, seen_by, bytes;  // places

@@ -88,6 +88,7 @@ def _tree(kind, **sizes):
     (False, 5003, ("random_tree", dict(seed=5003, n_nodes=14, max_len=90, nq=11, n_roots=2)), {}),
     (False, 777, ("random_tree", dict(seed=902, n_nodes=37, max_len=150, nq=40, n_roots=3)), dict(chunk=64, page=16)),
     (True, 777, ("random_tree", dict(seed=902, n_nodes=37, max_len=150, nq=40, n_roots=3)), dict(chunk=64, page=1)),
+    (False, 777, ("random_tree", dict(seed=901, n_nodes=20, max_len=40, nq=9, n_roots=2)), dict(chunk=64, page=1)),
     (True, 777, ("random_tree", dict(seed=903, n_nodes=54, max_len=90, nq=100, n_roots=4)), dict(chunk=64, flags=binding.SPLIT_MODES["query"])),
     (True, 30011, ("random_tree", dict(seed=77, n_nodes=300, max_len=12, nq=1100, n_roots=3)), {}),
     (True, 2500, ("config5_longcontext", dict(root=6000, branches=9, lo=1, hi=700)), dict(flags=binding.DEFT_SPLIT_BALANCED | binding.rows_per_query(4))),
@@ -102,6 +103,23 @@ def test_trees_of_the_tests_below_take_the_form_that_is_meant(sorts, vocab, tree
     # both forms are tested below, by these trees: where the line between them moves, they have to move with it
     plan = plan_of(_tree(tree[0], **tree[1]), **plan)[0]
     assert (binding.load_library().deft_logits_workspace_bytes(plan.handle, vocab) > 0) == sorts
+
+
+@pytest.mark.parametrize("page,unsorted,sorted_", [(1, (1, 512, 513, 600, 1000, 1500), (2500, 8193)), (8, (4096, 4097, 7000), (8193, 12000)), (16, (8191,), (9500, 16000)),
+                                                   (64, (8191, 8193, 10000), (12000, 32000))])
+def test_the_line_from_which_tokens_are_sorted_goes_by_tokens_and_pieces(page, unsorted, sorted_):
+    # pieces add to the cost as they are measured to; 512 of them, which are looked at together, are no limit by themselves
+    room = binding.load_library().deft_logits_workspace_bytes
+
+    def plan(n):
+        t = wl.Tree("line", np.array([0]), np.array([n]), np.array([-1]), np.array([0]), n, 8, 2, 128)
+        return plan_of(t, page=page)[0]
+
+    for vocab in (32000, 128000):
+        for n in unsorted:
+            assert room(plan(n).handle, vocab) == 0, (n, vocab)
+        for n in sorted_:
+            assert room(plan(n).handle, vocab) > 0, (n, vocab)
 
 
 # ---- on the GPU ----
