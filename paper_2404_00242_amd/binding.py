@@ -1191,9 +1191,10 @@ def _per_query(t, shape, dtype, index, name: str):
 
 def _table(t, width, dtype, row, of_nq, index, name: str):
     """(address, distance of rows, number of rows, address of the queries' row numbers) of a table of biases or masks."""
-    rows, *one = shape = t.shape if t.dim() != 1 else (1, t.shape[0])
-    if t.dtype is not dtype or len(shape) != 2 or rows < 1 or one[0] != width or t.get_device() != index or (width > 1 and t.stride(-1) != 1):
+    shape = t.shape if t.dim() != 1 else (1, t.shape[0])
+    if t.dtype is not dtype or len(shape) != 2 or shape[0] < 1 or shape[1] != width or t.get_device() != index or (width > 1 and t.stride(-1) != 1):
         raise DeftError(-1, f"deft_adjust_logits: {name} must be a {dtype} [rows, {width}] tensor of contiguous rows on the logits' device")
+    rows = shape[0]
     return t.data_ptr(), t.stride(0) if rows > 1 else 0, rows, 0 if row is None else _per_query(row, of_nq, _torch.int32, index, name + "_row")
 
 

@@ -427,6 +427,16 @@ def test_gpu_refusals():
 
 
 @pytest.mark.gpu
+def test_tables_of_no_and_of_three_dimensions_are_refused():
+    t = wl.random_tree(8, n_nodes=9, max_len=50, nq=6)
+    plan, x = plan_of(t)[0], torch.zeros((6, 1), device=dev())
+    for shape in ((), (1, 1, 1)):
+        for bad in (dict(bias=torch.zeros(shape, device=dev())), dict(mask=torch.zeros(shape, dtype=torch.int32, device=dev()))):
+            with pytest.raises(binding.DeftError, match="must be a"):
+                binding.deft_adjust_logits(plan, x, **bad)
+
+
+@pytest.mark.gpu
 def test_images_are_those_of_the_attention():
     t = wl.random_tree(8, n_nodes=9, max_len=50, nq=6, Hq=8, Hkv=2)
     s = Inputs(t, 300, 3, True)
