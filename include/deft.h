@@ -434,7 +434,8 @@ int deft_compact_pages(const int32_t *node_page_ptr, const int32_t *page_ids, in
  *   heads        : 0 .. DEFT_MAX_Q8_HEADS
  *
  * A head x with a weight becomes x * (weight + weight_offset) / sqrt(mean(x^2) + eps).  Sums and products are fp32, and a result is
- * rounded once, after the rotation (half a step of bf16, and at most 2^-19 of the pair's magnitude).
+ * rounded once, after the rotation (half a step of bf16, and at most 2^-19 of the pair's magnitude).  The product of 1 / sqrt and weight
+ * is one of them: it stays within fp32 for heads of any magnitude while weights with their offset are 0 or within 2^-60 .. 2^80.
  *
  * deft_rope_t: how positions turn heads.  Pair i < rot / 2 of a head turns by positions[token] * frequency[i] radians, and the result
  * is multiplied by factor: (a, b) becomes factor * (a cos - b sin, a sin + b cos).  The pair is elements (i, i + rot / 2) of the head
@@ -515,7 +516,7 @@ int deft_qkv_store_q8(const deft_kv_list_t *list, const void *dev_image, const d
  *                        strides are at most 2^31, out_stride at least vocab.  float where logits_f32, out_f32 are set, else bf16; bf16 logits may
  *                        become float ones.  out may be logits itself with its stride and type, otherwise it
  *                        must not overlap anything that the call reads.
- * vocab                : 1 .. DEFT_MAX_VOCAB
+ * vocab                : 1 .. DEFT_MAX_VOCAB, with ceil(vocab / 1024) * ceil(nq / 8) below 2^23
  * tokens               : device int32 [n_tokens], the token of every row of the KV cache that the plan is for (so a fork or a compaction copies
  *                        its pages like any pool's); at least deft_plan_rows(plan) of them.  Prompt tokens may have DEFT_TOKEN_PROMPT or-ed
  *                        to them: they count for the repetition penalty alone.  Negative numbers, and those from vocab on, are no token.
@@ -526,7 +527,8 @@ int deft_qkv_store_q8(const deft_kv_list_t *list, const void *dev_image, const d
  *                        set where token t is allowed
  * dev_image, group     : with tokens, the image of the plan that deft_plan_upload made for group = Hq / Hkv (any will do); else not looked at
  * workspace            : device, 16-byte aligned, deft_logits_workspace_bytes(plan, vocab) of them (0 where none is used); NULL is right too,
- *                        and slow over many tokens.  Not looked at without tokens.
+ *                        and slow over many tokens.  Not looked at without tokens.  A call's two launches use it one after the other: calls
+ *                        with one workspace are made in turn, also by two host threads on one stream.
  * Asynchronous on `stream`.  Errors: DEFT_EINVAL, DEFT_ENOTREADY, DEFT_EWORKSPACE, DEFT_EHIP as for deft_tree_attn_decode.
  */
 #define DEFT_TOKEN_PROMPT 0x40000000

@@ -983,7 +983,8 @@ def _positions_error(what: str, n):
 
 def deft_rotate(x, positions, rope: Rope, out=None, stream=None):
     """Turns heads by their positions.  x: bf16 [n, H, d] whose tokens and heads may lie apart by multiples of 16 bytes; positions:
-    int32 [n].  Returns bf16 [n, H, d]; out=x turns them in place.  Asynchronous on `stream` (default: torch's current stream); the
+    int32 [n].  Returns bf16 [n, H, d]; out=x turns them in place.  As of all calls here, autograd knows nothing of it: the result has no
+    gradient, and what is changed in place is changed unseen.  Asynchronous on `stream` (default: torch's current stream); the
     current stream has to wait for another one before it reads the result."""
     torch = _torch or _get_torch()
     index, bf16, shape = x.get_device(), torch.bfloat16, x.shape
@@ -1210,7 +1211,7 @@ def deft_adjust_logits(plan: Plan, logits, tokens=None, repetition=None, frequen
     is to count for the repetition penalty alone; -1: none); repetition, frequency, presence: float32 [nq].  bias: float32
     [rows, vocab], mask: int32 [rows, ceil(vocab / 32)] words of allowed tokens' bits; bias_row, mask_row: int32 [nq], the row of
     each query, -1: none (without them row 0 is everyone's).  Returns a new tensor of the logits' type or out_dtype (float32), or
-    out, which may be the logits.  A plan that no attention call has used yet needs plan.image(Hq, Hkv, device) first.
+    out, which may be the logits; autograd knows nothing of it.  A plan that no attention call has used yet needs plan.image(Hq, Hkv, device) first.
     Asynchronous on `stream` (default: torch's current stream); the current stream has to wait for another one before it reads the result."""
     torch = _torch or _get_torch()
     f32, i32, index, dtype = torch.float32, torch.int32, logits.get_device(), logits.dtype

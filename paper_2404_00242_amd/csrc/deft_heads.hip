@@ -167,7 +167,8 @@ __device__ __forceinline__ T uniform(const T *p, uint32_t i) {
 // heads: a lane makes one pair's cosine and sine, and the wave's LDS hands them round.
 // Bound by HBM where calls are large: 8192 tokens x 40 heads of 128, us: copied by this kernel 26.8, turned 27.1, normalised 27.1, both
 // 28.0 (6.0 TB/s); by the host's call, and 3 to 4 us of launch and dependent loads, where they are a decode iteration's.  Two or more
-// batches of heads to a wave, 8192 x 32 turned: 21.0 -> 21.8.  Stores that stay in the caches: 8192 x 32 20.7 -> 25.1.
+// batches of heads to a wave, 8192 x 32 turned: 21.0 -> 21.8.  Stores that stay in the caches: 8192 x 32 (67 MB) 20.7 -> 25.1; of a few
+// tokens, whose heads the attention reads next, the two are not compared.
 template <int D, int TURN, bool NORM>
 __device__ __forceinline__ void heads_of_wave(const HeadsArgs &a, uint32_t unit, float (*cs)[64]) {
     constexpr uint32_t kLanes = D / 16, kHeads = 64 / kLanes;
@@ -286,9 +287,12 @@ struct Cut {
 // of 32 one step after the other, as that kernel's have, takes three times the registers here and its steps wait for one another
 // (32 + 8 heads of 128, 300 tokens 9.7 -> 5.9 us, 8192 37.3 -> 33.1).  So the waves of a unit tell each other their scales, and those of
 // a workgroup make the angles of a block's rows together (8192 tokens, 32 heads: 5 % of the time is theirs).
-// Bound by HBM where calls are large: 8192 tokens, 32 + 8 heads of 128, 184 MB: 33.1 us, 5.6 TB/s, where deft_heads and deft_store_q8 need
-// 38.5; by the launch and dependent loads where they are an iteration's: 20 tokens 4.6 us, 6.5 by the two.  Queries by a launch of their
-// own in front, 8192 tokens: 36.6 -> 39.5 (2048: 13.1 -> 17.6).
+// Bound by HBM where calls are large and most heads are queries: 8192 tokens, 32 + 8 heads of 128, 184 MB: 33.1 us, 5.6 TB/s, where
+// deft_heads and deft_store_q8 need 38.5.  Where most are stored, by what stands between a row's loads and its stores: 32 KV heads of 128
+// alone, 201 MB, in blocks of 32 rows 45.5 us, 4.4 TB/s (a workgroup has one head, so that the angles and both barriers are each head's
+// own, and no loads follow a lane's first four), in blocks of 8 40.6; 32 + 8 heads of 64, 92 MB, 19.7 us, 4.7 TB/s.  By the launch and
+// dependent loads where calls are an iteration's: 20 tokens 4.6 us, 6.5 by the two.  Queries by a launch of their own in front, 8192
+// tokens: 36.6 -> 39.5 (2048: 13.1 -> 17.6).
 template <int D, int BLOCK>
 __global__ __launch_bounds__((Cut<D, BLOCK>::kThreads)) void deft_store_heads_q8(StoreArgs a) {
     using C = Cut<D, BLOCK>;

@@ -370,6 +370,25 @@ def test_extreme_heads(d, rot):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("eps", [0.0, 1e-6])
+def test_weights_at_the_ends_of_their_range(d, eps):
+    # heads of any magnitude with weights from 2^-60 to 2^80 and zeros: their product with the root's reciprocal stays within fp32
+    scale = [2.0 ** 120, 2.0 ** 50, 2.0 ** 49, 1.0, 2.0 ** -39, 2.0 ** -40, 2.0 ** -120]
+    x = values(len(scale), 3, d, 9, 0.0)
+    x = (x.double() * torch.tensor(scale, dtype=torch.float64)[:, None, None]).to(torch.bfloat16)
+    rng = np.random.default_rng(d)
+    w = torch.from_numpy(rng.choice([2.0 ** -60, -(2.0 ** -60), 1.0, 0.0, 2.0 ** 80, -(2.0 ** 80)], (3, d)).astype(np.float32))
+    p = positions(len(scale), 2)
+    for rope, f in ((None, None), (binding.deft_rope(d), model.frequencies(d)[0])):
+        for wide in (True, False):
+            weight = w if wide else w.to(torch.bfloat16)
+            want = model.heads(x.double().numpy(), p, f, 1.0, False, weight.double().numpy(), eps)
+            got, _ = binding.deft_qk_norm_rotate(x.to(dev()), x[:, :0].to(dev()), weight.to(dev()), None, on_gpu(p), rope, eps=eps)
+            close(got, *want)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("d,H", [(128, 9), (64, 17)])
 @pytest.mark.parametrize("layout", ["half", "interleaved"])
 def test_every_pair_has_its_own_angle_in_every_wave(d, H, layout):

@@ -62,6 +62,12 @@ def test_calls_that_are_refused():
         binding.deft_adjust_logits(plan, torch.zeros((4, 10)))
 
 
+def test_more_workgroups_than_a_launch_holds_are_refused():
+    plan = binding.deft_plan([0], [1], [-1], [0] * 300, 1)
+    packed = binding._pack_logits(1 << 20, 1 << 52, 1 << 28, 1 << 28, 1 << 28, 1, 1, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0)
+    assert binding.load_library().deft_adjust_logits(plan.handle, 0, 1, packed, None, 0, None) == EINVAL  # 2^18 * 38, not below 2^23
+
+
 def test_an_image_is_looked_for_while_another_thread_adds_one():
     t = wl.random_tree(3, n_nodes=5, nq=4)
     plan = plan_of(t)[0]
